@@ -55,6 +55,7 @@ typedef enum rdf2v_status {
 #define RDF2V_STATUS_ID_OUT_OF_RANGE 0x1 /* a subject/object/start id >= num_entities or < 0, or a predicate id out of range */
 #define RDF2V_STATUS_BAD_CSR 0x2         /* row_ptr not non-decreasing within [0, num_edges] */
 #define RDF2V_STATUS_BAD_LENGTH 0x4      /* a walk length outside [0, row_width] (treated as clamped), or a bad string offset */
+#define RDF2V_STATUS_BAD_VALUE 0x10      /* a log decay that is NaN or positive, or a logit of rdf2v_beam_select that is NaN or +inf */
 #define RDF2V_STATUS_CAPACITY 0x8        /* more results than the output holds (the rest are not written), or more distinct strings than a vocabulary bound */
 
 /* Longest walk, in hops. A walk row holds 2 * depth + 1 tokens. */
@@ -446,6 +447,238 @@ rdf2v_status rdf2v_build_vocabulary(const uint8_t *subj_chars, const int64_t *su
                                     int64_t num_triples, int64_t max_entities, int64_t max_predicates,
                                     int32_t *subj_ids, int32_t *pred_ids, int32_t *obj_ids, int64_t *counts_out,
                                     void *workspace, size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/*
+ * Operators of a sequence model over walk tokens.
+ *
+ * Walk rows are what a model trains on and answers with: rows of entity and
+ * predicate tokens of ragged length. The calls below are such a model's
+ * sequence mixer (linear attention with a decay for each head), its loss
+ * (distillation from a teacher's top logits) and its answers' search (beam
+ * selection). Their arguments follow the conventions above; floating arrays
+ * hold RDF2V_F32 or RDF2V_BF16 values, and everything in between is held in 32
+ * bits.
+ */
+typedef enum rdf2v_dtype {
+  RDF2V_F32 = 0,
+  RDF2V_BF16 = 1 /* the upper 16 bits of an IEEE float32, rounded to nearest even */
+} rdf2v_dtype;
+
+/* Largest key or value size of a head in the decay attention calls. */
+#define RDF2V_MAX_HEAD_SIZE 128
+
+/* Sizes and parameters that the decay attention calls share. */
+typedef struct rdf2v_attention {
+  int64_t rows;      /* independent rows of tokens, 0 .. 2^31 - 1 */
+  int64_t length;    /* tokens of a row, 0 .. 2^31 - 1 (not read by the step) */
+  int32_t heads;     /* query heads, 1 .. 65535: a multiple of kv_heads */
+  int32_t kv_heads;  /* key and value heads; query head h reads kv head h / (heads / kv_heads) */
+  int32_t dk, dv;    /* size of a key (and query) and of a value, 1 .. RDF2V_MAX_HEAD_SIZE */
+  int32_t dtype;     /* rdf2v_dtype of q, k, v, their gradients and the outputs */
+  float scale;       /* factor of the outputs, finite */
+  /* [heads] float32 (device): g_h <= 0, the log of the decay of a token. -inf
+   * is a decay of zero. NaN or positive values raise RDF2V_STATUS_BAD_VALUE and
+   * are taken as 0 (no decay). A constant: no gradient is computed for it. */
+  const float *log_decay;
+  /* [rows] int32 (device) or NULL: tokens of each row that count, as the walk
+   * calls write them. Values outside [0, length] raise RDF2V_STATUS_BAD_LENGTH
+   * and are clamped. NULL: all `length` tokens count. Not read by the step. */
+  const int32_t *len;
+} rdf2v_attention;
+
+/* An input of the decay attention calls: element (row, token, head, i) lies at
+ * data[row * row_stride + token * token_stride + head * head_stride + i].
+ * Strides count elements and may be anything that keeps the offsets inside the
+ * caller's memory (slices of one projection, heads before tokens, a broadcast
+ * of stride 0, ...); where data is 16-byte aligned and all strides are
+ * multiples of 16 bytes the reads are widest. */
+typedef struct rdf2v_heads_view {
+  const void *data; /* device; aligned to its element type */
+  int64_t row_stride, token_stride, head_stride;
+} rdf2v_heads_view;
+
+/* Bytes of device workspace that rdf2v_decay_attention and
+ * rdf2v_decay_attention_backward need (0 for sizes that they reject). Pure host
+ * functions of the sizes: pointers are not read. */
+size_t rdf2v_decay_attention_workspace_size(const rdf2v_attention *a);
+size_t rdf2v_decay_attention_backward_workspace_size(const rdf2v_attention *a);
+
+/*
+ * Linear attention with a decay for each head, over whole rows of tokens. For
+ * each row and query head, with gamma = exp(g_h), L the row's length and
+ * S_{-1} = state (zeros if NULL), for t = 0 .. L-1:
+ *
+ *   S_t = gamma S_{t-1} + k_t v_t^T            a dk x dv matrix
+ *   o_t = scale * S_t^T q_t                    dv values
+ *
+ *   q, k, v     views with `heads`, `kv_heads` and `kv_heads` heads of dk, dk
+ *               and dv values. Tokens at and beyond L are not used, whatever
+ *               they hold.
+ *   state       [rows][heads][dk][dv] float32 (device) or NULL.
+ *   out         [rows][length][heads][dv] of the dtype (device), written; zeros
+ *               for tokens at and beyond L.
+ *   state_out   [rows][heads][dk][dv] float32 (device) or NULL: S_{L-1} is
+ *               written. May be `state` itself.
+ *   workspace   rdf2v_decay_attention_workspace_size() bytes of device scratch,
+ *               256-byte aligned.
+ *   status_dev  device int32 or NULL (RDF2V_STATUS_BAD_VALUE,
+ *               RDF2V_STATUS_BAD_LENGTH).
+ *
+ * Outputs may not overlap inputs, but for state_out. The same inputs give the
+ * same bits on every call.
+ */
+rdf2v_status rdf2v_decay_attention(const rdf2v_attention *a, const rdf2v_heads_view *q, const rdf2v_heads_view *k,
+                                   const rdf2v_heads_view *v, const float *state, void *out, float *state_out,
+                                   void *workspace, size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/*
+ * Gradients of rdf2v_decay_attention, from those of its outputs: dout is that
+ * of out (a view with `heads` heads of dv values) and dstate_out that of
+ * state_out (NULL: zeros). With R_t the gradient of S_t,
+ *
+ *   R_t = gamma R_{t+1} + scale * q_t do_t^T,   R_{L-1} = scale * q do^T + dstate_out
+ *   dq_t = scale * S_t do_t,  dk_t = R_t v_t,  dv_t = R_t^T k_t,  dstate = gamma R_0
+ *
+ * (dstate = dstate_out for a row of length 0).
+ *
+ *   state   what the forward call was given, or NULL.
+ *   dq, dk, dv  [rows][length][heads][dk], [rows][length][kv_heads][dk] and
+ *           [rows][length][kv_heads][dv] of the dtype, written; zeros for
+ *           tokens at and beyond L. A kv head's gradients are the sums over
+ *           the query heads that read it, rounded once.
+ *   dstate  [rows][heads][dk][dv] float32 or NULL, written. May be dstate_out
+ *           itself.
+ */
+rdf2v_status rdf2v_decay_attention_backward(const rdf2v_attention *a, const rdf2v_heads_view *q,
+                                            const rdf2v_heads_view *k, const rdf2v_heads_view *v,
+                                            const rdf2v_heads_view *dout, const float *state,
+                                            const float *dstate_out, void *dq, void *dk, void *dv, float *dstate,
+                                            void *workspace, size_t workspace_bytes, int32_t *status_dev,
+                                            void *stream);
+
+/*
+ * One more token for each row: rdf2v_decay_attention at length 1 (a->length and
+ * a->len are not read), with the states taken from other rows where a beam
+ * search has reordered them.
+ *
+ *   q, k, v     views whose token_stride is not read.
+ *   state       [num_states][heads][dk][dv] float32 (device).
+ *   parents     [rows] int32 (device) or NULL: row r continues the state of
+ *               row parents[r] of `state` (as rdf2v_beam_select numbers them).
+ *               An index outside [0, num_states) raises
+ *               RDF2V_STATUS_ID_OUT_OF_RANGE and stands for zeros. NULL: row r
+ *               continues state r, and num_states must be `rows`.
+ *   out         [rows][heads][dv] of the dtype (device), written.
+ *   state_out   [rows][heads][dk][dv] float32 (device), written. Without
+ *               parents it may be `state` itself; with parents the two may not
+ *               overlap (RDF2V_ERR_INVALID_ARGUMENT).
+ */
+rdf2v_status rdf2v_decay_attention_step(const rdf2v_attention *a, const rdf2v_heads_view *q,
+                                        const rdf2v_heads_view *k, const rdf2v_heads_view *v, const float *state,
+                                        int64_t num_states, const int32_t *parents, void *out, float *state_out,
+                                        int32_t *status_dev, void *stream);
+
+/* Most beams, in or out, of a group of rdf2v_beam_select. */
+#define RDF2V_MAX_BEAMS 64
+
+/* Bytes of device workspace rdf2v_beam_select needs (0 for sizes it rejects).
+ * Pure host function. */
+size_t rdf2v_beam_select_workspace_size(int64_t groups, int32_t beams, int64_t vocab, int32_t num_out);
+
+/*
+ * Beam search's selection: of each group (one search) the num_out best
+ * continuations of its beams over the whole vocabulary.
+ *
+ * A beam b that is not finished has a candidate for each token x, of total
+ * scores[b] + (logits[b][x] - log sum_y exp logits[b][y]), computed in float32;
+ * a finished beam has one candidate, token -1 ("the walk has ended") at total
+ * scores[b]. Candidates of total -inf (masked tokens, beams whose score is
+ * -inf, beams without a token above -inf) are never chosen. The num_out largest
+ * totals are written in descending order, equal totals by ascending (beam,
+ * token). Where fewer candidates are left, the rest is score -inf, token -1 and
+ * the group's first row as parent.
+ *
+ *   logits      [groups * beams][logits_stride >= vocab] of the dtype (device).
+ *               NaN and +inf raise RDF2V_STATUS_BAD_VALUE and count as -inf.
+ *   scores      [groups][beams] float32 (device): the beams' totals so far;
+ *               NaN counts as -inf.
+ *   finished    [groups][beams] int32 (device) or NULL: nonzero = finished.
+ *               Logits of finished beams, and of beams whose score is -inf,
+ *               are not read.
+ *   scores_out, tokens_out, parents_out  [groups][num_out] float32, int32 and
+ *               int32 (device), written: total, token, and the row of the beam
+ *               that it continues, group * beams + b. scores_out may be
+ *               `scores` itself where num_out == beams.
+ *   workspace   rdf2v_beam_select_workspace_size() bytes of device scratch,
+ *               256-byte aligned.
+ * groups * beams < 2^31; 1 <= beams, num_out <= RDF2V_MAX_BEAMS;
+ * 1 <= vocab < 2^31.
+ */
+rdf2v_status rdf2v_beam_select(const void *logits, int64_t logits_stride, int32_t dtype, const float *scores,
+                               const int32_t *finished, int64_t groups, int32_t beams, int64_t vocab,
+                               int32_t num_out, float *scores_out, int32_t *tokens_out, int32_t *parents_out,
+                               void *workspace, size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/*
+ * States in the order of the chosen beams: row r of dst is row parents[r] of
+ * src, row_bytes bytes each (any states that are rows: token histories, decay
+ * attention states, ...). An index outside [0, num_src) raises
+ * RDF2V_STATUS_ID_OUT_OF_RANGE and gives a row of zeros. dst and src may not
+ * overlap.
+ */
+rdf2v_status rdf2v_beam_reorder(const void *src, int64_t num_src, int64_t row_bytes, const int32_t *parents,
+                                int64_t num_rows, void *dst, int32_t *status_dev, void *stream);
+
+/* Most teacher entries of a row in the distillation calls. */
+#define RDF2V_MAX_TEACHER_TOP 512
+
+/* Bytes of device workspace the distillation calls need (0 for sizes they
+ * reject). Pure host function. */
+size_t rdf2v_distill_workspace_size(int64_t rows, int64_t vocab, int32_t top, int32_t dtype);
+
+/*
+ * Distillation from a teacher's top logits: for each row, with z its logits,
+ * (id_k, t_k) the teacher's entries and tau the temperature,
+ *
+ *   p = softmax over the entries of t / tau,   q = softmax over the vocabulary of z / tau
+ *   loss = tau^2 * sum_k p_k (log p_k - log q[id_k])
+ *   dlogits[j] = dloss * tau * (q[j] - sum of the p_k with id_k = j)
+ *
+ * An entry whose id is negative, or whose t_k is -inf, is absent; a row without
+ * entries (padding after a walk's end) has loss 0, lse 0 and gradient 0, and
+ * its logits are not read. Logits of -inf have q = 0; a row of nothing else has
+ * lse = -inf, loss = +inf, and q = 0 everywhere. NaN and +inf give what the
+ * formulas give.
+ *
+ *   logits      [rows][logits_stride >= vocab] of the dtype (device).
+ *   ids         [rows][top] int32 (device); an id may occur more than once. An
+ *               id >= vocab raises RDF2V_STATUS_ID_OUT_OF_RANGE and is absent.
+ *   teacher     [rows][top] float32 (device).
+ *   top         0 .. RDF2V_MAX_TEACHER_TOP.
+ *   temperature finite and > 0.
+ *   loss, lse   [rows] float32 (device), written: the loss, and
+ *               log sum_j exp(z_j / tau) for the backward call.
+ *   dloss       [rows] float32 (device), or NULL: the loss's gradient. Given
+ *               together with dlogits the gradient is computed too, which reads
+ *               the logits from memory once where a call for each reads them
+ *               twice.
+ *   dlogits     [rows][dlogits_stride >= vocab] of the dtype (device) or NULL,
+ *               written. May be `logits` itself with the same stride.
+ *   workspace   rdf2v_distill_workspace_size() bytes of device scratch,
+ *               256-byte aligned.
+ */
+rdf2v_status rdf2v_distill_loss(const void *logits, int64_t logits_stride, int32_t dtype, const int32_t *ids,
+                                const float *teacher, int64_t rows, int64_t vocab, int32_t top, float temperature,
+                                float *loss, float *lse, const float *dloss, void *dlogits, int64_t dlogits_stride,
+                                void *workspace, size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/* The gradient alone, with the lse that rdf2v_distill_loss wrote; arguments as
+ * there. */
+rdf2v_status rdf2v_distill_loss_backward(const void *logits, int64_t logits_stride, int32_t dtype,
+                                         const int32_t *ids, const float *teacher, int64_t rows, int64_t vocab,
+                                         int32_t top, float temperature, const float *lse, const float *dloss,
+                                         void *dlogits, int64_t dlogits_stride, void *workspace,
+                                         size_t workspace_bytes, int32_t *status_dev, void *stream);
 
 /* Static, human-readable name of a status code (any int: values that are not
  * an rdf2v_status give "RDF2V_UNKNOWN_STATUS"). */

@@ -33,6 +33,11 @@ __all__ = [
     "rdf2v_skipgram_pairs", "rdf2v_skipgram_pairs_noalloc", "RDF2V_NOALLOC_MAX_WALKS",
     "RDF2V_NOALLOC_SCRATCH_BYTES", "rdf2v_cbow_examples_workspace_size", "rdf2v_cbow_examples",
     "rdf2v_build_vocabulary_workspace_size", "rdf2v_build_vocabulary",
+    "RDF2V_STATUS_BAD_VALUE", "RDF2V_MAX_HEAD_SIZE", "RDF2V_MAX_BEAMS", "RDF2V_MAX_TEACHER_TOP",
+    "rdf2v_decay_attention_workspace_size", "rdf2v_decay_attention",
+    "rdf2v_decay_attention_backward_workspace_size", "rdf2v_decay_attention_backward",
+    "rdf2v_decay_attention_step", "rdf2v_beam_select_workspace_size", "rdf2v_beam_select", "rdf2v_beam_reorder",
+    "rdf2v_distill_workspace_size", "rdf2v_distill_loss", "rdf2v_distill_loss_backward",
     "rdf2v_status_string", "check_device_status",
     "library_path",
 ]
@@ -49,12 +54,18 @@ RDF2V_STATUS_ID_OUT_OF_RANGE = 0x1
 RDF2V_STATUS_BAD_CSR = 0x2
 RDF2V_STATUS_BAD_LENGTH = 0x4
 RDF2V_STATUS_CAPACITY = 0x8
+RDF2V_STATUS_BAD_VALUE = 0x10
 RDF2V_MAX_DEPTH = 64
 RDF2V_TOKENS_TRIPLES = 0
 RDF2V_TOKENS_ENTITIES = 1
 RDF2V_TOKENS_PROPERTIES = 2
 RDF2V_NOALLOC_MAX_WALKS = 1 << 22
 RDF2V_NOALLOC_SCRATCH_BYTES = (32 << 20) + (64 << 10)
+RDF2V_F32 = 0
+RDF2V_BF16 = 1
+RDF2V_MAX_HEAD_SIZE = 128
+RDF2V_MAX_BEAMS = 64
+RDF2V_MAX_TEACHER_TOP = 512
 
 _lib = None
 
@@ -67,6 +78,18 @@ class _CsrStruct(ctypes.Structure):
     _fields_ = [("num_entities", ctypes.c_int32), ("num_predicates", ctypes.c_int32),
                 ("num_edges", ctypes.c_int64), ("row_ptr", ctypes.c_void_p),
                 ("edges", ctypes.c_void_p), ("walk_edges", ctypes.c_void_p)]
+
+
+class _AttentionStruct(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("length", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("log_decay", ctypes.c_void_p),
+                ("len", ctypes.c_void_p)]
+
+
+class _HeadsViewStruct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
 
 
 def _native():
@@ -119,6 +142,30 @@ def _native():
     lib.rdf2v_build_vocabulary_workspace_size.restype = sz
     lib.rdf2v_build_vocabulary.argtypes = [vp, vp, i64] * 3 + [i64, i64, i64, vp, vp, vp, vp, vp, sz, vp, vp]
     lib.rdf2v_build_vocabulary.restype = ctypes.c_int
+    att_p, view_p, f32 = ctypes.POINTER(_AttentionStruct), ctypes.POINTER(_HeadsViewStruct), ctypes.c_float
+    lib.rdf2v_decay_attention_workspace_size.argtypes = [att_p]
+    lib.rdf2v_decay_attention_workspace_size.restype = sz
+    lib.rdf2v_decay_attention.argtypes = [att_p, view_p, view_p, view_p, vp, vp, vp, vp, sz, vp, vp]
+    lib.rdf2v_decay_attention.restype = ctypes.c_int
+    lib.rdf2v_decay_attention_backward_workspace_size.argtypes = [att_p]
+    lib.rdf2v_decay_attention_backward_workspace_size.restype = sz
+    lib.rdf2v_decay_attention_backward.argtypes = [att_p] + [view_p] * 4 + [vp] * 7 + [sz, vp, vp]
+    lib.rdf2v_decay_attention_backward.restype = ctypes.c_int
+    lib.rdf2v_decay_attention_step.argtypes = [att_p, view_p, view_p, view_p, vp, i64, vp, vp, vp, vp, vp]
+    lib.rdf2v_decay_attention_step.restype = ctypes.c_int
+    lib.rdf2v_beam_select_workspace_size.argtypes = [i64, i32, i64, i32]
+    lib.rdf2v_beam_select_workspace_size.restype = sz
+    lib.rdf2v_beam_select.argtypes = [vp, i64, i32, vp, vp, i64, i32, i64, i32, vp, vp, vp, vp, sz, vp, vp]
+    lib.rdf2v_beam_select.restype = ctypes.c_int
+    lib.rdf2v_beam_reorder.argtypes = [vp, i64, i64, vp, i64, vp, vp, vp]
+    lib.rdf2v_beam_reorder.restype = ctypes.c_int
+    lib.rdf2v_distill_workspace_size.argtypes = [i64, i64, i32, i32]
+    lib.rdf2v_distill_workspace_size.restype = sz
+    lib.rdf2v_distill_loss.argtypes = [vp, i64, i32, vp, vp, i64, i64, i32, f32, vp, vp, vp, vp, i64, vp, sz, vp, vp]
+    lib.rdf2v_distill_loss.restype = ctypes.c_int
+    lib.rdf2v_distill_loss_backward.argtypes = [vp, i64, i32, vp, vp, i64, i64, i32, f32, vp, vp, vp, i64, vp, sz,
+                                                vp, vp]
+    lib.rdf2v_distill_loss_backward.restype = ctypes.c_int
     lib.rdf2v_status_string.argtypes = [ctypes.c_int]
     lib.rdf2v_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -630,6 +677,372 @@ def rdf2v_build_vocabulary(subj, pred, obj, max_entities: int, max_predicates: i
         return ids[0], ids[1], ids[2], counts
 
 
+_DTYPES = {torch.float32: RDF2V_F32, torch.bfloat16: RDF2V_BF16}
+
+
+def _float_dtype(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _heads_view(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> _HeadsViewStruct:
+    """A [rows, tokens, heads, size] (or [rows, heads, size]) input in any layout whose last dimension
+    is contiguous."""
+    if not isinstance(t, torch.Tensor) or t.device != like.device or t.dtype != like.dtype:
+        raise TypeError(f"{name} must be a {like.dtype} tensor on {like.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return _HeadsViewStruct(t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0, stride[-2])
+
+
+def _state(t: torch.Tensor | None, name: str, shape, dev: torch.device) -> torch.Tensor | None:
+    """An optional float32 state tensor of exactly this shape."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
+    return _out(t, name, torch.float32, 0, dev)
+
+
+def _exact(t: torch.Tensor, name: str, dtype: torch.dtype, shape, dev: torch.device) -> torch.Tensor:
+    _out(t, name, dtype, 0, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
+    return t
+
+
+class _Attention:
+    """The checked arguments that the decay attention calls share."""
+
+    __slots__ = ("c", "views", "dev")
+
+    def __init__(self, q, k, v, log_decay, scale, lens, ndim):
+        dtype = _float_dtype(q, "q")
+        if q.dim() != ndim or not isinstance(k, torch.Tensor) or k.dim() != ndim or not isinstance(v, torch.Tensor) \
+                or v.dim() != ndim:
+            raise ValueError(f"q, k and v must have {ndim} dimensions")
+        self.dev = dev = q.device
+        lead, (heads, dk), (kv_heads, dv) = q.shape[:-2], q.shape[-2:], v.shape[-2:]
+        if kv_heads < 1 or heads % kv_heads:
+            raise ValueError(f"{heads} query heads are no multiple of {kv_heads} key and value heads")
+        if not 1 <= dk <= RDF2V_MAX_HEAD_SIZE or not 1 <= dv <= RDF2V_MAX_HEAD_SIZE:
+            raise ValueError(f"head sizes {dk} and {dv}: 1 to {RDF2V_MAX_HEAD_SIZE} are supported")
+        self.views = (_heads_view(q, "q", q, lead + (heads, dk)), _heads_view(k, "k", q, lead + (kv_heads, dk)),
+                      _heads_view(v, "v", q, lead + (kv_heads, dv)))
+        _exact(log_decay, "log_decay", torch.float32, (heads,), dev)
+        if lens is not None:
+            _exact(lens, "lens", torch.int32, (lead[0],), dev)
+        self.c = _AttentionStruct(lead[0], lead[1] if ndim == 4 else 1, heads, kv_heads, dk, dv, dtype,
+                                  dk ** -0.5 if scale is None else scale, log_decay.data_ptr(), _ptr(lens))
+
+
+def rdf2v_decay_attention_workspace_size(rows: int, length: int, heads: int, kv_heads: int, dk: int, dv: int,
+                                         dtype: torch.dtype = torch.float32) -> int:
+    c = _AttentionStruct(rows, length, heads, kv_heads, dk, dv, _DTYPES.get(dtype, -1), 1.0, None, None)
+    return int(_native().rdf2v_decay_attention_workspace_size(ctypes.byref(c)))
+
+
+def rdf2v_decay_attention_backward_workspace_size(rows: int, length: int, heads: int, kv_heads: int, dk: int, dv: int,
+                                                  dtype: torch.dtype = torch.float32) -> int:
+    c = _AttentionStruct(rows, length, heads, kv_heads, dk, dv, _DTYPES.get(dtype, -1), 1.0, None, None)
+    return int(_native().rdf2v_decay_attention_backward_workspace_size(ctypes.byref(c)))
+
+
+def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, *,
+                          scale: float | None = None, lens: torch.Tensor | None = None,
+                          state: torch.Tensor | None = None, want_state: bool = False,
+                          out: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                          workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """Linear attention with a decay for each head over rows of tokens:
+    S_t = exp(log_decay) S_{t-1} + k_t v_t^T, out_t = scale * S_t^T q_t.
+
+    q [rows, length, heads, dk], k [rows, length, kv_heads, dk] and v [rows, length, kv_heads, dv] are
+    float32 or bfloat16 in any layout whose last dimension is contiguous; query head h reads key and
+    value head h // (heads // kv_heads). log_decay: float32 [heads], <= 0. scale defaults to dk ** -0.5.
+    lens: int32 [rows], the tokens of each row that count (as the walk calls return them). state: float32
+    [rows, heads, dk, dv] to begin from. Returns (out [rows, length, heads, dv], state_out), state_out
+    being None unless it is given or want_state is set."""
+    a = _Attention(q, k, v, log_decay, scale, lens, 4)
+    dev, c = a.dev, a.c
+    with _on_stream(dev, stream) as h:
+        shape = (c.rows, c.heads, c.dk, c.dv)
+        if out is None:
+            out = torch.empty((c.rows, c.length, c.heads, c.dv), dtype=q.dtype, device=dev)
+        else:
+            _exact(out, "out", q.dtype, (c.rows, c.length, c.heads, c.dv), dev)
+        if state_out is None:
+            if want_state:
+                state_out = torch.empty(shape, dtype=torch.float32, device=dev)
+        else:
+            _state(state_out, "state_out", shape, dev)
+        _state(state, "state", shape, dev)
+        _status(status, dev)
+        ref = ctypes.byref(c)
+        if workspace is None:
+            need = _native().rdf2v_decay_attention_workspace_size(ref)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        vq, vk, vv = a.views
+        st = _native().rdf2v_decay_attention(ref, vq, vk, vv, _ptr(state), _ptr(out), _ptr(state_out),
+                                             _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_decay_attention")
+        return out, state_out
+
+
+def rdf2v_decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                                   dout: torch.Tensor, *, scale: float | None = None,
+                                   lens: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                                   dstate_out: torch.Tensor | None = None, dq: torch.Tensor | None = None,
+                                   dk: torch.Tensor | None = None, dv: torch.Tensor | None = None,
+                                   dstate: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                                   status: torch.Tensor | None = None, stream=None):
+    """Gradients of rdf2v_decay_attention for its inputs, from dout (that of out) and dstate_out (that of
+    state_out; None: zeros). Returns (dq, dk, dv, dstate) in the shapes of q, k, v and state; dstate is
+    None unless state or dstate is given. log_decay is a constant and has no gradient."""
+    a = _Attention(q, k, v, log_decay, scale, lens, 4)
+    dev, c = a.dev, a.c
+    with _on_stream(dev, stream) as h:
+        shape = (c.rows, c.heads, c.dk, c.dv)
+        view = _heads_view(dout, "dout", q, (c.rows, c.length, c.heads, c.dv))
+        grads = []
+        for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+            grads.append(torch.empty(like.shape, dtype=q.dtype, device=dev) if t is None else
+                         _exact(t, name, q.dtype, like.shape, dev))
+        dq, dk, dv = grads
+        if dstate is None:
+            if state is not None:
+                dstate = torch.empty(shape, dtype=torch.float32, device=dev)
+        else:
+            _state(dstate, "dstate", shape, dev)
+        _state(state, "state", shape, dev)
+        _state(dstate_out, "dstate_out", shape, dev)
+        _status(status, dev)
+        ref = ctypes.byref(c)
+        if workspace is None:
+            need = _native().rdf2v_decay_attention_backward_workspace_size(ref)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        vq, vk, vv = a.views
+        st = _native().rdf2v_decay_attention_backward(ref, vq, vk, vv, view, _ptr(state), _ptr(dstate_out), _ptr(dq),
+                                                      _ptr(dk), _ptr(dv), _ptr(dstate), _ptr(workspace),
+                                                      _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_decay_attention_backward")
+        return dq, dk, dv, dstate
+
+
+def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                               state: torch.Tensor, *, scale: float | None = None,
+                               parents: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                               state_out: torch.Tensor | None = None, status: torch.Tensor | None = None,
+                               stream=None):
+    """rdf2v_decay_attention for one more token of each row: q [rows, heads, dk], k [rows, kv_heads, dk],
+    v [rows, kv_heads, dv], state float32 [num_states, heads, dk, dv]. Returns (out [rows, heads, dv],
+    state_out [rows, heads, dk, dv]).
+
+    With parents (int32, one per row), row r continues state parents[r], as rdf2v_beam_select numbers
+    them, and state_out must not overlap state. Without, row r continues state r, and state is updated
+    in place unless state_out is given."""
+    a = _Attention(q, k, v, log_decay, scale, None, 3)
+    dev, c = a.dev, a.c
+    with _on_stream(dev, stream) as h:
+        shape = (c.rows, c.heads, c.dk, c.dv)
+        num_states = c.rows
+        if parents is not None:
+            _exact(_dev_i32(parents, "parents").reshape(-1), "parents", torch.int32, (c.rows,), dev)
+            num_states = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() == 4 else c.rows
+        if state is None:
+            raise TypeError("state must be a CUDA (HIP) tensor")
+        _state(state, "state", (num_states,) + shape[1:], dev)
+        if out is None:
+            out = torch.empty((c.rows, c.heads, c.dv), dtype=q.dtype, device=dev)
+        else:
+            _exact(out, "out", q.dtype, (c.rows, c.heads, c.dv), dev)
+        if state_out is None:
+            state_out = state if parents is None else torch.empty(shape, dtype=torch.float32, device=dev)
+        else:
+            _state(state_out, "state_out", shape, dev)
+        _status(status, dev)
+        vq, vk, vv = a.views
+        st = _native().rdf2v_decay_attention_step(ctypes.byref(c), vq, vk, vv, _ptr(state), num_states,
+                                                  _ptr(parents), _ptr(out), _ptr(state_out), _ptr(status), h)
+        _check(st, "rdf2v_decay_attention_step")
+        return out, state_out
+
+
+def rdf2v_beam_select_workspace_size(groups: int, beams: int, vocab: int, num_out: int) -> int:
+    return int(_native().rdf2v_beam_select_workspace_size(groups, beams, vocab, num_out))
+
+
+def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, *,
+                      finished: torch.Tensor | None = None, scores_out: torch.Tensor | None = None,
+                      tokens: torch.Tensor | None = None, parents: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """The num_out best continuations of each group's beams: logits [groups, beams, vocab] (float32 or
+    bfloat16; beams contiguous up to a row stride), scores float32 [groups, beams]. Totals are
+    scores + log_softmax(logits); a beam whose `finished` (int32 [groups, beams]) is nonzero has one
+    candidate, token -1 at its score.
+
+    Returns (scores, tokens, parents), each [groups, num_out]: totals in descending order, ties to the
+    lowest (beam, token); parents are row numbers group * beams + beam, as rdf2v_beam_reorder and
+    rdf2v_decay_attention_step take them. Places without a candidate hold -inf, -1 and the group's first
+    row."""
+    dtype = _float_dtype(logits, "logits")
+    if logits.dim() != 3:
+        raise ValueError("logits must have shape [groups, beams, vocab]")
+    dev = logits.device
+    with _on_stream(dev, stream) as h:
+        groups, beams, vocab = logits.shape
+        gs, bs, vs = logits.stride()
+        if (vs != 1 and vocab > 1) or (gs != beams * bs and groups > 1 and beams > 1):
+            raise ValueError("logits must be rows of contiguous values at one row stride")
+        row = bs if beams > 1 else gs if groups > 1 else vocab
+        _exact(scores, "scores", torch.float32, (groups, beams), dev)
+        if finished is not None:
+            _exact(finished, "finished", torch.int32, (groups, beams), dev)
+        shape = (groups, num_out)
+        scores_out = (torch.empty(shape, dtype=torch.float32, device=dev) if scores_out is None else
+                      _exact(scores_out, "scores_out", torch.float32, shape, dev))
+        tokens = (torch.empty(shape, dtype=torch.int32, device=dev) if tokens is None else
+                  _exact(tokens, "tokens", torch.int32, shape, dev))
+        parents = (torch.empty(shape, dtype=torch.int32, device=dev) if parents is None else
+                   _exact(parents, "parents", torch.int32, shape, dev))
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            need = lib.rdf2v_beam_select_workspace_size(groups, beams, vocab, num_out)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        st = lib.rdf2v_beam_select(_ptr(logits), row, dtype, _ptr(scores), _ptr(finished), groups, beams, vocab,
+                                   num_out, _ptr(scores_out), _ptr(tokens), _ptr(parents), _ptr(workspace),
+                                   _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_beam_select")
+        return scores_out, tokens, parents
+
+
+def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.Tensor | None = None,
+                       status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Rows of src (any type, contiguous) in the order of parents (int32, any shape): out[r] =
+    src[parents.flatten()[r]]."""
+    _dev_i32(parents, "parents")
+    dev = parents.device
+    if not isinstance(src, torch.Tensor) or src.device != dev:
+        raise TypeError(f"src must be a CUDA (HIP) tensor on {dev}")
+    if src.dim() < 1 or not src.is_contiguous():
+        raise ValueError("src must be contiguous rows")
+    with _on_stream(dev, stream) as h:
+        rows, shape = parents.numel(), src.shape[1:]
+        if out is None:
+            out = torch.empty((rows,) + shape, dtype=src.dtype, device=dev)
+        else:
+            _exact(out, "out", src.dtype, (rows,) + shape, dev)
+        _status(status, dev)
+        row_bytes = src.element_size() * shape.numel()
+        st = _native().rdf2v_beam_reorder(_ptr(src), src.shape[0], row_bytes, _ptr(parents), rows, _ptr(out),
+                                          _ptr(status), h)
+        _check(st, "rdf2v_beam_reorder")
+        return out
+
+
+def rdf2v_distill_workspace_size(rows: int, vocab: int, top: int, dtype: torch.dtype = torch.float32) -> int:
+    return int(_native().rdf2v_distill_workspace_size(rows, vocab, top, _DTYPES.get(dtype, -1)))
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor) -> int:
+    """Row stride of a [rows, vocab] tensor with contiguous rows."""
+    if not isinstance(t, torch.Tensor) or t.device != like.device or t.dtype != like.dtype:
+        raise TypeError(f"{name} must be a {like.dtype} tensor on {like.device}")
+    if t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name} must have shape [rows, vocab]")
+    rows, vocab = t.shape
+    row, one = t.stride()
+    if one != 1 and vocab > 1:
+        raise ValueError(f"rows of {name} must be contiguous")
+    if row < vocab and rows > 1:
+        raise ValueError(f"rows of {name} must not overlap")
+    return row if rows > 1 else max(row, vocab)
+
+
+def _teacher(logits, ids, teacher):
+    dtype = _float_dtype(logits, "logits")
+    stride = _rows(logits, "logits", logits)
+    dev = logits.device
+    _dev_i32(ids, "ids")
+    if ids.dim() != 2 or ids.shape[0] != logits.shape[0]:
+        raise ValueError("ids must have shape [rows, top]")
+    _same_device(dev, ids=ids)
+    _exact(teacher, "teacher", torch.float32, ids.shape, dev)
+    return dtype, stride, dev
+
+
+def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, *, temperature: float = 1.0,
+                       dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None,
+                       lse: torch.Tensor | None = None, dlogits: torch.Tensor | None = None,
+                       workspace: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """Distillation from a teacher's top logits: temperature^2 * KL(softmax of the teacher's entries /
+    temperature || softmax(logits / temperature)) for each row.
+
+    logits [rows, vocab] float32 or bfloat16, rows contiguous; ids int32 [rows, top] (negative: absent)
+    and teacher float32 [rows, top]. Returns (loss, lse), float32 [rows]; with dloss (float32 [rows], the
+    gradient of loss) the gradient of the logits is computed in the same pass and (loss, lse, dlogits) is
+    returned. dlogits may be logits itself."""
+    dtype, stride, dev = _teacher(logits, ids, teacher)
+    with _on_stream(dev, stream) as h:
+        rows, vocab = logits.shape
+        loss = torch.empty(rows, dtype=torch.float32, device=dev) if loss is None else \
+            _exact(loss, "loss", torch.float32, (rows,), dev)
+        lse = torch.empty(rows, dtype=torch.float32, device=dev) if lse is None else \
+            _exact(lse, "lse", torch.float32, (rows,), dev)
+        dstride = vocab
+        if dloss is not None:
+            _exact(dloss, "dloss", torch.float32, (rows,), dev)
+            if dlogits is None:
+                dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
+            else:
+                dstride = _rows(dlogits, "dlogits", logits)
+        elif dlogits is not None:
+            raise ValueError("dlogits needs dloss")
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            need = lib.rdf2v_distill_workspace_size(rows, vocab, ids.shape[1], dtype)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        st = lib.rdf2v_distill_loss(_ptr(logits), stride, dtype, _ptr(ids), _ptr(teacher), rows, vocab, ids.shape[1],
+                                    temperature, _ptr(loss), _ptr(lse), _ptr(dloss), _ptr(dlogits), dstride,
+                                    _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_distill_loss")
+        return (loss, lse) if dloss is None else (loss, lse, dlogits)
+
+
+def rdf2v_distill_loss_backward(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
+                                dloss: torch.Tensor, *, temperature: float = 1.0, dlogits: torch.Tensor | None = None,
+                                workspace: torch.Tensor | None = None, status: torch.Tensor | None = None,
+                                stream=None) -> torch.Tensor:
+    """The gradient of the logits alone, with the lse that rdf2v_distill_loss returned."""
+    dtype, stride, dev = _teacher(logits, ids, teacher)
+    with _on_stream(dev, stream) as h:
+        rows, vocab = logits.shape
+        _exact(lse, "lse", torch.float32, (rows,), dev)
+        _exact(dloss, "dloss", torch.float32, (rows,), dev)
+        dstride = vocab
+        if dlogits is None:
+            dlogits = torch.empty((rows, vocab), dtype=logits.dtype, device=dev)
+        else:
+            dstride = _rows(dlogits, "dlogits", logits)
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            need = lib.rdf2v_distill_workspace_size(rows, vocab, ids.shape[1], dtype)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        st = lib.rdf2v_distill_loss_backward(_ptr(logits), stride, dtype, _ptr(ids), _ptr(teacher), rows, vocab,
+                                             ids.shape[1], temperature, _ptr(lse), _ptr(dloss), _ptr(dlogits),
+                                             dstride, _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_distill_loss_backward")
+        return dlogits
+
+
 def check_device_status(status: torch.Tensor, where: str = "device", stream=None) -> None:
     """Raise if a device status word (zeroed before the calls) has any bit set. The word is read
     on `stream` (default: the current stream), so pass the stream the calls were made on."""
@@ -638,5 +1051,6 @@ def check_device_status(status: torch.Tensor, where: str = "device", stream=None
     if v != 0:
         bits = [n for b, n in [(RDF2V_STATUS_ID_OUT_OF_RANGE, "ID_OUT_OF_RANGE"),
                                (RDF2V_STATUS_BAD_CSR, "BAD_CSR"), (RDF2V_STATUS_BAD_LENGTH, "BAD_LENGTH"),
-                               (RDF2V_STATUS_CAPACITY, "CAPACITY")] if v & b]
+                               (RDF2V_STATUS_CAPACITY, "CAPACITY"), (RDF2V_STATUS_BAD_VALUE, "BAD_VALUE")]
+                if v & b]
         raise Rdf2vError(RDF2V_ERR_ID_OUT_OF_RANGE, f"{where}: status bits {'|'.join(bits) or v}")
