@@ -42,6 +42,12 @@ struct ScanArgs {
   float oscale, sscale;
   bool transposed;  // s0 is stored [dout][di]
   bool reverse;
+  // set by launch_scan
+  float pscale;              // oscale * sscale
+  int32_t blocks_n;          // workgroups over the columns
+  int64_t segments, segment; // segments of a row, and their tokens (whole chunks)
+  float *seg_state;          // [rows][heads][segments][di][dout], or null for one segment
+  bool wide, wide_out;       // 16-byte reads, stores of four values
 };
 
 __device__ __forceinline__ float head_log_decay(const float *log_decay, int h, int32_t *status, bool report) {
@@ -64,77 +70,495 @@ __device__ __forceinline__ const T *operand_row(const ScanOperand &x, int64_t ro
   return static_cast<const T *>(x.data) + row * x.row + (h / x.share) * x.head;
 }
 
-constexpr int kColumns = 64;  // columns of S per workgroup, one to a lane
+constexpr int kChunk = 64;      // tokens of a chunk
+constexpr int kThreads = 256;   // four waves
+constexpr int kTile = 16;       // rows and columns of a matrix instruction
 
-// Token by token: lane n holds column n of S in registers.
-template <class T, class O, int DI>
-__global__ __launch_bounds__(kColumns) void scan_kernel(ScanArgs p, int64_t first) {
-  __shared__ float as[DI], bs[DI];
-  const int blocks_n = (p.dout + kColumns - 1) / kColumns;
-  const int64_t block = first + blockIdx.x;
-  const int nb = int(block % blocks_n);
-  const int h = int(block / blocks_n % p.heads);
-  const int64_t row = block / blocks_n / p.heads;
-  const int lane = threadIdx.x, n = nb * kColumns + lane;
-  const bool report = nb == 0 && lane == 0;
-  const float g = head_log_decay(p.log_decay, h, p.status, report && row == 0);
-  const float gamma = expf(g);
-  const int64_t len = row_length(p.len, row, p.length, p.status, report && h == 0);
-  const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h);
-  float s[DI];
+// Eight values of a row or column that one lane feeds to a matrix instruction.
+// Lane l serves row (of the first factor) or column (of the second) l % 16, and
+// with g = l / 16 its values are those at contraction indices
+// 16 (j / 4) + 4 g + j % 4 of a block of 32: both factors use this order, in
+// which a result of one instruction (rows 4 g + r, column l % 16) is an operand
+// of the next as it stands.
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+template <class T>
+struct Vec;
+template <>
+struct Vec<bf16> {
+  typedef bf16x4 four;
+  typedef bf16x8 eight;
+  typedef bf16x8 load;  // 16 bytes
+  // Operands of the matrix products that are computed values: the weights of a
+  // chunk's pairs and the states are fed as two bfloat16 pieces (16 bits, so
+  // that bfloat16 outputs are off by little more than their own rounding), the
+  // addends of the states, which are float32 outputs, as three (24 bits).
+  static constexpr int kPieces = 2, kStatePieces = 3, kPad = 8;
+};
+template <>
+struct Vec<float> {
+  typedef f32x4 four;
+  typedef f32x8 eight;
+  typedef f32x4 load;
+  static constexpr int kPieces = 1, kStatePieces = 1, kPad = 4;
+};
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
 #pragma unroll
-  for (int i = 0; i < DI; ++i) {
-    s[i] = 0.0f;
-    if (p.s0 != nullptr && i < p.di && n < p.dout) {
-      const float *s0 = p.s0 + (row * p.heads + h) * int64_t(p.di) * p.dout;
-      s[i] = p.transposed ? s0[int64_t(n) * p.di + i] : s0[int64_t(i) * p.dout + n];
-    }
-  }
-  O *out = static_cast<O *>(p.out) + (row * p.length * p.heads + h) * int64_t(p.dout);
-  const int64_t step = int64_t(p.heads) * p.dout;
-  for (int64_t u = 0; u < len; ++u) {
-    const int64_t t = p.reverse ? len - 1 - u : u;
-    __syncthreads();
-    for (int i = lane; i < DI; i += kColumns) {
-      as[i] = i < p.di ? to_f32(a[t * p.a.token + i]) : 0.0f;
-      bs[i] = i < p.di ? to_f32(b[t * p.b.token + i]) * p.sscale : 0.0f;
-    }
-    __syncthreads();
-    const float cv = n < p.dout ? to_f32(c[t * p.c.token + n]) : 0.0f;
-    const float d = p.reverse && u == 0 ? 1.0f : gamma;
-    float o = 0.0f;
-#pragma unroll
-    for (int i = 0; i < DI; ++i) {
-      s[i] = fmaf(s[i], d, bs[i] * cv);
-      o = fmaf(as[i], s[i], o);
-    }
-    if (n < p.dout) out[t * step + n] = from_f32<O>(o * p.oscale);
-  }
-  for (int64_t t = len; t < p.length; ++t)
-    if (n < p.dout) out[t * step + n] = from_f32<O>(0.0f);
-  if (p.s1 != nullptr && n < p.dout) {
-    float *s1 = p.s1 + (row * p.heads + h) * int64_t(p.di) * p.dout;
-    const float d = p.reverse && len > 0 ? gamma : 1.0f;
-#pragma unroll
-    for (int i = 0; i < DI; ++i)
-      if (i < p.di) s1[int64_t(i) * p.dout + n] = s[i] * d;
-  }
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
 }
 
-template <class T, class O>
-rdf2v_status launch_scan(const ScanArgs &p, hipStream_t stream) {
-  const int64_t blocks = p.rows * p.heads * ((p.dout + kColumns - 1) / kColumns);
-  return for_each_launch(blocks, kColumns, 1, [&](int64_t first, int64_t count) {
-    if (p.di <= 32)
-      scan_kernel<T, O, 32><<<dim3(unsigned(count)), dim3(kColumns), 0, stream>>>(p, first);
-    else if (p.di <= 64)
-      scan_kernel<T, O, 64><<<dim3(unsigned(count)), dim3(kColumns), 0, stream>>>(p, first);
-    else
-      scan_kernel<T, O, 128><<<dim3(unsigned(count)), dim3(kColumns), 0, stream>>>(p, first);
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+__device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// The next piece of x: x to the element type, and what is left in x.
+__device__ __forceinline__ bf16x8 take_piece(f32x8 &x, bf16) {
+  bf16x8 p;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    p[j] = bf16(x[j]);
+    x[j] -= float(p[j]);
+  }
+  return p;
+}
+__device__ __forceinline__ f32x8 take_piece(f32x8 &x, float) { return x; }
+__device__ __forceinline__ bf16x4 take_piece(f32x4 &x, bf16) {
+  bf16x4 p;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    p[j] = bf16(x[j]);
+    x[j] -= float(p[j]);
+  }
+  return p;
+}
+__device__ __forceinline__ f32x4 take_piece(f32x4 &x, float) { return x; }
+
+// Values of row `row`, indices of block kk, of a tile of rows in LDS.
+template <class T, int STRIDE>
+__device__ __forceinline__ typename Vec<T>::eight row_values(const T *tile, int row, int kk, int g) {
+  typedef typename Vec<T>::four four;
+  const T *p = tile + row * STRIDE + kk * 32 + 4 * g;
+  return join(*reinterpret_cast<const four *>(p), *reinterpret_cast<const four *>(p + 16));
+}
+// Values of column col0 + l % 16, rows of block kk. In bfloat16 the transposing
+// LDS read gives lane l of 16 the column l of the four rows that the lanes
+// 4 row + (0 .. 3) address.
+template <int STRIDE>
+__device__ __forceinline__ bf16x8 column_values(const bf16 *tile, int col0, int kk, int lane) {
+  typedef __attribute__((address_space(3))) i16x4 lds4;
+  const bf16 *p = tile + (kk * 32 + 4 * (lane / 16) + lane % 16 / 4) * STRIDE + col0 + 4 * (lane % 4);
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * STRIDE));
+  return join(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi));
+}
+template <int STRIDE>
+__device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int kk, int lane) {
+  const float *p = tile + (kk * 32 + 4 * (lane / 16)) * STRIDE + col0 + lane % 16;
+  f32x8 x;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = p[(16 * (j / 4) + j % 4) * STRIDE];
+  return x;
+}
+
+// A chunk's rows of one operand on their way from memory to LDS: 64 rows of W
+// values, zeros beyond the operand's size and beyond the chunk's `n` tokens.
+template <class T, int W>
+struct Loader {
+  typedef typename Vec<T>::load load;
+  static constexpr int kPer = 16 / sizeof(T), kStride = W + Vec<T>::kPad;
+  static constexpr int kLoads = kChunk * W / kPer / kThreads;
+  load r[kLoads];
+
+  // Row of a token: token u of the scan is t0 + dt * u of the row.
+  static __device__ __forceinline__ const T *row(const T *p, int64_t token, int64_t t0, int dt, int u) {
+    return p + (t0 + int64_t(dt) * u) * token;
+  }
+  __device__ __forceinline__ void fetch(const T *p, int64_t token, int64_t t0, int dt, int n, int size) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = i * kThreads + threadIdx.x, u = at / (W / kPer), col = at % (W / kPer) * kPer;
+      r[i] = load{};
+      if (u < n && col < size) r[i] = *reinterpret_cast<const load *>(row(p, token, t0, dt, u) + col);
+    }
+  }
+  __device__ __forceinline__ void store(T *tile) const {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = i * kThreads + threadIdx.x, u = at / (W / kPer), col = at % (W / kPer) * kPer;
+      *reinterpret_cast<load *>(tile + u * kStride + col) = r[i];
+    }
+  }
+  // Value by value, for rows that 16-byte reads do not fit.
+  static __device__ __forceinline__ void copy(T *tile, const T *p, int64_t token, int64_t t0, int dt, int n,
+                                              int size) {
+    for (int at = threadIdx.x; at < kChunk * W; at += kThreads) {
+      const int u = at / W, col = at % W;
+      tile[u * kStride + col] = u < n && col < size ? row(p, token, t0, dt, u)[col] : T(0.0f);
+    }
+  }
+};
+
+// One workgroup scans the chunks of one segment of a row for one head and NB
+// columns of c and S.
+//
+// A chunk's part of the sum is the matrix product of the weights
+// P[t][s] = gamma^{t-s} (a_t . b_s), s <= t, with c; the earlier chunks' part is
+// gamma^{t+e} S^T a_t; then S becomes gamma^n S + sum_s gamma^{n-e-s} b_s c_s^T.
+// Every wave owns some columns of S, which stay in its registers as the
+// accumulators of the update and, in the order above, are the operands of the
+// earlier chunks' part; wave w computes the weights of tokens 16 w .. 16 w + 15
+// for all, through LDS. The next chunk is fetched while this one is computed.
+//
+// OUT: outputs are wanted; otherwise only S of the segment (from zeros).
+template <class T, class O, int DI, int NB, bool OUT>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(ScanArgs p, int64_t first) {
+  constexpr int kWavesN = NB >= 64 ? 4 : NB / kTile;       // waves side by side over the columns
+  constexpr int kWavesT = 4 / kWavesN;                     // and over the chunk's tokens
+  constexpr int kTilesN = NB / kTile / kWavesN, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
+  constexpr int kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
+  constexpr int kAB = DI + Vec<T>::kPad, kC = NB + Vec<T>::kPad, kP = kChunk + Vec<T>::kPad;
+  __shared__ __attribute__((aligned(16))) T as[OUT ? kChunk * kAB : 1], bs[kChunk * kAB], cs[kChunk * kC];
+  __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? kChunk * kP : 1];
+  typedef typename Vec<T>::four four;
+  typedef typename Vec<T>::eight eight;
+
+  const int64_t block = first + blockIdx.x;
+  const int nb = int(block % p.blocks_n);
+  const int64_t seg = block / p.blocks_n % p.segments;
+  const int h = int(block / p.blocks_n / p.segments % p.heads);
+  const int64_t row = block / p.blocks_n / p.segments / p.heads;
+  const int wave = threadIdx.x / kWave, lane = lane_id(), l16 = lane % 16, g = lane / 16;
+  const int wn = wave % kWavesN, wt = wave / kWavesN;
+  const int n0 = nb * NB;                                  // first column of the workgroup
+  const int nw = wn * kTilesN * kTile;                     // first column of the wave in it
+  const bool report = nb == 0 && seg == 0 && threadIdx.x == 0;
+  const float log2_gamma = head_log_decay(p.log_decay, h, p.status, report && row == 0) * 1.44269504088896341f;
+  const int64_t len = row_length(p.len, row, p.length, p.status, report && h == 0);
+  const int e = p.reverse ? 0 : 1;
+  const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h) + n0;
+  const int dout = min(NB, p.dout - n0);
+  const int64_t u_begin = seg * p.segment, u_end = min(p.length, u_begin + p.segment);
+  const int64_t u_valid = min(u_end, len);
+  const int dt = p.reverse ? -1 : 1;
+
+  f32x4 s[kTilesN][kTilesI];
+  const int64_t state_at = (row * p.heads + h) * int64_t(p.di) * p.dout;
+  {
+    const float *s0 = OUT && p.seg_state != nullptr
+                          ? p.seg_state + (row * p.heads + h) * p.segments * int64_t(p.di) * p.dout +
+                                seg * int64_t(p.di) * p.dout
+                          : (OUT && p.s0 != nullptr ? p.s0 + state_at : nullptr);
+    const bool transposed = p.transposed && p.seg_state == nullptr;
+    const int per_k = transposed ? 1 : p.dout, per_col = transposed ? p.di : 1;
+#pragma unroll
+    for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+      for (int i = 0; i < kTilesI; ++i) {
+        s[n][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (s0 == nullptr) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int col = n0 + nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+          if (k < p.di && col < p.dout) s[n][i][r] = s0[unsigned(k * per_k + col * per_col)];
+        }
+      }
+  }
+
+  Loader<T, DI> la, lb;
+  Loader<T, NB> lc;
+  auto fetch = [&](int64_t u0) {
+    const int n = int(min(int64_t(kChunk), u_valid - u0));
+    const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
+    if (OUT) la.fetch(a, p.a.token, t0, dt, n, p.di);
+    lb.fetch(b, p.b.token, t0, dt, n, p.di);
+    lc.fetch(c, p.c.token, t0, dt, n, dout);
+  };
+  if (p.wide && u_begin < u_valid) fetch(u_begin);
+
+  for (int64_t u0 = u_begin; u0 < u_valid; u0 += kChunk) {
+    const int n_valid = int(min(int64_t(kChunk), u_valid - u0));
+    const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
+    const int tiles = (n_valid + kTile - 1) / kTile;       // of tokens that count
+    const bool last = u0 + kChunk >= u_valid;
+    if (p.wide) {
+      if (OUT) la.store(as);
+      lb.store(bs);
+      lc.store(cs);
+    } else {
+      if (OUT) Loader<T, DI>::copy(as, a, p.a.token, t0, dt, n_valid, p.di);
+      Loader<T, DI>::copy(bs, b, p.b.token, t0, dt, n_valid, p.di);
+      Loader<T, NB>::copy(cs, c, p.c.token, t0, dt, n_valid, dout);
+    }
+    __syncthreads();
+    if (p.wide && !last) fetch(u0 + kChunk);
+
+    if (OUT && wave < tiles) {
+      // the weights of tokens 16 wave .. 16 wave + 15
+      const int t = wave * kTile + l16;
+      eight av[kK];
+#pragma unroll
+      for (int kk = 0; kk < kK; ++kk) av[kk] = row_values<T, kAB>(as, t, kk, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i > (wave | 1)) continue;                      // blocks of 32 that the products below read
+        f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (i <= wave) {
+#pragma unroll
+          for (int kk = 0; kk < kK; ++kk) w = mma(row_values<T, kAB>(bs, i * kTile + l16, kk, g), av[kk], w);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int d = t - (i * kTile + 4 * g + r);
+            w[r] = d >= 0 ? w[r] * p.pscale * __builtin_amdgcn_exp2f(float(max(d, 0)) * log2_gamma) : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x)
+          *reinterpret_cast<four *>(ps[x] + t * kP + i * kTile + 4 * g) = take_piece(w, T());
+      }
+    }
+
+    __builtin_amdgcn_sched_barrier(0);  // operands of the next products are not read ahead: registers
+    eight cv[kTilesN][2];
+#pragma unroll
+    for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) cv[n][kk] = column_values<kC>(cs, nw + n * kTile, kk, lane);
+
+    f32x4 o[kTilesT][kTilesN];
+    if (OUT) {
+#pragma unroll
+      for (int t = 0; t < kTilesT; ++t)
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n) o[t][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int kk = 0; kk < kK; ++kk) {
+        eight sv[kTilesN][kPieces];
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n) {
+          f32x8 x = join(s[n][2 * kk], s[n][2 * kk + 1]);
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) sv[n][i] = take_piece(x, T());
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < kTilesT; ++t) {
+          if (wt * kTilesT + t >= tiles) continue;
+          const eight av = row_values<T, kAB>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
+#pragma unroll
+          for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) o[t][n] = mma(sv[n][i], av, o[t][n]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < kTilesT; ++t) {
+        const int u = (wt * kTilesT + t) * kTile + l16;
+        const float d = p.oscale * __builtin_amdgcn_exp2f(float(u + e) * log2_gamma);
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n) o[t][n] *= d;
+      }
+    }
+
+    __builtin_amdgcn_sched_barrier(0);
+    if (!OUT || !last || (p.s1 != nullptr && p.seg_state == nullptr)) {
+      const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
+#pragma unroll
+      for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+        for (int i = 0; i < kTilesI; ++i) s[n][i] *= d;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        if (kk * 32 >= n_valid) continue;
+        eight wv[kTilesN][kStatePieces];
+        f32x8 x[kTilesN];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+          const float w = p.sscale * __builtin_amdgcn_exp2f(float(max(n_valid - e - u, 0)) * log2_gamma);
+#pragma unroll
+          for (int n = 0; n < kTilesN; ++n) x[n][j] = to_f32(cv[n][kk][j]) * w;
+        }
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+          for (int i = 0; i < kStatePieces; ++i) wv[n][i] = take_piece(x[n], T());
+#pragma unroll
+        for (int i = 0; i < kTilesI; ++i) {
+          const eight bv = column_values<kAB>(bs, i * kTile, kk, lane);
+#pragma unroll
+          for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+            for (int x = 0; x < kStatePieces; ++x) s[n][i] = mma(bv, wv[n][x], s[n][i]);
+        }
+      }
+    }
+    __syncthreads();  // the weights are there, and a, b and c are read
+
+    if (OUT) {
+      O *out = static_cast<O *>(p.out) + (row * p.length * p.heads + h) * int64_t(p.dout) + n0;
+#pragma unroll
+      for (int t = 0; t < kTilesT; ++t) {
+        const int tt = wt * kTilesT + t;
+        if (tt >= tiles) continue;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          if (kk * 2 > tt) continue;
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            const eight pv = row_values<T, kP>(ps[i], tt * kTile + l16, kk, g);
+#pragma unroll
+            for (int n = 0; n < kTilesN; ++n) o[t][n] = mma(cv[n][kk], pv, o[t][n]);
+          }
+        }
+        const int u = tt * kTile + l16;
+        if (u >= n_valid) continue;
+        O *to = out + (t0 + int64_t(dt) * u) * p.heads * p.dout;
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n) {
+          const int col = nw + n * kTile + 4 * g;
+          typename Vec<O>::four v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = from_f32<O>(o[t][n][r]);
+          if (p.wide_out) {
+            if (col < dout) *reinterpret_cast<typename Vec<O>::four *>(to + col) = v;
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (col + r < dout) to[col + r] = v[r];
+          }
+        }
+      }
+    }
+  }
+
+  if (OUT) {  // tokens beyond the row's length
+    const int64_t t_begin = max(u_begin, len);
+    O *out = static_cast<O *>(p.out) + ((row * p.length + t_begin) * p.heads + h) * int64_t(p.dout) + n0;
+    const int per = 4;
+    const int cols = (dout + per - 1) / per;
+    for (int64_t i = threadIdx.x; i < (u_end - t_begin) * cols; i += kThreads) {
+      O *to = out + i / cols * p.heads * p.dout + i % cols * per;
+      if (p.wide_out)
+        *reinterpret_cast<typename Vec<O>::four *>(to) = typename Vec<O>::four{};
+      else
+        for (int r = 0; r < per && i % cols * per + r < dout; ++r) to[r] = from_f32<O>(0.0f);
+    }
+  }
+  float *s1 = OUT ? (p.seg_state == nullptr ? p.s1 : nullptr) : p.seg_state;
+  if (s1 == nullptr) return;
+  s1 += OUT ? state_at : (row * p.heads + h) * p.segments * int64_t(p.di) * p.dout + seg * int64_t(p.di) * p.dout;
+#pragma unroll
+  for (int n = 0; n < kTilesN; ++n)
+#pragma unroll
+    for (int i = 0; i < kTilesI; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int col = n0 + nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+        if (wt == 0 && k < p.di && col < p.dout) s1[unsigned(k * p.dout + col)] = s[n][i][r];
+      }
+}
+
+// The states that the segments of a row begin with, in place of the segments'
+// own, and the row's last state.
+__global__ __launch_bounds__(kThreads) void join_kernel(ScanArgs p, int64_t first) {
+  const int64_t size = int64_t(p.di) * p.dout, parts = (size + kThreads - 1) / kThreads;
+  const int64_t block = first + blockIdx.x, rh = block / parts, at = block % parts * kThreads + threadIdx.x;
+  if (at >= size) return;
+  const float log2_gamma = head_log_decay(p.log_decay, int(rh % p.heads), nullptr, false) * 1.44269504088896341f;
+  const int64_t len = row_length(p.len, rh / p.heads, p.length, nullptr, false);
+  float cur = 0.0f;
+  if (p.s0 != nullptr) cur = p.s0[rh * size + (p.transposed ? at % p.dout * p.di + at / p.dout : at)];
+  float *x = p.seg_state + rh * p.segments * size + at;
+  constexpr int kAhead = 8;
+  for (int64_t seg = 0; seg < p.segments; seg += kAhead) {
+    float own[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) own[i] = seg + i < p.segments ? x[(seg + i) * size] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (seg + i >= p.segments) break;
+      x[(seg + i) * size] = cur;
+      const int64_t n = max(int64_t(0), min(p.segment, len - (seg + i) * p.segment));
+      cur = fmaf(cur, __builtin_amdgcn_exp2f(float(n) * log2_gamma), own[i]);
+    }
+  }
+  if (p.s1 != nullptr) p.s1[rh * size + at] = cur;
+}
+
+template <class T, class O, bool OUT>
+rdf2v_status launch_chunks(const ScanArgs &p, hipStream_t stream) {
+  return for_each_launch(p.rows * p.heads * p.segments * p.blocks_n, kThreads, 1, [&](int64_t first, int64_t count) {
+    const dim3 grid{unsigned(count)}, threads(kThreads);
+    const int di = p.di <= 32 ? 32 : p.di <= 64 ? 64 : 128, nb = p.dout <= 32 ? 32 : p.dout <= 64 ? 64 : 128;
+#define RDF2V_SCAN(DI, NB) \
+  if (di == DI && nb == NB) scan_kernel<T, O, DI, NB, OUT><<<grid, threads, 0, stream>>>(p, first);
+    RDF2V_SCAN(32, 32) RDF2V_SCAN(32, 64) RDF2V_SCAN(32, 128)
+    RDF2V_SCAN(64, 32) RDF2V_SCAN(64, 64) RDF2V_SCAN(64, 128)
+    RDF2V_SCAN(128, 32) RDF2V_SCAN(128, 64) RDF2V_SCAN(128, 128)
+#undef RDF2V_SCAN
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });
 }
+
+// Segments of a row: one, unless there are too few rows and heads to fill the
+// chip with a workgroup each. Then a row is cut into segments of whole chunks,
+// the states of the segments are computed first and joined, and all segments
+// run at once: b and c are read twice, and a state is written and read for
+// each segment. At least kLeastChunks chunks to a segment keep that traffic
+// below what the segment itself reads.
+constexpr int64_t kFill = 512;
+constexpr int64_t kLeastChunks = 4;
+
+int64_t segment_count(int64_t rows, int64_t length, int64_t heads) {
+  const int64_t chunks = (length + kChunk - 1) / kChunk, base = rows * heads;
+  if (base >= kFill || chunks < 2 * kLeastChunks) return 1;
+  const int64_t want = (kFill + base - 1) / base, most = chunks / kLeastChunks;
+  const int64_t count = want < most ? want : most, per = (chunks + count - 1) / count;
+  return (chunks + per - 1) / per;
+}
+
+template <class T, class O>
+rdf2v_status launch_scan(ScanArgs p, float *seg_state, hipStream_t stream) {
+  p.pscale = p.oscale * p.sscale;
+  p.blocks_n = 1;
+  p.segments = segment_count(p.rows, p.length, p.heads);
+  const int64_t chunks = (p.length + kChunk - 1) / kChunk;
+  p.segment = (chunks + p.segments - 1) / p.segments * kChunk;
+  auto fits = [](const ScanOperand &x, int d) {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(x.data) |
+                          uintptr_t(x.row | x.token | x.head | int64_t(d)) * sizeof(T);
+    return (all & 15) == 0;
+  };
+  p.wide = fits(p.a, p.di) && fits(p.b, p.di) && fits(p.c, p.dout);
+  p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
+  if (p.segments == 1) return launch_chunks<T, O, true>(p, stream);
+  p.seg_state = seg_state;
+  rdf2v_status st = launch_chunks<T, O, false>(p, stream);
+  if (st != RDF2V_OK) return st;
+  const int64_t parts = (int64_t(p.di) * p.dout + kThreads - 1) / kThreads;
+  st = for_each_launch(p.rows * p.heads * parts, kThreads, 1, [&](int64_t first, int64_t count) {
+    join_kernel<<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
+  return st == RDF2V_OK ? launch_chunks<T, O, true>(p, stream) : st;
+}
+
+size_t segment_state_bytes(const rdf2v_attention &a) {
+  const int64_t segments = segment_count(a.rows, a.length, a.heads);
+  return segments == 1 ? 0 : align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float), 256);
+}
+
+constexpr int kColumns = 64;  // columns of S per workgroup of the step, one to a lane
 
 // Sums of the gradients of `share` query heads, in head order.
 template <class T>
@@ -176,8 +600,8 @@ ScanArgs scan_args(const rdf2v_attention &a, int32_t *status) {
 
 template <class T>
 rdf2v_status forward(const rdf2v_attention &a, const rdf2v_heads_view &q, const rdf2v_heads_view &k,
-                     const rdf2v_heads_view &v, const float *state, void *out, float *state_out, int32_t *status,
-                     hipStream_t stream) {
+                     const rdf2v_heads_view &v, const float *state, void *out, float *state_out, void *workspace,
+                     int32_t *status, hipStream_t stream) {
   const int share = a.heads / a.kv_heads;
   ScanArgs p = scan_args(a, status);
   p.a = operand(q, 1);
@@ -189,7 +613,7 @@ rdf2v_status forward(const rdf2v_attention &a, const rdf2v_heads_view &q, const 
   p.s1 = state_out;
   p.out = out;
   p.oscale = a.scale;
-  return launch_scan<T, T>(p, stream);
+  return launch_scan<T, T>(p, static_cast<float *>(workspace), stream);
 }
 
 template <class T>
@@ -199,6 +623,7 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
                       int32_t *status, hipStream_t stream) {
   const int share = a.heads / a.kv_heads;
   const int64_t tokens = a.rows * a.length;
+  float *seg = static_cast<float *>(workspace), *part = seg + segment_state_bytes(a) / sizeof(float);
   ScanArgs p = scan_args(a, status);
   p.a = operand(dout, 1);
   p.b = operand(v, share);
@@ -209,10 +634,9 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
   p.transposed = true;
   p.out = dq;
   p.oscale = a.scale;
-  rdf2v_status st = launch_scan<T, T>(p, stream);
+  rdf2v_status st = launch_scan<T, T>(p, seg, stream);
   if (st != RDF2V_OK) return st;
 
-  float *part = static_cast<float *>(workspace);
   p = scan_args(a, status);
   p.reverse = true;
   p.sscale = a.scale;
@@ -224,7 +648,7 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
   p.s0 = dstate_out;
   p.transposed = true;
   p.out = share > 1 ? part : dk;
-  st = share > 1 ? launch_scan<T, float>(p, stream) : launch_scan<T, T>(p, stream);
+  st = share > 1 ? launch_scan<T, float>(p, seg, stream) : launch_scan<T, T>(p, seg, stream);
   if (st == RDF2V_OK && share > 1) st = launch_share_sum<T>(part, dk, tokens * a.kv_heads, share, a.dk, stream);
   if (st != RDF2V_OK) return st;
 
@@ -236,7 +660,7 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
   p.transposed = false;
   p.out = share > 1 ? part : dv;
   p.s1 = dstate;
-  st = share > 1 ? launch_scan<T, float>(p, stream) : launch_scan<T, T>(p, stream);
+  st = share > 1 ? launch_scan<T, float>(p, seg, stream) : launch_scan<T, T>(p, seg, stream);
   if (st == RDF2V_OK && share > 1) st = launch_share_sum<T>(part, dv, tokens * a.kv_heads, share, a.dv, stream);
   return st;
 }
@@ -289,15 +713,16 @@ __global__ __launch_bounds__(kColumns) void step_kernel(StepArgs p, int64_t firs
 }  // namespace
 
 size_t decay_attention_workspace_bytes(const rdf2v_attention &a, bool backward) {
-  if (!backward || a.heads == a.kv_heads) return 0;
-  return align_up(size_t(a.rows) * a.length * a.heads * (a.dk > a.dv ? a.dk : a.dv) * sizeof(float), 256);
+  const size_t seg = segment_state_bytes(a);
+  if (!backward || a.heads == a.kv_heads) return seg;
+  return seg + align_up(size_t(a.rows) * a.length * a.heads * (a.dk > a.dv ? a.dk : a.dv) * sizeof(float), 256);
 }
 
 rdf2v_status launch_decay_attention(const rdf2v_attention &a, const rdf2v_heads_view &q, const rdf2v_heads_view &k,
                                     const rdf2v_heads_view &v, const float *state, void *out, float *state_out,
-                                    void *, int32_t *status_dev, hipStream_t stream) {
-  return a.dtype == RDF2V_BF16 ? forward<bf16>(a, q, k, v, state, out, state_out, status_dev, stream)
-                               : forward<float>(a, q, k, v, state, out, state_out, status_dev, stream);
+                                    void *workspace, int32_t *status_dev, hipStream_t stream) {
+  return a.dtype == RDF2V_BF16 ? forward<bf16>(a, q, k, v, state, out, state_out, workspace, status_dev, stream)
+                               : forward<float>(a, q, k, v, state, out, state_out, workspace, status_dev, stream);
 }
 
 rdf2v_status launch_decay_attention_backward(const rdf2v_attention &a, const rdf2v_heads_view &q,
