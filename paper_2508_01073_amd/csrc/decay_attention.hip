@@ -71,7 +71,7 @@ __device__ __forceinline__ const T *operand_row(const ScanOperand &x, int64_t ro
 }
 
 constexpr int kChunk = 64;      // tokens of a chunk
-constexpr int kThreads = 256;   // four waves
+constexpr int kThreads = 256;   // of the kernels below that are not scans
 constexpr int kTile = 16;       // rows and columns of a matrix instruction
 
 // Eight values of a row or column that one lane feeds to a matrix instruction.
@@ -119,27 +119,29 @@ __device__ __forceinline__ f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
-// The next piece of x: x to the element type, and what is left in x.
-__device__ __forceinline__ bf16x8 take_piece(f32x8 &x, bf16) {
-  bf16x8 p;
+// The next piece of x: x rounded to the element type, and what is left in x.
+template <class F>
+__device__ __forceinline__ auto take_piece(F &x, bf16) {
+  constexpr int kN = sizeof(F) / 4;
+  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  typedef unsigned words __attribute__((ext_vector_type(kN / 2)));
+  typedef bf16 piece __attribute__((ext_vector_type(kN)));
+  words p;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    p[j] = bf16(x[j]);
-    x[j] -= float(p[j]);
+  for (int j = 0; j < kN; j += 2) {
+    p[j / 2] = __builtin_bit_cast(unsigned, bf16x2{bf16(x[j]), bf16(x[j + 1])});
+    x[j] -= __uint_as_float(p[j / 2] << 16);
+    x[j + 1] -= __uint_as_float(p[j / 2] & 0xffff0000u);
   }
-  return p;
+  return __builtin_bit_cast(piece, p);
 }
-__device__ __forceinline__ f32x8 take_piece(f32x8 &x, float) { return x; }
-__device__ __forceinline__ bf16x4 take_piece(f32x4 &x, bf16) {
-  bf16x4 p;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    p[j] = bf16(x[j]);
-    x[j] -= float(p[j]);
-  }
-  return p;
+template <class F>
+__device__ __forceinline__ F take_piece(F &x, float) {
+  return x;
 }
-__device__ __forceinline__ f32x4 take_piece(f32x4 &x, float) { return x; }
+
+// LDS reads are not moved ahead of this: what they would hold costs registers.
+__device__ __forceinline__ void keep_order() { asm volatile("" ::: "memory"); }
 
 // Values of row `row`, indices of block kk, of a tile of rows in LDS.
 template <class T, int STRIDE>
@@ -170,38 +172,39 @@ __device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int 
 
 // A chunk's rows of one operand on their way from memory to LDS: 64 rows of W
 // values, zeros beyond the operand's size and beyond the chunk's `n` tokens.
-template <class T, int W>
+// Every thread reads the same columns of rows kRows apart.
+template <class T, int W, int THREADS>
 struct Loader {
   typedef typename Vec<T>::load load;
-  static constexpr int kPer = 16 / sizeof(T), kStride = W + Vec<T>::kPad;
-  static constexpr int kLoads = kChunk * W / kPer / kThreads;
+  static constexpr int kPer = 16 / sizeof(T), kStride = W + Vec<T>::kPad, kCols = W / kPer;
+  static constexpr int kRows = THREADS / kCols < kChunk ? THREADS / kCols : kChunk;
+  static constexpr int kLoads = kChunk / kRows;
   load r[kLoads];
 
-  // Row of a token: token u of the scan is t0 + dt * u of the row.
-  static __device__ __forceinline__ const T *row(const T *p, int64_t token, int64_t t0, int dt, int u) {
-    return p + (t0 + int64_t(dt) * u) * token;
-  }
-  __device__ __forceinline__ void fetch(const T *p, int64_t token, int64_t t0, int dt, int n, int size) {
+  // `chunk` points to the chunk's first token in the scan's order, `token` is
+  // the distance to the next one. What is not there is read from a place that
+  // is, and dropped on the way to LDS, so that the reads need no branches.
+  __device__ __forceinline__ void fetch(unsigned thread, const T *chunk, int64_t token, int n, int size) {
+    const int u = thread / kCols, col = thread % kCols * kPer;
+    const T *at = chunk + (col < size ? col : 0);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = i * kThreads + threadIdx.x, u = at / (W / kPer), col = at % (W / kPer) * kPer;
-      r[i] = load{};
-      if (u < n && col < size) r[i] = *reinterpret_cast<const load *>(row(p, token, t0, dt, u) + col);
-    }
+    for (int i = 0; i < kLoads; ++i)
+      r[i] = *reinterpret_cast<const load *>(at + min(u + i * kRows, n - 1) * token);
   }
-  __device__ __forceinline__ void store(T *tile) const {
+  __device__ __forceinline__ void store(unsigned thread, T *tile, int n, int size) const {
+    const int u = thread / kCols, col = thread % kCols * kPer;
+    if (THREADS / kCols > kChunk && u >= kRows) return;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = i * kThreads + threadIdx.x, u = at / (W / kPer), col = at % (W / kPer) * kPer;
-      *reinterpret_cast<load *>(tile + u * kStride + col) = r[i];
-    }
+    for (int i = 0; i < kLoads; ++i)
+      *reinterpret_cast<load *>(tile + (u + i * kRows) * kStride + col) =
+          u + i * kRows < n && col < size ? r[i] : load{};
   }
   // Value by value, for rows that 16-byte reads do not fit.
-  static __device__ __forceinline__ void copy(T *tile, const T *p, int64_t token, int64_t t0, int dt, int n,
+  static __device__ __forceinline__ void copy(unsigned thread, T *tile, const T *chunk, int64_t token, int n,
                                               int size) {
-    for (int at = threadIdx.x; at < kChunk * W; at += kThreads) {
+    for (int at = thread; at < kChunk * W; at += THREADS) {
       const int u = at / W, col = at % W;
-      tile[u * kStride + col] = u < n && col < size ? row(p, token, t0, dt, u)[col] : T(0.0f);
+      tile[u * kStride + col] = u < n && col < size ? chunk[u * token + col] : T(0.0f);
     }
   }
 };
@@ -214,15 +217,24 @@ struct Loader {
 // gamma^{t+e} S^T a_t; then S becomes gamma^n S + sum_s gamma^{n-e-s} b_s c_s^T.
 // Every wave owns some columns of S, which stay in its registers as the
 // accumulators of the update and, in the order above, are the operands of the
-// earlier chunks' part; wave w computes the weights of tokens 16 w .. 16 w + 15
-// for all, through LDS. The next chunk is fetched while this one is computed.
+// earlier chunks' part; the weights are computed once, a wave a tile of 16
+// tokens, and shared through LDS. The next chunk is fetched while this one is
+// computed.
 //
 // OUT: outputs are wanted; otherwise only S of the segment (from zeros).
+//
+// A tile of 16 columns to a wave keeps all of that in 128 registers up to heads
+// of 128, so that 16 waves share a CU; two tiles to a wave spilled, and the
+// waits for the spills made it 2.x times slower.
+constexpr int scan_waves(int nb) { return nb > 64 ? 8 : 4; }
+
 template <class T, class O, int DI, int NB, bool OUT>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(ScanArgs p, int64_t first) {
-  constexpr int kWavesN = NB >= 64 ? 4 : NB / kTile;       // waves side by side over the columns
-  constexpr int kWavesT = 4 / kWavesN;                     // and over the chunk's tokens
-  constexpr int kTilesN = NB / kTile / kWavesN, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
+__global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) void scan_kernel(ScanArgs p,
+                                                                                             int64_t first) {
+  constexpr int kWaves = scan_waves(NB), kThreads = kWaves * kWave;
+  constexpr int kWavesN = NB / kTile;                      // waves side by side over the columns
+  constexpr int kWavesT = kWaves / kWavesN;                // and over the chunk's tokens
+  constexpr int kTilesN = 1, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
   constexpr int kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
   constexpr int kAB = DI + Vec<T>::kPad, kC = NB + Vec<T>::kPad, kP = kChunk + Vec<T>::kPad;
   __shared__ __attribute__((aligned(16))) T as[OUT ? kChunk * kAB : 1], bs[kChunk * kAB], cs[kChunk * kC];
@@ -235,12 +247,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
   const int64_t seg = block / p.blocks_n % p.segments;
   const int h = int(block / p.blocks_n / p.segments % p.heads);
   const int64_t row = block / p.blocks_n / p.segments / p.heads;
-  const int wave = threadIdx.x / kWave, lane = lane_id(), l16 = lane % 16, g = lane / 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lane = lane_id(), l16 = lane % 16, g = lane / 16;
   const int wn = wave % kWavesN, wt = wave / kWavesN;
   const int n0 = nb * NB;                                  // first column of the workgroup
   const int nw = wn * kTilesN * kTile;                     // first column of the wave in it
   const bool report = nb == 0 && seg == 0 && threadIdx.x == 0;
-  const float log2_gamma = head_log_decay(p.log_decay, h, p.status, report && row == 0) * 1.44269504088896341f;
+  const float head_log2_gamma =
+      head_log_decay(p.log_decay, h, p.status, report && row == 0) * 1.44269504088896341f;
   const int64_t len = row_length(p.len, row, p.length, p.status, report && h == 0);
   const int e = p.reverse ? 0 : 1;
   const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h) + n0;
@@ -272,51 +286,59 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
       }
   }
 
-  Loader<T, DI> la, lb;
-  Loader<T, NB> lc;
-  auto fetch = [&](int64_t u0) {
+  Loader<T, DI, kThreads> la, lb;
+  Loader<T, NB, kThreads> lc;
+  auto fetch = [&](unsigned thread, int64_t u0) {
     const int n = int(min(int64_t(kChunk), u_valid - u0));
     const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
-    if (OUT) la.fetch(a, p.a.token, t0, dt, n, p.di);
-    lb.fetch(b, p.b.token, t0, dt, n, p.di);
-    lc.fetch(c, p.c.token, t0, dt, n, dout);
+    if (OUT) la.fetch(thread, a + t0 * p.a.token, dt * p.a.token, n, p.di);
+    lb.fetch(thread, b + t0 * p.b.token, dt * p.b.token, n, p.di);
+    lc.fetch(thread, c + t0 * p.c.token, dt * p.c.token, n, dout);
   };
-  if (p.wide && u_begin < u_valid) fetch(u_begin);
+  if (p.wide && u_begin < u_valid) fetch(threadIdx.x, u_begin);
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
 
   for (int64_t u0 = u_begin; u0 < u_valid; u0 += kChunk) {
+    // The decays and places of a chunk's tokens are the same in every chunk; kept for all of them they
+    // would take the registers that the products need, so they are computed again.
+    float log2_gamma = head_log2_gamma;
+    unsigned thread = threadIdx.x;
+    asm volatile("" : "+v"(log2_gamma), "+v"(thread));
+    const int lane = thread % kWave, l16 = lane % 16, g = lane / 16;
     const int n_valid = int(min(int64_t(kChunk), u_valid - u0));
     const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
     const int tiles = (n_valid + kTile - 1) / kTile;       // of tokens that count
     const bool last = u0 + kChunk >= u_valid;
     if (p.wide) {
-      if (OUT) la.store(as);
-      lb.store(bs);
-      lc.store(cs);
+      if (OUT) la.store(thread, as, n_valid, p.di);
+      lb.store(thread, bs, n_valid, p.di);
+      lc.store(thread, cs, n_valid, dout);
     } else {
-      if (OUT) Loader<T, DI>::copy(as, a, p.a.token, t0, dt, n_valid, p.di);
-      Loader<T, DI>::copy(bs, b, p.b.token, t0, dt, n_valid, p.di);
-      Loader<T, NB>::copy(cs, c, p.c.token, t0, dt, n_valid, dout);
+      if (OUT) la.copy(thread, as, a + t0 * p.a.token, dt * p.a.token, n_valid, p.di);
+      lb.copy(thread, bs, b + t0 * p.b.token, dt * p.b.token, n_valid, p.di);
+      lc.copy(thread, cs, c + t0 * p.c.token, dt * p.c.token, n_valid, dout);
     }
     __syncthreads();
-    if (p.wide && !last) fetch(u0 + kChunk);
+    if (p.wide && !last) fetch(thread, u0 + kChunk);
 
-    if (OUT && wave < tiles) {
-      // the weights of tokens 16 wave .. 16 wave + 15
-      const int t = wave * kTile + l16;
+    if (OUT && wave % 4 < tiles) {
+      // the weights of tokens 16 w .. 16 w + 15, and of half of the tokens before them where two waves share
+      const int w4 = wave % 4, t = w4 * kTile + l16;
       eight av[kK];
 #pragma unroll
       for (int kk = 0; kk < kK; ++kk) av[kk] = row_values<T, kAB>(as, t, kk, g);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i > (wave | 1)) continue;                      // blocks of 32 that the products below read
+      for (int j = 0; j < 16 / kWaves; ++j) {
+        const int i = wave / 4 * (16 / kWaves) + j;
+        if (i > (w4 | 1)) continue;                        // blocks of 32 that the products below read
         f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (i <= wave) {
+        if (i <= w4) {
 #pragma unroll
           for (int kk = 0; kk < kK; ++kk) w = mma(row_values<T, kAB>(bs, i * kTile + l16, kk, g), av[kk], w);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int d = t - (i * kTile + 4 * g + r);
-            w[r] = d >= 0 ? w[r] * p.pscale * __builtin_amdgcn_exp2f(float(max(d, 0)) * log2_gamma) : 0.0f;
+            w[r] *= d >= 0 ? p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
           }
         }
 #pragma unroll
@@ -325,7 +347,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
       }
     }
 
-    __builtin_amdgcn_sched_barrier(0);  // operands of the next products are not read ahead: registers
+    keep_order();
     eight cv[kTilesN][2];
 #pragma unroll
     for (int n = 0; n < kTilesN; ++n)
@@ -347,10 +369,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
 #pragma unroll
           for (int i = 0; i < kPieces; ++i) sv[n][i] = take_piece(x, T());
         }
-        __builtin_amdgcn_sched_barrier(0);
+        keep_order();
 #pragma unroll
         for (int t = 0; t < kTilesT; ++t) {
           if (wt * kTilesT + t >= tiles) continue;
+          keep_order();
           const eight av = row_values<T, kAB>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
 #pragma unroll
           for (int n = 0; n < kTilesN; ++n)
@@ -367,7 +390,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
       }
     }
 
-    __builtin_amdgcn_sched_barrier(0);
+    keep_order();
     if (!OUT || !last || (p.s1 != nullptr && p.seg_state == nullptr)) {
       const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
 #pragma unroll
@@ -392,6 +415,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
           for (int i = 0; i < kStatePieces; ++i) wv[n][i] = take_piece(x[n], T());
 #pragma unroll
         for (int i = 0; i < kTilesI; ++i) {
+          if (i % 4 == 0) keep_order();
           const eight bv = column_values<kAB>(bs, i * kTile, kk, lane);
 #pragma unroll
           for (int n = 0; n < kTilesN; ++n)
@@ -403,7 +427,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
     __syncthreads();  // the weights are there, and a, b and c are read
 
     if (OUT) {
-      O *out = static_cast<O *>(p.out) + (row * p.length * p.heads + h) * int64_t(p.dout) + n0;
+      O *out = static_cast<O *>(p.out) + ((row * p.length + t0) * p.heads + h) * int64_t(p.dout) + n0;
 #pragma unroll
       for (int t = 0; t < kTilesT; ++t) {
         const int tt = wt * kTilesT + t;
@@ -411,6 +435,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
           if (kk * 2 > tt) continue;
+          keep_order();
 #pragma unroll
           for (int i = 0; i < kPieces; ++i) {
             const eight pv = row_values<T, kP>(ps[i], tt * kTile + l16, kk, g);
@@ -420,7 +445,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void scan_kernel(
         }
         const int u = tt * kTile + l16;
         if (u >= n_valid) continue;
-        O *to = out + (t0 + int64_t(dt) * u) * p.heads * p.dout;
+        O *to = out + dt * u * (p.heads * p.dout);  // 64 tokens of 65,535 heads stay below 2^31
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n) {
           const int col = nw + n * kTile + 4 * g;
@@ -495,9 +520,9 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ScanArgs p, int64_t firs
 
 template <class T, class O, bool OUT>
 rdf2v_status launch_chunks(const ScanArgs &p, hipStream_t stream) {
-  return for_each_launch(p.rows * p.heads * p.segments * p.blocks_n, kThreads, 1, [&](int64_t first, int64_t count) {
-    const dim3 grid{unsigned(count)}, threads(kThreads);
+  return for_each_launch(p.rows * p.heads * p.segments * p.blocks_n, 8 * kWave, 1, [&](int64_t first, int64_t count) {
     const int di = p.di <= 32 ? 32 : p.di <= 64 ? 64 : 128, nb = p.dout <= 32 ? 32 : p.dout <= 64 ? 64 : 128;
+    const dim3 grid{unsigned(count)}, threads{unsigned(scan_waves(nb) * kWave)};
 #define RDF2V_SCAN(DI, NB) \
   if (di == DI && nb == NB) scan_kernel<T, O, DI, NB, OUT><<<grid, threads, 0, stream>>>(p, first);
     RDF2V_SCAN(32, 32) RDF2V_SCAN(32, 64) RDF2V_SCAN(32, 128)
