@@ -97,14 +97,14 @@ struct Vec<bf16> {
   // chunk's pairs and the states are fed as two bfloat16 pieces (16 bits, so
   // that bfloat16 outputs are off by little more than their own rounding), the
   // addends of the states, which are float32 outputs, as three (24 bits).
-  static constexpr int kPieces = 2, kStatePieces = 3, kPad = 8;
+  static constexpr int kPieces = 2, kStatePieces = 3;
 };
 template <>
 struct Vec<float> {
   typedef f32x4 four;
   typedef f32x8 eight;
   typedef f32x4 load;
-  static constexpr int kPieces = 1, kStatePieces = 1, kPad = 4;
+  static constexpr int kPieces = 1, kStatePieces = 1;
 };
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -143,30 +143,52 @@ __device__ __forceinline__ F take_piece(F &x, float) {
 // LDS reads are not moved ahead of this: what they would hold costs registers.
 __device__ __forceinline__ void keep_order() { asm volatile("" ::: "memory"); }
 
-// Values of row `row`, indices of block kk, of a tile of rows in LDS.
-template <class T, int STRIDE>
+// A tile of rows of W values in LDS. In bfloat16 the groups of four values of a
+// row are permuted by the row: reads of one group of 16 rows (an operand's
+// row) and of four groups of 8 rows (the transposing reads) then meet every
+// bank once in half a wave; padded rows had conflicts in one or the other.
+// Pairs of groups stay together for the 16-byte writes. Float32 rows are padded
+// by 16 bytes, which is free of conflicts there.
+template <class T, int W>
+struct Tile;
+template <int W>
+struct Tile<bf16, W> {
+  static constexpr int kSize = kChunk * W;
+  static __device__ __forceinline__ int at(int row, int group) {
+    const int swap = (row % 8 * (W / 4) / 32 * 4 | row / 8 % 2 * 2) % (W / 4);
+    return row * W + (group ^ swap) * 4;
+  }
+};
+template <int W>
+struct Tile<float, W> {
+  static constexpr int kSize = kChunk * (W + 4);
+  static __device__ __forceinline__ int at(int row, int group) { return row * (W + 4) + group * 4; }
+};
+
+// Values of row `row`, indices of block kk.
+template <int W, class T>
 __device__ __forceinline__ typename Vec<T>::eight row_values(const T *tile, int row, int kk, int g) {
   typedef typename Vec<T>::four four;
-  const T *p = tile + row * STRIDE + kk * 32 + 4 * g;
-  return join(*reinterpret_cast<const four *>(p), *reinterpret_cast<const four *>(p + 16));
+  return join(*reinterpret_cast<const four *>(tile + Tile<T, W>::at(row, kk * 8 + g)),
+              *reinterpret_cast<const four *>(tile + Tile<T, W>::at(row, kk * 8 + 4 + g)));
 }
 // Values of column col0 + l % 16, rows of block kk. In bfloat16 the transposing
 // LDS read gives lane l of 16 the column l of the four rows that the lanes
 // 4 row + (0 .. 3) address.
-template <int STRIDE>
+template <int W>
 __device__ __forceinline__ bf16x8 column_values(const bf16 *tile, int col0, int kk, int lane) {
   typedef __attribute__((address_space(3))) i16x4 lds4;
-  const bf16 *p = tile + (kk * 32 + 4 * (lane / 16) + lane % 16 / 4) * STRIDE + col0 + 4 * (lane % 4);
-  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p));
-  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(p + 16 * STRIDE));
+  const int row = kk * 32 + 4 * (lane / 16) + lane % 16 / 4, group = col0 / 4 + lane % 4;
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + Tile<bf16, W>::at(row, group)));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + Tile<bf16, W>::at(row + 16, group)));
   return join(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi));
 }
-template <int STRIDE>
+template <int W>
 __device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int kk, int lane) {
-  const float *p = tile + (kk * 32 + 4 * (lane / 16)) * STRIDE + col0 + lane % 16;
+  const float *p = tile + Tile<float, W>::at(kk * 32 + 4 * (lane / 16), col0 / 4) + lane % 16;
   f32x8 x;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = p[(16 * (j / 4) + j % 4) * STRIDE];
+  for (int j = 0; j < 8; ++j) x[j] = p[(16 * (j / 4) + j % 4) * (W + 4)];
   return x;
 }
 
@@ -176,35 +198,43 @@ __device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int 
 template <class T, int W, int THREADS>
 struct Loader {
   typedef typename Vec<T>::load load;
-  static constexpr int kPer = 16 / sizeof(T), kStride = W + Vec<T>::kPad, kCols = W / kPer;
+  static constexpr int kPer = 16 / sizeof(T), kCols = W / kPer;
   static constexpr int kRows = THREADS / kCols < kChunk ? THREADS / kCols : kChunk;
   static constexpr int kLoads = kChunk / kRows;
   load r[kLoads];
 
-  // `chunk` points to the chunk's first token in the scan's order, `token` is
-  // the distance to the next one. What is not there is read from a place that
-  // is, and dropped on the way to LDS, so that the reads need no branches.
-  __device__ __forceinline__ void fetch(unsigned thread, const T *chunk, int64_t token, int n, int size) {
+  // `low` points to the chunk's token of the lowest number, `token` is the
+  // distance to the next one (64 of them stay below 2^31 bytes). What is not
+  // there is read from a place that is, and dropped on the way to LDS.
+  __device__ __forceinline__ void fetch(unsigned thread, const T *low, int token, bool reverse, int n, int size) {
     const int u = thread / kCols, col = thread % kCols * kPer;
-    const T *at = chunk + (col < size ? col : 0);
+    const unsigned at = col < size ? col : 0;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      r[i] = *reinterpret_cast<const load *>(at + min(u + i * kRows, n - 1) * token);
+    for (int i = 0; i < kLoads; ++i) {
+      const int row = min(u + i * kRows, n - 1);
+      r[i] = *reinterpret_cast<const load *>(low + (unsigned(__mul24(reverse ? n - 1 - row : row, token)) + at));
+    }
   }
   __device__ __forceinline__ void store(unsigned thread, T *tile, int n, int size) const {
     const int u = thread / kCols, col = thread % kCols * kPer;
     if (THREADS / kCols > kChunk && u >= kRows) return;
+    if (n == kChunk && size == W) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      *reinterpret_cast<load *>(tile + (u + i * kRows) * kStride + col) =
-          u + i * kRows < n && col < size ? r[i] : load{};
+      for (int i = 0; i < kLoads; ++i)
+        *reinterpret_cast<load *>(tile + Tile<T, W>::at(u + i * kRows, col / 4)) = r[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        *reinterpret_cast<load *>(tile + Tile<T, W>::at(u + i * kRows, col / 4)) =
+            u + i * kRows < n && col < size ? r[i] : load{};
+    }
   }
   // Value by value, for rows that 16-byte reads do not fit.
   static __device__ __forceinline__ void copy(unsigned thread, T *tile, const T *chunk, int64_t token, int n,
                                               int size) {
     for (int at = thread; at < kChunk * W; at += THREADS) {
       const int u = at / W, col = at % W;
-      tile[u * kStride + col] = u < n && col < size ? chunk[u * token + col] : T(0.0f);
+      tile[Tile<T, W>::at(u, col / 4) + col % 4] = u < n && col < size ? chunk[u * token + col] : T(0.0f);
     }
   }
 };
@@ -236,9 +266,9 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   constexpr int kWavesT = kWaves / kWavesN;                // and over the chunk's tokens
   constexpr int kTilesN = 1, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
   constexpr int kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
-  constexpr int kAB = DI + Vec<T>::kPad, kC = NB + Vec<T>::kPad, kP = kChunk + Vec<T>::kPad;
-  __shared__ __attribute__((aligned(16))) T as[OUT ? kChunk * kAB : 1], bs[kChunk * kAB], cs[kChunk * kC];
-  __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? kChunk * kP : 1];
+  __shared__ __attribute__((aligned(16))) T as[OUT ? Tile<T, DI>::kSize : 1], bs[Tile<T, DI>::kSize],
+      cs[Tile<T, NB>::kSize];
+  __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? Tile<T, kChunk>::kSize : 1];
   typedef typename Vec<T>::four four;
   typedef typename Vec<T>::eight eight;
 
@@ -262,6 +292,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   const int64_t u_begin = seg * p.segment, u_end = min(p.length, u_begin + p.segment);
   const int64_t u_valid = min(u_end, len);
   const int dt = p.reverse ? -1 : 1;
+  // a state that is written needs all three pieces of its addends; one that only outputs are made of, two
+  const bool exact_state = !OUT || (p.s1 != nullptr && p.seg_state == nullptr);
 
   f32x4 s[kTilesN][kTilesI];
   const int64_t state_at = (row * p.heads + h) * int64_t(p.di) * p.dout;
@@ -291,9 +323,10 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   auto fetch = [&](unsigned thread, int64_t u0) {
     const int n = int(min(int64_t(kChunk), u_valid - u0));
     const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
-    if (OUT) la.fetch(thread, a + t0 * p.a.token, dt * p.a.token, n, p.di);
-    lb.fetch(thread, b + t0 * p.b.token, dt * p.b.token, n, p.di);
-    lc.fetch(thread, c + t0 * p.c.token, dt * p.c.token, n, dout);
+    const int64_t low = p.reverse ? t0 - (n - 1) : t0;
+    if (OUT) la.fetch(thread, a + low * p.a.token, int(p.a.token), p.reverse, n, p.di);
+    lb.fetch(thread, b + low * p.b.token, int(p.b.token), p.reverse, n, p.di);
+    lc.fetch(thread, c + low * p.c.token, int(p.c.token), p.reverse, n, dout);
   };
   if (p.wide && u_begin < u_valid) fetch(threadIdx.x, u_begin);
   __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
@@ -326,7 +359,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       const int w4 = wave % 4, t = w4 * kTile + l16;
       eight av[kK];
 #pragma unroll
-      for (int kk = 0; kk < kK; ++kk) av[kk] = row_values<T, kAB>(as, t, kk, g);
+      for (int kk = 0; kk < kK; ++kk) av[kk] = row_values<DI>(as, t, kk, g);
 #pragma unroll
       for (int j = 0; j < 16 / kWaves; ++j) {
         const int i = wave / 4 * (16 / kWaves) + j;
@@ -334,7 +367,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
         if (i <= w4) {
 #pragma unroll
-          for (int kk = 0; kk < kK; ++kk) w = mma(row_values<T, kAB>(bs, i * kTile + l16, kk, g), av[kk], w);
+          for (int kk = 0; kk < kK; ++kk) w = mma(row_values<DI>(bs, i * kTile + l16, kk, g), av[kk], w);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int d = t - (i * kTile + 4 * g + r);
@@ -343,7 +376,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         }
 #pragma unroll
         for (int x = 0; x < kPieces; ++x)
-          *reinterpret_cast<four *>(ps[x] + t * kP + i * kTile + 4 * g) = take_piece(w, T());
+          *reinterpret_cast<four *>(ps[x] + Tile<T, kChunk>::at(t, i * 4 + g)) = take_piece(w, T());
       }
     }
 
@@ -352,7 +385,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
     for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) cv[n][kk] = column_values<kC>(cs, nw + n * kTile, kk, lane);
+      for (int kk = 0; kk < 2; ++kk) cv[n][kk] = column_values<NB>(cs, nw + n * kTile, kk, lane);
 
     f32x4 o[kTilesT][kTilesN];
     if (OUT) {
@@ -374,7 +407,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         for (int t = 0; t < kTilesT; ++t) {
           if (wt * kTilesT + t >= tiles) continue;
           keep_order();
-          const eight av = row_values<T, kAB>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
+          const eight av = row_values<DI>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
 #pragma unroll
           for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
@@ -391,8 +424,9 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     }
 
     keep_order();
-    if (!OUT || !last || (p.s1 != nullptr && p.seg_state == nullptr)) {
+    if (!last || exact_state) {
       const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
+      const float left = float(n_valid - e - 4 * g);  // gamma^{n-e-u}; tokens u >= n have no c
 #pragma unroll
       for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
@@ -404,23 +438,25 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         f32x8 x[kTilesN];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-          const float w = p.sscale * __builtin_amdgcn_exp2f(float(max(n_valid - e - u, 0)) * log2_gamma);
+          const float w = p.sscale * __builtin_amdgcn_exp2f(
+                                         fmaxf(left - float(32 * kk + 16 * (j / 4) + j % 4), 0.0f) * log2_gamma);
 #pragma unroll
           for (int n = 0; n < kTilesN; ++n) x[n][j] = to_f32(cv[n][kk][j]) * w;
         }
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
-          for (int i = 0; i < kStatePieces; ++i) wv[n][i] = take_piece(x[n], T());
+          for (int i = 0; i < kStatePieces; ++i)
+            if (i < 2 || exact_state) wv[n][i] = take_piece(x[n], T());
 #pragma unroll
         for (int i = 0; i < kTilesI; ++i) {
           if (i % 4 == 0) keep_order();
-          const eight bv = column_values<kAB>(bs, i * kTile, kk, lane);
+          const eight bv = column_values<DI>(bs, i * kTile, kk, lane);
 #pragma unroll
           for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
-            for (int x = 0; x < kStatePieces; ++x) s[n][i] = mma(bv, wv[n][x], s[n][i]);
+            for (int x = 0; x < kStatePieces; ++x)
+              if (x < 2 || exact_state) s[n][i] = mma(bv, wv[n][x], s[n][i]);
         }
       }
     }
@@ -438,7 +474,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
           keep_order();
 #pragma unroll
           for (int i = 0; i < kPieces; ++i) {
-            const eight pv = row_values<T, kP>(ps[i], tt * kTile + l16, kk, g);
+            const eight pv = row_values<kChunk>(ps[i], tt * kTile + l16, kk, g);
 #pragma unroll
             for (int n = 0; n < kTilesN; ++n) o[t][n] = mma(cv[n][kk], pv, o[t][n]);
           }
@@ -559,6 +595,7 @@ rdf2v_status launch_scan(ScanArgs p, float *seg_state, hipStream_t stream) {
   const int64_t chunks = (p.length + kChunk - 1) / kChunk;
   p.segment = (chunks + p.segments - 1) / p.segments * kChunk;
   auto fits = [](const ScanOperand &x, int d) {
+    if (x.token < 0 || x.token >= int64_t(1) << 23) return false;
     const uintptr_t all = reinterpret_cast<uintptr_t>(x.data) |
                           uintptr_t(x.row | x.token | x.head | int64_t(d)) * sizeof(T);
     return (all & 15) == 0;
