@@ -1,9 +1,15 @@
 // Beam search's selection and the reordering of states on gfx950.
 //
-// Of a beam only its num_out largest logits can be chosen, so a row of logits
-// is reduced to those and its log-sum-exp, and a group's beams are merged by
-// total. Places are compared as (value descending, index ascending), a total
-// order, so the choice does not depend on the order of the work.
+// Of a beam only the best logits can be chosen, so the logits are read once, in
+// slices of a workgroup each, and reduced to the slice's num_out + 1 best and
+// its part of the log-sum-exp; a workgroup per group then merges by total.
+// Places are compared as (value descending, index ascending), a total order,
+// so the choice does not depend on the order of the work.
+//
+// Totals are rounded sums, so logits that differ can have equal totals, of
+// which the lowest token counts. The last entry of a slice bounds the totals of
+// what the slice left out: only where that bound reaches the last chosen total
+// is the beam's row read again and its best found by total.
 
 #include "model.hpp"
 
@@ -11,9 +17,13 @@ namespace rdf2v {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
 constexpr float kInf = __builtin_huge_valf();
+constexpr int kVectors = 8;                    // 16-byte loads of a thread: 32 KB to a workgroup, all in flight
+constexpr int kSlice = kVectors * kThreads;    // vectors of a slice
+constexpr int kList = 1024;                    // candidates of a slice that are ranked at once
 
-// Descending (value, -index) as one unsigned number: larger is better.
+// Descending (value, -index) as one unsigned number: larger is better, 0 is none.
 __device__ __forceinline__ uint64_t order_key(float x, uint32_t index) {
   const uint32_t b = __float_as_uint(x + 0.0f);  // -0 becomes +0
   const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -25,6 +35,22 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - uint32_t(key); }
 
+// Largest value of a wave's lanes, in every lane: the row scan of
+// wave_inclusive_sum with the maximum.
+__device__ __forceinline__ float wave_max(float x) {
+  const int none = __float_as_int(-kInf);
+#define RDF2V_MAX_STEP(CTRL, ROWS) \
+  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(none, __float_as_int(x), CTRL, ROWS, 0xf, false)));
+  RDF2V_MAX_STEP(0x111, 0xf)
+  RDF2V_MAX_STEP(0x112, 0xf)
+  RDF2V_MAX_STEP(0x114, 0xf)
+  RDF2V_MAX_STEP(0x118, 0xf)
+  RDF2V_MAX_STEP(0x142, 0xa)
+  RDF2V_MAX_STEP(0x143, 0xc)
+#undef RDF2V_MAX_STEP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), kWave - 1));
+}
+
 template <class V, class Op>
 __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
 #pragma unroll
@@ -34,97 +60,380 @@ __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
   __syncthreads();
   x = scratch[0];
 #pragma unroll
-  for (int i = 1; i < kThreads / kWave; ++i) x = op(x, scratch[i]);
+  for (int i = 1; i < kWaves; ++i) x = op(x, scratch[i]);
   return x;
+}
+__device__ __forceinline__ uint64_t block_max_key(uint64_t x, uint64_t *scratch) {
+  return block_reduce(x, scratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+}
+
+// A bound that at least k of the values that the threads' maxima x come from
+// reach: in each wave the k / kWaves-th of its lanes' distinct maxima, and the
+// least of those. -inf where the values are fewer. One barrier pair.
+__device__ __forceinline__ float block_bound(float x, int k, float *scratch) {
+  float at = kInf;
+  for (int i = 0; i < (k + kWaves - 1) / kWaves; ++i) {
+    at = wave_max(x);
+    if (x == at) x = -kInf;
+  }
+  __syncthreads();
+  if (lane_id() == 0) scratch[threadIdx.x / kWave] = at;
+  __syncthreads();
+  at = scratch[0];
+#pragma unroll
+  for (int i = 1; i < kWaves; ++i) at = fminf(at, scratch[i]);
+  return at;
+}
+
+// The k largest of the n distinct keys in `list`, descending, zeros beyond n, to put(rank, key).
+template <class Put>
+__device__ __forceinline__ void rank_list(const uint64_t *list, int n, int k, Put put) {
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t key = list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += list[j] > key ? 1 : 0;
+    if (rank < k) put(rank, key);
+  }
+  for (int i = n + threadIdx.x; i < k; i += kThreads) put(i, uint64_t(0));
 }
 
 // A logit that can be chosen, or -inf.
-__device__ __forceinline__ float usable(float x, bool &bad) {
-  if (x < kInf) return x;
-  bad = true;
-  return -kInf;
+__device__ __forceinline__ float usable(float x) { return x < kInf ? x : -kInf; }
+
+// Vectors start with the row, whatever its alignment (global loads need none),
+// so that sums do not depend on where a row lies.
+template <class T>
+struct Row {
+  static constexpr int kPer = 16 / sizeof(T);
+  // Elements v * kPer .. of a row of n; -inf beyond it.
+  static __device__ __forceinline__ void load(const T *row, int64_t n, int64_t v, float (&x)[kPer]) {
+    typedef T vec __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+    const int64_t at = v * kPer;
+    if (at + kPer <= n) {
+      const vec y = *reinterpret_cast<const vec *>(row + at);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[i] = to_f32(y[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[i] = at + i < n ? to_f32(row[at + i]) : -kInf;
+    }
+  }
+};
+
+__host__ __device__ __forceinline__ int64_t slice_count(int64_t vocab, int per) {
+  return ((vocab + per - 1) / per + kSlice - 1) / kSlice;
 }
 
-// One workgroup to a row: its log-sum-exp and its num_out best places.
+struct SelectArgs {
+  const void *logits;
+  const float *scores;
+  const int32_t *finished;
+  float *scores_out;
+  int32_t *tokens_out, *parents_out, *status;
+  float2 *parts;     // [rows][slices] largest logit, sum of exponentials over it
+  uint64_t *best;    // [rows][slices][num_out + 1] logits and tokens, descending
+  int64_t stride, vocab, slices;
+  int32_t beams, num_out;
+};
+
+__device__ __forceinline__ bool row_counts(const SelectArgs &p, int64_t row) {
+  return p.scores[row] > -kInf && (p.finished == nullptr || p.finished[row] == 0);
+}
+
+// One workgroup to a slice. HBM-bound: the logits are read once, 16 bytes a
+// lane and kVectors of them in flight.
 template <class T>
-__global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *logits, int64_t stride, const float *scores,
-                                                             const int32_t *finished, int64_t vocab, int num_out,
-                                                             float *lse, uint64_t *best, int32_t *status,
-                                                             int64_t first) {
-  __shared__ float fscratch[kThreads / kWave];
-  __shared__ uint64_t kscratch[kThreads / kWave];
-  const int64_t row = first + blockIdx.x;
-  if (!(scores[row] > -kInf) || (finished != nullptr && finished[row] != 0)) return;
-  const T *z = logits + row * stride;
-  bool bad = false;
-  float m = -kInf, s = 0.0f;
-  for (int64_t j = threadIdx.x; j < vocab; j += kThreads) m = fmaxf(m, usable(to_f32(z[j]), bad));
-  if (bad && status != nullptr) atomicOr(status, RDF2V_STATUS_BAD_VALUE);
-  m = block_reduce(m, fscratch, [](float a, float b) { return fmaxf(a, b); });
-  for (int64_t j = threadIdx.x; j < vocab; j += kThreads) {
-    const float x = usable(to_f32(z[j]), bad);
-    s += x == -kInf ? 0.0f : expf(x - m);
+__global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64_t first) {
+  constexpr int kPer = Row<T>::kPer;
+  __shared__ float scratch[2 * kWaves];
+  __shared__ uint64_t list[kList], kscratch[kWaves];
+  __shared__ int count;
+  const int64_t block = first + blockIdx.x, row = block / p.slices, slice = block % p.slices;
+  if (!row_counts(p, row)) return;
+  const T *z = static_cast<const T *>(p.logits) + row * p.stride;
+  const int k = p.num_out + 1;
+  const int64_t v0 = slice * kSlice + threadIdx.x;
+  if (threadIdx.x == 0) count = 0;
+  float x[kVectors][kPer];
+#pragma unroll
+  for (int i = 0; i < kVectors; ++i) Row<T>::load(z, p.vocab, v0 + i * kThreads, x[i]);
+  float top = -kInf, sum = 0.0f;
+  auto fold = [&] {
+    top = -kInf;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) top = fmaxf(top, x[i][j]);
+    const float from = top == -kInf ? 0.0f : top;
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) sum += __expf(x[i][j] - from);
+  };
+  fold();
+  if (!(sum < kInf) || !(top < kInf)) {  // NaN or +inf among them
+    if (p.status != nullptr) atomicOr(p.status, RDF2V_STATUS_BAD_VALUE);
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) x[i][j] = usable(x[i][j]);
+    fold();
   }
-  s = block_reduce(s, fscratch, [](float a, float b) { return a + b; });
-  if (threadIdx.x == 0) lse[row] = m + logf(s);
-  uint64_t last = ~uint64_t(0);
-  for (int k = 0; k < num_out; ++k) {
-    uint64_t key = 0;
-    for (int64_t j = threadIdx.x; j < vocab; j += kThreads) {
-      const float x = usable(to_f32(z[j]), bad);
-      const uint64_t c = x == -kInf ? 0 : order_key(x, uint32_t(j));
-      if (c < last && c > key) key = c;
+  const float bound = block_bound(top, k, scratch);  // its barriers also order `count`
+  {
+    const float most = wave_max(top), from = most == -kInf ? 0.0f : most;
+    sum *= __expf(top - from);
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+    __syncthreads();
+    if (lane_id() == 0) {
+      scratch[threadIdx.x / kWave] = most;
+      scratch[kWaves + threadIdx.x / kWave] = sum;
     }
-    last = block_reduce(key, kscratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-    if (threadIdx.x == 0) best[row * num_out + k] = last;
   }
+  if (top >= bound) {
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (x[i][j] >= bound && x[i][j] > -kInf) {
+          const int at = atomicAdd(&count, 1);
+          if (at < kList) list[at] = order_key(x[i][j], uint32_t((v0 + i * kThreads) * kPer + j));
+        }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float most = scratch[0], all = 0.0f;
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) most = fmaxf(most, scratch[i]);
+    if (most > -kInf)
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) all += scratch[kWaves + i] * __expf(scratch[i] - most);
+    p.parts[row * p.slices + slice] = make_float2(most, all);
+  }
+  uint64_t *best = p.best + (row * p.slices + slice) * k;
+  const int n = count;
+  if (n <= kList) {
+    rank_list(list, n, k, [&](int rank, uint64_t key) { best[rank] = key; });
+    return;
+  }
+  // more ties at the bound than the list holds: one by one
+  uint64_t last = ~uint64_t(0);
+  for (int r = 0; r < k; ++r) {
+    uint64_t key = 0;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const uint64_t c = x[i][j] > -kInf ? order_key(x[i][j], uint32_t((v0 + i * kThreads) * kPer + j)) : 0;
+        if (c < last && c > key) key = c;
+      }
+    last = block_max_key(key, kscratch);
+    if (threadIdx.x == 0) best[r] = last;
+  }
+}
+
+// Candidates of the merge that are ranked at once: all of them where there are
+// fewer lists than places to fill.
+constexpr int kMergeList = RDF2V_MAX_BEAMS * (RDF2V_MAX_BEAMS + 1);
+
+// The next value of the element type below x, which is one.
+template <class T>
+__device__ __forceinline__ float previous(float x) {
+  constexpr uint32_t kOne = sizeof(T) == 2 ? 0x10000u : 1u;
+  const uint32_t b = __float_as_uint(x);
+  return __uint_as_float(x == 0.0f ? 0x80000000u + kOne : x > 0.0f ? b - kOne : b + kOne);
 }
 
 // One workgroup to a group: its beams' candidates by total.
-__global__ __launch_bounds__(kThreads) void beam_merge_kernel(const float *scores, const int32_t *finished, int beams,
-                                                              int num_out, const float *lse, const uint64_t *best,
-                                                              float *scores_out, int32_t *tokens_out,
-                                                              int32_t *parents_out, int64_t first) {
-  __shared__ float total[RDF2V_MAX_BEAMS * RDF2V_MAX_BEAMS];
-  __shared__ uint64_t kscratch[kThreads / kWave];
-  const int64_t group = first + blockIdx.x, row0 = group * beams;
-  const int count = beams * num_out;
-  for (int c = threadIdx.x; c < count; c += kThreads) {
-    const int64_t row = row0 + c / num_out;
-    const float score = scores[row];
-    float t = -kInf;
-    if (score > -kInf) {
-      if (finished != nullptr && finished[row] != 0) {
-        t = c % num_out == 0 ? score : -kInf;
-      } else {
-        const uint64_t key = best[row * num_out + c % num_out];
-        if (key != 0) t = score + (key_value(key) - lse[row]);
+template <class T>
+__global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int64_t first) {
+  __shared__ float lse[RDF2V_MAX_BEAMS], score[RDF2V_MAX_BEAMS];
+  __shared__ uint8_t counts[RDF2V_MAX_BEAMS], ended[RDF2V_MAX_BEAMS], again[RDF2V_MAX_BEAMS];
+  __shared__ float fscratch[kWaves];
+  __shared__ uint64_t kscratch[kWaves];
+  __shared__ uint64_t list[kMergeList];
+  __shared__ uint32_t place[kMergeList];
+  __shared__ uint64_t chosen[RDF2V_MAX_BEAMS];
+  __shared__ uint32_t chosen_place[RDF2V_MAX_BEAMS];
+  __shared__ int count, any_again;
+  const int64_t group = first + blockIdx.x, row0 = group * p.beams;
+  const int k = p.num_out + 1;
+  const int64_t slices = p.slices;
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+
+  for (int b = wave; b < p.beams; b += kWaves) {
+    const int64_t row = row0 + b;
+    const bool use = row_counts(p, row);
+    float most = -kInf, sum = 0.0f;
+    if (use)
+      for (int64_t i = lane; i < slices; i += kWave) {
+        const float2 part = p.parts[row * slices + i];
+        if (part.x > most) {
+          sum = sum * __expf(most - part.x) + part.y;
+          most = part.x;
+        } else if (part.x > -kInf) {
+          sum += part.y * __expf(part.x - most);
+        }
       }
+    const float all = wave_max(most);
+    sum *= most > -kInf ? __expf(most - all) : 0.0f;
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+    if (lane == 0) {
+      lse[b] = all + logf(sum);
+      score[b] = p.scores[row];
+      counts[b] = use && all > -kInf;
+      ended[b] = !use && score[b] > -kInf;
+      again[b] = 0;
     }
-    total[c] = t;
   }
   __syncthreads();
-  uint64_t last = ~uint64_t(0);
-  for (int k = 0; k < num_out; ++k) {
-    uint64_t key = 0;
-    for (int c = threadIdx.x; c < count; c += kThreads) {
-      const uint64_t x = total[c] > -kInf ? order_key(total[c], uint32_t(c)) : 0;
-      if (x < last && x > key) key = x;
+
+  // the total of a beam's logit, in the order of the definition
+  auto total_of = [&](int b, float x) { return score[b] + (x - lse[b]); };
+  // candidates are compared by total, then by beam and token: (total, beam) is unique up to the token
+  const int lists = p.beams * int(slices);
+  for (int round = 0;; ++round) {
+    if (threadIdx.x == 0) count = any_again = 0;
+    // the lists' first entries: num_out of them bound the last chosen total
+    float head = -kInf;
+    for (int l = wave + kWaves * lane; l < lists; l += kThreads) {  // as many to each wave
+      const int b = l / int(slices);
+      if (!counts[b]) continue;
+      const uint64_t key = p.best[(row0 * slices + l) * k];
+      if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
     }
-    last = block_reduce(key, kscratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-    if (threadIdx.x == 0) {
-      const int64_t to = group * num_out + k;
-      int32_t token = -1;
-      int64_t row = row0;
-      if (last != 0) {
-        const uint32_t c = key_index(last);
-        row = row0 + c / num_out;
-        if (finished == nullptr || finished[row] == 0) token = int32_t(key_index(best[row * num_out + c % num_out]));
+    const float bound = block_bound(head, p.num_out, fscratch);
+    for (int l = threadIdx.x; l < lists; l += kThreads) {
+      const int b = l / int(slices);
+      if (!counts[b]) continue;
+      const uint64_t *keys = p.best + (row0 * slices + l) * k;
+      // Descending logits have descending totals; the last entry only bounds what was left out, but for
+      // a beam whose entries are already the best by total.
+      for (int i = 0; i < p.num_out; ++i) {
+        const uint64_t key = keys[i];
+        if (key == 0) break;
+        const float t = total_of(b, key_value(key));
+        if (t < bound || t == -kInf) break;
+        const int at = atomicAdd(&count, 1);
+        if (at < kMergeList) {
+          list[at] = order_key(t, uint32_t(b) << 26);
+          place[at] = key_index(key);
+        }
       }
-      scores_out[to] = last != 0 ? key_value(last) : -kInf;
-      tokens_out[to] = token;
-      parents_out[to] = int32_t(row);
     }
+    for (int b = threadIdx.x; b < p.beams; b += kThreads)
+      if (ended[b]) {
+        const int at = atomicAdd(&count, 1);
+        if (at < kMergeList) {
+          list[at] = order_key(score[b], uint32_t(b) << 26 | 1u);
+          place[at] = 0;
+        }
+      }
+    __syncthreads();
+    const int n = count;
+    if (n <= kMergeList) {
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        int rank = 0;
+        for (int j = 0; j < n; ++j)
+          rank += list[j] > list[i] || (list[j] == list[i] && place[j] < place[i]) ? 1 : 0;
+        if (rank < p.num_out) {
+          chosen[rank] = list[i];
+          chosen_place[rank] = place[i];
+        }
+      }
+      for (int i = n + threadIdx.x; i < p.num_out; i += kThreads) chosen[i] = 0;
+    } else {
+      // one by one, from the lists
+      uint64_t last = ~uint64_t(0);
+      uint32_t last_place = 0;
+      for (int r = 0; r < p.num_out; ++r) {
+        uint64_t key = 0;
+        uint32_t at = 0xffffffffu;
+        auto offer = [&](uint64_t c, uint32_t token) {
+          const bool below = c < last || (c == last && token > last_place);
+          if (below && (c > key || (c == key && token < at))) {
+            key = c;
+            at = token;
+          }
+        };
+        for (int l = threadIdx.x; l < lists; l += kThreads) {
+          const int b = l / int(slices);
+          if (!counts[b]) continue;
+          for (int i = 0; i < p.num_out; ++i) {
+            const uint64_t c = p.best[(row0 * slices + l) * k + i];
+            if (c == 0) break;
+            const float t = total_of(b, key_value(c));
+            if (t > -kInf) offer(order_key(t, uint32_t(b) << 26), key_index(c));
+          }
+        }
+        for (int b = threadIdx.x; b < p.beams; b += kThreads)
+          if (ended[b]) offer(order_key(score[b], uint32_t(b) << 26 | 1u), 0);
+        const uint64_t top = block_max_key(key, kscratch);
+        const uint64_t low = block_max_key(key == top && top != 0 ? uint64_t(0xffffffffu - at) + 1 : 0, kscratch);
+        last = top;
+        last_place = low == 0 ? 0 : 0xffffffffu - uint32_t(low - 1);
+        if (threadIdx.x == 0) {
+          chosen[r] = last;
+          chosen_place[r] = last_place;
+        }
+      }
+    }
+    __syncthreads();
+    if (round > 0) break;
+    // Whether something that a slice left out could belong to the chosen: its logit is below the
+    // slice's last entry, or equal to it with a higher token, which loses to that entry.
+    const uint64_t worst = chosen[p.num_out - 1];
+    const float least = worst != 0 ? key_value(worst) : -kInf;
+    for (int l = threadIdx.x; l < lists; l += kThreads) {
+      const int b = l / int(slices);
+      if (!counts[b]) continue;
+      const uint64_t key = p.best[(row0 * slices + l) * k + p.num_out];
+      if (key == 0) continue;
+      const float t = total_of(b, previous<T>(key_value(key)));
+      if (t >= least && t > -kInf) {
+        again[b] = 1;
+        any_again = 1;
+      }
+    }
+    __syncthreads();
+    if (!any_again) break;
+    // such beams' best by total, from the whole row, in place of their lists
+    for (int b = 0; b < p.beams; ++b) {
+      if (!again[b]) continue;
+      const int64_t row = row0 + b;
+      const T *z = static_cast<const T *>(p.logits) + row * p.stride;
+      uint64_t last = ~uint64_t(0);
+      for (int r = 0; r < p.num_out; ++r) {
+        uint64_t key = 0;
+        float x_of = 0.0f;
+        for (int64_t j = threadIdx.x; j < p.vocab; j += kThreads) {
+          const float x = usable(to_f32(z[j])), t = total_of(b, x);
+          const uint64_t c = x > -kInf && t > -kInf ? order_key(t, uint32_t(j)) : 0;
+          if (c < last && c > key) {
+            key = c;
+            x_of = x;
+          }
+        }
+        last = block_max_key(key, kscratch);
+        if (last != 0 && key == last) p.best[row * slices * k + r] = order_key(x_of, key_index(last));
+        if (last == 0 && threadIdx.x == 0) p.best[row * slices * k + r] = 0;
+      }
+      for (int64_t i = 1 + threadIdx.x; i < slices; i += kThreads) p.best[(row * slices + i) * k] = 0;
+    }
+    __threadfence_block();
+    __syncthreads();
+  }
+
+  for (int r = threadIdx.x; r < p.num_out; r += kThreads) {
+    const uint64_t key = chosen[r];
+    const uint32_t at = key_index(key);
+    const int64_t to = group * p.num_out + r;
+    p.scores_out[to] = key != 0 ? key_value(key) : -kInf;
+    p.tokens_out[to] = key != 0 && at % (1u << 26) == 0 ? int32_t(chosen_place[r]) : -1;
+    p.parents_out[to] = int32_t(row0 + (key != 0 ? at >> 26 : 0));
   }
 }
 
@@ -161,33 +470,46 @@ rdf2v_status reorder(const void *src, int64_t num_src, int64_t row_bytes, const 
 
 }  // namespace
 
-size_t beam_select_workspace_bytes(int64_t groups, int32_t beams, int64_t, int32_t num_out) {
-  const size_t rows = size_t(groups) * beams;
-  return align_up(rows * num_out * sizeof(uint64_t), 256) + align_up(rows * sizeof(float), 256);
+size_t beam_select_workspace_bytes(int64_t groups, int32_t beams, int64_t vocab, int32_t num_out) {
+  const size_t lists = size_t(groups) * beams * slice_count(vocab, 4);  // float32 has the more slices
+  return align_up(lists * (num_out + 1) * sizeof(uint64_t), 256) + align_up(lists * sizeof(float2), 256);
 }
 
 rdf2v_status launch_beam_select(const void *logits, int64_t stride, int32_t dtype, const float *scores,
                                 const int32_t *finished, int64_t groups, int32_t beams, int64_t vocab,
                                 int32_t num_out, float *scores_out, int32_t *tokens_out, int32_t *parents_out,
                                 void *workspace, int32_t *status_dev, hipStream_t stream) {
-  const int64_t rows = groups * beams;
-  uint64_t *best = static_cast<uint64_t *>(workspace);
-  float *lse = reinterpret_cast<float *>(static_cast<char *>(workspace) +
-                                         align_up(size_t(rows) * num_out * sizeof(uint64_t), 256));
-  rdf2v_status st = for_each_launch(rows, kThreads, 1, [&](int64_t first, int64_t count) {
+  SelectArgs p{};
+  p.logits = logits;
+  p.scores = scores;
+  p.finished = finished;
+  p.scores_out = scores_out;
+  p.tokens_out = tokens_out;
+  p.parents_out = parents_out;
+  p.status = status_dev;
+  p.stride = stride;
+  p.vocab = vocab;
+  p.slices = slice_count(vocab, dtype == RDF2V_BF16 ? 8 : 4);
+  p.beams = beams;
+  p.num_out = num_out;
+  const size_t lists = size_t(groups) * beams * p.slices;
+  p.best = static_cast<uint64_t *>(workspace);
+  p.parts = reinterpret_cast<float2 *>(static_cast<char *>(workspace) +
+                                       align_up(lists * (num_out + 1) * sizeof(uint64_t), 256));
+  rdf2v_status st = for_each_launch(int64_t(lists), kThreads, 1, [&](int64_t first, int64_t count) {
     if (dtype == RDF2V_BF16)
-      beam_rows_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(
-          static_cast<const bf16 *>(logits), stride, scores, finished, vocab, num_out, lse, best, status_dev, first);
+      beam_rows_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
     else
-      beam_rows_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(
-          static_cast<const float *>(logits), stride, scores, finished, vocab, num_out, lse, best, status_dev, first);
+      beam_rows_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });
   if (st != RDF2V_OK) return st;
   return for_each_launch(groups, kThreads, 1, [&](int64_t first, int64_t count) {
-    beam_merge_kernel<<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(
-        scores, finished, beams, num_out, lse, best, scores_out, tokens_out, parents_out, first);
+    if (dtype == RDF2V_BF16)
+      beam_merge_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+    else
+      beam_merge_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });

@@ -227,3 +227,31 @@ def test_refusals():
         rd.rdf2v_beam_reorder(src.T, p)
     with pytest.raises(TypeError):
         rd.rdf2v_beam_reorder(src, p.long())
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [300, 5_000, 40_000])
+def test_totals_that_round_together(vocab, type_):
+    """Scores so low that many logits have the same total: the lowest tokens of it are chosen, wherever
+    their logits stand. The totals here are exact to predict: scores are powers of two whose float32
+    step is far above the logits' spread, or at it."""
+    say(f"[beam] totals that round together, vocabulary of {vocab} {type_}")
+    g = torch.Generator(device=device())
+    g.manual_seed(vocab)
+    for power in (10, 16, 22, 30):
+        logits = torch.randn(2, 2, vocab, device=device(), generator=g).to(type_)
+        scores = torch.tensor([[-2.0 ** power, -2.0 ** power], [-2.0 ** power, -2.0 ** power * 1.5]], device=device())
+        got, tokens, parents = rd.rdf2v_beam_select(logits, scores, 7)
+        x = logits.float().cpu()
+        # the totals with the log-sum-exp as float32 has it, one unit up and down: the choice is that of one of them
+        lse = torch.logsumexp(x.double(), -1, keepdim=True).float()
+        ok = torch.zeros(2, dtype=torch.bool)
+        steps = [lse, torch.nextafter(lse, lse + 1), torch.nextafter(lse, lse - 1)]
+        for a in steps:
+            for b in steps:
+                both = torch.cat([a[:, :1], b[:, 1:]], 1)
+                total = (scores.cpu()[..., None] + (x - both)).flatten(1)
+                place = total.sort(dim=1, descending=True, stable=True).indices[:, :7]
+                mine = (parents.cpu() - torch.arange(2)[:, None] * 2).long() * vocab + tokens.cpu().long()
+                ok |= (place == mine).all(1)
+        assert bool(ok.all()), (power, ok)
