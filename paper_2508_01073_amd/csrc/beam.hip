@@ -100,28 +100,28 @@ __device__ __forceinline__ void rank_list(const uint64_t *list, int n, int k, Pu
 // A logit that can be chosen, or -inf.
 __device__ __forceinline__ float usable(float x) { return x < kInf ? x : -kInf; }
 
-// Vectors start with the row, whatever its alignment (global loads need none),
-// so that sums do not depend on where a row lies.
+// A row as whole 16-byte vectors and the values after the last of them. Vectors
+// start with the row, whatever its alignment (global loads need none), so that
+// sums do not depend on where a row lies.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
 template <class T>
 struct Row {
   static constexpr int kPer = 16 / sizeof(T);
-  // Elements v * kPer .. of a row of n; -inf beyond it.
-  static __device__ __forceinline__ void load(const T *row, int64_t n, int64_t v, float (&x)[kPer]) {
-    typedef T vec __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
-    const int64_t at = v * kPer;
-    if (at + kPer <= n) {
-      const vec y = *reinterpret_cast<const vec *>(row + at);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) x[i] = to_f32(y[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) x[i] = at + i < n ? to_f32(row[at + i]) : -kInf;
-    }
+  typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
+  // Vector v of the first `end` ones of a row; -inf beyond.
+  static __device__ __forceinline__ Words load(const T *row, int64_t end, int64_t v) {
+    constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    const Words x = *reinterpret_cast<const Unaligned *>(row + min(v, end - 1) * kPer);
+    return v < end ? x : Words{kNone, kNone, kNone, kNone};
+  }
+  static __device__ __forceinline__ float value(const Words &x, int j) {
+    if (sizeof(T) == 4) return __uint_as_float(x[j]);
+    return __uint_as_float(j % 2 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
   }
 };
 
 __host__ __device__ __forceinline__ int64_t slice_count(int64_t vocab, int per) {
-  return ((vocab + per - 1) / per + kSlice - 1) / kSlice;
+  return vocab / per < kSlice ? 1 : (vocab / per + kSlice - 1) / kSlice;
 }
 
 struct SelectArgs {
@@ -152,33 +152,43 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
   if (!row_counts(p, row)) return;
   const T *z = static_cast<const T *>(p.logits) + row * p.stride;
   const int k = p.num_out + 1;
-  const int64_t v0 = slice * kSlice + threadIdx.x;
   if (threadIdx.x == 0) count = 0;
-  float x[kVectors][kPer];
+  const int64_t whole = p.vocab / kPer;
+  // Slices of equal size, and a short row spread over all waves: the bound of the candidates is that of the
+  // wave that has least.
+  const int64_t per = (whole + p.slices - 1) / p.slices, begin = slice * per, end = min(whole, begin + per);
+  const int place = whole < kThreads ? lane_id() * kWaves + threadIdx.x / kWave : threadIdx.x;
+  const int64_t v0 = begin + place;
+  Words x[kVectors];  // as they lie in memory: half the registers for bfloat16
+  if (whole > 0) {
 #pragma unroll
-  for (int i = 0; i < kVectors; ++i) Row<T>::load(z, p.vocab, v0 + i * kThreads, x[i]);
-  float top = -kInf, sum = 0.0f;
-  auto fold = [&] {
-    top = -kInf;
+    for (int i = 0; i < kVectors; ++i) x[i] = Row<T>::load(z, end, v0 + i * kThreads);
+  }
+  // the values after the last vector, one to a thread of the first slice
+  const int64_t rest_at = whole * kPer + threadIdx.x;
+  float rest = slice == 0 && rest_at < p.vocab ? to_f32(z[rest_at]) : -kInf;
+  // Values are made from the words anew in each pass: kept, they would take the registers of other waves.
+  auto each = [&](auto take) {
+    if (whole > 0) {
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i)
+      for (int i = 0; i < kVectors; ++i) {
+        asm volatile("" : "+v"(x[i]));
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) top = fmaxf(top, x[i][j]);
-    const float from = top == -kInf ? 0.0f : top;
-    sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kVectors; ++i)
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) sum += __expf(x[i][j] - from);
+        for (int j = 0; j < kPer; ++j)
+          take(Row<T>::value(x[i], j), [&] { return uint32_t((v0 + i * kThreads) * kPer + j); });
+      }
+    }
+    take(rest, [&] { return uint32_t(rest_at); });
   };
-  fold();
+  float top = -kInf, sum = 0.0f;
+  each([&](float y, auto) { top = fmaxf(top, y); });
+  each([&](float y, auto) { sum += __expf(y - (top == -kInf ? 0.0f : top)); });
   if (!(sum < kInf) || !(top < kInf)) {  // NaN or +inf among them
     if (p.status != nullptr) atomicOr(p.status, RDF2V_STATUS_BAD_VALUE);
-#pragma unroll
-    for (int i = 0; i < kVectors; ++i)
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) x[i][j] = usable(x[i][j]);
-    fold();
+    top = -kInf;
+    sum = 0.0f;
+    each([&](float y, auto) { top = fmaxf(top, usable(y)); });
+    each([&](float y, auto) { sum += __expf(usable(y) - (top == -kInf ? 0.0f : top)); });
   }
   const float bound = block_bound(top, k, scratch);  // its barriers also order `count`
   {
@@ -192,16 +202,24 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
       scratch[kWaves + threadIdx.x / kWave] = sum;
     }
   }
-  if (top >= bound) {
+  auto collect = [&](float y, uint32_t index) {
+    if (!(y >= bound) || !(usable(y) > -kInf)) return;
+    const int at = atomicAdd(&count, 1);
+    if (at < kList) list[at] = order_key(y, index);
+  };
+  if (whole > 0) {
 #pragma unroll
-    for (int i = 0; i < kVectors; ++i)
+    for (int i = 0; i < kVectors; ++i) {
+      asm volatile("" : "+v"(x[i]));
+      float most = Row<T>::value(x[i], 0);
 #pragma unroll
+      for (int j = 1; j < kPer; ++j) most = fmaxf(most, Row<T>::value(x[i], j));
+      if (__ballot(most >= bound) == 0) continue;  // few vectors of a wave have any
       for (int j = 0; j < kPer; ++j)
-        if (x[i][j] >= bound && x[i][j] > -kInf) {
-          const int at = atomicAdd(&count, 1);
-          if (at < kList) list[at] = order_key(x[i][j], uint32_t((v0 + i * kThreads) * kPer + j));
-        }
+        collect(Row<T>::value(x[i], j), uint32_t((v0 + i * kThreads) * kPer + j));
+    }
   }
+  collect(rest, uint32_t(rest_at));
   __syncthreads();
   if (threadIdx.x == 0) {
     float most = scratch[0], all = 0.0f;
@@ -218,17 +236,17 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
     rank_list(list, n, k, [&](int rank, uint64_t key) { best[rank] = key; });
     return;
   }
-  // more ties at the bound than the list holds: one by one
+  // more ties at the bound than the list holds: one by one, from memory
   uint64_t last = ~uint64_t(0);
   for (int r = 0; r < k; ++r) {
     uint64_t key = 0;
-#pragma unroll
-    for (int i = 0; i < kVectors; ++i)
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const uint64_t c = x[i][j] > -kInf ? order_key(x[i][j], uint32_t((v0 + i * kThreads) * kPer + j)) : 0;
-        if (c < last && c > key) key = c;
-      }
+    auto offer = [&](int64_t j) {
+      const float y = usable(to_f32(z[j]));
+      const uint64_t c = y > -kInf ? order_key(y, uint32_t(j)) : 0;
+      if (c < last && c > key) key = c;
+    };
+    for (int64_t j = begin * kPer + threadIdx.x; j < end * kPer; j += kThreads) offer(j);
+    if (slice == 0 && rest_at < p.vocab) offer(rest_at);
     last = block_max_key(key, kscratch);
     if (threadIdx.x == 0) best[r] = last;
   }
@@ -236,6 +254,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
 
 // Candidates of the merge that are ranked at once: all of them where there are
 // fewer lists than places to fill.
+constexpr int kAhead = 4;  // entries of a list that are read together
 constexpr int kMergeList = RDF2V_MAX_BEAMS * (RDF2V_MAX_BEAMS + 1);
 
 // The next value of the element type below x, which is one.
@@ -312,15 +331,21 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
       const uint64_t *keys = p.best + (row0 * slices + l) * k;
       // Descending logits have descending totals; the last entry only bounds what was left out, but for
       // a beam whose entries are already the best by total.
-      for (int i = 0; i < p.num_out; ++i) {
-        const uint64_t key = keys[i];
-        if (key == 0) break;
-        const float t = total_of(b, key_value(key));
-        if (t < bound || t == -kInf) break;
-        const int at = atomicAdd(&count, 1);
-        if (at < kMergeList) {
-          list[at] = order_key(t, uint32_t(b) << 26);
-          place[at] = key_index(key);
+      bool more = true;
+      for (int i = 0; more && i < p.num_out; i += kAhead) {
+        uint64_t key[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) key[j] = i + j < p.num_out ? keys[i + j] : 0;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const float t = total_of(b, key_value(key[j]));
+          more = more && key[j] != 0 && t >= bound && t > -kInf;
+          if (!more) continue;
+          const int at = atomicAdd(&count, 1);
+          if (at < kMergeList) {
+            list[at] = order_key(t, uint32_t(b) << 26);
+            place[at] = key_index(key[j]);
+          }
         }
       }
     }
