@@ -91,6 +91,7 @@ __device__ __forceinline__ void rank_list(const uint64_t *list, int n, int k, Pu
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t key = list[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) rank += list[j] > key ? 1 : 0;
     if (rank < k) put(rank, key);
   }
@@ -255,6 +256,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
 // Candidates of the merge that are ranked at once: all of them where there are
 // fewer lists than places to fill.
 constexpr int kAhead = 4;  // entries of a list that are read together
+constexpr int kOwn = 2;    // lists of a thread that are read ahead
 constexpr int kMergeList = RDF2V_MAX_BEAMS * (RDF2V_MAX_BEAMS + 1);
 
 // The next value of the element type below x, which is one.
@@ -282,30 +284,57 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
   const int64_t slices = p.slices;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
 
-  for (int b = wave; b < p.beams; b += kWaves) {
-    const int64_t row = row0 + b;
-    const bool use = row_counts(p, row);
+  // One trip to memory for what nearly every group needs: the scores, a wave's first parts and the first
+  // entries and the last one of a thread's first lists. Lists of beams that do not count hold anything.
+  const int lists = p.beams * int(slices);
+  const int l0 = wave + kWaves * lane;  // lists l0, l0 + kThreads, ...: as many to each wave
+  uint64_t own[kOwn][kAhead + 1];
+  auto read_ahead = [&] {
+#pragma unroll
+    for (int o = 0; o < kOwn; ++o) {
+      const uint64_t *keys = p.best + (row0 * slices + min(l0 + o * kThreads, lists - 1)) * k;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) own[o][i] = keys[min(i, p.num_out)];
+      own[o][kAhead] = keys[p.num_out];
+    }
+  };
+  read_ahead();
+  float2 parts[kOwn];
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o)
+    parts[o] = p.parts[(row0 + min(wave + o * kWaves, p.beams - 1)) * slices + min(int64_t(lane), slices - 1)];
+  if (int(threadIdx.x) < p.beams) {
+    const float x = p.scores[row0 + threadIdx.x];
+    const bool end = p.finished != nullptr && p.finished[row0 + threadIdx.x] != 0;
+    score[threadIdx.x] = x;
+    counts[threadIdx.x] = x > -kInf && !end;
+    ended[threadIdx.x] = x > -kInf && end;
+    again[threadIdx.x] = 0;
+  }
+  __syncthreads();
+  for (int b = wave, o = 0; b < p.beams; b += kWaves, ++o) {
+    if (!counts[b]) continue;
     float most = -kInf, sum = 0.0f;
-    if (use)
-      for (int64_t i = lane; i < slices; i += kWave) {
-        const float2 part = p.parts[row * slices + i];
-        if (part.x > most) {
-          sum = sum * __expf(most - part.x) + part.y;
-          most = part.x;
-        } else if (part.x > -kInf) {
-          sum += part.y * __expf(part.x - most);
-        }
+    for (int64_t i = lane; i < slices; i += kWave) {
+      float2 part;
+      if (o < kOwn && i < kWave)
+        part = o == 0 ? parts[0] : parts[1];
+      else
+        part = p.parts[(row0 + b) * slices + i];
+      if (part.x > most) {
+        sum = sum * __expf(most - part.x) + part.y;
+        most = part.x;
+      } else if (part.x > -kInf) {
+        sum += part.y * __expf(part.x - most);
       }
+    }
     const float all = wave_max(most);
     sum *= most > -kInf ? __expf(most - all) : 0.0f;
 #pragma unroll
     for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
     if (lane == 0) {
       lse[b] = all + logf(sum);
-      score[b] = p.scores[row];
-      counts[b] = use && all > -kInf;
-      ended[b] = !use && score[b] > -kInf;
-      again[b] = 0;
+      counts[b] = all > -kInf;
     }
   }
   __syncthreads();
@@ -313,42 +342,49 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
   // the total of a beam's logit, in the order of the definition
   auto total_of = [&](int b, float x) { return score[b] + (x - lse[b]); };
   // candidates are compared by total, then by beam and token: (total, beam) is unique up to the token
-  const int lists = p.beams * int(slices);
   for (int round = 0;; ++round) {
     if (threadIdx.x == 0) count = any_again = 0;
+    // take(beam, list, its first entries) for every list of this thread
+    auto each_list = [&](auto take) {
+#pragma unroll
+      for (int o = 0; o < kOwn; ++o) {
+        const int l = l0 + o * kThreads, b = min(l, lists - 1) / int(slices);
+        if (l < lists && counts[b]) take(b, l, own[o]);
+      }
+      for (int l = l0 + kOwn * kThreads; l < lists; l += kThreads) {
+        const int b = l / int(slices);
+        if (!counts[b]) continue;
+        const uint64_t *keys = p.best + (row0 * slices + l) * k;
+        uint64_t next[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) next[i] = keys[min(i, p.num_out)];
+        next[kAhead] = keys[p.num_out];
+        take(b, l, next);
+      }
+    };
     // the lists' first entries: num_out of them bound the last chosen total
     float head = -kInf;
-    for (int l = wave + kWaves * lane; l < lists; l += kThreads) {  // as many to each wave
-      const int b = l / int(slices);
-      if (!counts[b]) continue;
-      const uint64_t key = p.best[(row0 * slices + l) * k];
-      if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
-    }
+    each_list([&](int b, int, const uint64_t(&key)[kAhead + 1]) {
+      if (key[0] != 0) head = fmaxf(head, total_of(b, key_value(key[0])));
+    });
     const float bound = block_bound(head, p.num_out, fscratch);
-    for (int l = threadIdx.x; l < lists; l += kThreads) {
-      const int b = l / int(slices);
-      if (!counts[b]) continue;
-      const uint64_t *keys = p.best + (row0 * slices + l) * k;
-      // Descending logits have descending totals; the last entry only bounds what was left out, but for
-      // a beam whose entries are already the best by total.
-      bool more = true;
-      for (int i = 0; more && i < p.num_out; i += kAhead) {
-        uint64_t key[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) key[j] = i + j < p.num_out ? keys[i + j] : 0;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-          const float t = total_of(b, key_value(key[j]));
-          more = more && key[j] != 0 && t >= bound && t > -kInf;
-          if (!more) continue;
-          const int at = atomicAdd(&count, 1);
-          if (at < kMergeList) {
-            list[at] = order_key(t, uint32_t(b) << 26);
-            place[at] = key_index(key[j]);
-          }
+    each_list([&](int b, int l, const uint64_t(&key)[kAhead + 1]) {
+      // Descending logits have descending totals; the last entry only bounds what was left out.
+      auto offer = [&](uint64_t x) {
+        const float t = total_of(b, key_value(x));
+        if (x == 0 || !(t >= bound) || t == -kInf) return false;
+        const int at = atomicAdd(&count, 1);
+        if (at < kMergeList) {
+          list[at] = order_key(t, uint32_t(b) << 26);
+          place[at] = key_index(x);
         }
-      }
-    }
+        return true;
+      };
+      bool more = true;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) more = more && i < p.num_out && offer(key[i]);
+      for (int i = kAhead; more && i < p.num_out; ++i) more = offer(p.best[(row0 * slices + l) * k + i]);
+    });
     for (int b = threadIdx.x; b < p.beams; b += kThreads)
       if (ended[b]) {
         const int at = atomicAdd(&count, 1);
@@ -361,12 +397,14 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
     const int n = count;
     if (n <= kMergeList) {
       for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t key = list[i];
+        const uint32_t at = place[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j)
-          rank += list[j] > list[i] || (list[j] == list[i] && place[j] < place[i]) ? 1 : 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) rank += list[j] > key || (list[j] == key && place[j] < at) ? 1 : 0;
         if (rank < p.num_out) {
-          chosen[rank] = list[i];
-          chosen_place[rank] = place[i];
+          chosen[rank] = key;
+          chosen_place[rank] = at;
         }
       }
       for (int i = n + threadIdx.x; i < p.num_out; i += kThreads) chosen[i] = 0;
@@ -412,17 +450,14 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
     // slice's last entry, or equal to it with a higher token, which loses to that entry.
     const uint64_t worst = chosen[p.num_out - 1];
     const float least = worst != 0 ? key_value(worst) : -kInf;
-    for (int l = threadIdx.x; l < lists; l += kThreads) {
-      const int b = l / int(slices);
-      if (!counts[b]) continue;
-      const uint64_t key = p.best[(row0 * slices + l) * k + p.num_out];
-      if (key == 0) continue;
-      const float t = total_of(b, previous<T>(key_value(key)));
+    each_list([&](int b, int, const uint64_t(&key)[kAhead + 1]) {
+      if (key[kAhead] == 0) return;
+      const float t = total_of(b, previous<T>(key_value(key[kAhead])));
       if (t >= least && t > -kInf) {
         again[b] = 1;
         any_again = 1;
       }
-    }
+    });
     __syncthreads();
     if (!any_again) break;
     // such beams' best by total, from the whole row, in place of their lists
@@ -448,8 +483,8 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
       }
       for (int64_t i = 1 + threadIdx.x; i < slices; i += kThreads) p.best[(row * slices + i) * k] = 0;
     }
-    __threadfence_block();
     __syncthreads();
+    read_ahead();
   }
 
   for (int r = threadIdx.x; r < p.num_out; r += kThreads) {
