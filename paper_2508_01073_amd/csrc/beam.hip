@@ -11,14 +11,13 @@
 // what the slice left out: only where that bound reaches the last chosen total
 // is the beam's row read again and its best found by total.
 
-#include "model.hpp"
+#include "logits.hpp"
 
 namespace rdf2v {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr float kInf = __builtin_huge_valf();
 constexpr int kVectors = 8;                    // 16-byte loads of a thread: 32 KB to a workgroup, all in flight
 constexpr int kSlice = kVectors * kThreads;    // vectors of a slice
 constexpr int kList = 1024;                    // candidates of a slice that are ranked at once
@@ -34,22 +33,6 @@ __device__ __forceinline__ float key_value(uint64_t key) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - uint32_t(key); }
-
-// Largest value of a wave's lanes, in every lane: the row scan of
-// wave_inclusive_sum with the maximum.
-__device__ __forceinline__ float wave_max(float x) {
-  const int none = __float_as_int(-kInf);
-#define RDF2V_MAX_STEP(CTRL, ROWS) \
-  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(none, __float_as_int(x), CTRL, ROWS, 0xf, false)));
-  RDF2V_MAX_STEP(0x111, 0xf)
-  RDF2V_MAX_STEP(0x112, 0xf)
-  RDF2V_MAX_STEP(0x114, 0xf)
-  RDF2V_MAX_STEP(0x118, 0xf)
-  RDF2V_MAX_STEP(0x142, 0xa)
-  RDF2V_MAX_STEP(0x143, 0xc)
-#undef RDF2V_MAX_STEP
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), kWave - 1));
-}
 
 template <class V, class Op>
 __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
@@ -100,26 +83,6 @@ __device__ __forceinline__ void rank_list(const uint64_t *list, int n, int k, Pu
 
 // A logit that can be chosen, or -inf.
 __device__ __forceinline__ float usable(float x) { return x < kInf ? x : -kInf; }
-
-// A row as whole 16-byte vectors and the values after the last of them. Vectors
-// start with the row, whatever its alignment (global loads need none), so that
-// sums do not depend on where a row lies.
-typedef uint32_t Words __attribute__((ext_vector_type(4)));
-template <class T>
-struct Row {
-  static constexpr int kPer = 16 / sizeof(T);
-  typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
-  // Vector v of the first `end` ones of a row; -inf beyond.
-  static __device__ __forceinline__ Words load(const T *row, int64_t end, int64_t v) {
-    constexpr uint32_t kNone = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-    const Words x = *reinterpret_cast<const Unaligned *>(row + min(v, end - 1) * kPer);
-    return v < end ? x : Words{kNone, kNone, kNone, kNone};
-  }
-  static __device__ __forceinline__ float value(const Words &x, int j) {
-    if (sizeof(T) == 4) return __uint_as_float(x[j]);
-    return __uint_as_float(j % 2 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
-  }
-};
 
 __host__ __device__ __forceinline__ int64_t slice_count(int64_t vocab, int per) {
   return vocab / per < kSlice ? 1 : (vocab / per + kSlice - 1) / kSlice;

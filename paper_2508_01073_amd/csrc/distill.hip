@@ -2,128 +2,374 @@
 //
 // With p the softmax of the teacher's entries over the temperature tau and q
 // that of the logits over the whole vocabulary,
-//   loss = tau^2 (sum_k p_k log p_k - sum_k p_k z_{id_k} / tau + lse)
+//   loss = tau^2 (sum_k p_k (log p_k - z_{id_k} / tau) + lse)
 //   dlogits = dloss tau (q - p)
 // so a row needs its log-sum-exp, the logits at the teacher's ids, and for the
-// gradient one more pass over the row.
+// gradient one more look at the row. HBM-bound: the floor is one read, and one
+// write for the gradient. A row that fits the registers of a workgroup stays
+// there between the two looks. A longer one is cut into slices of a workgroup
+// each, in two launches, over as many rows at a time as the Infinity Cache
+// holds, so that the second look does not go to HBM.
+//
+// The gradient at the teacher's ids is written after the row's q, by the
+// workgroup that wrote that q, so it is rounded once; every occurrence of a
+// repeated id writes the same value.
 
-#include "model.hpp"
+#include "logits.hpp"
 
 namespace rdf2v {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr float kInf = __builtin_huge_valf();
+constexpr int kVectors = 8;  // 16-byte loads of a thread, all in flight
+constexpr int kSliceThreads = 256;
+constexpr int64_t kSlice = int64_t(kVectors) * kSliceThreads;  // vectors of a slice of a long row
+constexpr int64_t kLargest = int64_t(kVectors) * 1024;         // vectors of a row that stays in registers
+constexpr int64_t kCached = int64_t(96) << 20;                 // bytes of logits between the two looks
+constexpr float kLog2e = 1.44269504088896341f;
 
-template <class Op>
-__device__ __forceinline__ float block_reduce(float x, float *scratch, Op op) {
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) x = op(x, __shfl_xor(x, off, kWave));
-  __syncthreads();
-  if (lane_id() == 0) scratch[threadIdx.x / kWave] = x;
-  __syncthreads();
-  x = scratch[0];
-#pragma unroll
-  for (int i = 1; i < kThreads / kWave; ++i) x = op(x, scratch[i]);
-  return x;
-}
-__device__ __forceinline__ float block_max(float x, float *scratch) {
-  return block_reduce(x, scratch, [](float a, float b) { return fmaxf(a, b); });
-}
-__device__ __forceinline__ float block_add(float x, float *scratch) {
-  return block_reduce(x, scratch, [](float a, float b) { return a + b; });
+// What the two launches over a long row hand on, for each row.
+struct Workspace {
+  float2 *parts;  // [rows][slices] largest logit, sum of exponentials over it
+  float *zk;      // [rows][top] the logits at the teacher's ids, over tau
+  int64_t slices;
+};
+
+// A row's teacher entries: every wave computes their log-sum-exp for itself;
+// `each(k, id, t / tau)` is called by one lane of the calling wave for each.
+struct Teacher {
+  float lse;
+  bool valid;
+};
+template <class Each>
+__device__ __forceinline__ Teacher read_teacher(const DistillArgs &a, int64_t row, float inv_tau, bool report,
+                                                Each each) {
+  float most = -kInf, sum = 0.0f;
+  bool any = false;
+  for (int k = lane_id(); k < a.top; k += kWave) {
+    int32_t id = a.ids[row * a.top + k];
+    const float t = a.teacher[row * a.top + k] * inv_tau;
+    if (int64_t(id) >= a.vocab) {
+      if (report && a.status != nullptr) atomicOr(a.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
+      id = -1;
+    }
+    if (t == -kInf) id = -1;
+    each(k, id, t);
+    if (id < 0) continue;
+    any = true;
+    const float up = fmaxf(most, t);
+    sum = sum * (most == -kInf ? 0.0f : expf(most - up)) + expf(t - up);
+    most = up;
+  }
+  const float top = wave_max(most);
+  sum = wave_sum(any ? sum * expf(most - top) : 0.0f);
+  return {top + logf(sum), __ballot(any) != 0};
 }
 
-// One workgroup to a row.
-template <class T>
-__global__ __launch_bounds__(kThreads) void distill_kernel(DistillArgs a, int64_t first) {
-  __shared__ float p[RDF2V_MAX_TEACHER_TOP];
-  __shared__ float zk[RDF2V_MAX_TEACHER_TOP];
-  __shared__ int32_t id[RDF2V_MAX_TEACHER_TOP];
-  __shared__ float scratch[kThreads / kWave];
+// Calls take(words, i, whether the vector is there) for the vectors of this thread.
+template <class T, int THREADS>
+struct Slice {
+  Words x[kVectors];
+  float rest;
+
+  // Vectors begin .. end of a row and, for the workgroup that has them, the values after the row's last.
+  __device__ __forceinline__ void load(const T *z, int64_t begin, int64_t end, int64_t rest_at, int64_t vocab) {
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i)
+      if (begin + i * THREADS < end) x[i] = Row<T>::load(z, end, begin + i * THREADS + threadIdx.x);
+    rest = rest_at < vocab ? to_f32(z[rest_at]) : -kInf;
+  }
+  // (largest, sum of exponentials over it) of this thread's values over tau
+  __device__ __forceinline__ float2 fold(int64_t begin, int64_t end, float inv_tau) {
+    float top = rest;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      if (begin + i * THREADS >= end) break;
+#pragma unroll
+      for (int j = 0; j < Row<T>::kPer; ++j) top = fmaxf(top, Row<T>::value(x[i], j));
+    }
+    const float from = top == -kInf ? 0.0f : top, c = inv_tau * kLog2e;
+    float sum = __builtin_amdgcn_exp2f((rest - from) * c);
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      if (begin + i * THREADS >= end) break;
+      asm volatile("" : "+v"(x[i]));  // made from the words anew: kept, the values would cost registers
+#pragma unroll
+      for (int j = 0; j < Row<T>::kPer; ++j)
+        sum += __builtin_amdgcn_exp2f((Row<T>::value(x[i], j) - from) * c);
+    }
+    return make_float2(top * inv_tau, sum);
+  }
+  __device__ __forceinline__ void store(T *dz, int64_t begin, int64_t end, int64_t rest_at, int64_t vocab,
+                                        float inv_tau, float lse, float w) {
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      if (begin + i * THREADS >= end) break;
+      asm volatile("" : "+v"(x[i]));
+      const int64_t v = begin + i * THREADS + threadIdx.x;
+      if (v >= end) break;
+      typedef T vec __attribute__((ext_vector_type(Row<T>::kPer)));
+      typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
+      vec y;
+#pragma unroll
+      for (int j = 0; j < Row<T>::kPer; ++j) y[j] = from_f32<T>(w * q(Row<T>::value(x[i], j), inv_tau, lse));
+      __builtin_nontemporal_store(__builtin_bit_cast(Words, y), reinterpret_cast<Unaligned *>(dz + v * Row<T>::kPer));
+    }
+    if (rest_at < vocab) dz[rest_at] = from_f32<T>(w * q(rest, inv_tau, lse));
+  }
+  static __device__ __forceinline__ float q(float z, float inv_tau, float lse) {
+    return __builtin_amdgcn_exp2f(fmaf(z, inv_tau, -lse) * kLog2e);
+  }
+};
+
+// Zeros for a row without entries.
+template <class T, int THREADS>
+__device__ __forceinline__ void store_zeros(T *dz, int64_t begin, int64_t end, int64_t rest_at, int64_t vocab) {
+  typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
+  for (int64_t v = begin + threadIdx.x; v < end; v += THREADS)
+    __builtin_nontemporal_store(Words{0, 0, 0, 0}, reinterpret_cast<Unaligned *>(dz + v * Row<T>::kPer));
+  if (rest_at < vocab) dz[rest_at] = from_f32<T>(0.0f);
+}
+
+// (largest, sum) pairs of all threads, in every thread. One barrier.
+template <int THREADS>
+__device__ __forceinline__ float2 block_fold(float2 x, float2 *scratch) {
+  const float most = wave_max(x.x);
+  const float sum = wave_sum(x.y * (x.x == -kInf && most == -kInf ? 1.0f : expf(x.x - most)));
+  if (THREADS == kWave) return make_float2(most, sum);
+  if (lane_id() == 0) scratch[threadIdx.x / kWave] = make_float2(most, sum);
+  __syncthreads();
+  float top = scratch[0].x, all = 0.0f;
+#pragma unroll
+  for (int i = 1; i < THREADS / kWave; ++i) top = fmaxf(top, scratch[i].x);
+#pragma unroll
+  for (int i = 0; i < THREADS / kWave; ++i)
+    all += scratch[i].y * (scratch[i].x == top ? 1.0f : expf(scratch[i].x - top));
+  return make_float2(top, all);
+}
+
+__device__ __forceinline__ float log_sum(float2 x) { return x.x == -kInf && x.y == 0.0f ? -kInf : x.x + logf(x.y); }
+
+// What row_loss and the gradient at the ids read; ids that count are not negative.
+struct Entries {
+  const float *t, *zk;  // over tau
+  const int32_t *id;
+};
+
+// The loss of a row, by one wave.
+__device__ __forceinline__ float row_loss(const DistillArgs &a, const Entries &e, float lse_t, float lse) {
+  float loss = 0.0f;
+  for (int k = lane_id(); k < a.top; k += kWave) {
+    if (e.id[k] < 0) continue;
+    const float log_p = e.t[k] - lse_t;
+    loss += expf(log_p) * (log_p - (e.zk[k] == -kInf ? -kInf : e.zk[k] - lse));
+  }
+  return a.temperature * a.temperature * wave_sum(loss);
+}
+
+// The gradient at the ids in [lo, hi).
+template <class T, int THREADS>
+__device__ __forceinline__ void store_entries(const DistillArgs &a, const Entries &e, T *dz, int64_t lo, int64_t hi,
+                                              float lse_t, float lse, float w) {
+  for (int k = threadIdx.x; k < a.top; k += THREADS) {
+    const int32_t id = e.id[k];
+    if (id < 0 || id < lo || id >= hi) continue;
+    float p = 0.0f;
+    for (int m = 0; m < a.top; ++m)
+      if (e.id[m] == id) p += expf(e.t[m] - lse_t);
+    dz[id] = from_f32<T>(w * (__builtin_amdgcn_exp2f((e.zk[k] - lse) * kLog2e) - p));
+  }
+}
+
+// One workgroup to a row that stays in its registers.
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int64_t first) {
+  extern __shared__ float shared[];
+  float *t = shared, *zk = shared + a.top;
+  int32_t *id = reinterpret_cast<int32_t *>(shared + 2 * a.top);
+  __shared__ float2 scratch[THREADS / kWave];
   const int64_t row = first + blockIdx.x;
   const T *z = static_cast<const T *>(a.logits) + row * a.stride;
-  const float inv_tau = 1.0f / a.temperature;
-  float top = -kInf;
-  for (int k = threadIdx.x; k < a.top; k += kThreads) {
-    int32_t i = a.ids[row * a.top + k];
-    if (int64_t(i) >= a.vocab) {
-      if (a.status != nullptr) atomicOr(a.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
-      i = -1;
-    }
-    const float t = a.teacher[row * a.top + k] * inv_tau;
-    if (t == -kInf) i = -1;
-    id[k] = i;
-    p[k] = t;
-    zk[k] = i >= 0 ? to_f32(z[i]) * inv_tau : 0.0f;
-    if (i >= 0) top = fmaxf(top, t);
-  }
-  float any = 0.0f;
-  for (int k = threadIdx.x; k < a.top; k += kThreads) any = id[k] >= 0 ? 1.0f : any;
-  const bool valid = block_max(any, scratch) > 0.0f;
   T *dz = a.dlogits == nullptr ? nullptr : static_cast<T *>(a.dlogits) + row * a.dstride;
-  if (!valid) {
+  const float inv_tau = 1.0f / a.temperature;
+  const int64_t whole = a.vocab / Row<T>::kPer, rest_at = whole * Row<T>::kPer + threadIdx.x;
+  const bool first_wave = threadIdx.x < kWave;
+  const Teacher teacher = read_teacher(a, row, inv_tau, first_wave, [&](int k, int32_t i, float x) {
+    if (!first_wave) return;
+    t[k] = x;
+    id[k] = i;
+    zk[k] = i >= 0 ? to_f32(z[i]) * inv_tau : 0.0f;
+  });
+  if (!teacher.valid) {
     if (threadIdx.x == 0 && a.loss != nullptr) a.loss[row] = a.lse[row] = 0.0f;
-    if (dz != nullptr)
-      for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) dz[j] = from_f32<T>(0.0f);
+    if (dz != nullptr) store_zeros<T, THREADS>(dz, 0, whole, rest_at, a.vocab);
     return;
   }
-  top = block_max(top, scratch);
-  float sum = 0.0f;
-  for (int k = threadIdx.x; k < a.top; k += kThreads) sum += id[k] >= 0 ? expf(p[k] - top) : 0.0f;
-  const float lse_t = top + logf(block_add(sum, scratch));
+  Slice<T, THREADS> slice;
+  slice.load(z, 0, whole, rest_at, a.vocab);
   float lse;
   if (a.loss != nullptr) {
-    float m = -kInf, s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) m = fmaxf(m, to_f32(z[j]) * inv_tau);
-    m = block_max(m, scratch);
-    for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads)
-      s += m == -kInf ? 0.0f : expf(to_f32(z[j]) * inv_tau - m);
-    s = block_add(s, scratch);
-    lse = m == -kInf ? -kInf : m + logf(s);
-    float loss = 0.0f;
-    for (int k = threadIdx.x; k < a.top; k += kThreads) {
-      const float log_p = p[k] - lse_t, pk = expf(log_p);
-      if (id[k] >= 0) loss += pk * (log_p - (zk[k] == -kInf ? -kInf : zk[k] - lse));
-    }
-    loss = block_add(loss, scratch);
-    if (threadIdx.x == 0) {
-      a.loss[row] = a.temperature * a.temperature * loss;
-      a.lse[row] = lse;
+    lse = log_sum(block_fold<THREADS>(slice.fold(0, whole, inv_tau), scratch));
+    if (first_wave) {
+      const float loss = row_loss(a, {t, zk, id}, teacher.lse, lse);
+      if (threadIdx.x == 0) {
+        a.loss[row] = loss;
+        a.lse[row] = lse;
+      }
     }
   } else {
     lse = a.lse_in[row];
   }
   if (dz == nullptr) return;
-  const float w = a.dloss[row] * a.temperature;
-  for (int64_t j = threadIdx.x; j < a.vocab; j += kThreads) {
-    const float x = to_f32(z[j]) * inv_tau;
-    dz[j] = from_f32<T>(w * (x == -kInf ? 0.0f : expf(x - lse)));
-  }
+  __syncthreads();  // in place: the logits at the ids have been read
+  const float w = a.dloss[row] * a.temperature, from = lse == -kInf ? 0.0f : lse;  // all masked: q = 0
+  slice.store(dz, 0, whole, rest_at, a.vocab, inv_tau, from, w);
   __syncthreads();
-  // every occurrence of an id writes the same value
-  for (int k = threadIdx.x; k < a.top; k += kThreads) {
-    if (id[k] < 0) continue;
-    float pj = 0.0f;
-    for (int m = 0; m < a.top; ++m)
-      if (id[m] == id[k]) pj += expf(p[m] - lse_t);
-    dz[id[k]] = from_f32<T>(w * ((zk[k] == -kInf ? 0.0f : expf(zk[k] - lse)) - pj));
+  store_entries<T, THREADS>(a, {t, zk, id}, dz, 0, a.vocab, teacher.lse, from, w);
+}
+
+// One workgroup to a slice of a long row: its part of the log-sum-exp, and with
+// the first slice the logits at the ids, which an in-place gradient overwrites.
+template <class T>
+__global__ __launch_bounds__(kSliceThreads) void distill_stats_kernel(DistillArgs a, Workspace ws, int64_t first) {
+  __shared__ float2 scratch[kSliceThreads / kWave];
+  const int64_t slices = a.loss != nullptr ? ws.slices : 1;  // the gradient alone needs the first only
+  const int64_t block = first + blockIdx.x, row = block / slices, at = block % slices;
+  const T *z = static_cast<const T *>(a.logits) + row * a.stride;
+  const float inv_tau = 1.0f / a.temperature;
+  const bool gather = at == 0 && threadIdx.x < kWave;
+  const Teacher teacher = read_teacher(a, row, inv_tau, gather, [&](int k, int32_t i, float) {
+    if (gather) ws.zk[row * a.top + k] = i >= 0 ? to_f32(z[i]) * inv_tau : 0.0f;
+  });
+  if (!teacher.valid || a.loss == nullptr) return;
+  const int64_t whole = a.vocab / Row<T>::kPer, per = (whole + slices - 1) / slices;
+  const int64_t begin = at * per, end = min(whole, begin + per);
+  const int64_t rest_at = at == 0 ? whole * Row<T>::kPer + threadIdx.x : a.vocab;
+  Slice<T, kSliceThreads> slice;
+  slice.load(z, begin, end, rest_at, a.vocab);
+  const float2 part = block_fold<kSliceThreads>(slice.fold(begin, end, inv_tau), scratch);
+  if (threadIdx.x == 0) ws.parts[row * slices + at] = part;
+}
+
+// One workgroup to a slice of a long row: its gradient; with the first slice
+// the loss.
+template <class T>
+__global__ __launch_bounds__(kSliceThreads) void distill_grad_kernel(DistillArgs a, Workspace ws, int64_t first) {
+  extern __shared__ float shared[];
+  float *t = shared, *zk = shared + a.top;
+  int32_t *id = reinterpret_cast<int32_t *>(shared + 2 * a.top);
+  const int64_t slices = a.dlogits != nullptr ? ws.slices : 1;  // the loss alone needs the first only
+  const int64_t block = first + blockIdx.x, row = block / slices, at = block % slices;
+  const T *z = static_cast<const T *>(a.logits) + row * a.stride;
+  T *dz = a.dlogits == nullptr ? nullptr : static_cast<T *>(a.dlogits) + row * a.dstride;
+  const float inv_tau = 1.0f / a.temperature;
+  const int64_t whole = a.vocab / Row<T>::kPer, per = (whole + ws.slices - 1) / ws.slices;
+  const int64_t begin = at * per, end = min(whole, begin + per);
+  const int64_t rest_at = at == 0 ? whole * Row<T>::kPer + threadIdx.x : a.vocab;
+  const bool first_wave = threadIdx.x < kWave;
+  const Teacher teacher = read_teacher(a, row, inv_tau, false, [&](int k, int32_t i, float x) {
+    if (!first_wave) return;
+    t[k] = x;
+    id[k] = i;
+    zk[k] = ws.zk[row * a.top + k];
+  });
+  if (!teacher.valid) {
+    if (at == 0 && threadIdx.x == 0 && a.loss != nullptr) a.loss[row] = a.lse[row] = 0.0f;
+    if (dz != nullptr) store_zeros<T, kSliceThreads>(dz, begin, end, rest_at, a.vocab);
+    return;
   }
+  Slice<T, kSliceThreads> slice;
+  if (dz != nullptr) slice.load(z, begin, end, rest_at, a.vocab);
+  float lse;
+  if (a.loss != nullptr) {
+    // every wave joins the row's parts for itself
+    float2 x = make_float2(-kInf, 0.0f);
+    for (int64_t i = lane_id(); i < ws.slices; i += kWave) {
+      const float2 y = ws.parts[row * ws.slices + i];
+      const float up = fmaxf(x.x, y.x);
+      const float keep = x.x == up ? 1.0f : expf(x.x - up), add = y.x == up ? 1.0f : expf(y.x - up);
+      x = make_float2(up, x.y * keep + y.y * add);
+    }
+    const float most = wave_max(x.x);
+    lse = log_sum(make_float2(most, wave_sum(x.y * (x.x == most ? 1.0f : expf(x.x - most)))));
+    if (at == 0 && first_wave) {
+      const float loss = row_loss(a, {t, zk, id}, teacher.lse, lse);
+      if (threadIdx.x == 0) {
+        a.loss[row] = loss;
+        a.lse[row] = lse;
+      }
+    }
+  } else {
+    lse = a.lse_in[row];
+  }
+  if (dz == nullptr) return;
+  const float w = a.dloss[row] * a.temperature, from = lse == -kInf ? 0.0f : lse;  // all masked: q = 0
+  slice.store(dz, begin, end, rest_at, a.vocab, inv_tau, from, w);
+  __syncthreads();
+  const Entries e{t, zk, id};
+  store_entries<T, kSliceThreads>(a, e, dz, begin * Row<T>::kPer, end * Row<T>::kPer, teacher.lse, from, w);
+  if (at == 0) store_entries<T, kSliceThreads>(a, e, dz, whole * Row<T>::kPer, a.vocab, teacher.lse, from, w);
+}
+
+int64_t row_vectors(int64_t vocab, int32_t dtype) { return vocab / (dtype == RDF2V_BF16 ? 8 : 4); }
+int64_t slice_count(int64_t vocab, int32_t dtype) { return (row_vectors(vocab, dtype) + kSlice - 1) / kSlice; }
+
+size_t entry_bytes(const DistillArgs &a) { return size_t(a.top) * 12; }
+
+template <class T, int THREADS>
+rdf2v_status launch_rows(const DistillArgs &a, hipStream_t stream) {
+  return for_each_launch(a.rows, THREADS, 1, [&](int64_t first, int64_t count) {
+    distill_row_kernel<T, THREADS>
+        <<<dim3(unsigned(count)), dim3(THREADS), entry_bytes(a), stream>>>(a, first);
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
+}
+
+template <class T>
+rdf2v_status launch(const DistillArgs &a, void *workspace, hipStream_t stream) {
+  const int64_t vectors = row_vectors(a.vocab, a.dtype);
+  if (vectors <= int64_t(kVectors) * kWave) return launch_rows<T, kWave>(a, stream);
+  if (vectors <= kSlice) return launch_rows<T, kSliceThreads>(a, stream);
+  if (vectors <= kLargest) return launch_rows<T, 1024>(a, stream);
+  Workspace ws{};
+  ws.slices = slice_count(a.vocab, a.dtype);
+  ws.parts = static_cast<float2 *>(workspace);
+  ws.zk = reinterpret_cast<float *>(static_cast<char *>(workspace) +
+                                    align_up(size_t(a.rows) * ws.slices * sizeof(float2), 256));
+  // as many rows at a time as stay cached between the two launches
+  int64_t batch = a.dlogits == nullptr || a.loss == nullptr ? a.rows : kCached / (a.vocab * int64_t(sizeof(T)));
+  if (batch < 1) batch = 1;
+  for (int64_t row = 0; row < a.rows; row += batch) {
+    const int64_t rows = a.rows - row < batch ? a.rows - row : batch;
+    const int64_t stats = a.loss != nullptr ? ws.slices : 1, grads = a.dlogits != nullptr ? ws.slices : 1;
+    rdf2v_status st = for_each_launch(rows * stats, kSliceThreads, 1, [&](int64_t first, int64_t count) {
+      distill_stats_kernel<T>
+          <<<dim3(unsigned(count)), dim3(kSliceThreads), 0, stream>>>(a, ws, row * stats + first);
+      RDF2V_LAUNCH_CHECK();
+      return RDF2V_OK;
+    });
+    if (st != RDF2V_OK) return st;
+    st = for_each_launch(rows * grads, kSliceThreads, 1, [&](int64_t first, int64_t count) {
+      distill_grad_kernel<T>
+          <<<dim3(unsigned(count)), dim3(kSliceThreads), entry_bytes(a), stream>>>(a, ws, row * grads + first);
+      RDF2V_LAUNCH_CHECK();
+      return RDF2V_OK;
+    });
+    if (st != RDF2V_OK) return st;
+  }
+  return RDF2V_OK;
 }
 
 }  // namespace
 
-size_t distill_workspace_bytes(int64_t, int64_t, int32_t, int32_t) { return 0; }
+size_t distill_workspace_bytes(int64_t rows, int64_t vocab, int32_t top, int32_t dtype) {
+  if (row_vectors(vocab, dtype) <= kLargest) return 0;
+  return align_up(size_t(rows) * slice_count(vocab, dtype) * sizeof(float2), 256) +
+         align_up(size_t(rows) * top * sizeof(float), 256);
+}
 
-rdf2v_status launch_distill(const DistillArgs &a, void *, hipStream_t stream) {
-  return for_each_launch(a.rows, kThreads, 1, [&](int64_t first, int64_t count) {
-    if (a.dtype == RDF2V_BF16)
-      distill_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(a, first);
-    else
-      distill_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(a, first);
-    RDF2V_LAUNCH_CHECK();
-    return RDF2V_OK;
-  });
+rdf2v_status launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream) {
+  return a.dtype == RDF2V_BF16 ? launch<bf16>(a, workspace, stream) : launch<float>(a, workspace, stream);
 }
 
 }  // namespace rdf2v
