@@ -620,8 +620,6 @@ size_t segment_state_bytes(const rdf2v_attention &a) {
   return segments == 1 ? 0 : align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float), 256);
 }
 
-constexpr int kColumns = 64;  // columns of S per workgroup of the step, one to a lane
-
 // Sums of the gradients of `share` query heads, in head order.
 template <class T>
 __global__ __launch_bounds__(256) void share_sum_kernel(const float *part, T *out, int64_t groups, int share, int d,
@@ -739,16 +737,18 @@ struct StepArgs {
   float scale;
 };
 
-template <class T>
-__global__ __launch_bounds__(kColumns) void step_kernel(StepArgs p, int64_t first) {
-  const int blocks_n = (p.dv + kColumns - 1) / kColumns;
-  const int64_t block = first + blockIdx.x;
-  const int nb = int(block % blocks_n);
-  const int h = int(block / blocks_n % p.heads);
-  const int64_t row = block / blocks_n / p.heads;
-  const int n = nb * kColumns + threadIdx.x;
-  const bool report = nb == 0 && threadIdx.x == 0;
-  const float gamma = expf(head_log_decay(p.log_decay, h, p.status, report && row == 0));
+// One workgroup to a row and head. HBM-bound: a state is read and written once,
+// 2 operations a byte, VEC values a lane and kAhead loads of a lane in flight
+// (a state of 128 x 128 is 16 loads of 16 bytes a thread).
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void step_kernel(StepArgs p, int64_t first) {
+  typedef float vec __attribute__((ext_vector_type(VEC)));
+  constexpr int kAhead = 16;
+  __shared__ float ks[RDF2V_MAX_HEAD_SIZE], qs[RDF2V_MAX_HEAD_SIZE];
+  __shared__ vec part[kThreads];
+  const int64_t block = first + blockIdx.x, row = block / p.heads;
+  const int h = int(block % p.heads);
+  const bool report = threadIdx.x == 0;
   int64_t from = row;
   if (p.parents != nullptr) {
     from = p.parents[row];
@@ -757,19 +757,65 @@ __global__ __launch_bounds__(kColumns) void step_kernel(StepArgs p, int64_t firs
       if (report && h == 0 && p.status != nullptr) atomicOr(p.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
     }
   }
-  const T *q = operand_row<T>(p.q, row, h), *k = operand_row<T>(p.k, row, h), *v = operand_row<T>(p.v, row, h);
-  if (n >= p.dv) return;
+  const int cols = p.dv / VEC, rows = kThreads / cols;  // lanes over a row of the state, rows side by side
+  const int col = threadIdx.x % cols, r0 = threadIdx.x / cols;
+  const bool active = r0 < rows;
   const int64_t size = int64_t(p.dk) * p.dv;
-  const float *s0 = p.state + (from * p.heads + h) * size + n;
-  float *s1 = p.state_out + (row * p.heads + h) * size + n;
-  const float vn = to_f32(v[n]);
-  float o = 0.0f;
-  for (int i = 0; i < p.dk; ++i) {
-    const float s = fmaf(from < 0 ? 0.0f : s0[int64_t(i) * p.dv], gamma, to_f32(k[i]) * vn);
-    s1[int64_t(i) * p.dv] = s;
-    o = fmaf(to_f32(q[i]), s, o);
+  const vec *s0 = reinterpret_cast<const vec *>(p.state + (from < 0 ? 0 : from * p.heads + h) * size);
+  vec *s1 = reinterpret_cast<vec *>(p.state_out + (row * p.heads + h) * size);
+  const int last = from < 0 || !active ? 0 : p.dk;      // rows of the state that are read
+  vec s[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int r = r0 + i * rows;
+    s[i] = vec(0.0f);
+    if (r < last) s[i] = __builtin_nontemporal_load(s0 + r * cols + col);
   }
-  static_cast<T *>(p.out)[(row * p.heads + h) * p.dv + n] = from_f32<T>(o * p.scale);
+  const float gamma = expf(head_log_decay(p.log_decay, h, p.status, report && row == 0));
+  if (int(threadIdx.x) < p.dk) {
+    ks[threadIdx.x] = to_f32(operand_row<T>(p.k, row, h)[threadIdx.x]);
+    qs[threadIdx.x] = to_f32(operand_row<T>(p.q, row, h)[threadIdx.x]);
+  }
+  const T *v = operand_row<T>(p.v, row, h) + col * VEC;
+  vec vn;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) vn[j] = to_f32(v[j]);
+  __syncthreads();
+  vec o = vec(0.0f);
+  if (active)
+    for (int base = r0; base < p.dk; base += kAhead * rows) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int r = base + i * rows;
+        if (base != r0) s[i] = r < last ? s0[r * cols + col] : vec(0.0f);
+        if (r >= p.dk) continue;
+        const vec x = s[i] * gamma + vn * ks[r];
+        __builtin_nontemporal_store(x, s1 + r * cols + col);
+        o += x * qs[r];
+      }
+    }
+  part[threadIdx.x] = o;
+  __syncthreads();
+  T *out = static_cast<T *>(p.out) + (row * p.heads + h) * p.dv;
+  for (int n = threadIdx.x; n < p.dv; n += kThreads) {
+    float sum = 0.0f;
+    for (int r = 0; r < rows; ++r) sum += part[r * cols + n / VEC][n % VEC];
+    out[n] = from_f32<T>(sum * p.scale);
+  }
+}
+
+template <class T>
+rdf2v_status launch_step(const StepArgs &p, hipStream_t stream) {
+  const bool wide = p.dv % 4 == 0 &&
+                    ((reinterpret_cast<uintptr_t>(p.state) | reinterpret_cast<uintptr_t>(p.state_out)) & 15) == 0;
+  return for_each_launch(p.rows * p.heads, kThreads, 1, [&](int64_t first, int64_t count) {
+    if (wide)
+      step_kernel<T, 4><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+    else
+      step_kernel<T, 1><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
 }
 
 }  // namespace
@@ -805,15 +851,7 @@ rdf2v_status launch_decay_attention_step(const rdf2v_attention &a, const rdf2v_h
   const int share = a.heads / a.kv_heads;
   const StepArgs p{operand(q, 1), operand(k, share), operand(v, share), a.log_decay, state, parents, out, state_out,
                    status_dev, num_states, a.rows, a.heads, a.dk, a.dv, a.scale};
-  const int64_t blocks = a.rows * a.heads * ((a.dv + kColumns - 1) / kColumns);
-  return for_each_launch(blocks, kColumns, 1, [&](int64_t first, int64_t count) {
-    if (a.dtype == RDF2V_BF16)
-      step_kernel<bf16><<<dim3(unsigned(count)), dim3(kColumns), 0, stream>>>(p, first);
-    else
-      step_kernel<float><<<dim3(unsigned(count)), dim3(kColumns), 0, stream>>>(p, first);
-    RDF2V_LAUNCH_CHECK();
-    return RDF2V_OK;
-  });
+  return a.dtype == RDF2V_BF16 ? launch_step<bf16>(p, stream) : launch_step<float>(p, stream);
 }
 
 }  // namespace rdf2v
