@@ -248,6 +248,11 @@ class _on_stream:
     __slots__ = ("_handle", "_switch")
 
     def __init__(self, device: torch.device, stream):
+        if stream is None and device.index == torch.cuda.current_device():
+            # the handle alone: a stream object would cost a small call a tenth of its time
+            self._switch = None
+            self._handle = torch._C._cuda_getCurrentRawStream(device.index)
+            return
         if stream is None:
             s = torch.cuda.current_stream(device)
         elif isinstance(stream, torch.cuda.Stream):
@@ -256,8 +261,7 @@ class _on_stream:
             s = torch.cuda.ExternalStream(int(stream), device=device)
         if s.device != device:
             raise TypeError(f"stream is on {s.device}, the call's tensors on {device}")
-        current = stream is None and device.index == torch.cuda.current_device()
-        self._switch = None if current else torch.cuda.stream(s)
+        self._switch = torch.cuda.stream(s)
         self._handle = s.cuda_stream
 
     def __enter__(self) -> int:
@@ -688,11 +692,11 @@ def _float_dtype(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _heads_view(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> _HeadsViewStruct:
+def _heads_view(t: torch.Tensor, name: str, dtype: torch.dtype, dev: torch.device, shape) -> _HeadsViewStruct:
     """A [rows, tokens, heads, size] (or [rows, heads, size]) input in any layout whose last dimension
     is contiguous."""
-    if not isinstance(t, torch.Tensor) or t.device != like.device or t.dtype != like.dtype:
-        raise TypeError(f"{name} must be a {like.dtype} tensor on {like.device}")
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev:
+        raise TypeError(f"{name} must be a {dtype} tensor on {dev}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
     stride = t.stride()
@@ -701,20 +705,17 @@ def _heads_view(t: torch.Tensor, name: str, like: torch.Tensor, shape) -> _Heads
     return _HeadsViewStruct(t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0, stride[-2])
 
 
+def _exact(t: torch.Tensor, name: str, dtype: torch.dtype, shape, dev: torch.device) -> torch.Tensor:
+    """A contiguous tensor of exactly this shape, type and device."""
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype == dtype and t.device == dev and t.is_contiguous():
+        return t
+    _out(t, name, dtype, 0, dev)
+    raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
+
+
 def _state(t: torch.Tensor | None, name: str, shape, dev: torch.device) -> torch.Tensor | None:
     """An optional float32 state tensor of exactly this shape."""
-    if t is None:
-        return None
-    if isinstance(t, torch.Tensor) and t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
-    return _out(t, name, torch.float32, 0, dev)
-
-
-def _exact(t: torch.Tensor, name: str, dtype: torch.dtype, shape, dev: torch.device) -> torch.Tensor:
-    _out(t, name, dtype, 0, dev)
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
-    return t
+    return None if t is None else _exact(t, name, torch.float32, shape, dev)
 
 
 class _Attention:
@@ -724,17 +725,21 @@ class _Attention:
 
     def __init__(self, q, k, v, log_decay, scale, lens, ndim):
         dtype = _float_dtype(q, "q")
-        if q.dim() != ndim or not isinstance(k, torch.Tensor) or k.dim() != ndim or not isinstance(v, torch.Tensor) \
-                or v.dim() != ndim:
+        if not isinstance(v, torch.Tensor):
+            raise TypeError("v must be a CUDA (HIP) tensor")
+        shape, kind = q.shape, q.dtype
+        if len(shape) != ndim or v.dim() != ndim:
             raise ValueError(f"q, k and v must have {ndim} dimensions")
         self.dev = dev = q.device
-        lead, (heads, dk), (kv_heads, dv) = q.shape[:-2], q.shape[-2:], v.shape[-2:]
+        heads, dk = shape[-2:]
+        kv_heads, dv = v.shape[-2:]
         if kv_heads < 1 or heads % kv_heads:
             raise ValueError(f"{heads} query heads are no multiple of {kv_heads} key and value heads")
         if not 1 <= dk <= RDF2V_MAX_HEAD_SIZE or not 1 <= dv <= RDF2V_MAX_HEAD_SIZE:
             raise ValueError(f"head sizes {dk} and {dv}: 1 to {RDF2V_MAX_HEAD_SIZE} are supported")
-        self.views = (_heads_view(q, "q", q, lead + (heads, dk)), _heads_view(k, "k", q, lead + (kv_heads, dk)),
-                      _heads_view(v, "v", q, lead + (kv_heads, dv)))
+        lead = shape[:-2]
+        self.views = (_heads_view(q, "q", kind, dev, shape), _heads_view(k, "k", kind, dev, (*lead, kv_heads, dk)),
+                      _heads_view(v, "v", kind, dev, (*lead, kv_heads, dv)))
         _exact(log_decay, "log_decay", torch.float32, (heads,), dev)
         if lens is not None:
             _exact(lens, "lens", torch.int32, (lead[0],), dev)
@@ -808,7 +813,7 @@ def rdf2v_decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Te
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
         shape = (c.rows, c.heads, c.dk, c.dv)
-        view = _heads_view(dout, "dout", q, (c.rows, c.length, c.heads, c.dv))
+        view = _heads_view(dout, "dout", q.dtype, dev, (c.rows, c.length, c.heads, c.dv))
         grads = []
         for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
             grads.append(torch.empty(like.shape, dtype=q.dtype, device=dev) if t is None else
@@ -852,7 +857,9 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
         shape = (c.rows, c.heads, c.dk, c.dv)
         num_states = c.rows
         if parents is not None:
-            _exact(_dev_i32(parents, "parents").reshape(-1), "parents", torch.int32, (c.rows,), dev)
+            _out(parents, "parents", torch.int32, 0, dev)
+            if parents.numel() != c.rows:
+                raise ValueError(f"parents holds {parents.numel()} elements; this call needs {c.rows}")
             num_states = state.shape[0] if isinstance(state, torch.Tensor) and state.dim() == 4 else c.rows
         if state is None:
             raise TypeError("state must be a CUDA (HIP) tensor")
