@@ -40,15 +40,24 @@ struct ScanArgs {
   int64_t rows, length;
   int32_t heads, di, dout;
   float oscale, sscale;
-  bool transposed;  // s0 is stored [dout][di]
+  bool transposed;  // s0 and seg_state are stored [dout][di]
   bool reverse;
   // set by launch_scan
   float pscale;              // oscale * sscale
-  int32_t blocks_n;          // workgroups over the columns
   int64_t segments, segment; // segments of a row, and their tokens (whole chunks)
-  float *seg_state;          // [rows][heads][segments][di][dout], or null for one segment
-  bool wide, wide_out;       // 16-byte reads, stores of four values
+  // [rows][heads][segments][dk][dv] states that the segments begin with (a state scan: their own), or null
+  float *seg_state;
+  bool wide, wide_out;       // 16-byte reads (rows of one chunk: of four values), stores of four values
+  bool out_f32;              // out is float32 whatever the element type: to be summed over heads
 };
+
+// Scans that run side by side.
+struct ScanRoles {
+  ScanArgs role[3];
+  int32_t count;
+};
+
+constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float head_log_decay(const float *log_decay, int h, int32_t *status, bool report) {
   const float g = log_decay[h];
@@ -239,6 +248,44 @@ struct Loader {
   }
 };
 
+// Role and item of a workgroup: the roles of an item, which read the same
+// operands, run on one XCD (workgroups are dealt to the 8 in turn) and soon
+// after one another.
+constexpr int kXcds = 8;
+__device__ __forceinline__ int role_of(int64_t block, int count, int64_t &item) {
+  const int per = kXcds * count;
+  item = block / per * kXcds + block % kXcds;
+  return int(block % per) / kXcds;
+}
+
+// Four values of an output row, of which `col` is the first column.
+template <class T>
+__device__ __forceinline__ void store_four(const ScanArgs &p, int64_t at, int col, f32x4 x) {
+  typedef typename Vec<T>::four four;
+  if (p.out_f32) {
+    float *to = static_cast<float *>(p.out) + at;
+    if (p.wide_out) {
+      if (col < p.dout) *reinterpret_cast<f32x4 *>(to) = x;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (col + r < p.dout) to[r] = x[r];
+    }
+  } else {
+    T *to = static_cast<T *>(p.out) + at;
+    if (p.wide_out) {
+      four y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = from_f32<T>(x[r]);
+      if (col < p.dout) *reinterpret_cast<four *>(to) = y;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (col + r < p.dout) to[r] = from_f32<T>(x[r]);
+    }
+  }
+}
+
 // One workgroup scans the chunks of one segment of a row for one head and NB
 // columns of c and S.
 //
@@ -258,8 +305,9 @@ struct Loader {
 // waits for the spills made it 2.x times slower.
 constexpr int scan_waves(int nb) { return nb > 64 ? 8 : 4; }
 
-template <class T, class O, int DI, int NB, bool OUT>
-__global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) void scan_kernel(ScanArgs p,
+template <class T, int DI, int NB, bool OUT>
+__global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) void scan_kernel(ScanRoles roles,
+                                                                                             int64_t items,
                                                                                              int64_t first) {
   constexpr int kWaves = scan_waves(NB), kThreads = kWaves * kWave;
   constexpr int kWavesN = NB / kTile;                      // waves side by side over the columns
@@ -272,23 +320,21 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   typedef typename Vec<T>::four four;
   typedef typename Vec<T>::eight eight;
 
-  const int64_t block = first + blockIdx.x;
-  const int nb = int(block % p.blocks_n);
-  const int64_t seg = block / p.blocks_n % p.segments;
-  const int h = int(block / p.blocks_n / p.segments % p.heads);
-  const int64_t row = block / p.blocks_n / p.segments / p.heads;
+  int64_t item;
+  const ScanArgs &p = roles.role[role_of(first + blockIdx.x, roles.count, item)];
+  if (item >= items) return;
+  const int64_t seg = item % p.segments, rh = item / p.segments, row = rh / p.heads;
+  const int h = int(rh % p.heads);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id(), l16 = lane % 16, g = lane / 16;
   const int wn = wave % kWavesN, wt = wave / kWavesN;
-  const int n0 = nb * NB;                                  // first column of the workgroup
-  const int nw = wn * kTilesN * kTile;                     // first column of the wave in it
-  const bool report = nb == 0 && seg == 0 && threadIdx.x == 0;
+  const int nw = wn * kTilesN * kTile;                     // first column of the wave
+  const bool report = seg == 0 && threadIdx.x == 0;
   const float head_log2_gamma =
-      head_log_decay(p.log_decay, h, p.status, report && row == 0) * 1.44269504088896341f;
+      head_log_decay(p.log_decay, h, p.status, report && row == 0) * kLog2e;
   const int64_t len = row_length(p.len, row, p.length, p.status, report && h == 0);
   const int e = p.reverse ? 0 : 1;
-  const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h) + n0;
-  const int dout = min(NB, p.dout - n0);
+  const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h);
   const int64_t u_begin = seg * p.segment, u_end = min(p.length, u_begin + p.segment);
   const int64_t u_valid = min(u_end, len);
   const int dt = p.reverse ? -1 : 1;
@@ -296,14 +342,13 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   const bool exact_state = !OUT || (p.s1 != nullptr && p.seg_state == nullptr);
 
   f32x4 s[kTilesN][kTilesI];
-  const int64_t state_at = (row * p.heads + h) * int64_t(p.di) * p.dout;
+  const int64_t size = int64_t(p.di) * p.dout;
   {
-    const float *s0 = OUT && p.seg_state != nullptr
-                          ? p.seg_state + (row * p.heads + h) * p.segments * int64_t(p.di) * p.dout +
-                                seg * int64_t(p.di) * p.dout
-                          : (OUT && p.s0 != nullptr ? p.s0 + state_at : nullptr);
-    const bool transposed = p.transposed && p.seg_state == nullptr;
-    const int per_k = transposed ? 1 : p.dout, per_col = transposed ? p.di : 1;
+    const float *s0 = !OUT                     ? nullptr
+                      : p.seg_state != nullptr ? p.seg_state + (rh * p.segments + seg) * size
+                      : p.s0 != nullptr        ? p.s0 + rh * size
+                                               : nullptr;
+    const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
 #pragma unroll
     for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
@@ -312,7 +357,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         if (s0 == nullptr) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int col = n0 + nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+          const int col = nw + n * kTile + l16, k = i * kTile + 4 * g + r;
           if (k < p.di && col < p.dout) s[n][i][r] = s0[unsigned(k * per_k + col * per_col)];
         }
       }
@@ -326,7 +371,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     const int64_t low = p.reverse ? t0 - (n - 1) : t0;
     if (OUT) la.fetch(thread, a + low * p.a.token, int(p.a.token), p.reverse, n, p.di);
     lb.fetch(thread, b + low * p.b.token, int(p.b.token), p.reverse, n, p.di);
-    lc.fetch(thread, c + low * p.c.token, int(p.c.token), p.reverse, n, dout);
+    lc.fetch(thread, c + low * p.c.token, int(p.c.token), p.reverse, n, p.dout);
   };
   if (p.wide && u_begin < u_valid) fetch(threadIdx.x, u_begin);
   __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
@@ -345,11 +390,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     if (p.wide) {
       if (OUT) la.store(thread, as, n_valid, p.di);
       lb.store(thread, bs, n_valid, p.di);
-      lc.store(thread, cs, n_valid, dout);
+      lc.store(thread, cs, n_valid, p.dout);
     } else {
       if (OUT) la.copy(thread, as, a + t0 * p.a.token, dt * p.a.token, n_valid, p.di);
       lb.copy(thread, bs, b + t0 * p.b.token, dt * p.b.token, n_valid, p.di);
-      lc.copy(thread, cs, c + t0 * p.c.token, dt * p.c.token, n_valid, dout);
+      lc.copy(thread, cs, c + t0 * p.c.token, dt * p.c.token, n_valid, p.dout);
     }
     __syncthreads();
     if (p.wide && !last) fetch(thread, u0 + kChunk);
@@ -463,7 +508,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     __syncthreads();  // the weights are there, and a, b and c are read
 
     if (OUT) {
-      O *out = static_cast<O *>(p.out) + ((row * p.length + t0) * p.heads + h) * int64_t(p.dout) + n0;
+      const int64_t out_at = ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
 #pragma unroll
       for (int t = 0; t < kTilesT; ++t) {
         const int tt = wt * kTilesT + t;
@@ -481,20 +526,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         }
         const int u = tt * kTile + l16;
         if (u >= n_valid) continue;
-        O *to = out + dt * u * (p.heads * p.dout);  // 64 tokens of 65,535 heads stay below 2^31
+        const int64_t at = out_at + dt * u * (p.heads * p.dout);  // 64 tokens of 65,535 heads stay below 2^31
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n) {
           const int col = nw + n * kTile + 4 * g;
-          typename Vec<O>::four v;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[r] = from_f32<O>(o[t][n][r]);
-          if (p.wide_out) {
-            if (col < dout) *reinterpret_cast<typename Vec<O>::four *>(to + col) = v;
-          } else {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (col + r < dout) to[col + r] = v[r];
-          }
+          store_four<T>(p, at + col, col, o[t][n]);
         }
       }
     }
@@ -502,41 +538,234 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 
   if (OUT) {  // tokens beyond the row's length
     const int64_t t_begin = max(u_begin, len);
-    O *out = static_cast<O *>(p.out) + ((row * p.length + t_begin) * p.heads + h) * int64_t(p.dout) + n0;
-    const int per = 4;
-    const int cols = (dout + per - 1) / per;
+    const int64_t out_at = ((row * p.length + t_begin) * p.heads + h) * int64_t(p.dout);
+    const int cols = (p.dout + 3) / 4;
     for (int64_t i = threadIdx.x; i < (u_end - t_begin) * cols; i += kThreads) {
-      O *to = out + i / cols * p.heads * p.dout + i % cols * per;
-      if (p.wide_out)
-        *reinterpret_cast<typename Vec<O>::four *>(to) = typename Vec<O>::four{};
-      else
-        for (int r = 0; r < per && i % cols * per + r < dout; ++r) to[r] = from_f32<O>(0.0f);
+      const int col = int(i % cols) * 4;
+      store_four<T>(p, out_at + i / cols * p.heads * p.dout + col, col, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
     }
   }
   float *s1 = OUT ? (p.seg_state == nullptr ? p.s1 : nullptr) : p.seg_state;
   if (s1 == nullptr) return;
-  s1 += OUT ? state_at : (row * p.heads + h) * p.segments * int64_t(p.di) * p.dout + seg * int64_t(p.di) * p.dout;
+  s1 += OUT ? rh * size : (rh * p.segments + seg) * size;
 #pragma unroll
   for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
     for (int i = 0; i < kTilesI; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int col = n0 + nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+        const int col = nw + n * kTile + l16, k = i * kTile + 4 * g + r;
         if (wt == 0 && k < p.di && col < p.dout) s1[unsigned(k * p.dout + col)] = s[n][i][r];
       }
 }
 
+// Rows of at most one chunk: one wave to a row and head, in registers alone.
+//
+// The results of the weights' products are, in the order of the contractions
+// above, operands of the products with c as they stand, so the wave needs no
+// LDS and no barrier, and many waves share a CU: with a workgroup to a row,
+// rows of 17 tokens left most of its waves idle at its barriers
+// (16,000 rows and heads of 17 x 32 in bfloat16: 73 us against 1x us here).
+//
+// TT: most tiles of 16 tokens.
+constexpr int kShortWaves = 4;  // of a workgroup, each for itself
+
+template <class T>
+__device__ __forceinline__ typename Vec<T>::eight short_row(const T *token, int kk, int g, int di, bool quads) {
+  typedef typename Vec<T>::four four;
+  typedef T any_four __attribute__((ext_vector_type(4), aligned(2)));
+  four x[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int col = kk * 32 + i * 16 + 4 * g;
+    x[i] = four{};
+    if (quads) {
+      const four y = *reinterpret_cast<const any_four *>(token + (col < di ? col : 0));
+      if (col < di) x[i] = y;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (col + r < di) x[i][r] = token[col + r];
+    }
+  }
+  return join(x[0], x[1]);
+}
+
+template <class T, int DI, int TT>
+__global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRoles roles, int64_t items,
+                                                                         int64_t first) {
+  constexpr int kK = DI / 32, kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
+  typedef typename Vec<T>::eight eight;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t item = (first + blockIdx.x) * kShortWaves + wave;
+  if (item >= items) return;
+  const ScanArgs &p = roles.role[item % roles.count];
+  const int64_t rh = item / roles.count, row = rh / p.heads;
+  const int h = int(rh % p.heads);
+  const int lane = lane_id(), l16 = lane % 16, g = lane / 16;
+  const bool report = lane == 0;
+  const float log2_gamma = head_log_decay(p.log_decay, h, p.status, report && row == 0) * kLog2e;
+  const int len = int(row_length(p.len, row, p.length, p.status, report && h == 0));
+  const int tiles = (len + kTile - 1) / kTile, blocks = (len + 31) / 32;
+  const int e = p.reverse ? 0 : 1;
+  const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h);
+  // the token that is u-th in the scan's order
+  auto token_of = [&](int u) { return int64_t(p.reverse ? len - 1 - u : u); };
+
+  // weights of the pairs (t, s) as operands: tile t, blocks of 32 of s
+  eight w[TT][(TT + 1) / 2][kPieces];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    if (t >= tiles) break;
+    const T *at = a + token_of(min(t * kTile + l16, len - 1)) * p.a.token;
+    eight av[kK];
+#pragma unroll
+    for (int kk = 0; kk < kK; ++kk)
+      if (kk * 32 < p.di) av[kk] = short_row(at, kk, g, p.di, p.wide);
+#pragma unroll
+    for (int s32 = 0; s32 <= t / 2; ++s32) {
+      f32x4 x[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int st = 2 * s32 + i;
+        x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (st > t) continue;
+        const T *bt = b + token_of(min(st * kTile + l16, len - 1)) * p.b.token;
+#pragma unroll
+        for (int kk = 0; kk < kK; ++kk)
+          if (kk * 32 < p.di) x[i] = mma(short_row(bt, kk, g, p.di, p.wide), av[kk], x[i]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int d = (t - st) * kTile + l16 - 4 * g - r;
+          x[i][r] = d >= 0 ? x[i][r] * p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
+        }
+      }
+      f32x8 both = join(x[0], x[1]);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) w[t][s32][i] = take_piece(both, T());
+    }
+  }
+
+  const int64_t state_at = rh * int64_t(p.di) * p.dout;
+  const float *s0 = p.s0 == nullptr ? nullptr : p.s0 + state_at;
+  const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
+  const int64_t out_step = int64_t(p.heads) * p.dout;
+  const int64_t out_at = (row * p.length * p.heads + h) * p.dout;
+  for (int n0 = 0; n0 < p.dout; n0 += kTile) {
+    const int col = n0 + l16;
+    eight cv[(TT + 1) / 2];
+#pragma unroll
+    for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
+      if (kk >= blocks) break;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+        const T x = c[token_of(min(u, len - 1)) * p.c.token + min(col, p.dout - 1)];
+        cv[kk][j] = u < len && col < p.dout ? x : T(0.0f);
+      }
+    }
+    f32x4 o[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (s0 != nullptr) {
+#pragma unroll
+      for (int kk = 0; kk < kK; ++kk) {
+        if (kk * 32 >= p.di) break;
+        f32x8 x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int k = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+          x[j] = k < p.di && col < p.dout ? s0[unsigned(k * per_k + col * per_col)] : 0.0f;
+        }
+        eight sv[kPieces];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) sv[i] = take_piece(x, T());
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          if (t >= tiles) break;
+          const T *at = a + token_of(min(t * kTile + l16, len - 1)) * p.a.token;
+          const eight av = short_row(at, kk, g, p.di, p.wide);
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) o[t] = mma(sv[i], av, o[t]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+        o[t] *= p.oscale * __builtin_amdgcn_exp2f(float(t * kTile + l16 + e) * log2_gamma);
+    }
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      if (t >= tiles) break;
+#pragma unroll
+      for (int kk = 0; kk <= t / 2; ++kk)
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) o[t] = mma(cv[kk], w[t][kk][i], o[t]);
+      const int u = t * kTile + l16;
+      if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
+    }
+    if (p.s1 == nullptr) continue;
+    // S at the row's end, a tile at a time
+    const float whole = __builtin_amdgcn_exp2f(float(len) * log2_gamma);
+    eight wv[(TT + 1) / 2][kStatePieces];
+#pragma unroll
+    for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
+      if (kk >= blocks) break;
+      f32x8 x;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+        x[j] = to_f32(cv[kk][j]) * p.sscale * __builtin_amdgcn_exp2f(float(max(len - e - u, 0)) * log2_gamma);
+      }
+#pragma unroll
+      for (int i = 0; i < kStatePieces; ++i) wv[kk][i] = take_piece(x, T());
+    }
+    for (int i0 = 0; i0 < p.di; i0 += kTile) {
+      f32x4 s;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int k = i0 + 4 * g + r;
+        s[r] = s0 != nullptr && k < p.di && col < p.dout ? s0[unsigned(k * per_k + col * per_col)] * whole : 0.0f;
+      }
+#pragma unroll
+      for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
+        if (kk >= blocks) break;
+        eight bv;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+          const T x = b[token_of(min(u, len - 1)) * p.b.token + min(i0 + l16, p.di - 1)];
+          bv[j] = u < len && i0 + l16 < p.di ? x : T(0.0f);
+        }
+#pragma unroll
+        for (int i = 0; i < kStatePieces; ++i) s = mma(bv, wv[kk][i], s);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int k = i0 + 4 * g + r;
+        if (k < p.di && col < p.dout) p.s1[state_at + k * p.dout + col] = s[r];
+      }
+    }
+  }
+  // tokens beyond the row's length
+  const int cols = (p.dout + 3) / 4;
+  for (int i = lane; i < (int(p.length) - len) * cols; i += kWave) {
+    const int col = i % cols * 4;
+    store_four<T>(p, out_at + (len + i / cols) * out_step + col, col, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+  }
+}
+
 // The states that the segments of a row begin with, in place of the segments'
 // own, and the row's last state.
-__global__ __launch_bounds__(kThreads) void join_kernel(ScanArgs p, int64_t first) {
+__global__ __launch_bounds__(kThreads) void join_kernel(ScanRoles roles, int64_t first) {
+  const int64_t block = first + blockIdx.x;
+  const ScanArgs &p = roles.role[block % roles.count];
   const int64_t size = int64_t(p.di) * p.dout, parts = (size + kThreads - 1) / kThreads;
-  const int64_t block = first + blockIdx.x, rh = block / parts, at = block % parts * kThreads + threadIdx.x;
+  const int64_t rh = block / roles.count / parts, at = block / roles.count % parts * kThreads + threadIdx.x;
   if (at >= size) return;
-  const float log2_gamma = head_log_decay(p.log_decay, int(rh % p.heads), nullptr, false) * 1.44269504088896341f;
+  const float log2_gamma = head_log_decay(p.log_decay, int(rh % p.heads), nullptr, false) * kLog2e;
   const int64_t len = row_length(p.len, rh / p.heads, p.length, nullptr, false);
   float cur = 0.0f;
-  if (p.s0 != nullptr) cur = p.s0[rh * size + (p.transposed ? at % p.dout * p.di + at / p.dout : at)];
+  if (p.s0 != nullptr) cur = p.s0[rh * size + at];
   float *x = p.seg_state + rh * p.segments * size + at;
   constexpr int kAhead = 8;
   for (int64_t seg = 0; seg < p.segments; seg += kAhead) {
@@ -554,17 +783,42 @@ __global__ __launch_bounds__(kThreads) void join_kernel(ScanArgs p, int64_t firs
   if (p.s1 != nullptr) p.s1[rh * size + at] = cur;
 }
 
-template <class T, class O, bool OUT>
-rdf2v_status launch_chunks(const ScanArgs &p, hipStream_t stream) {
-  return for_each_launch(p.rows * p.heads * p.segments * p.blocks_n, 8 * kWave, 1, [&](int64_t first, int64_t count) {
-    const int di = p.di <= 32 ? 32 : p.di <= 64 ? 64 : 128, nb = p.dout <= 32 ? 32 : p.dout <= 64 ? 64 : 128;
+int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
+
+// Scans of one size side by side.
+template <class T, bool OUT>
+rdf2v_status launch_chunks(const ScanRoles &roles, hipStream_t stream) {
+  const ScanArgs &p = roles.role[0];
+  const int64_t items = p.rows * p.heads * p.segments;
+  const int64_t blocks = (items + kXcds - 1) / kXcds * kXcds * roles.count;
+  return for_each_launch(blocks, 8 * kWave, 1, [&](int64_t first, int64_t count) {
+    const int di = padded(p.di), nb = padded(p.dout);
     const dim3 grid{unsigned(count)}, threads{unsigned(scan_waves(nb) * kWave)};
 #define RDF2V_SCAN(DI, NB) \
-  if (di == DI && nb == NB) scan_kernel<T, O, DI, NB, OUT><<<grid, threads, 0, stream>>>(p, first);
+  if (di == DI && nb == NB) scan_kernel<T, DI, NB, OUT><<<grid, threads, 0, stream>>>(roles, items, first);
     RDF2V_SCAN(32, 32) RDF2V_SCAN(32, 64) RDF2V_SCAN(32, 128)
     RDF2V_SCAN(64, 32) RDF2V_SCAN(64, 64) RDF2V_SCAN(64, 128)
     RDF2V_SCAN(128, 32) RDF2V_SCAN(128, 64) RDF2V_SCAN(128, 128)
 #undef RDF2V_SCAN
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
+}
+
+template <class T>
+rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
+  const int64_t items = roles.role[0].rows * roles.role[0].heads * roles.count;
+  int di = 0;
+  for (int i = 0; i < roles.count; ++i) di = roles.role[i].di > di ? roles.role[i].di : di;
+  const int64_t blocks = (items + kShortWaves - 1) / kShortWaves;
+  return for_each_launch(blocks, kShortWaves * kWave, 1, [&](int64_t first, int64_t count) {
+    const dim3 grid{unsigned(count)}, threads{kShortWaves * kWave};
+#define RDF2V_SHORT(DI, TT)                                                                 \
+  if (padded(di) == DI && (roles.role[0].length <= 2 * kTile ? 2 : 4) == TT)                \
+    short_scan_kernel<T, DI, TT><<<grid, threads, 0, stream>>>(roles, items, first);
+    RDF2V_SHORT(32, 2) RDF2V_SHORT(64, 2) RDF2V_SHORT(128, 2)
+    RDF2V_SHORT(32, 4) RDF2V_SHORT(64, 4) RDF2V_SHORT(128, 4)
+#undef RDF2V_SHORT
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });
@@ -575,49 +829,88 @@ rdf2v_status launch_chunks(const ScanArgs &p, hipStream_t stream) {
 // the states of the segments are computed first and joined, and all segments
 // run at once: b and c are read twice, and a state is written and read for
 // each segment. At least kLeastChunks chunks to a segment keep that traffic
-// below what the segment itself reads.
+// below what the segment itself reads. kFill: one row of 20,011 x 8 heads of
+// 128 took 117 us at 256 workgroups, 112 at 512 and 112 at 1,024; four rows of
+// 4,096 x 16 heads, all gradients, 637, 565 and 644.
 constexpr int64_t kFill = 512;
 constexpr int64_t kLeastChunks = 4;
 
-int64_t segment_count(int64_t rows, int64_t length, int64_t heads) {
-  const int64_t chunks = (length + kChunk - 1) / kChunk, base = rows * heads;
-  if (base >= kFill || chunks < 2 * kLeastChunks) return 1;
-  const int64_t want = (kFill + base - 1) / base, most = chunks / kLeastChunks;
+int64_t segment_count(int64_t scans, int64_t length) {
+  const int64_t chunks = (length + kChunk - 1) / kChunk;
+  if (scans >= kFill || chunks < 2 * kLeastChunks) return 1;
+  const int64_t want = (kFill + scans - 1) / scans, most = chunks / kLeastChunks;
   const int64_t count = want < most ? want : most, per = (chunks + count - 1) / count;
   return (chunks + per - 1) / per;
 }
 
-template <class T, class O>
-rdf2v_status launch_scan(ScanArgs p, float *seg_state, hipStream_t stream) {
+template <class T>
+void finish(ScanArgs &p, bool one_chunk, int64_t segments) {
   p.pscale = p.oscale * p.sscale;
-  p.blocks_n = 1;
-  p.segments = segment_count(p.rows, p.length, p.heads);
   const int64_t chunks = (p.length + kChunk - 1) / kChunk;
-  p.segment = (chunks + p.segments - 1) / p.segments * kChunk;
+  p.segments = segments;
+  p.segment = (chunks + segments - 1) / segments * kChunk;
   auto fits = [](const ScanOperand &x, int d) {
     if (x.token < 0 || x.token >= int64_t(1) << 23) return false;
     const uintptr_t all = reinterpret_cast<uintptr_t>(x.data) |
                           uintptr_t(x.row | x.token | x.head | int64_t(d)) * sizeof(T);
     return (all & 15) == 0;
   };
-  p.wide = fits(p.a, p.di) && fits(p.b, p.di) && fits(p.c, p.dout);
-  p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(O) - 1)) == 0;
-  if (p.segments == 1) return launch_chunks<T, O, true>(p, stream);
-  p.seg_state = seg_state;
-  rdf2v_status st = launch_chunks<T, O, false>(p, stream);
-  if (st != RDF2V_OK) return st;
-  const int64_t parts = (int64_t(p.di) * p.dout + kThreads - 1) / kThreads;
-  st = for_each_launch(p.rows * p.heads * parts, kThreads, 1, [&](int64_t first, int64_t count) {
-    join_kernel<<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
-    RDF2V_LAUNCH_CHECK();
-    return RDF2V_OK;
-  });
-  return st == RDF2V_OK ? launch_chunks<T, O, true>(p, stream) : st;
+  p.wide = one_chunk ? p.di % 4 == 0 : (p.a.data == nullptr || fits(p.a, p.di)) && fits(p.b, p.di) && fits(p.c, p.dout);
+  p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (p.out_f32 || sizeof(T) == 4 ? 15 : 7)) == 0;
 }
 
-size_t segment_state_bytes(const rdf2v_attention &a) {
-  const int64_t segments = segment_count(a.rows, a.length, a.heads);
-  return segments == 1 ? 0 : align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float), 256);
+// `count` scans; states[state_of[i]] is the scan that gives scan i its states
+// where rows are cut into segments (its own s0 and s1 are then not used).
+template <class T>
+rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_states, const int *state_of,
+                          float *seg_state, bool together, hipStream_t stream) {
+  const bool one_chunk = scans[0].length <= kChunk;
+  const int64_t segments = segment_count(scans[0].rows * scans[0].heads * count, scans[0].length);
+  if (segments > 1) {
+    ScanRoles roles{};
+    for (int i = 0; i < num_states; ++i) {
+      finish<T>(states[i], false, segments);
+      states[i].seg_state = seg_state + i * states[i].rows * states[i].heads * segments * states[i].di * states[i].dout;
+      roles.role[roles.count++] = states[i];
+    }
+    rdf2v_status st = launch_chunks<T, false>(roles, stream);
+    if (st != RDF2V_OK) return st;
+    const ScanArgs &p = states[0];
+    const int64_t parts = (int64_t(p.di) * p.dout + kThreads - 1) / kThreads;
+    st = for_each_launch(p.rows * p.heads * parts * num_states, kThreads, 1, [&](int64_t first, int64_t blocks) {
+      join_kernel<<<dim3(unsigned(blocks)), dim3(kThreads), 0, stream>>>(roles, first);
+      RDF2V_LAUNCH_CHECK();
+      return RDF2V_OK;
+    });
+    if (st != RDF2V_OK) return st;
+    for (int i = 0; i < count; ++i) {
+      scans[i].seg_state = states[state_of[i]].seg_state;
+      scans[i].s1 = nullptr;
+    }
+    together = true;
+  }
+  bool done[3] = {};
+  for (int i = 0; i < count; ++i) {
+    if (done[i]) continue;
+    ScanRoles roles{};
+    for (int j = i; j < count; ++j) {
+      const bool same = one_chunk || (padded(scans[j].di) == padded(scans[i].di) &&
+                                      padded(scans[j].dout) == padded(scans[i].dout));
+      if (done[j] || !same || (j > i && !together)) continue;
+      finish<T>(scans[j], one_chunk, segments);
+      roles.role[roles.count++] = scans[j];
+      done[j] = true;
+    }
+    const rdf2v_status st = one_chunk ? launch_short<T>(roles, stream) : launch_chunks<T, true>(roles, stream);
+    if (st != RDF2V_OK) return st;
+  }
+  return RDF2V_OK;
+}
+
+size_t segment_state_bytes(const rdf2v_attention &a, bool backward) {
+  const int64_t segments = segment_count(a.rows * a.heads * (backward ? 3 : 1), a.length);
+  if (segments == 1) return 0;
+  return align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float) * (backward ? 2 : 1), 256);
 }
 
 // Sums of the gradients of `share` query heads, in head order.
@@ -662,7 +955,7 @@ template <class T>
 rdf2v_status forward(const rdf2v_attention &a, const rdf2v_heads_view &q, const rdf2v_heads_view &k,
                      const rdf2v_heads_view &v, const float *state, void *out, float *state_out, void *workspace,
                      int32_t *status, hipStream_t stream) {
-  const int share = a.heads / a.kv_heads;
+  const int share = a.heads / a.kv_heads, state_of[1] = {0};
   ScanArgs p = scan_args(a, status);
   p.a = operand(q, 1);
   p.b = operand(k, share);
@@ -673,7 +966,9 @@ rdf2v_status forward(const rdf2v_attention &a, const rdf2v_heads_view &q, const 
   p.s1 = state_out;
   p.out = out;
   p.oscale = a.scale;
-  return launch_scan<T, T>(p, static_cast<float *>(workspace), stream);
+  ScanArgs own = p;
+  own.a = ScanOperand{};
+  return launch_scans<T>(&p, 1, &own, 1, state_of, static_cast<float *>(workspace), true, stream);
 }
 
 template <class T>
@@ -681,48 +976,60 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
                       const rdf2v_heads_view &v, const rdf2v_heads_view &dout, const float *state,
                       const float *dstate_out, void *dq, void *dk, void *dv, float *dstate, void *workspace,
                       int32_t *status, hipStream_t stream) {
-  const int share = a.heads / a.kv_heads;
+  const int share = a.heads / a.kv_heads, state_of[3] = {0, 1, 1};
   const int64_t tokens = a.rows * a.length;
-  float *seg = static_cast<float *>(workspace), *part = seg + segment_state_bytes(a) / sizeof(float);
-  ScanArgs p = scan_args(a, status);
-  p.a = operand(dout, 1);
-  p.b = operand(v, share);
-  p.c = operand(k, share);
-  p.di = a.dv;
-  p.dout = a.dk;
-  p.s0 = state;
-  p.transposed = true;
-  p.out = dq;
-  p.oscale = a.scale;
-  rdf2v_status st = launch_scan<T, T>(p, seg, stream);
-  if (st != RDF2V_OK) return st;
+  float *seg = static_cast<float *>(workspace);
+  float *part_k = seg + segment_state_bytes(a, true) / sizeof(float), *part_v = part_k + tokens * a.heads * a.dk;
 
-  p = scan_args(a, status);
-  p.reverse = true;
-  p.sscale = a.scale;
-  p.a = operand(v, share);
-  p.b = operand(dout, 1);
-  p.c = operand(q, 1);
-  p.di = a.dv;
-  p.dout = a.dk;
-  p.s0 = dstate_out;
-  p.transposed = true;
-  p.out = share > 1 ? part : dk;
-  st = share > 1 ? launch_scan<T, float>(p, seg, stream) : launch_scan<T, T>(p, seg, stream);
-  if (st == RDF2V_OK && share > 1) st = launch_share_sum<T>(part, dk, tokens * a.kv_heads, share, a.dk, stream);
-  if (st != RDF2V_OK) return st;
+  ScanArgs scans[3], states[2];
+  ScanArgs &s = states[0], &r = states[1];  // S of the forward pass, and its gradient
+  s = r = scan_args(a, status);
+  s.di = r.di = a.dk;
+  s.dout = r.dout = a.dv;
+  s.b = operand(k, share);
+  s.c = operand(v, share);
+  s.s0 = state;
+  r.b = operand(q, 1);
+  r.c = operand(dout, 1);
+  r.reverse = true;
+  r.sscale = a.scale;
+  r.s0 = dstate_out;
+  r.s1 = dstate;
 
-  p.a = operand(k, share);
-  p.b = operand(q, 1);
-  p.c = operand(dout, 1);
-  p.di = a.dk;
-  p.dout = a.dv;
-  p.transposed = false;
-  p.out = share > 1 ? part : dv;
-  p.s1 = dstate;
-  st = share > 1 ? launch_scan<T, float>(p, seg, stream) : launch_scan<T, T>(p, seg, stream);
-  if (st == RDF2V_OK && share > 1) st = launch_share_sum<T>(part, dv, tokens * a.kv_heads, share, a.dv, stream);
-  return st;
+  ScanArgs &pq = scans[0], &pk = scans[1], &pv = scans[2];
+  pq = scan_args(a, status);
+  pq.a = operand(dout, 1);
+  pq.b = operand(v, share);
+  pq.c = operand(k, share);
+  pq.di = a.dv;
+  pq.dout = a.dk;
+  pq.s0 = state;
+  pq.transposed = true;
+  pq.out = dq;
+  pq.oscale = a.scale;
+  pk = scan_args(a, status);
+  pk.a = operand(v, share);
+  pk.b = operand(dout, 1);
+  pk.c = operand(q, 1);
+  pk.di = a.dv;
+  pk.dout = a.dk;
+  pk.s0 = dstate_out;
+  pk.transposed = true;
+  pk.reverse = true;
+  pk.sscale = a.scale;
+  pk.out = share > 1 ? part_k : dk;
+  pk.out_f32 = share > 1;
+  pv = r;
+  pv.a = operand(k, share);
+  pv.out = share > 1 ? part_v : dv;
+  pv.out_f32 = share > 1;
+
+  // dv's scan writes dstate while dk's reads dstate_out: one after the other where they are one array
+  const bool together = dstate == nullptr || dstate != dstate_out;
+  rdf2v_status st = launch_scans<T>(scans, 3, states, 2, state_of, seg, together, stream);
+  if (st != RDF2V_OK || share == 1) return st;
+  st = launch_share_sum<T>(part_k, dk, tokens * a.kv_heads, share, a.dk, stream);
+  return st == RDF2V_OK ? launch_share_sum<T>(part_v, dv, tokens * a.kv_heads, share, a.dv, stream) : st;
 }
 
 struct StepArgs {
@@ -821,9 +1128,9 @@ rdf2v_status launch_step(const StepArgs &p, hipStream_t stream) {
 }  // namespace
 
 size_t decay_attention_workspace_bytes(const rdf2v_attention &a, bool backward) {
-  const size_t seg = segment_state_bytes(a);
+  const size_t seg = segment_state_bytes(a, backward);
   if (!backward || a.heads == a.kv_heads) return seg;
-  return seg + align_up(size_t(a.rows) * a.length * a.heads * (a.dk > a.dv ? a.dk : a.dv) * sizeof(float), 256);
+  return seg + align_up(size_t(a.rows) * a.length * a.heads * (a.dk + a.dv) * sizeof(float), 256);
 }
 
 rdf2v_status launch_decay_attention(const rdf2v_attention &a, const rdf2v_heads_view &q, const rdf2v_heads_view &k,
