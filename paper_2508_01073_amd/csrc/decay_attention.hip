@@ -102,18 +102,21 @@ struct Vec<bf16> {
   typedef bf16x4 four;
   typedef bf16x8 eight;
   typedef bf16x8 load;  // 16 bytes
-  // Operands of the matrix products that are computed values: the weights of a
-  // chunk's pairs and the states are fed as two bfloat16 pieces (16 bits, so
-  // that bfloat16 outputs are off by little more than their own rounding), the
-  // addends of the states, which are float32 outputs, as three (24 bits).
-  static constexpr int kPieces = 2, kStatePieces = 3;
+  // Operands of the matrix products that are computed values. The weights of a
+  // chunk's pairs are fed as two bfloat16 pieces (16 bits). A state that earlier
+  // chunks have left is held in float32 and rounded once to be an operand: the
+  // outputs' error is then up to 1.4 times that of their own rounding; with two
+  // pieces it would be 1.0 times, and the scan take 1.2 times as long. What is
+  // added to a state keeps 24 bits, as three pieces, where the state is an
+  // output in float32, and 16 where only bfloat16 outputs are made of it.
+  static constexpr int kPieces = 2, kOperand = 1, kStatePieces = 3;
 };
 template <>
 struct Vec<float> {
   typedef f32x4 four;
   typedef f32x8 eight;
   typedef f32x4 load;
-  static constexpr int kPieces = 1, kStatePieces = 1;
+  static constexpr int kPieces = 1, kOperand = 1, kStatePieces = 1;
 };
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -149,9 +152,6 @@ __device__ __forceinline__ F take_piece(F &x, float) {
   return x;
 }
 
-// LDS reads are not moved ahead of this: what they would hold costs registers.
-__device__ __forceinline__ void keep_order() { asm volatile("" ::: "memory"); }
-
 // A tile of rows of W values in LDS. In bfloat16 the groups of four values of a
 // row are permuted by the row: reads of one group of 16 rows (an operand's
 // row) and of four groups of 8 rows (the transposing reads) then meet every
@@ -163,10 +163,10 @@ struct Tile;
 template <int W>
 struct Tile<bf16, W> {
   static constexpr int kSize = kChunk * W;
-  static __device__ __forceinline__ int at(int row, int group) {
-    const int swap = (row % 8 * (W / 4) / 32 * 4 | row / 8 % 2 * 2) % (W / 4);
-    return row * W + (group ^ swap) * 4;
+  static __device__ __forceinline__ int swap(int row) {
+    return (row % 8 * (W / 4) / 32 * 4 | row / 8 % 2 * 2) % (W / 4);
   }
+  static __device__ __forceinline__ int at(int row, int group) { return row * W + (group ^ swap(row)) * 4; }
 };
 template <int W>
 struct Tile<float, W> {
@@ -203,39 +203,62 @@ __device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int 
 
 // A chunk's rows of one operand on their way from memory to LDS: 64 rows of W
 // values, zeros beyond the operand's size and beyond the chunk's `n` tokens.
-// Every thread reads the same columns of rows kRows apart.
+// `low` points to the chunk's token of the lowest number, `token` is the
+// distance to the next one (64 of them stay below 2^31 bytes).
 template <class T, int W, int THREADS>
 struct Loader {
   typedef typename Vec<T>::load load;
   static constexpr int kPer = 16 / sizeof(T), kCols = W / kPer;
+  // Whole bfloat16 rows go to LDS past the registers, 1 KB a wave and instruction: lane l's 16 bytes land
+  // at 16 l, so each lane reads what the permuted tile has there. Float32 rows, which are padded, wait in
+  // registers.
+  static constexpr bool kDirect = sizeof(T) == 2;
   static constexpr int kRows = THREADS / kCols < kChunk ? THREADS / kCols : kChunk;
   static constexpr int kLoads = kChunk / kRows;
-  load r[kLoads];
+  load r[kDirect ? 1 : kLoads];
 
-  // `low` points to the chunk's token of the lowest number, `token` is the
-  // distance to the next one (64 of them stay below 2^31 bytes). What is not
-  // there is read from a place that is, and dropped on the way to LDS.
-  __device__ __forceinline__ void fetch(unsigned thread, const T *low, int token, bool reverse, int n, int size) {
-    const int u = thread / kCols, col = thread % kCols * kPer;
-    const unsigned at = col < size ? col : 0;
+  __device__ __forceinline__ void fetch(unsigned thread, T *tile, const T *low, int token, bool reverse) {
+    if constexpr (kDirect) {
+      typedef __attribute__((address_space(3))) void lds;
+      typedef const __attribute__((address_space(1))) void global;
+      constexpr int kAtOnce = 512 / W, kSteps = kChunk / kAtOnce;  // rows of an instruction, instructions
+      const int wave = __builtin_amdgcn_readfirstlane(thread / kWave), lane = thread % kWave;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = min(u + i * kRows, n - 1);
-      r[i] = *reinterpret_cast<const load *>(low + (unsigned(__mul24(reverse ? n - 1 - row : row, token)) + at));
+      for (int i = 0; i < (kSteps + THREADS / kWave - 1) / (THREADS / kWave); ++i) {
+        const int step = i * (THREADS / kWave) + wave;
+        if (step >= kSteps) break;
+        const int row = step * kAtOnce + lane / kCols;
+        const int col = (lane % kCols ^ Tile<T, W>::swap(row) / 2) * kPer;
+        const T *from = low + unsigned(__mul24(reverse ? kChunk - 1 - row : row, token) + col);
+        __builtin_amdgcn_global_load_lds((global *)from, (lds *)(tile + step * 512), 16, 0, 0);
+      }
+    } else {
+      const int u = thread / kCols, col = thread % kCols * kPer;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = min(u + i * kRows, kChunk - 1);
+        r[i] = *reinterpret_cast<const load *>(low + unsigned(__mul24(reverse ? kChunk - 1 - row : row, token) + col));
+      }
     }
   }
-  __device__ __forceinline__ void store(unsigned thread, T *tile, int n, int size) const {
-    const int u = thread / kCols, col = thread % kCols * kPer;
-    if (THREADS / kCols > kChunk && u >= kRows) return;
-    if (n == kChunk && size == W) {
+  __device__ __forceinline__ void store(unsigned thread, T *tile) const {
+    if constexpr (!kDirect) {
+      const int u = thread / kCols, col = thread % kCols * kPer;
+      if (THREADS / kCols > kChunk && u >= kRows) return;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         *reinterpret_cast<load *>(tile + Tile<T, W>::at(u + i * kRows, col / 4)) = r[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        *reinterpret_cast<load *>(tile + Tile<T, W>::at(u + i * kRows, col / 4)) =
-            u + i * kRows < n && col < size ? r[i] : load{};
+    }
+  }
+  // A chunk that is not whole, or narrower than the tile.
+  static __device__ __forceinline__ void copy_part(unsigned thread, T *tile, const T *low, int token, bool reverse,
+                                                   int n, int size) {
+    for (int at = thread; at < kChunk * kCols; at += THREADS) {
+      const int row = at / kCols, col = at % kCols * kPer;
+      load x{};
+      if (row < n && col < size)
+        x = *reinterpret_cast<const load *>(low + unsigned(__mul24(reverse ? n - 1 - row : row, token) + col));
+      *reinterpret_cast<load *>(tile + Tile<T, W>::at(row, col / 4)) = x;
     }
   }
   // Value by value, for rows that 16-byte reads do not fit.
@@ -313,7 +336,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   constexpr int kWavesN = NB / kTile;                      // waves side by side over the columns
   constexpr int kWavesT = kWaves / kWavesN;                // and over the chunk's tokens
   constexpr int kTilesN = 1, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
-  constexpr int kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
+  constexpr int kPieces = Vec<T>::kPieces, kOperand = Vec<T>::kOperand, kStatePieces = Vec<T>::kStatePieces;
   __shared__ __attribute__((aligned(16))) T as[OUT ? Tile<T, DI>::kSize : 1], bs[Tile<T, DI>::kSize],
       cs[Tile<T, NB>::kSize];
   __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? Tile<T, kChunk>::kSize : 1];
@@ -365,15 +388,16 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 
   Loader<T, DI, kThreads> la, lb;
   Loader<T, NB, kThreads> lc;
+  // Chunks that fill the tiles are fetched ahead.
+  const bool fills = p.wide && p.di == DI && p.dout == NB;
+  auto whole = [&](int64_t u0) { return fills && u0 + kChunk <= u_valid; };
   auto fetch = [&](unsigned thread, int64_t u0) {
-    const int n = int(min(int64_t(kChunk), u_valid - u0));
-    const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
-    const int64_t low = p.reverse ? t0 - (n - 1) : t0;
-    if (OUT) la.fetch(thread, a + low * p.a.token, int(p.a.token), p.reverse, n, p.di);
-    lb.fetch(thread, b + low * p.b.token, int(p.b.token), p.reverse, n, p.di);
-    lc.fetch(thread, c + low * p.c.token, int(p.c.token), p.reverse, n, p.dout);
+    const int64_t low = p.reverse ? len - u0 - kChunk : u0;
+    if (OUT) la.fetch(thread, as, a + low * p.a.token, int(p.a.token), p.reverse);
+    lb.fetch(thread, bs, b + low * p.b.token, int(p.b.token), p.reverse);
+    lc.fetch(thread, cs, c + low * p.c.token, int(p.c.token), p.reverse);
   };
-  if (p.wide && u_begin < u_valid) fetch(threadIdx.x, u_begin);
+  if (whole(u_begin)) fetch(threadIdx.x, u_begin);
   __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
 
   for (int64_t u0 = u_begin; u0 < u_valid; u0 += kChunk) {
@@ -385,21 +409,31 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     const int lane = thread % kWave, l16 = lane % 16, g = lane / 16;
     const int n_valid = int(min(int64_t(kChunk), u_valid - u0));
     const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
-    const int tiles = (n_valid + kTile - 1) / kTile;       // of tokens that count
     const bool last = u0 + kChunk >= u_valid;
-    if (p.wide) {
-      if (OUT) la.store(thread, as, n_valid, p.di);
-      lb.store(thread, bs, n_valid, p.di);
-      lc.store(thread, cs, n_valid, p.dout);
+    if (whole(u0)) {
+      if (OUT) la.store(thread, as);
+      lb.store(thread, bs);
+      lc.store(thread, cs);
+      if (la.kDirect) {
+        // This wave's part of the chunk is in LDS: what may still be under way are the last chunk's stores,
+        // at least kTilesT of them, where the wave has columns to store.
+        if (OUT && u0 > u_begin && nw < p.dout)
+          __builtin_amdgcn_s_waitcnt(0x0f70 | kTilesT);
+        else
+          __builtin_amdgcn_s_waitcnt(0x0f70);
+      }
+    } else if (p.wide) {
+      const int64_t low = p.reverse ? t0 - (n_valid - 1) : t0;
+      if (OUT) la.copy_part(thread, as, a + low * p.a.token, int(p.a.token), p.reverse, n_valid, p.di);
+      lb.copy_part(thread, bs, b + low * p.b.token, int(p.b.token), p.reverse, n_valid, p.di);
+      lc.copy_part(thread, cs, c + low * p.c.token, int(p.c.token), p.reverse, n_valid, p.dout);
     } else {
       if (OUT) la.copy(thread, as, a + t0 * p.a.token, dt * p.a.token, n_valid, p.di);
       lb.copy(thread, bs, b + t0 * p.b.token, dt * p.b.token, n_valid, p.di);
       lc.copy(thread, cs, c + t0 * p.c.token, dt * p.c.token, n_valid, p.dout);
     }
     __syncthreads();
-    if (p.wide && !last) fetch(thread, u0 + kChunk);
-
-    if (OUT && wave % 4 < tiles) {
+    if (OUT) {
       // the weights of tokens 16 w .. 16 w + 15, and of half of the tokens before them where two waves share
       const int w4 = wave % 4, t = w4 * kTile + l16;
       eight av[kK];
@@ -408,7 +442,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
       for (int j = 0; j < 16 / kWaves; ++j) {
         const int i = wave / 4 * (16 / kWaves) + j;
-        if (i > (w4 | 1)) continue;                        // blocks of 32 that the products below read
+        // blocks of 32 that the products below read
+        if (kWavesT == 1 && i > (w4 | 1)) continue;
         f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
         if (i <= w4) {
 #pragma unroll
@@ -425,7 +460,6 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       }
     }
 
-    keep_order();
     eight cv[kTilesN][2];
 #pragma unroll
     for (int n = 0; n < kTilesN; ++n)
@@ -440,24 +474,23 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         for (int n = 0; n < kTilesN; ++n) o[t][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int kk = 0; kk < kK; ++kk) {
-        eight sv[kTilesN][kPieces];
+        eight sv[kTilesN][kOperand];
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n) {
           f32x8 x = join(s[n][2 * kk], s[n][2 * kk + 1]);
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) sv[n][i] = take_piece(x, T());
+          for (int i = 0; i < kOperand; ++i) sv[n][i] = take_piece(x, T());
         }
-        keep_order();
+        eight av[kTilesT];
 #pragma unroll
-        for (int t = 0; t < kTilesT; ++t) {
-          if (wt * kTilesT + t >= tiles) continue;
-          keep_order();
-          const eight av = row_values<DI>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
+        for (int t = 0; t < kTilesT; ++t) av[t] = row_values<DI>(as, (wt * kTilesT + t) * kTile + l16, kk, g);
+        // one piece for all tiles, then the next: no product waits for the one before it
 #pragma unroll
-          for (int n = 0; n < kTilesN; ++n)
+        for (int i = 0; i < kOperand; ++i)
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) o[t][n] = mma(sv[n][i], av, o[t][n]);
-        }
+          for (int t = 0; t < kTilesT; ++t)
+#pragma unroll
+            for (int n = 0; n < kTilesN; ++n) o[t][n] = mma(sv[n][i], av[t], o[t][n]);
       }
 #pragma unroll
       for (int t = 0; t < kTilesT; ++t) {
@@ -468,10 +501,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       }
     }
 
-    keep_order();
     if (!last || exact_state) {
       const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
-      const float left = float(n_valid - e - 4 * g);  // gamma^{n-e-u}; tokens u >= n have no c
+      float near[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) near[r] = __builtin_amdgcn_exp2f(float(15 - 4 * g - r) * log2_gamma);
 #pragma unroll
       for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
@@ -481,50 +515,64 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         if (kk * 32 >= n_valid) continue;
         eight wv[kTilesN][kStatePieces];
         f32x8 x[kTilesN];
+        float w[8];  // gamma^{n-e-u}, u = 32 kk + 16 (j / 4) + 4 g + j % 4; tokens u >= n have no c
+        if (n_valid == kChunk) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float w = p.sscale * __builtin_amdgcn_exp2f(
-                                         fmaxf(left - float(32 * kk + 16 * (j / 4) + j % 4), 0.0f) * log2_gamma);
+          for (int j = 0; j < 8; ++j)
+            w[j] = near[j % 4] * (p.sscale * __builtin_amdgcn_exp2f(float(49 - e - 32 * kk - 16 * (j / 4)) * log2_gamma));
+        } else {
 #pragma unroll
-          for (int n = 0; n < kTilesN; ++n) x[n][j] = to_f32(cv[n][kk][j]) * w;
+          for (int j = 0; j < 8; ++j)
+            w[j] = p.sscale * __builtin_amdgcn_exp2f(
+                                  float(max(n_valid - e - 4 * g - 32 * kk - 16 * (j / 4) - j % 4, 0)) * log2_gamma);
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int n = 0; n < kTilesN; ++n) x[n][j] = to_f32(cv[n][kk][j]) * w[j];
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
           for (int i = 0; i < kStatePieces; ++i)
             if (i < 2 || exact_state) wv[n][i] = take_piece(x[n], T());
+        constexpr int kGroup = kTilesI < 4 ? kTilesI : 4;
 #pragma unroll
-        for (int i = 0; i < kTilesI; ++i) {
-          if (i % 4 == 0) keep_order();
-          const eight bv = column_values<DI>(bs, i * kTile, kk, lane);
+        for (int i0 = 0; i0 < kTilesI; i0 += kGroup) {
+          eight bv[kGroup];
 #pragma unroll
-          for (int n = 0; n < kTilesN; ++n)
+          for (int i = 0; i < kGroup; ++i) bv[i] = column_values<DI>(bs, (i0 + i) * kTile, kk, lane);
 #pragma unroll
-            for (int x = 0; x < kStatePieces; ++x)
-              if (x < 2 || exact_state) s[n][i] = mma(bv, wv[n][x], s[n][i]);
+          for (int x = 0; x < kStatePieces; ++x) {
+            if (x >= 2 && !exact_state) continue;
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i)
+#pragma unroll
+              for (int n = 0; n < kTilesN; ++n) s[n][i0 + i] = mma(bv[i], wv[n][x], s[n][i0 + i]);
+          }
         }
       }
     }
     __syncthreads();  // the weights are there, and a, b and c are read
+    if (whole(u0 + kChunk)) fetch(thread, u0 + kChunk);
+    __builtin_amdgcn_sched_barrier(0);  // before the stores, which the wait for it counts
 
     if (OUT) {
       const int64_t out_at = ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
 #pragma unroll
-      for (int t = 0; t < kTilesT; ++t) {
-        const int tt = wt * kTilesT + t;
-        if (tt >= tiles) continue;
+      for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          if (kk * 2 > tt) continue;
-          keep_order();
+        for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) {
+          for (int t = 0; t < kTilesT; ++t) {
+            const int tt = wt * kTilesT + t;
+            if (kWavesT == 1 && kk * 2 > tt) continue;  // with more waves over the tokens: zeros
             const eight pv = row_values<kChunk>(ps[i], tt * kTile + l16, kk, g);
 #pragma unroll
             for (int n = 0; n < kTilesN; ++n) o[t][n] = mma(cv[n][kk], pv, o[t][n]);
           }
-        }
-        const int u = tt * kTile + l16;
+#pragma unroll
+      for (int t = 0; t < kTilesT; ++t) {
+        const int u = (wt * kTilesT + t) * kTile + l16;
         if (u >= n_valid) continue;
         const int64_t at = out_at + dt * u * (p.heads * p.dout);  // 64 tokens of 65,535 heads stay below 2^31
 #pragma unroll
