@@ -106,7 +106,7 @@ struct Vec<bf16> {
   // chunk's pairs are fed as two bfloat16 pieces (16 bits). A state that earlier
   // chunks have left is held in float32 and rounded once to be an operand: the
   // outputs' error is then up to 1.4 times that of their own rounding; with two
-  // pieces it would be 1.0 times, and the scan take 1.2 times as long. What is
+  // pieces it would be 1.0 times, and the scan take 1.05 times as long. What is
   // added to a state keeps 24 bits, as three pieces, where the state is an
   // output in float32, and 16 where only bfloat16 outputs are made of it.
   static constexpr int kPieces = 2, kOperand = 1, kStatePieces = 3;
@@ -626,11 +626,13 @@ __device__ __forceinline__ typename Vec<T>::eight short_row(const T *token, int 
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int col = kk * 32 + i * 16 + 4 * g;
-    x[i] = four{};
-    if (quads) {
+    if (kk * 32 + i * 16 + 16 <= di) {
+      x[i] = *reinterpret_cast<const any_four *>(token + col);
+    } else if (quads) {
       const four y = *reinterpret_cast<const any_four *>(token + (col < di ? col : 0));
-      if (col < di) x[i] = y;
+      x[i] = col < di ? y : four{};
     } else {
+      x[i] = four{};
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (col + r < di) x[i][r] = token[col + r];
@@ -639,10 +641,23 @@ __device__ __forceinline__ typename Vec<T>::eight short_row(const T *token, int 
   return join(x[0], x[1]);
 }
 
+// The values of a column at the byte offsets of eight rows: of tokens that are
+// there, whatever the chunk's length, so what is not a token's has to meet a
+// weight of 0.
+template <class T>
+__device__ __forceinline__ typename Vec<T>::eight short_column(const T *base, const unsigned (&at)[8], unsigned col) {
+  typename Vec<T>::eight x;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    x[j] = *reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + (at[j] + col));
+  return x;
+}
+
 template <class T, int DI, int TT>
 __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRoles roles, int64_t items,
                                                                          int64_t first) {
-  constexpr int kK = DI / 32, kPieces = Vec<T>::kPieces, kStatePieces = Vec<T>::kStatePieces;
+  constexpr int kK = DI / 32, kBlocks = (TT + 1) / 2, kPieces = Vec<T>::kPieces, kOperand = Vec<T>::kOperand,
+                kStatePieces = Vec<T>::kStatePieces;
   typedef typename Vec<T>::eight eight;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int64_t item = (first + blockIdx.x) * kShortWaves + wave;
@@ -657,148 +672,158 @@ __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRol
   const int tiles = (len + kTile - 1) / kTile, blocks = (len + 31) / 32;
   const int e = p.reverse ? 0 : 1;
   const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h);
-  // the token that is u-th in the scan's order
-  auto token_of = [&](int u) { return int64_t(p.reverse ? len - 1 - u : u); };
-
-  // weights of the pairs (t, s) as operands: tile t, blocks of 32 of s
-  eight w[TT][(TT + 1) / 2][kPieces];
-#pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    if (t >= tiles) break;
-    const T *at = a + token_of(min(t * kTile + l16, len - 1)) * p.a.token;
-    eight av[kK];
-#pragma unroll
-    for (int kk = 0; kk < kK; ++kk)
-      if (kk * 32 < p.di) av[kk] = short_row(at, kk, g, p.di, p.wide);
-#pragma unroll
-    for (int s32 = 0; s32 <= t / 2; ++s32) {
-      f32x4 x[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int st = 2 * s32 + i;
-        x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (st > t) continue;
-        const T *bt = b + token_of(min(st * kTile + l16, len - 1)) * p.b.token;
-#pragma unroll
-        for (int kk = 0; kk < kK; ++kk)
-          if (kk * 32 < p.di) x[i] = mma(short_row(bt, kk, g, p.di, p.wide), av[kk], x[i]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = (t - st) * kTile + l16 - 4 * g - r;
-          x[i][r] = d >= 0 ? x[i][r] * p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
-        }
-      }
-      f32x8 both = join(x[0], x[1]);
-#pragma unroll
-      for (int i = 0; i < kPieces; ++i) w[t][s32][i] = take_piece(both, T());
-    }
-  }
-
+  // the token that is u-th in the scan's order, or one that is there
+  auto token_of = [&](int u) { return p.reverse ? max(len - 1 - u, 0) : min(u, len - 1); };
   const int64_t state_at = rh * int64_t(p.di) * p.dout;
   const float *s0 = p.s0 == nullptr ? nullptr : p.s0 + state_at;
-  const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
-  const int64_t out_step = int64_t(p.heads) * p.dout;
-  const int64_t out_at = (row * p.length * p.heads + h) * p.dout;
-  for (int n0 = 0; n0 < p.dout; n0 += kTile) {
-    const int col = n0 + l16;
-    eight cv[(TT + 1) / 2];
-#pragma unroll
-    for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
-      if (kk >= blocks) break;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-        const T x = c[token_of(min(u, len - 1)) * p.c.token + min(col, p.dout - 1)];
-        cv[kk][j] = u < len && col < p.dout ? x : T(0.0f);
-      }
-    }
-    f32x4 o[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (s0 != nullptr) {
-#pragma unroll
-      for (int kk = 0; kk < kK; ++kk) {
-        if (kk * 32 >= p.di) break;
-        f32x8 x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int k = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-          x[j] = k < p.di && col < p.dout ? s0[unsigned(k * per_k + col * per_col)] : 0.0f;
-        }
-        eight sv[kPieces];
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) sv[i] = take_piece(x, T());
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-          if (t >= tiles) break;
-          const T *at = a + token_of(min(t * kTile + l16, len - 1)) * p.a.token;
-          const eight av = short_row(at, kk, g, p.di, p.wide);
-#pragma unroll
-          for (int i = 0; i < kPieces; ++i) o[t] = mma(sv[i], av, o[t]);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-        o[t] *= p.oscale * __builtin_amdgcn_exp2f(float(t * kTile + l16 + e) * log2_gamma);
-    }
+
+  if (len > 0) {
+    // weights of the pairs (t, s) as operands: tile t, blocks of 32 of s
+    eight w[TT][kBlocks][kPieces];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       if (t >= tiles) break;
+      const T *at = a + token_of(t * kTile + l16) * p.a.token;
+      eight av[kK];
 #pragma unroll
-      for (int kk = 0; kk <= t / 2; ++kk)
+      for (int kk = 0; kk < kK; ++kk)
+        if (kk * 32 < p.di) av[kk] = short_row(at, kk, g, p.di, p.wide);
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) o[t] = mma(cv[kk], w[t][kk][i], o[t]);
-      const int u = t * kTile + l16;
-      if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
+      for (int s32 = 0; s32 <= t / 2; ++s32) {
+        f32x4 x[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int st = 2 * s32 + i;
+          x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          if (st > t) continue;
+          const T *bt = b + token_of(st * kTile + l16) * p.b.token;
+#pragma unroll
+          for (int kk = 0; kk < kK; ++kk)
+            if (kk * 32 < p.di) x[i] = mma(short_row(bt, kk, g, p.di, p.wide), av[kk], x[i]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int d = (t - st) * kTile + l16 - 4 * g - r;
+            const float y = x[i][r] * p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma);
+            x[i][r] = d >= 0 ? y : 0.0f;
+          }
+        }
+        f32x8 both = join(x[0], x[1]);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) w[t][s32][i] = take_piece(both, T());
+      }
     }
-    if (p.s1 == nullptr) continue;
-    // S at the row's end, a tile at a time
-    const float whole = __builtin_amdgcn_exp2f(float(len) * log2_gamma);
-    eight wv[(TT + 1) / 2][kStatePieces];
+
+    // places of the rows of c and b that a lane reads columns of
+    unsigned c_at[kBlocks][8], b_at[kBlocks][8];
 #pragma unroll
-    for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
-      if (kk >= blocks) break;
-      f32x8 x;
+    for (int kk = 0; kk < kBlocks; ++kk)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-        x[j] = to_f32(cv[kk][j]) * p.sscale * __builtin_amdgcn_exp2f(float(max(len - e - u, 0)) * log2_gamma);
+        const int token = token_of(kk * 32 + 16 * (j / 4) + 4 * g + j % 4);
+        c_at[kk][j] = unsigned(token) * unsigned(p.c.token) * unsigned(sizeof(T));
+        b_at[kk][j] = unsigned(token) * unsigned(p.b.token) * unsigned(sizeof(T));
       }
+
+    const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
+    const int64_t out_step = int64_t(p.heads) * p.dout;
+    const int64_t out_at = (row * p.length * p.heads + h) * p.dout;
+    const float whole = __builtin_amdgcn_exp2f(float(len) * log2_gamma);
+    for (int n0 = 0; n0 < p.dout; n0 += kTile) {
+      const int col = min(n0 + l16, p.dout - 1);  // columns beyond the last are not stored
+      eight cv[kBlocks];
 #pragma unroll
-      for (int i = 0; i < kStatePieces; ++i) wv[kk][i] = take_piece(x, T());
-    }
-    for (int i0 = 0; i0 < p.di; i0 += kTile) {
-      f32x4 s;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int k = i0 + 4 * g + r;
-        s[r] = s0 != nullptr && k < p.di && col < p.dout ? s0[unsigned(k * per_k + col * per_col)] * whole : 0.0f;
-      }
-#pragma unroll
-      for (int kk = 0; kk < (TT + 1) / 2; ++kk) {
+      for (int kk = 0; kk < kBlocks; ++kk) {
         if (kk >= blocks) break;
-        eight bv;
+        cv[kk] = short_column(c, c_at[kk], unsigned(col) * unsigned(sizeof(T)));
+      }
+      f32x4 o[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (s0 != nullptr) {
+#pragma unroll
+        for (int kk = 0; kk < kK; ++kk) {
+          if (kk * 32 >= p.di) break;
+          f32x8 x;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int k = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
+            x[j] = k < p.di ? s0[unsigned(k * per_k + col * per_col)] : 0.0f;
+          }
+          eight sv[kOperand];
+#pragma unroll
+          for (int i = 0; i < kOperand; ++i) sv[i] = take_piece(x, T());
+#pragma unroll
+          for (int t = 0; t < TT; ++t) {
+            if (t >= tiles) break;
+            const T *at = a + token_of(t * kTile + l16) * p.a.token;
+            const eight av = short_row(at, kk, g, p.di, p.wide);
+#pragma unroll
+            for (int i = 0; i < kOperand; ++i) o[t] = mma(sv[i], av, o[t]);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+          o[t] *= p.oscale * __builtin_amdgcn_exp2f(float(t * kTile + l16 + e) * log2_gamma);
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        if (t >= tiles) break;
+#pragma unroll
+        for (int kk = 0; kk <= t / 2; ++kk)
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) o[t] = mma(cv[kk], w[t][kk][i], o[t]);
+        const int u = t * kTile + l16;
+        if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
+      }
+      if (p.s1 == nullptr) continue;
+      // S at the row's end, a tile at a time
+      eight wv[kBlocks][kStatePieces];
+#pragma unroll
+      for (int kk = 0; kk < kBlocks; ++kk) {
+        if (kk >= blocks) break;
+        f32x8 x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-          const T x = b[token_of(min(u, len - 1)) * p.b.token + min(i0 + l16, p.di - 1)];
-          bv[j] = u < len && i0 + l16 < p.di ? x : T(0.0f);
+          const float y = to_f32(cv[kk][j]) * p.sscale * __builtin_amdgcn_exp2f(float(len - e - u) * log2_gamma);
+          x[j] = u < len ? y : 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < kStatePieces; ++i) s = mma(bv, wv[kk][i], s);
+        for (int i = 0; i < kStatePieces; ++i) wv[kk][i] = take_piece(x, T());
       }
+      for (int i0 = 0; i0 < p.di; i0 += kTile) {
+        const unsigned k_of = min(i0 + l16, p.di - 1);  // rows beyond the last are not stored
+        f32x4 s;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int k = i0 + 4 * g + r;
-        if (k < p.di && col < p.dout) p.s1[state_at + k * p.dout + col] = s[r];
+        for (int r = 0; r < 4; ++r) {
+          const int k = min(i0 + 4 * g + r, p.di - 1);
+          s[r] = s0 != nullptr ? s0[unsigned(k * per_k + col * per_col)] * whole : 0.0f;
+        }
+#pragma unroll
+        for (int kk = 0; kk < kBlocks; ++kk) {
+          if (kk >= blocks) break;
+          const eight bv = short_column(b, b_at[kk], k_of * unsigned(sizeof(T)));
+#pragma unroll
+          for (int i = 0; i < kStatePieces; ++i) s = mma(bv, wv[kk][i], s);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int k = i0 + 4 * g + r;
+          if (k < p.di && n0 + l16 < p.dout) p.s1[state_at + k * p.dout + n0 + l16] = s[r];
+        }
       }
     }
+  } else if (p.s1 != nullptr) {  // a row without tokens leaves its state as it is
+    for (int i = lane; i < p.di * p.dout; i += kWave)
+      p.s1[state_at + i] = s0 == nullptr ? 0.0f : s0[p.transposed ? i % p.dout * p.di + i / p.dout : i];
   }
   // tokens beyond the row's length
+  const int64_t out_step = int64_t(p.heads) * p.dout;
   const int cols = (p.dout + 3) / 4;
   for (int i = lane; i < (int(p.length) - len) * cols; i += kWave) {
     const int col = i % cols * 4;
-    store_four<T>(p, out_at + (len + i / cols) * out_step + col, col, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    store_four<T>(p, ((row * p.length + len + i / cols) * p.heads + h) * p.dout + col, col,
+                  f32x4{0.0f, 0.0f, 0.0f, 0.0f});
   }
 }
 
@@ -861,10 +886,13 @@ rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
   const int64_t blocks = (items + kShortWaves - 1) / kShortWaves;
   return for_each_launch(blocks, kShortWaves * kWave, 1, [&](int64_t first, int64_t count) {
     const dim3 grid{unsigned(count)}, threads{kShortWaves * kWave};
-#define RDF2V_SHORT(DI, TT)                                                                 \
-  if (padded(di) == DI && (roles.role[0].length <= 2 * kTile ? 2 : 4) == TT)                \
-    short_scan_kernel<T, DI, TT><<<grid, threads, 0, stream>>>(roles, items, first);
+    const int64_t length = roles.role[0].length;
+    const int tiles = length <= kTile ? 1 : int((length + kTile - 1) / kTile);
+#define RDF2V_SHORT(DI, TT) \
+  if (padded(di) == DI && tiles == TT) short_scan_kernel<T, DI, TT><<<grid, threads, 0, stream>>>(roles, items, first);
+    RDF2V_SHORT(32, 1) RDF2V_SHORT(64, 1) RDF2V_SHORT(128, 1)
     RDF2V_SHORT(32, 2) RDF2V_SHORT(64, 2) RDF2V_SHORT(128, 2)
+    RDF2V_SHORT(32, 3) RDF2V_SHORT(64, 3) RDF2V_SHORT(128, 3)
     RDF2V_SHORT(32, 4) RDF2V_SHORT(64, 4) RDF2V_SHORT(128, 4)
 #undef RDF2V_SHORT
     RDF2V_LAUNCH_CHECK();
@@ -912,7 +940,11 @@ void finish(ScanArgs &p, bool one_chunk, int64_t segments) {
 template <class T>
 rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_states, const int *state_of,
                           float *seg_state, bool together, hipStream_t stream) {
-  const bool one_chunk = scans[0].length <= kChunk;
+  // a wave's 32-bit offsets take 64 tokens that are less than 2^23 values apart, in ascending order
+  bool one_chunk = scans[0].length <= kChunk;
+  for (int i = 0; i < count; ++i)
+    for (const ScanOperand *x : {&scans[i].a, &scans[i].b, &scans[i].c})
+      one_chunk = one_chunk && x->token >= 0 && x->token < int64_t(1) << 23;
   const int64_t segments = segment_count(scans[0].rows * scans[0].heads * count, scans[0].length);
   if (segments > 1) {
     ScanRoles roles{};
