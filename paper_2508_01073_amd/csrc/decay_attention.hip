@@ -713,20 +713,17 @@ __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRol
       }
     }
 
-    // places of the rows of c and b that a lane reads columns of
-    unsigned c_at[kBlocks][8], b_at[kBlocks][8];
+    // places of the rows of c that a lane reads columns of
+    unsigned c_at[kBlocks][8];
 #pragma unroll
     for (int kk = 0; kk < kBlocks; ++kk)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int token = token_of(kk * 32 + 16 * (j / 4) + 4 * g + j % 4);
-        c_at[kk][j] = unsigned(token) * unsigned(p.c.token) * unsigned(sizeof(T));
-        b_at[kk][j] = unsigned(token) * unsigned(p.b.token) * unsigned(sizeof(T));
-      }
+      for (int j = 0; j < 8; ++j)
+        c_at[kk][j] = unsigned(token_of(kk * 32 + 16 * (j / 4) + 4 * g + j % 4)) * unsigned(p.c.token) *
+                      unsigned(sizeof(T));
 
     const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
-    const int64_t out_step = int64_t(p.heads) * p.dout;
-    const int64_t out_at = (row * p.length * p.heads + h) * p.dout;
+    const int64_t out_step = int64_t(p.heads) * p.dout, out_at = (row * p.length * p.heads + h) * p.dout;
     const float whole = __builtin_amdgcn_exp2f(float(len) * log2_gamma);
     for (int n0 = 0; n0 < p.dout; n0 += kTile) {
       const int col = min(n0 + l16, p.dout - 1);  // columns beyond the last are not stored
@@ -740,6 +737,8 @@ __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRol
 #pragma unroll
       for (int t = 0; t < TT; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if (s0 != nullptr) {
+        int g = lane / 16, l16 = lane % 16;
+        asm volatile("" : "+v"(g), "+v"(l16));
 #pragma unroll
         for (int kk = 0; kk < kK; ++kk) {
           if (kk * 32 >= p.di) break;
@@ -776,7 +775,16 @@ __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRol
         if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
       }
       if (p.s1 == nullptr) continue;
-      // S at the row's end, a tile at a time
+      // S at the row's end, a tile at a time; what it needs besides is made here, not kept
+      int g = lane / 16;
+      asm volatile("" : "+v"(g));
+      unsigned b_at[kBlocks][8];
+#pragma unroll
+      for (int kk = 0; kk < kBlocks; ++kk)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          b_at[kk][j] = unsigned(token_of(kk * 32 + 16 * (j / 4) + 4 * g + j % 4)) * unsigned(p.b.token) *
+                        unsigned(sizeof(T));
       eight wv[kBlocks][kStatePieces];
 #pragma unroll
       for (int kk = 0; kk < kBlocks; ++kk) {
@@ -818,7 +826,6 @@ __global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRol
       p.s1[state_at + i] = s0 == nullptr ? 0.0f : s0[p.transposed ? i % p.dout * p.di + i / p.dout : i];
   }
   // tokens beyond the row's length
-  const int64_t out_step = int64_t(p.heads) * p.dout;
   const int cols = (p.dout + 3) / 4;
   for (int i = lane; i < (int(p.length) - len) * cols; i += kWave) {
     const int col = i % cols * 4;
