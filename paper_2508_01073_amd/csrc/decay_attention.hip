@@ -47,7 +47,7 @@ struct ScanArgs {
   int64_t segments, segment; // segments of a row, and their tokens (whole chunks)
   // [rows][heads][segments][dk][dv] states that the segments begin with (a state scan: their own), or null
   float *seg_state;
-  bool wide, wide_out;       // 16-byte reads (rows of one chunk: of four values), stores of four values
+  bool wide, wide_out;       // 16-byte reads (short rows: of four values), stores of four values
   bool out_f32;              // out is float32 whatever the element type: to be summed over heads
 };
 
@@ -607,13 +607,14 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       }
 }
 
-// Rows of at most one chunk: one wave to a row and head, in registers alone.
+// Short rows: one wave to a row and head, in registers alone.
 //
 // The results of the weights' products are, in the order of the contractions
 // above, operands of the products with c as they stand, so the wave needs no
-// LDS and no barrier, and many waves share a CU: with a workgroup to a row,
-// rows of 17 tokens left most of its waves idle at its barriers
-// (16,000 rows and heads of 17 x 32 in bfloat16: 73 us against 1x us here).
+// LDS and no barrier, and many waves share a CU; a workgroup to a row leaves
+// most of its waves idle at its barriers. 4,000 rows of up to 17 tokens (half
+// of them there), 4 heads of 32 in bfloat16: 22 us, 2.0 TB/s, bound by the
+// latency of a wave's few dependent loads; 73 us with workgroups.
 //
 // TT: most tiles of 16 tokens.
 constexpr int kShortWaves = 4;  // of a workgroup, each for itself
@@ -654,8 +655,9 @@ __device__ __forceinline__ typename Vec<T>::eight short_column(const T *base, co
 }
 
 template <class T, int DI, int TT>
-__global__ __launch_bounds__(kShortWaves * kWave) void short_scan_kernel(ScanRoles roles, int64_t items,
-                                                                         int64_t first) {
+__global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_scan_kernel(ScanRoles roles,
+                                                                                          int64_t items,
+                                                                                          int64_t first) {
   constexpr int kK = DI / 32, kBlocks = (TT + 1) / 2, kPieces = Vec<T>::kPieces, kOperand = Vec<T>::kOperand,
                 kStatePieces = Vec<T>::kStatePieces;
   typedef typename Vec<T>::eight eight;
@@ -900,7 +902,6 @@ rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
     RDF2V_SHORT(32, 1) RDF2V_SHORT(64, 1) RDF2V_SHORT(128, 1)
     RDF2V_SHORT(32, 2) RDF2V_SHORT(64, 2) RDF2V_SHORT(128, 2)
     RDF2V_SHORT(32, 3) RDF2V_SHORT(64, 3) RDF2V_SHORT(128, 3)
-    RDF2V_SHORT(32, 4) RDF2V_SHORT(64, 4) RDF2V_SHORT(128, 4)
 #undef RDF2V_SHORT
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
@@ -927,7 +928,7 @@ int64_t segment_count(int64_t scans, int64_t length) {
 }
 
 template <class T>
-void finish(ScanArgs &p, bool one_chunk, int64_t segments) {
+void finish(ScanArgs &p, bool short_rows, int64_t segments) {
   p.pscale = p.oscale * p.sscale;
   const int64_t chunks = (p.length + kChunk - 1) / kChunk;
   p.segments = segments;
@@ -938,8 +939,30 @@ void finish(ScanArgs &p, bool one_chunk, int64_t segments) {
                           uintptr_t(x.row | x.token | x.head | int64_t(d)) * sizeof(T);
     return (all & 15) == 0;
   };
-  p.wide = one_chunk ? p.di % 4 == 0 : (p.a.data == nullptr || fits(p.a, p.di)) && fits(p.b, p.di) && fits(p.c, p.dout);
+  p.wide = short_rows ? p.di % 4 == 0 : (p.a.data == nullptr || fits(p.a, p.di)) && fits(p.b, p.di) && fits(p.c, p.dout);
   p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (p.out_f32 || sizeof(T) == 4 ? 15 : 7)) == 0;
+}
+
+// Whether a wave to a row and head is the faster way. us with a wave / with a
+// workgroup and chunks, 8 heads, 2^27 values of q, k, v and out (bfloat16):
+//   tokens   sizes 32    64          128         sizes 32, states in and out   64          128
+//   16       35 / 162    35 / 118    38 / 120    167 / 241                     369 / 226   806 / 341
+//   32       36 / 88     46 / 66     45 / 72     120 / 135                     281 / 125   435 / 186
+//   33       58 / 87     61 / 70     67 / 75     161 / 139                     267 / 139   511 / 195
+//   64       87 / 47     90 / 37     93 / 41     136 / 71                      236 / 72    469 / 108
+// and in float32 59 / 342, 60 / 342, 63 / 424; 207 / 454, 386 / 491, 761 / 758
+// at 16 tokens, 82 / 202, 89 / 216, 100 / 255; 175 / 271, 288 / 324, 803 / 461
+// at 33. A wave's 32-bit places take tokens less than 2^23 values apart, in
+// ascending order.
+bool use_short(const ScanArgs *scans, int count) {
+  for (int i = 0; i < count; ++i) {
+    const ScanArgs &p = scans[i];
+    if (p.length > 3 * kTile) return false;
+    if ((p.s0 != nullptr || p.s1 != nullptr) && (p.di > 32 || p.dout > 32)) return false;
+    for (const ScanOperand *x : {&p.a, &p.b, &p.c})
+      if (x->token < 0 || x->token >= int64_t(1) << 23) return false;
+  }
+  return true;
 }
 
 // `count` scans; states[state_of[i]] is the scan that gives scan i its states
@@ -947,11 +970,7 @@ void finish(ScanArgs &p, bool one_chunk, int64_t segments) {
 template <class T>
 rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_states, const int *state_of,
                           float *seg_state, bool together, hipStream_t stream) {
-  // a wave's 32-bit offsets take 64 tokens that are less than 2^23 values apart, in ascending order
-  bool one_chunk = scans[0].length <= kChunk;
-  for (int i = 0; i < count; ++i)
-    for (const ScanOperand *x : {&scans[i].a, &scans[i].b, &scans[i].c})
-      one_chunk = one_chunk && x->token >= 0 && x->token < int64_t(1) << 23;
+  const bool short_rows = use_short(scans, count);
   const int64_t segments = segment_count(scans[0].rows * scans[0].heads * count, scans[0].length);
   if (segments > 1) {
     ScanRoles roles{};
@@ -981,14 +1000,14 @@ rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_
     if (done[i]) continue;
     ScanRoles roles{};
     for (int j = i; j < count; ++j) {
-      const bool same = one_chunk || (padded(scans[j].di) == padded(scans[i].di) &&
+      const bool same = short_rows || (padded(scans[j].di) == padded(scans[i].di) &&
                                       padded(scans[j].dout) == padded(scans[i].dout));
       if (done[j] || !same || (j > i && !together)) continue;
-      finish<T>(scans[j], one_chunk, segments);
+      finish<T>(scans[j], short_rows, segments);
       roles.role[roles.count++] = scans[j];
       done[j] = true;
     }
-    const rdf2v_status st = one_chunk ? launch_short<T>(roles, stream) : launch_chunks<T, true>(roles, stream);
+    const rdf2v_status st = short_rows ? launch_short<T>(roles, stream) : launch_chunks<T, true>(roles, stream);
     if (st != RDF2V_OK) return st;
   }
   return RDF2V_OK;
