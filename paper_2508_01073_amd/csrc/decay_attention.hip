@@ -83,12 +83,12 @@ constexpr int kChunk = 64;      // tokens of a chunk
 constexpr int kThreads = 256;   // of the kernels below that are not scans
 constexpr int kTile = 16;       // rows and columns of a matrix instruction
 
-// Eight values of a row or column that one lane feeds to a matrix instruction.
-// Lane l serves row (of the first factor) or column (of the second) l % 16, and
-// with g = l / 16 its values are those at contraction indices
-// 16 (j / 4) + 4 g + j % 4 of a block of 32: both factors use this order, in
-// which a result of one instruction (rows 4 g + r, column l % 16) is an operand
-// of the next as it stands.
+// Eight values of a row or column are what one lane feeds to a matrix
+// instruction. Lane l serves row (of the first factor) or column (of the second)
+// l % 16, and with g = l / 16 its values are any eight of a block of 32
+// contraction indices, the same for both factors. A result holds rows 4 g + r of
+// column l % 16: two results are an operand of the next product as they stand,
+// if its other factor is read in their order.
 typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -153,18 +153,18 @@ __device__ __forceinline__ F take_piece(F &x, float) {
 }
 
 // A tile of rows of W values in LDS. In bfloat16 the groups of four values of a
-// row are permuted by the row: reads of one group of 16 rows (an operand's
-// row) and of four groups of 8 rows (the transposing reads) then meet every
-// bank once in half a wave; padded rows had conflicts in one or the other.
-// Pairs of groups stay together for the 16-byte writes. Float32 rows are padded
-// by 16 bytes, which is free of conflicts there.
+// row are permuted by the row: the 16-byte reads of 16 rows at one place, and
+// the transposing reads of four neighbouring groups of eight rows, then meet
+// every bank once. Pairs of groups stay together for the 16-byte accesses.
+// Float32 rows are padded by 16 bytes.
 template <class T, int W>
 struct Tile;
 template <int W>
 struct Tile<bf16, W> {
   static constexpr int kSize = kChunk * W;
   static __device__ __forceinline__ int swap(int row) {
-    return (row % 8 * (W / 4) / 32 * 4 | row / 8 % 2 * 2) % (W / 4);
+    const int low = W == 128 ? row % 4 * 4 : W == 64 ? row / 2 % 2 * 4 : 0;
+    return low | row / 8 % 2 * (W / 8) | row / 4 % 2 * 2;
   }
   static __device__ __forceinline__ int at(int row, int group) { return row * W + (group ^ swap(row)) * 4; }
 };
@@ -174,32 +174,42 @@ struct Tile<float, W> {
   static __device__ __forceinline__ int at(int row, int group) { return row * (W + 4) + group * 4; }
 };
 
+// Operands of the chunks' products: lane l holds values 32 kk + 8 g + j of row
+// (or column) l % 16.
+//
 // Values of row `row`, indices of block kk.
-template <int W, class T>
-__device__ __forceinline__ typename Vec<T>::eight row_values(const T *tile, int row, int kk, int g) {
-  typedef typename Vec<T>::four four;
-  return join(*reinterpret_cast<const four *>(tile + Tile<T, W>::at(row, kk * 8 + g)),
-              *reinterpret_cast<const four *>(tile + Tile<T, W>::at(row, kk * 8 + 4 + g)));
-}
-// Values of column col0 + l % 16, rows of block kk. In bfloat16 the transposing
-// LDS read gives lane l of 16 the column l of the four rows that the lanes
-// 4 row + (0 .. 3) address.
 template <int W>
-__device__ __forceinline__ bf16x8 column_values(const bf16 *tile, int col0, int kk, int lane) {
+__device__ __forceinline__ bf16x8 row_values(const bf16 *tile, int row, int kk, int g) {
+  return *reinterpret_cast<const bf16x8 *>(tile + Tile<bf16, W>::at(row, kk * 8 + 2 * g));
+}
+template <int W>
+__device__ __forceinline__ f32x8 row_values(const float *tile, int row, int kk, int g) {
+  const float *p = tile + Tile<float, W>::at(row, kk * 8 + 2 * g);
+  return join(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4));
+}
+// Values of 16 columns, rows of block kk: columns group0 * 4 + step * 4 * (l16 / 4)
+// + l16 % 4. In bfloat16 the transposing LDS read gives lane l of 16 the column l
+// of the four groups of four rows that the lanes 4 row + (0 .. 3) address.
+template <int W>
+__device__ __forceinline__ bf16x8 column_values(const bf16 *tile, int group0, int step, int kk, int lane) {
   typedef __attribute__((address_space(3))) i16x4 lds4;
-  const int row = kk * 32 + 4 * (lane / 16) + lane % 16 / 4, group = col0 / 4 + lane % 4;
+  const int row = kk * 32 + 8 * (lane / 16) + lane % 16 / 4, group = group0 + step * (lane % 4);
   const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + Tile<bf16, W>::at(row, group)));
-  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + Tile<bf16, W>::at(row + 16, group)));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(tile + Tile<bf16, W>::at(row + 4, group)));
   return join(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi));
 }
 template <int W>
-__device__ __forceinline__ f32x8 column_values(const float *tile, int col0, int kk, int lane) {
-  const float *p = tile + Tile<float, W>::at(kk * 32 + 4 * (lane / 16), col0 / 4) + lane % 16;
+__device__ __forceinline__ f32x8 column_values(const float *tile, int group0, int step, int kk, int lane) {
+  const int group = group0 + step * (lane % 16 / 4);
+  const float *p = tile + Tile<float, W>::at(kk * 32 + 8 * (lane / 16), group) + lane % 4;
   f32x8 x;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = p[(16 * (j / 4) + j % 4) * (W + 4)];
+  for (int j = 0; j < 8; ++j) x[j] = p[j * (W + 4)];
   return x;
 }
+// Row r of tile i of a state, in lane group g: such that the accumulators of
+// tiles 2 kk and 2 kk + 1 are the operand of block kk.
+__device__ __forceinline__ int state_row(int i, int g, int r) { return i / 2 * 32 + 8 * g + i % 2 * 4 + r; }
 
 // A chunk's rows of one operand on their way from memory to LDS: 64 rows of W
 // values, zeros beyond the operand's size and beyond the chunk's `n` tokens.
@@ -380,7 +390,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         if (s0 == nullptr) continue;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int col = nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+          const int col = nw + n * kTile + l16, k = state_row(i, g, r);
           if (k < p.di && col < p.dout) s[n][i][r] = s0[unsigned(k * per_k + col * per_col)];
         }
       }
@@ -464,7 +474,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
     for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
-      for (int kk = 0; kk < 2; ++kk) cv[n][kk] = column_values<NB>(cs, nw + n * kTile, kk, lane);
+      for (int kk = 0; kk < 2; ++kk) cv[n][kk] = column_values<NB>(cs, (nw + n * kTile) / 4, 1, kk, lane);
 
     f32x4 o[kTilesT][kTilesN];
     if (OUT) {
@@ -503,9 +513,9 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 
     if (!last || exact_state) {
       const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
-      float near[4];
+      float near[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) near[r] = __builtin_amdgcn_exp2f(float(15 - 4 * g - r) * log2_gamma);
+      for (int j = 0; j < 8; ++j) near[j] = __builtin_amdgcn_exp2f(float(31 - 8 * g - j) * log2_gamma);
 #pragma unroll
       for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
@@ -515,16 +525,15 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         if (kk * 32 >= n_valid) continue;
         eight wv[kTilesN][kStatePieces];
         f32x8 x[kTilesN];
-        float w[8];  // gamma^{n-e-u}, u = 32 kk + 16 (j / 4) + 4 g + j % 4; tokens u >= n have no c
+        float w[8];  // gamma^{n-e-u}, u = 32 kk + 8 g + j; tokens u >= n have no c
         if (n_valid == kChunk) {
+          const float far = p.sscale * __builtin_amdgcn_exp2f(float(33 - e - 32 * kk) * log2_gamma);
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            w[j] = near[j % 4] * (p.sscale * __builtin_amdgcn_exp2f(float(49 - e - 32 * kk - 16 * (j / 4)) * log2_gamma));
+          for (int j = 0; j < 8; ++j) w[j] = near[j] * far;
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            w[j] = p.sscale * __builtin_amdgcn_exp2f(
-                                  float(max(n_valid - e - 4 * g - 32 * kk - 16 * (j / 4) - j % 4, 0)) * log2_gamma);
+            w[j] = p.sscale * __builtin_amdgcn_exp2f(float(max(n_valid - e - 32 * kk - 8 * g - j, 0)) * log2_gamma);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -540,7 +549,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         for (int i0 = 0; i0 < kTilesI; i0 += kGroup) {
           eight bv[kGroup];
 #pragma unroll
-          for (int i = 0; i < kGroup; ++i) bv[i] = column_values<DI>(bs, (i0 + i) * kTile, kk, lane);
+          for (int i = 0; i < kGroup; ++i) bv[i] = column_values<DI>(bs, (i0 + i) / 2 * 8 + (i0 + i) % 2, 2, kk, lane);
 #pragma unroll
           for (int x = 0; x < kStatePieces; ++x) {
             if (x >= 2 && !exact_state) continue;
@@ -602,7 +611,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     for (int i = 0; i < kTilesI; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int col = nw + n * kTile + l16, k = i * kTile + 4 * g + r;
+        const int col = nw + n * kTile + l16, k = state_row(i, g, r);
         if (wt == 0 && k < p.di && col < p.dout) s1[unsigned(k * p.dout + col)] = s[n][i][r];
       }
 }
