@@ -48,6 +48,7 @@ struct ScanArgs {
   // [rows][heads][segments][dk][dv] states that the segments begin with (a state scan: their own), or null
   float *seg_state;
   bool wide, wide_out;       // 16-byte reads (short rows: of four values), stores of four values
+  bool whole_out;            // out is bfloat16 in rows of whole 16 bytes
   bool out_f32;              // out is float32 whatever the element type: to be summed over heads
 };
 
@@ -350,6 +351,10 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   __shared__ __attribute__((aligned(16))) T as[OUT ? Tile<T, DI>::kSize : 1], bs[Tile<T, DI>::kSize],
       cs[Tile<T, NB>::kSize];
   __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? Tile<T, kChunk>::kSize : 1];
+  // A chunk's outputs, put together to whole rows: a wave's 32 bytes of a row each would make four times the
+  // requests. They are stored when the next chunk is in LDS, behind the same barrier.
+  constexpr bool kStage = OUT && sizeof(T) == 2;
+  __shared__ __attribute__((aligned(16))) T os[kStage ? Tile<T, NB>::kSize : 1];
   typedef typename Vec<T>::four four;
   typedef typename Vec<T>::eight eight;
 
@@ -407,6 +412,21 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     lb.fetch(thread, bs, b + low * p.b.token, int(p.b.token), p.reverse);
     lc.fetch(thread, cs, c + low * p.c.token, int(p.c.token), p.reverse);
   };
+  const bool stage = kStage && p.whole_out;
+  auto flush = [&](unsigned thread, int64_t u0) {  // the staged outputs of the chunk at u0
+    constexpr int kCols = NB / 8;
+    typedef bf16x8 vec;
+    const int n = int(min(int64_t(kChunk), u_valid - u0));
+    const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
+    T *out = static_cast<T *>(p.out) + ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
+#pragma unroll
+    for (int i = 0; i < kChunk * kCols / kThreads; ++i) {
+      const int at = i * kThreads + thread, u = at / kCols, col = at % kCols * 8;
+      if (u < n && col < p.dout)
+        *reinterpret_cast<vec *>(out + dt * u * (p.heads * p.dout) + col) =
+            *reinterpret_cast<const vec *>(os + Tile<T, NB>::at(u, col / 4));
+    }
+  };
   if (whole(u_begin)) fetch(threadIdx.x, u_begin);
   __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
 
@@ -424,14 +444,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       if (OUT) la.store(thread, as);
       lb.store(thread, bs);
       lc.store(thread, cs);
-      if (la.kDirect) {
-        // This wave's part of the chunk is in LDS: what may still be under way are the last chunk's stores,
-        // at least kTilesT of them, where the wave has columns to store.
-        if (OUT && u0 > u_begin && nw < p.dout)
-          __builtin_amdgcn_s_waitcnt(0x0f70 | kTilesT);
-        else
-          __builtin_amdgcn_s_waitcnt(0x0f70);
-      }
+      if (la.kDirect) __builtin_amdgcn_s_waitcnt(0x0f70);  // this wave's part of the chunk is in LDS
     } else if (p.wide) {
       const int64_t low = p.reverse ? t0 - (n_valid - 1) : t0;
       if (OUT) la.copy_part(thread, as, a + low * p.a.token, int(p.a.token), p.reverse, n_valid, p.di);
@@ -443,6 +456,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       lc.copy(thread, cs, c + t0 * p.c.token, dt * p.c.token, n_valid, p.dout);
     }
     __syncthreads();
+    if constexpr (kStage)
+      if (stage && u0 > u_begin) flush(thread, u0 - kChunk);
     if (OUT) {
       // the weights of tokens 16 w .. 16 w + 15, and of half of the tokens before them where two waves share
       const int w4 = wave % 4, t = w4 * kTile + l16;
@@ -563,7 +578,6 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     }
     __syncthreads();  // the weights are there, and a, b and c are read
     if (whole(u0 + kChunk)) fetch(thread, u0 + kChunk);
-    __builtin_amdgcn_sched_barrier(0);  // before the stores, which the wait for it counts
 
     if (OUT) {
       const int64_t out_at = ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
@@ -582,6 +596,14 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
       for (int t = 0; t < kTilesT; ++t) {
         const int u = (wt * kTilesT + t) * kTile + l16;
+        if (kStage && stage) {
+#pragma unroll
+          for (int n = 0; n < kTilesN; ++n)
+            *reinterpret_cast<four *>(os + Tile<T, NB>::at(u, (nw + n * kTile) / 4 + g)) =
+                four{from_f32<T>(o[t][n][0]), from_f32<T>(o[t][n][1]), from_f32<T>(o[t][n][2]),
+                     from_f32<T>(o[t][n][3])};
+          continue;
+        }
         if (u >= n_valid) continue;
         const int64_t at = out_at + dt * u * (p.heads * p.dout);  // 64 tokens of 65,535 heads stay below 2^31
 #pragma unroll
@@ -592,6 +614,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       }
     }
   }
+  if constexpr (kStage)
+    if (stage && u_begin < u_valid) {
+      __syncthreads();
+      flush(threadIdx.x, u_begin + (u_valid - 1 - u_begin) / kChunk * kChunk);
+    }
 
   if (OUT) {  // tokens beyond the row's length
     const int64_t t_begin = max(u_begin, len);
@@ -949,6 +976,7 @@ void finish(ScanArgs &p, bool short_rows, int64_t segments) {
     return (all & 15) == 0;
   };
   p.wide = short_rows ? p.di % 4 == 0 : (p.a.data == nullptr || fits(p.a, p.di)) && fits(p.b, p.di) && fits(p.c, p.dout);
+  p.whole_out = !p.out_f32 && sizeof(T) == 2 && p.dout % 8 == 0 && (reinterpret_cast<uintptr_t>(p.out) & 15) == 0;
   p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (p.out_f32 || sizeof(T) == 4 ? 15 : 7)) == 0;
 }
 
