@@ -348,8 +348,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   constexpr int kWavesT = kWaves / kWavesN;                // and over the chunk's tokens
   constexpr int kTilesN = 1, kTilesT = 4 / kWavesT, kTilesI = DI / kTile, kK = DI / 32;
   constexpr int kPieces = Vec<T>::kPieces, kOperand = Vec<T>::kOperand, kStatePieces = Vec<T>::kStatePieces;
-  __shared__ __attribute__((aligned(16))) T as[OUT ? Tile<T, DI>::kSize : 1], bs[Tile<T, DI>::kSize],
-      cs[Tile<T, NB>::kSize];
+  // A scan for the state alone has LDS for two chunks: the next one is on its way while this one is used, and
+  // a chunk has one barrier.
+  constexpr int kBuffers = !OUT && Loader<T, DI, kThreads>::kDirect ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) T as[OUT ? Tile<T, DI>::kSize : 1], b_tiles[kBuffers][Tile<T, DI>::kSize],
+      c_tiles[kBuffers][Tile<T, NB>::kSize];
   __shared__ __attribute__((aligned(16))) T ps[OUT ? kPieces : 1][OUT ? Tile<T, kChunk>::kSize : 1];
   // A chunk's outputs, put together to whole rows: a wave's 32 bytes of a row each would make four times the
   // requests. They are stored when the next chunk is in LDS, behind the same barrier.
@@ -406,11 +409,12 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   // Chunks that fill the tiles are fetched ahead.
   const bool fills = p.wide && p.di == DI && p.dout == NB;
   auto whole = [&](int64_t u0) { return fills && u0 + kChunk <= u_valid; };
-  auto fetch = [&](unsigned thread, int64_t u0) {
+  int buffer = 0;
+  auto fetch = [&](unsigned thread, int64_t u0, int to) {
     const int64_t low = p.reverse ? len - u0 - kChunk : u0;
     if (OUT) la.fetch(thread, as, a + low * p.a.token, int(p.a.token), p.reverse);
-    lb.fetch(thread, bs, b + low * p.b.token, int(p.b.token), p.reverse);
-    lc.fetch(thread, cs, c + low * p.c.token, int(p.c.token), p.reverse);
+    lb.fetch(thread, b_tiles[to], b + low * p.b.token, int(p.b.token), p.reverse);
+    lc.fetch(thread, c_tiles[to], c + low * p.c.token, int(p.c.token), p.reverse);
   };
   const bool stage = kStage && p.whole_out;
   auto flush = [&](unsigned thread, int64_t u0) {  // the staged outputs of the chunk at u0
@@ -427,7 +431,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
             *reinterpret_cast<const vec *>(os + Tile<T, NB>::at(u, col / 4));
     }
   };
-  if (whole(u_begin)) fetch(threadIdx.x, u_begin);
+  if (whole(u_begin)) fetch(threadIdx.x, u_begin, 0);
   __builtin_amdgcn_s_waitcnt(0x0f70);  // all loads: the loop then waits for its own chunks only
 
   for (int64_t u0 = u_begin; u0 < u_valid; u0 += kChunk) {
@@ -440,6 +444,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     const int n_valid = int(min(int64_t(kChunk), u_valid - u0));
     const int64_t t0 = p.reverse ? len - 1 - u0 : u0;
     const bool last = u0 + kChunk >= u_valid;
+    T *bs = b_tiles[buffer], *cs = c_tiles[buffer];
+    buffer = (buffer + 1) % kBuffers;
     if (whole(u0)) {
       if (OUT) la.store(thread, as);
       lb.store(thread, bs);
@@ -458,6 +464,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     __syncthreads();
     if constexpr (kStage)
       if (stage && u0 > u_begin) flush(thread, u0 - kChunk);
+    if (!OUT && whole(u0 + kChunk)) fetch(thread, u0 + kChunk, buffer);
     if (OUT) {
       // the weights of tokens 16 w .. 16 w + 15, and of half of the tokens before them where two waves share
       const int w4 = wave % 4, t = w4 * kTile + l16;
@@ -576,8 +583,9 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         }
       }
     }
+    if (kBuffers == 2) continue;
     __syncthreads();  // the weights are there, and a, b and c are read
-    if (whole(u0 + kChunk)) fetch(thread, u0 + kChunk);
+    if (OUT && whole(u0 + kChunk)) fetch(thread, u0 + kChunk, 0);
 
     if (OUT) {
       const int64_t out_at = ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
