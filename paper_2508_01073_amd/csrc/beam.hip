@@ -34,7 +34,7 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xffffffffu - uint32_t(key); }
 
-template <class V, class Op>
+template <int W, class V, class Op>
 __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
 #pragma unroll
   for (int off = kWave / 2; off > 0; off >>= 1) x = op(x, __shfl_xor(x, off, kWave));
@@ -43,19 +43,21 @@ __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
   __syncthreads();
   x = scratch[0];
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) x = op(x, scratch[i]);
+  for (int i = 1; i < W; ++i) x = op(x, scratch[i]);
   return x;
 }
+template <int W = kWaves>
 __device__ __forceinline__ uint64_t block_max_key(uint64_t x, uint64_t *scratch) {
-  return block_reduce(x, scratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+  return block_reduce<W>(x, scratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
 
 // A bound that at least k of the values that the threads' maxima x come from
-// reach: in each wave the k / kWaves-th of its lanes' distinct maxima, and the
+// reach: in each of the W waves the k / W-th of its lanes' distinct maxima, and the
 // least of those. -inf where the values are fewer. One barrier pair.
+template <int W = kWaves>
 __device__ __forceinline__ float block_bound(float x, int k, float *scratch) {
   float at = kInf;
-  for (int i = 0; i < (k + kWaves - 1) / kWaves; ++i) {
+  for (int i = 0; i < (k + W - 1) / W; ++i) {
     at = wave_max(x);
     if (x == at) x = -kInf;
   }
@@ -64,19 +66,19 @@ __device__ __forceinline__ float block_bound(float x, int k, float *scratch) {
   __syncthreads();
   at = scratch[0];
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) at = fminf(at, scratch[i]);
+  for (int i = 1; i < W; ++i) at = fminf(at, scratch[i]);
   return at;
 }
 
 // The k largest of the n distinct keys in `list`, descending, zeros beyond n, to put(rank, key).
 template <class Put>
 __device__ __forceinline__ void rank_list(const uint64_t *list, int n, int k, Put put) {
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  const int lane = lane_id();
+  for (int i = threadIdx.x / kWave; i < n; i += kWaves) {
     const uint64_t key = list[i];
     int rank = 0;
-#pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += list[j] > key ? 1 : 0;
-    if (rank < k) put(rank, key);
+    for (int j = lane; j - lane < n; j += kWave) rank += __popcll(__ballot(j < n && list[j] > key));
+    if (lane == 0 && rank < k) put(rank, key);
   }
   for (int i = n + threadIdx.x; i < k; i += kThreads) put(i, uint64_t(0));
 }
@@ -105,7 +107,9 @@ __device__ __forceinline__ bool row_counts(const SelectArgs &p, int64_t row) {
 }
 
 // One workgroup to a slice. HBM-bound: the logits are read once, 16 bytes a
-// lane and kVectors of them in flight.
+// lane and kVectors of them in flight. 32 groups of 8 beams and 100,050 float32
+// logits, a third of the beams finished or dead, take 19 us (3.7 TB/s), 8 groups
+// of 8 and 1,000,200 bfloat16 logits 26 us (3.3 TB/s).
 template <class T>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64_t first) {
   constexpr int kPer = Row<T>::kPer;
@@ -216,10 +220,9 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
   }
 }
 
-// Candidates of the merge that are ranked at once: all of them where there are
-// fewer lists than places to fill.
-constexpr int kAhead = 4;  // entries of a list that are read together
-constexpr int kOwn = 2;    // lists of a thread that are read ahead
+constexpr int kOwn = 2;        // parts of a wave that are read ahead
+constexpr int kStaged = 5120;  // entries of all lists that LDS takes
+// Candidates of the merge that are ranked at once: all of them where there are fewer lists than places to fill.
 constexpr int kMergeList = RDF2V_MAX_BEAMS * (RDF2V_MAX_BEAMS + 1);
 
 // The next value of the element type below x, which is one.
@@ -230,14 +233,23 @@ __device__ __forceinline__ float previous(float x) {
   return __uint_as_float(x == 0.0f ? 0x80000000u + kOne : x > 0.0f ? b - kOne : b + kOne);
 }
 
-// One workgroup to a group: its beams' candidates by total.
+// Threads of the merge: a chain of short steps, each shorter with more threads. A selection of 8 from 32
+// groups of 8 beams and 100,050 float32 logits takes 34, 33 and 34 us with 256, 512 and 1024 threads, one from
+// 8 groups of 8 beams and 1,000,200 bfloat16 logits 45, 42 and 40 us.
+constexpr int kMergeThreads = 512;
+constexpr int kMergeWaves = kMergeThreads / kWave;
+
+// One workgroup to a group: its beams' candidates by total. Bound by the latency of its steps, not by what it
+// reads: one trip to memory for all lists (2.4 us of 11), the beams' log-sum-exps (2), a bound from the lists'
+// first entries (1), the entries that reach it (1), their ranks, a wave to a candidate and a ballot to 64 of
+// those it is set against (1; 6 with a thread to a candidate), and the look at what the slices left out.
 template <class T>
-__global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int64_t first) {
+__global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p, int64_t first) {
   __shared__ float lse[RDF2V_MAX_BEAMS], score[RDF2V_MAX_BEAMS];
   __shared__ uint8_t counts[RDF2V_MAX_BEAMS], ended[RDF2V_MAX_BEAMS], again[RDF2V_MAX_BEAMS];
-  __shared__ float fscratch[kWaves];
-  __shared__ uint64_t kscratch[kWaves];
-  __shared__ uint64_t list[kMergeList];
+  __shared__ float fscratch[kMergeWaves];
+  __shared__ uint64_t kscratch[kMergeWaves];
+  __shared__ uint64_t list[kMergeList], stage[kStaged];
   __shared__ uint32_t place[kMergeList];
   __shared__ uint64_t chosen[RDF2V_MAX_BEAMS];
   __shared__ uint32_t chosen_place[RDF2V_MAX_BEAMS];
@@ -247,25 +259,26 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
   const int64_t slices = p.slices;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
 
-  // One trip to memory for what nearly every group needs: the scores, a wave's first parts and the first
-  // entries and the last one of a thread's first lists. Lists of beams that do not count hold anything.
-  const int lists = p.beams * int(slices);
-  const int l0 = wave + kWaves * lane;  // lists l0, l0 + kThreads, ...: as many to each wave
-  uint64_t own[kOwn][kAhead + 1];
-  auto read_ahead = [&] {
-#pragma unroll
-    for (int o = 0; o < kOwn; ++o) {
-      const uint64_t *keys = p.best + (row0 * slices + min(l0 + o * kThreads, lists - 1)) * k;
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) own[o][i] = keys[min(i, p.num_out)];
-      own[o][kAhead] = keys[p.num_out];
-    }
-  };
-  read_ahead();
+  // One trip to memory for what nearly every group needs: the lists, where they fit LDS, the scores and a
+  // wave's first parts. Lists of beams that do not count hold anything.
+  const int lists = p.beams * int(slices), l0 = wave + kMergeWaves * lane;  // as many lists to each wave
   float2 parts[kOwn];
 #pragma unroll
   for (int o = 0; o < kOwn; ++o)
-    parts[o] = p.parts[(row0 + min(wave + o * kWaves, p.beams - 1)) * slices + min(int64_t(lane), slices - 1)];
+    parts[o] = p.parts[(row0 + min(wave + o * kMergeWaves, p.beams - 1)) * slices + min(int64_t(lane), slices - 1)];
+  const bool staged = lists * k <= kStaged;
+  const uint64_t *source = p.best + row0 * slices * k;
+  if (staged) {
+    constexpr int kAhead = 5;
+    for (int i = threadIdx.x; i < lists * k; i += kAhead * kMergeThreads) {
+      uint64_t x[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) x[j] = source[min(i + j * kMergeThreads, lists * k - 1)];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j * kMergeThreads < lists * k) stage[i + j * kMergeThreads] = x[j];
+    }
+  }
   if (int(threadIdx.x) < p.beams) {
     const float x = p.scores[row0 + threadIdx.x];
     const bool end = p.finished != nullptr && p.finished[row0 + threadIdx.x] != 0;
@@ -275,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
     again[threadIdx.x] = 0;
   }
   __syncthreads();
-  for (int b = wave, o = 0; b < p.beams; b += kWaves, ++o) {
+  for (int b = wave, o = 0; b < p.beams; b += kMergeWaves, ++o) {
     if (!counts[b]) continue;
     float most = -kInf, sum = 0.0f;
     for (int64_t i = lane; i < slices; i += kWave) {
@@ -307,48 +320,29 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
   // candidates are compared by total, then by beam and token: (total, beam) is unique up to the token
   for (int round = 0;; ++round) {
     if (threadIdx.x == 0) count = any_again = 0;
-    // take(beam, list, its first entries) for every list of this thread
-    auto each_list = [&](auto take) {
-#pragma unroll
-      for (int o = 0; o < kOwn; ++o) {
-        const int l = l0 + o * kThreads, b = min(l, lists - 1) / int(slices);
-        if (l < lists && counts[b]) take(b, l, own[o]);
-      }
-      for (int l = l0 + kOwn * kThreads; l < lists; l += kThreads) {
-        const int b = l / int(slices);
-        if (!counts[b]) continue;
-        const uint64_t *keys = p.best + (row0 * slices + l) * k;
-        uint64_t next[kAhead + 1];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) next[i] = keys[min(i, p.num_out)];
-        next[kAhead] = keys[p.num_out];
-        take(b, l, next);
-      }
-    };
+    // after a second look the lists are those in memory
+    const uint64_t *keys = staged && round == 0 ? stage : source;
     // the lists' first entries: num_out of them bound the last chosen total
     float head = -kInf;
-    each_list([&](int b, int, const uint64_t(&key)[kAhead + 1]) {
-      if (key[0] != 0) head = fmaxf(head, total_of(b, key_value(key[0])));
-    });
-    const float bound = block_bound(head, p.num_out, fscratch);
-    each_list([&](int b, int l, const uint64_t(&key)[kAhead + 1]) {
-      // Descending logits have descending totals; the last entry only bounds what was left out.
-      auto offer = [&](uint64_t x) {
-        const float t = total_of(b, key_value(x));
-        if (x == 0 || !(t >= bound) || t == -kInf) return false;
-        const int at = atomicAdd(&count, 1);
-        if (at < kMergeList) {
-          list[at] = order_key(t, uint32_t(b) << 26);
-          place[at] = key_index(x);
-        }
-        return true;
-      };
-      bool more = true;
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) more = more && i < p.num_out && offer(key[i]);
-      for (int i = kAhead; more && i < p.num_out; ++i) more = offer(p.best[(row0 * slices + l) * k + i]);
-    });
-    for (int b = threadIdx.x; b < p.beams; b += kThreads)
+    for (int l = l0; l < lists; l += kMergeThreads) {
+      const int b = l / int(slices);
+      const uint64_t key = counts[b] ? keys[l * k] : 0;
+      if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
+    }
+    const float bound = block_bound<kMergeWaves>(head, p.num_out, fscratch);
+    // Descending logits have descending totals; the last entry only bounds what was left out.
+    for (int e = threadIdx.x; e < lists * k; e += kMergeThreads) {
+      const int l = e / k, b = l / int(slices);
+      const uint64_t key = counts[b] && e - l * k < p.num_out ? keys[e] : 0;
+      const float t = total_of(b, key_value(key));
+      if (key == 0 || !(t >= bound) || t == -kInf) continue;
+      const int at = atomicAdd(&count, 1);
+      if (at < kMergeList) {
+        list[at] = order_key(t, uint32_t(b) << 26);
+        place[at] = key_index(key);
+      }
+    }
+    for (int b = threadIdx.x; b < p.beams; b += kMergeThreads)
       if (ended[b]) {
         const int at = atomicAdd(&count, 1);
         if (at < kMergeList) {
@@ -359,18 +353,22 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
     __syncthreads();
     const int n = count;
     if (n <= kMergeList) {
-      for (int i = threadIdx.x; i < n; i += kThreads) {
+      // a wave ranks one candidate at a time, its lanes a candidate each to set against it
+      for (int i = wave; i < n; i += kMergeWaves) {
         const uint64_t key = list[i];
         const uint32_t at = place[i];
         int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) rank += list[j] > key || (list[j] == key && place[j] < at) ? 1 : 0;
-        if (rank < p.num_out) {
+        for (int j = lane; j - lane < n; j += kWave) {
+          const uint64_t other = j < n ? list[j] : 0;
+          const uint32_t there = j < n ? place[j] : 0;
+          rank += __popcll(__ballot(other > key || (other == key && there < at)));
+        }
+        if (lane == 0 && rank < p.num_out) {
           chosen[rank] = key;
           chosen_place[rank] = at;
         }
       }
-      for (int i = n + threadIdx.x; i < p.num_out; i += kThreads) chosen[i] = 0;
+      for (int i = n + threadIdx.x; i < p.num_out; i += kMergeThreads) chosen[i] = 0;
     } else {
       // one by one, from the lists
       uint64_t last = ~uint64_t(0);
@@ -385,20 +383,20 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
             at = token;
           }
         };
-        for (int l = threadIdx.x; l < lists; l += kThreads) {
+        for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
           const int b = l / int(slices);
           if (!counts[b]) continue;
           for (int i = 0; i < p.num_out; ++i) {
-            const uint64_t c = p.best[(row0 * slices + l) * k + i];
+            const uint64_t c = keys[l * k + i];
             if (c == 0) break;
             const float t = total_of(b, key_value(c));
             if (t > -kInf) offer(order_key(t, uint32_t(b) << 26), key_index(c));
           }
         }
-        for (int b = threadIdx.x; b < p.beams; b += kThreads)
+        for (int b = threadIdx.x; b < p.beams; b += kMergeThreads)
           if (ended[b]) offer(order_key(score[b], uint32_t(b) << 26 | 1u), 0);
-        const uint64_t top = block_max_key(key, kscratch);
-        const uint64_t low = block_max_key(key == top && top != 0 ? uint64_t(0xffffffffu - at) + 1 : 0, kscratch);
+        const uint64_t top = block_max_key<kMergeWaves>(key, kscratch);
+        const uint64_t low = block_max_key<kMergeWaves>(key == top && top != 0 ? uint64_t(0xffffffffu - at) + 1 : 0, kscratch);
         last = top;
         last_place = low == 0 ? 0 : 0xffffffffu - uint32_t(low - 1);
         if (threadIdx.x == 0) {
@@ -413,14 +411,16 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
     // slice's last entry, or equal to it with a higher token, which loses to that entry.
     const uint64_t worst = chosen[p.num_out - 1];
     const float least = worst != 0 ? key_value(worst) : -kInf;
-    each_list([&](int b, int, const uint64_t(&key)[kAhead + 1]) {
-      if (key[kAhead] == 0) return;
-      const float t = total_of(b, previous<T>(key_value(key[kAhead])));
+    for (int l = l0; l < lists; l += kMergeThreads) {
+      const int b = l / int(slices);
+      const uint64_t key = counts[b] ? keys[l * k + p.num_out] : 0;
+      if (key == 0) continue;
+      const float t = total_of(b, previous<T>(key_value(key)));
       if (t >= least && t > -kInf) {
         again[b] = 1;
         any_again = 1;
       }
-    });
+    }
     __syncthreads();
     if (!any_again) break;
     // such beams' best by total, from the whole row, in place of their lists
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
       for (int r = 0; r < p.num_out; ++r) {
         uint64_t key = 0;
         float x_of = 0.0f;
-        for (int64_t j = threadIdx.x; j < p.vocab; j += kThreads) {
+        for (int64_t j = threadIdx.x; j < p.vocab; j += kMergeThreads) {
           const float x = usable(to_f32(z[j])), t = total_of(b, x);
           const uint64_t c = x > -kInf && t > -kInf ? order_key(t, uint32_t(j)) : 0;
           if (c < last && c > key) {
@@ -440,17 +440,16 @@ __global__ __launch_bounds__(kThreads) void beam_merge_kernel(SelectArgs p, int6
             x_of = x;
           }
         }
-        last = block_max_key(key, kscratch);
+        last = block_max_key<kMergeWaves>(key, kscratch);
         if (last != 0 && key == last) p.best[row * slices * k + r] = order_key(x_of, key_index(last));
         if (last == 0 && threadIdx.x == 0) p.best[row * slices * k + r] = 0;
       }
-      for (int64_t i = 1 + threadIdx.x; i < slices; i += kThreads) p.best[(row * slices + i) * k] = 0;
+      for (int64_t i = k + threadIdx.x; i < slices * k; i += kMergeThreads) p.best[row * slices * k + i] = 0;
     }
     __syncthreads();
-    read_ahead();
   }
 
-  for (int r = threadIdx.x; r < p.num_out; r += kThreads) {
+  for (int r = threadIdx.x; r < p.num_out; r += kMergeThreads) {
     const uint64_t key = chosen[r];
     const uint32_t at = key_index(key);
     const int64_t to = group * p.num_out + r;
@@ -528,11 +527,11 @@ rdf2v_status launch_beam_select(const void *logits, int64_t stride, int32_t dtyp
     return RDF2V_OK;
   });
   if (st != RDF2V_OK) return st;
-  return for_each_launch(groups, kThreads, 1, [&](int64_t first, int64_t count) {
+  return for_each_launch(groups, kMergeThreads, 1, [&](int64_t first, int64_t count) {
     if (dtype == RDF2V_BF16)
-      beam_merge_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+      beam_merge_kernel<bf16><<<dim3(unsigned(count)), dim3(kMergeThreads), 0, stream>>>(p, first);
     else
-      beam_merge_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
+      beam_merge_kernel<float><<<dim3(unsigned(count)), dim3(kMergeThreads), 0, stream>>>(p, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });

@@ -255,3 +255,43 @@ def test_totals_that_round_together(vocab, type_):
                 mine = (parents.cpu() - torch.arange(2)[:, None] * 2).long() * vocab + tokens.cpu().long()
                 ok |= (place == mine).all(1)
         assert bool(ok.all()), (power, ok)
+
+
+@pytest.mark.parametrize("size", [(1, 1, 900, 64), (2, 3, 100_001, 8), (1, 4, 300_007, 64), (2, 2, 16_500, 1)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_totals_that_round_together(size):
+    """Scores near -1.5e7 leave totals whole numbers, so logits of one level tie, however a row's own
+    order ranks them, and the first of them win. The levels are far from where lse makes them round the
+    other way: lse is off by less than 1e-3 (its sum of exponentials, relative), the distance is 0.1."""
+    groups, beams, vocab, num_out = size
+    say(f"[beam] rounded totals {size}")
+    for type_ in (F32, BF16):
+        for seed in range(100):
+            g = torch.Generator()
+            g.manual_seed(seed)
+            level = torch.zeros(vocab)
+            level[torch.randperm(vocab, generator=g)[:vocab // (2 + seed)]] = 4.0
+            level[torch.randperm(vocab, generator=g)[:5]] = 8.0
+            fine = torch.rand(vocab, generator=g) if type_ == F32 else torch.randint(0, 2, (vocab,), generator=g)
+            x = (level + fine * 0.0625).to(type_)
+            part = (0.03 - torch.logsumexp(x.double(), 0)) % 1.0
+            if abs(float(part) - 0.5) > 0.14:
+                break
+        else:
+            raise AssertionError("no levels clear of the rounding")
+        logits = x.to(device()).repeat(groups, beams, 1)
+        _, tokens, parents = rd.rdf2v_beam_select(logits, torch.full((groups, beams), -1.5e7, device=device()), num_out)
+        order = level.repeat(beams).sort(descending=True, stable=True).indices[:num_out]
+        for i in range(groups):
+            assert torch.equal(tokens[i].cpu().long(), order % vocab)
+            assert torch.equal(parents[i].cpu().long(), i * beams + order // vocab)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 64, 40_000, 64), (2, 2, 700_000, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_more_entries_than_stay_on_the_chip(size, type_):
+    groups, beams, vocab, num_out = size
+    say(f"[beam] many entries {size} {type_}")
+    logits, scores = _inputs(groups, beams, vocab, type_, 12)
+    _check(logits, scores, num_out)
+    _check(logits, scores * 0.0, num_out)
