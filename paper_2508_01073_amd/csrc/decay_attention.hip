@@ -336,7 +336,7 @@ __device__ __forceinline__ void store_four(const ScanArgs &p, int64_t at, int co
 //
 // A tile of 16 columns to a wave keeps all of that in 128 registers up to heads
 // of 128, so that 16 waves share a CU; two tiles to a wave spilled, and the
-// waits for the spills made it 2.x times slower.
+// waits for the spills made it more than twice as slow.
 constexpr int scan_waves(int nb) { return nb > 64 ? 8 : 4; }
 
 template <class T, int DI, int NB, bool OUT>
@@ -957,16 +957,23 @@ rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
 // the states of the segments are computed first and joined, and all segments
 // run at once: b and c are read twice, and a state is written and read for
 // each segment. At least kLeastChunks chunks to a segment keep that traffic
-// below what the segment itself reads. kFill: one row of 20,011 x 8 heads of
-// 128 took 117 us at 256 workgroups, 112 at 512 and 112 at 1,024; four rows of
-// 4,096 x 16 heads, all gradients, 637, 565 and 644.
+// below what the segment itself reads.
+//
+// kFill: two workgroups of a scan share a CU, so 512 are one round of them.
+// One row of 20,011 x 8 heads of 128, forward, takes 110, 114, 104 and 106 us
+// with 256, 384, 512 and 768. The segments are as many as the state scans (two
+// of them backwards) need to fill a round: with the 512 counted over the three
+// scans of the gradients, four rows of 4,096 x 16 heads of 128, forward and
+// backward, take 508 us, not 460, and two of 8,192 x 16 heads of 64 take 253,
+// not 215. But rows whose three scans fill a round by themselves are not cut:
+// 12 rows of 2,048 x 16 heads of 128 take 606 us whole and 741 in two.
 constexpr int64_t kFill = 512;
 constexpr int64_t kLeastChunks = 4;
 
-int64_t segment_count(int64_t scans, int64_t length) {
-  const int64_t chunks = (length + kChunk - 1) / kChunk;
-  if (scans >= kFill || chunks < 2 * kLeastChunks) return 1;
-  const int64_t want = (kFill + scans - 1) / scans, most = chunks / kLeastChunks;
+int64_t segment_count(int64_t rows_heads, int scans, int state_scans, int64_t length) {
+  const int64_t chunks = (length + kChunk - 1) / kChunk, states = rows_heads * state_scans;
+  if (rows_heads * scans >= kFill || chunks < 2 * kLeastChunks) return 1;
+  const int64_t want = (kFill + states - 1) / states, most = chunks / kLeastChunks;
   const int64_t count = want < most ? want : most, per = (chunks + count - 1) / count;
   return (chunks + per - 1) / per;
 }
@@ -1016,7 +1023,7 @@ template <class T>
 rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_states, const int *state_of,
                           float *seg_state, bool together, hipStream_t stream) {
   const bool short_rows = use_short(scans, count);
-  const int64_t segments = segment_count(scans[0].rows * scans[0].heads * count, scans[0].length);
+  const int64_t segments = segment_count(scans[0].rows * scans[0].heads, count, num_states, scans[0].length);
   if (segments > 1) {
     ScanRoles roles{};
     for (int i = 0; i < num_states; ++i) {
@@ -1059,7 +1066,7 @@ rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_
 }
 
 size_t segment_state_bytes(const rdf2v_attention &a, bool backward) {
-  const int64_t segments = segment_count(a.rows * a.heads * (backward ? 3 : 1), a.length);
+  const int64_t segments = segment_count(a.rows * a.heads, backward ? 3 : 1, backward ? 2 : 1, a.length);
   if (segments == 1) return 0;
   return align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float) * (backward ? 2 : 1), 256);
 }
