@@ -129,6 +129,14 @@ __device__ __forceinline__ f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
   return c;
 }
 
+// The same where the last four values of each lane are zeros.
+__device__ __forceinline__ f32x4 mma_low(bf16x8 a, bf16x8 b, f32x4 c) { return mma(a, b, c); }
+__device__ __forceinline__ f32x4 mma_low(f32x8 a, f32x8 b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ f32x8 join(f32x4 a, f32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 
@@ -724,36 +732,51 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
   const float *s0 = p.s0 == nullptr ? nullptr : p.s0 + state_at;
 
   if (len > 0) {
+    // a_t . b_s of the pairs of tiles: every row is read once, and of all tiles together
+    f32x4 x[TT][TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int st = 0; st < TT; ++st) x[t][st] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int kk = 0; kk < kK; ++kk) {
+      if (kk * 32 >= p.di) break;
+      eight av[TT], bv[TT];
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        if (t >= tiles) break;
+        const int64_t u = token_of(t * kTile + l16);
+        av[t] = short_row(a + u * p.a.token, kk, g, p.di, p.wide);
+        bv[t] = short_row(b + u * p.b.token, kk, g, p.di, p.wide);
+      }
+      const bool low = kk * 32 + kTile >= p.di;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        if (t >= tiles) break;
+#pragma unroll
+        for (int st = 0; st <= t; ++st)
+          x[t][st] = low ? mma_low(bv[st], av[t], x[t][st]) : mma(bv[st], av[t], x[t][st]);
+      }
+    }
     // weights of the pairs (t, s) as operands: tile t, blocks of 32 of s
     eight w[TT][kBlocks][kPieces];
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       if (t >= tiles) break;
-      const T *at = a + token_of(t * kTile + l16) * p.a.token;
-      eight av[kK];
-#pragma unroll
-      for (int kk = 0; kk < kK; ++kk)
-        if (kk * 32 < p.di) av[kk] = short_row(at, kk, g, p.di, p.wide);
 #pragma unroll
       for (int s32 = 0; s32 <= t / 2; ++s32) {
-        f32x4 x[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int st = 2 * s32 + i;
-          x[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
           if (st > t) continue;
-          const T *bt = b + token_of(st * kTile + l16) * p.b.token;
-#pragma unroll
-          for (int kk = 0; kk < kK; ++kk)
-            if (kk * 32 < p.di) x[i] = mma(short_row(bt, kk, g, p.di, p.wide), av[kk], x[i]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int d = (t - st) * kTile + l16 - 4 * g - r;
-            const float y = x[i][r] * p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma);
-            x[i][r] = d >= 0 ? y : 0.0f;
+            const float y = x[t][st][r] * p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma);
+            x[t][st][r] = d >= 0 ? y : 0.0f;
           }
         }
-        f32x8 both = join(x[0], x[1]);
+        f32x8 both = join(x[t][2 * s32], 2 * s32 + 1 <= t ? x[t][2 * s32 + 1 < TT ? 2 * s32 + 1 : 0] : f32x4{});
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) w[t][s32][i] = take_piece(both, T());
       }
@@ -816,7 +839,8 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
 #pragma unroll
         for (int kk = 0; kk <= t / 2; ++kk)
 #pragma unroll
-          for (int i = 0; i < kPieces; ++i) o[t] = mma(cv[kk], w[t][kk][i], o[t]);
+          for (int i = 0; i < kPieces; ++i)  // of the last block an even tile has the lower half
+            o[t] = 2 * kk == t ? mma_low(cv[kk], w[t][kk][i], o[t]) : mma(cv[kk], w[t][kk][i], o[t]);
         const int u = t * kTile + l16;
         if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
       }
