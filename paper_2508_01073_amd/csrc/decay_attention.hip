@@ -636,7 +636,7 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
       flush(threadIdx.x, u_begin + (u_valid - 1 - u_begin) / kChunk * kChunk);
     }
 
-  if (OUT) {  // tokens beyond the row's length
+  if (OUT && !p.out_f32) {  // tokens beyond the row's length (of a sum over heads, the sum has them)
     const int64_t t_begin = max(u_begin, len);
     const int64_t out_at = ((row * p.length + t_begin) * p.heads + h) * int64_t(p.dout);
     const int cols = (p.dout + 3) / 4;
@@ -895,7 +895,8 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
     for (int i = lane; i < p.di * p.dout; i += kWave)
       p.s1[state_at + i] = s0 == nullptr ? 0.0f : s0[p.transposed ? i % p.dout * p.di + i / p.dout : i];
   }
-  // tokens beyond the row's length
+  if (p.out_f32) return;
+  // tokens beyond the row's length (of a sum over heads, the sum has them)
   const int cols = (p.dout + 3) / 4;
   for (int i = lane; i < (int(p.length) - len) * cols; i += kWave) {
     const int col = i % cols * 4;
@@ -1095,23 +1096,55 @@ size_t segment_state_bytes(const rdf2v_attention &a, bool backward) {
   return align_up(size_t(a.rows) * a.heads * segments * a.dk * a.dv * sizeof(float) * (backward ? 2 : 1), 256);
 }
 
-// Sums of the gradients of `share` query heads, in head order.
-template <class T>
-__global__ __launch_bounds__(256) void share_sum_kernel(const float *part, T *out, int64_t groups, int share, int d,
-                                                        int64_t first) {
-  const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
-  if (i >= groups * d) return;
-  const float *x = part + i / d * share * d + i % d;
-  float sum = 0.0f;
-  for (int j = 0; j < share; ++j) sum += x[int64_t(j) * d];
-  out[i] = from_f32<T>(sum);
+// The gradients of `share` query heads' keys and values summed in head order,
+// and zeros for the tokens beyond a row's length, whose parts are not there. A
+// wave takes a token, VEC values a lane: HBM-bound. 1,024 rows of up to 33
+// tokens (half of them there), 6 heads on 3 of 48 and 80 in float32: 16 us,
+// where a launch for each gradient over the padding too takes 37.
+struct ShareArgs {
+  const float *part[2];
+  void *out[2];
+  int32_t d[2];
+  const int32_t *len;
+  int64_t rows, length;
+  int32_t kv_heads, share;
+};
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void share_sum_kernel(ShareArgs p, int64_t first) {
+  typedef float in __attribute__((ext_vector_type(VEC), aligned(4)));
+  typedef T to __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
+  constexpr int kWaves = kThreads / kWave;
+  const int64_t token = (first + blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (token >= p.rows * p.length) return;
+  const bool there = token % p.length < row_length(p.len, token / p.length, p.length, nullptr, false);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int per = p.d[i] / VEC;
+    const float *part = p.part[i] + token * p.kv_heads * p.share * p.d[i];
+    T *out = static_cast<T *>(p.out[i]) + token * p.kv_heads * p.d[i];
+    for (int at = lane_id(); at < p.kv_heads * per; at += kWave) {
+      const float *x = part + (unsigned(at) / unsigned(per) * p.share * per + unsigned(at) % unsigned(per)) * VEC;
+      in sum{};
+      if (there)
+        for (int j = 0; j < p.share; ++j) sum += *reinterpret_cast<const in *>(x + j * p.d[i]);
+      to y;
+#pragma unroll
+      for (int r = 0; r < VEC; ++r) y[r] = from_f32<T>(sum[r]);
+      *reinterpret_cast<to *>(out + at * VEC) = y;
+    }
+  }
 }
 
 template <class T>
-rdf2v_status launch_share_sum(const float *part, void *out, int64_t groups, int share, int d, hipStream_t stream) {
-  return for_each_launch((groups * d + 255) / 256, 256, 1, [&](int64_t first, int64_t count) {
-    share_sum_kernel<T>
-        <<<dim3(unsigned(count)), dim3(256), 0, stream>>>(part, static_cast<T *>(out), groups, share, d, first);
+rdf2v_status launch_share_sum(const ShareArgs &p, hipStream_t stream) {
+  constexpr int kWaves = kThreads / kWave;
+  return for_each_launch((p.rows * p.length + kWaves - 1) / kWaves, kThreads, 1, [&](int64_t first, int64_t count) {
+    const dim3 grid{unsigned(count)}, threads{kThreads};
+    if (p.d[0] % 4 == 0 && p.d[1] % 4 == 0)
+      share_sum_kernel<T, 4><<<grid, threads, 0, stream>>>(p, first);
+    else
+      share_sum_kernel<T, 1><<<grid, threads, 0, stream>>>(p, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });
@@ -1210,8 +1243,8 @@ rdf2v_status backward(const rdf2v_attention &a, const rdf2v_heads_view &q, const
   const bool together = dstate == nullptr || dstate != dstate_out;
   rdf2v_status st = launch_scans<T>(scans, 3, states, 2, state_of, seg, together, stream);
   if (st != RDF2V_OK || share == 1) return st;
-  st = launch_share_sum<T>(part_k, dk, tokens * a.kv_heads, share, a.dk, stream);
-  return st == RDF2V_OK ? launch_share_sum<T>(part_v, dv, tokens * a.kv_heads, share, a.dv, stream) : st;
+  return launch_share_sum<T>({{part_k, part_v}, {dk, dv}, {a.dk, a.dv}, a.len, a.rows, a.length, a.kv_heads, share},
+                             stream);
 }
 
 struct StepArgs {
