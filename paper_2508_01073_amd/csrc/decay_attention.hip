@@ -665,8 +665,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 // above, operands of the products with c as they stand, so the wave needs no
 // LDS and no barrier, and many waves share a CU; a workgroup to a row leaves
 // most of its waves idle at its barriers. 4,000 rows of up to 17 tokens (half
-// of them there), 4 heads of 32 in bfloat16: 22 us, 2.0 TB/s, bound by the
-// latency of a wave's few dependent loads; 73 us with workgroups.
+// of them there), 4 heads of 32 in bfloat16: 19 us, 2.3 TB/s, bound by the
+// latency of a wave's few dependent loads; 73 us with workgroups. 1,024 rows of
+// up to 33 in float32, 6 heads on 3 of 48 and 80: 38 us, and 76 for the three
+// gradients, of which the matrix instructions take a quarter and the requests
+// to L1 a third.
 //
 // TT: most tiles of 16 tokens.
 constexpr int kShortWaves = 4;  // of a workgroup, each for itself
@@ -1021,21 +1024,25 @@ void finish(ScanArgs &p, bool short_rows, int64_t segments) {
 }
 
 // Whether a wave to a row and head is the faster way. us with a wave / with a
-// workgroup and chunks, 8 heads, 2^27 values of q, k, v and out (bfloat16):
-//   tokens   sizes 32    64          128         sizes 32, states in and out   64          128
-//   16       35 / 162    35 / 118    38 / 120    167 / 241                     369 / 226   806 / 341
-//   32       36 / 88     46 / 66     45 / 72     120 / 135                     281 / 125   435 / 186
-//   33       58 / 87     61 / 70     67 / 75     161 / 139                     267 / 139   511 / 195
-//   64       87 / 47     90 / 37     93 / 41     136 / 71                      236 / 72    469 / 108
-// and in float32 59 / 342, 60 / 342, 63 / 424; 207 / 454, 386 / 491, 761 / 758
-// at 16 tokens, 82 / 202, 89 / 216, 100 / 255; 175 / 271, 288 / 324, 803 / 461
-// at 33. A wave's 32-bit places take tokens less than 2^23 values apart, in
-// ascending order.
+// workgroup and chunks, 8 heads, 256 MB of q, k, v and out:
+//              tokens  sizes 32   64         128        sizes 32, states   64         128
+//   bfloat16   16      56 / 356   61 / 282   63 / 218   310 / 546          659 / 543  1388 / 646
+//              32      53 / 182   71 / 146   93 / 123   216 / 288          464 / 283   999 / 341
+//              33      75 / 178  104 / 153  105 / 119   273 / 295          492 / 305   909 / 358
+//              48      64 / 126  101 / 111  106 / 88    205 / 210          424 / 221   867 / 259
+//   float32    16      44 / 316   47 / 320   46 / 402   201 / 445          373 / 497   743 / 763
+//              32      48 / 165   50 / 180   56 / 221   157 / 235          276 / 293   465 / 413
+//              33      58 / 174   55 / 184   61 / 226   161 / 263          263 / 325   514 / 460
+//              48      51 / 126   54 / 136   55 / 166   141 / 192          255 / 236   422 / 330
+// (states: float32 in and out). A wave's 32-bit places take tokens less than
+// 2^23 values apart, in ascending order.
+template <class T>
 bool use_short(const ScanArgs *scans, int count) {
+  constexpr int kStates = sizeof(T) == 4 ? 64 : 32;
   for (int i = 0; i < count; ++i) {
     const ScanArgs &p = scans[i];
     if (p.length > 3 * kTile) return false;
-    if ((p.s0 != nullptr || p.s1 != nullptr) && (p.di > 32 || p.dout > 32)) return false;
+    if ((p.s0 != nullptr || p.s1 != nullptr) && (p.di > kStates || p.dout > kStates)) return false;
     for (const ScanOperand *x : {&p.a, &p.b, &p.c})
       if (x->token < 0 || x->token >= int64_t(1) << 23) return false;
   }
@@ -1047,7 +1054,7 @@ bool use_short(const ScanArgs *scans, int count) {
 template <class T>
 rdf2v_status launch_scans(ScanArgs *scans, int count, ScanArgs *states, int num_states, const int *state_of,
                           float *seg_state, bool together, hipStream_t stream) {
-  const bool short_rows = use_short(scans, count);
+  const bool short_rows = use_short<T>(scans, count);
   const int64_t segments = segment_count(scans[0].rows * scans[0].heads, count, num_states, scans[0].length);
   if (segments > 1) {
     ScanRoles roles{};
