@@ -525,7 +525,9 @@ size_t rdf2v_decay_attention_backward_workspace_size(const rdf2v_attention *a);
  *               RDF2V_STATUS_BAD_LENGTH).
  *
  * Outputs may not overlap inputs, but for state_out. The same inputs give the
- * same bits on every call.
+ * same bits on every call. A NaN or infinity in a token below L reaches, beyond
+ * the outputs of the formula, those of up to 63 tokens before it, whose weights
+ * for it are zeros.
  */
 rdf2v_status rdf2v_decay_attention(const rdf2v_attention *a, const rdf2v_heads_view *q, const rdf2v_heads_view *k,
                                    const rdf2v_heads_view *v, const float *state, void *out, float *state_out,

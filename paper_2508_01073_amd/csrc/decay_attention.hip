@@ -342,6 +342,13 @@ __device__ __forceinline__ void store_four(const ScanArgs &p, int64_t at, int co
 //
 // OUT: outputs are wanted; otherwise only S of the segment (from zeros).
 //
+// One row of 20,011 tokens, 8 heads of 128 in bfloat16, in 63 segments: 49 us
+// with outputs (4.0 TB/s, states included), 31 us for the states alone (3.7) and
+// 16 us to join them (4.1). Four rows of 4,096, 16 heads: 78 us for the outputs
+// and 225 for the three gradients. The issue of vector instructions, half of
+// the cycles, and the waits at a chunk's two barriers bound the scans with
+// outputs, HBM those without.
+//
 // A tile of 16 columns to a wave keeps all of that in 128 registers up to heads
 // of 128, so that 16 waves share a CU; two tiles to a wave spilled, and the
 // waits for the spills made it more than twice as slow.
@@ -1268,7 +1275,8 @@ struct StepArgs {
 
 // One workgroup to a row and head. HBM-bound: a state is read and written once,
 // 2 operations a byte, VEC values a lane and kAhead loads of a lane in flight
-// (a state of 128 x 128 is 16 loads of 16 bytes a thread).
+// (a state of 128 x 128 is 16 loads of 16 bytes a thread). 512 rows of 8 heads
+// of 128 x 128 that take over the states of their parents: 82 us, 5.4 TB/s.
 template <class T, int VEC>
 __global__ __launch_bounds__(kThreads) void step_kernel(StepArgs p, int64_t first) {
   typedef float vec __attribute__((ext_vector_type(VEC)));

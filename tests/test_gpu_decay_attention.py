@@ -333,3 +333,30 @@ def test_refusals():
     with pytest.raises(rd.Rdf2vError):
         rd.rdf2v_decay_attention_backward(q, k, v, g, x["dout"],
                                           workspace=torch.empty(16, dtype=torch.uint8, device=device()))
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(6, 33, 4, 2, 48, 64), (5, 48, 2, 2, 64, 33), (300, 16, 6, 2, 40, 20),
+                                  (9, 47, 3, 1, 52, 36)], ids=lambda s: "x".join(map(str, s)))
+def test_short_rows_with_states(size, type_):
+    say(f"[attention] short rows with states {size} {type_}")
+    x = _inputs(*size, type_, 17, True, True)
+    ref, sizes = _reference(x, size[4] ** -0.5)
+    _check(_run(x), ref, attention_bounds(ref, sizes, type_, size[2] // size[3]), f"{size}")
+
+
+def test_gradients_of_shared_heads_beyond_a_row():
+    """Zeros for tokens beyond a row's length, whatever the outputs and the workspace hold."""
+    say("[attention] shared heads' gradients of the padding")
+    for length, type_ in ((20, F32), (20, BF16), (150, F32), (150, BF16)):
+        x = _inputs(7, length, 6, 2, 24, 20, type_, 23, True)
+        ws = torch.full((rd.rdf2v_decay_attention_backward_workspace_size(7, length, 6, 2, 24, 20, type_),), 255,
+                        dtype=torch.uint8, device=device())
+        outs = dict(dq=torch.full_like(x["q"], math.nan), dk=torch.full_like(x["k"], math.nan),
+                    dv=torch.full_like(x["v"], math.nan))
+        args = (x["q"], x["k"], x["v"], x["log_decay"], x["dout"])
+        rd.rdf2v_decay_attention_backward(*args, lens=x["lens"], workspace=ws, **outs)
+        ref = rd.rdf2v_decay_attention_backward(*args, lens=x["lens"])
+        beyond = torch.arange(length, device=device()) >= x["lens"][:, None]
+        for name, want in zip(("dq", "dk", "dv"), ref):
+            assert torch.equal(outs[name], want) and bool((outs[name][beyond] == 0).all()), (length, type_, name)
