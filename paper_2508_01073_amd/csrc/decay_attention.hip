@@ -388,6 +388,12 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   const bool report = seg == 0 && threadIdx.x == 0;
   const float head_log2_gamma =
       head_log_decay(p.log_decay, h, p.status, report && row == 0) * kLog2e;
+  // decays over 1 .. 7 tokens and over a tile of them, the same in all lanes
+  float by_tokens[7], by_tile;
+  auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
+#pragma unroll
+  for (int j = 0; j < 7; ++j) by_tokens[j] = uniform(__builtin_amdgcn_exp2f(float(j + 1) * head_log2_gamma));
+  by_tile = uniform(__builtin_amdgcn_exp2f(float(kTile) * head_log2_gamma));
   const int64_t len = row_length(p.len, row, p.length, p.status, report && h == 0);
   const int e = p.reverse ? 0 : 1;
   const T *a = operand_row<T>(p.a, row, h), *b = operand_row<T>(p.b, row, h), *c = operand_row<T>(p.c, row, h);
@@ -539,20 +545,21 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
             for (int n = 0; n < kTilesN; ++n) o[t][n] = mma(sv[n][i], av[t], o[t][n]);
       }
+      float d = p.oscale * __builtin_amdgcn_exp2f(float(wt * kTilesT * kTile + l16 + e) * log2_gamma);
 #pragma unroll
       for (int t = 0; t < kTilesT; ++t) {
-        const int u = (wt * kTilesT + t) * kTile + l16;
-        const float d = p.oscale * __builtin_amdgcn_exp2f(float(u + e) * log2_gamma);
 #pragma unroll
         for (int n = 0; n < kTilesN; ++n) o[t][n] *= d;
+        d *= by_tile;
       }
     }
 
     if (!last || exact_state) {
       const float d = __builtin_amdgcn_exp2f(float(n_valid) * log2_gamma);
       float near[8];
+      near[7] = __builtin_amdgcn_exp2f(float(24 - 8 * g) * log2_gamma);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) near[j] = __builtin_amdgcn_exp2f(float(31 - 8 * g - j) * log2_gamma);
+      for (int j = 0; j < 7; ++j) near[j] = near[7] * by_tokens[6 - j];
 #pragma unroll
       for (int n = 0; n < kTilesN; ++n)
 #pragma unroll
