@@ -388,7 +388,9 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   const bool report = seg == 0 && threadIdx.x == 0;
   const float head_log2_gamma =
       head_log_decay(p.log_decay, h, p.status, report && row == 0) * kLog2e;
-  // decays over 1 .. 7 tokens and over a tile of them, the same in all lanes
+  // Decays over 1 .. 7 tokens and over a tile of them, the same in all lanes: of neighbouring tokens' decays
+  // one is computed and the others are its products (gradients of 12 rows of 2,048 x 16 heads of 128 with
+  // the forward pass 606 -> 593 us, of two of 8,192 x 16 of 64 215 -> 203).
   float by_tokens[7], by_tile;
   auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
 #pragma unroll
@@ -501,10 +503,16 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
         if (i <= w4) {
 #pragma unroll
           for (int kk = 0; kk < kK; ++kk) w = mma(row_values<DI>(bs, i * kTile + l16, kk, g), av[kk], w);
+          const int d3 = t - (i * kTile + 4 * g + 3);  // of r = 3; positive off the diagonal
+          if (i < w4) {
+            const float decay = p.pscale * __builtin_amdgcn_exp2f(float(d3) * log2_gamma);
+            w *= f32x4{decay * by_tokens[2], decay * by_tokens[1], decay * by_tokens[0], decay};
+          } else {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int d = t - (i * kTile + 4 * g + r);
-            w[r] *= d >= 0 ? p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
+            for (int r = 0; r < 4; ++r) {
+              const int d = d3 + 3 - r;
+              w[r] *= d >= 0 ? p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
+            }
           }
         }
 #pragma unroll
@@ -1006,9 +1014,9 @@ rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
 // with 256, 384, 512 and 768. The segments are as many as the state scans (two
 // of them backwards) need to fill a round: with the 512 counted over the three
 // scans of the gradients, four rows of 4,096 x 16 heads of 128, forward and
-// backward, take 508 us, not 460, and two of 8,192 x 16 heads of 64 take 253,
+// backward, take 508 us, not 460, and two of 8,192 x 16 heads of 64 took 253,
 // not 215. But rows whose three scans fill a round by themselves are not cut:
-// 12 rows of 2,048 x 16 heads of 128 take 606 us whole and 741 in two.
+// 12 rows of 2,048 x 16 heads of 128 took 606 us whole and 741 in two.
 constexpr int64_t kFill = 512;
 constexpr int64_t kLeastChunks = 4;
 
