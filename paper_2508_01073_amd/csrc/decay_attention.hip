@@ -1022,7 +1022,7 @@ constexpr int64_t kLeastChunks = 4;
 
 int64_t segment_count(int64_t rows_heads, int scans, int state_scans, int64_t length) {
   const int64_t chunks = (length + kChunk - 1) / kChunk, states = rows_heads * state_scans;
-  if (rows_heads * scans >= kFill || chunks < 2 * kLeastChunks) return 1;
+  if (rows_heads == 0 || rows_heads * scans >= kFill || chunks < 2 * kLeastChunks) return 1;
   const int64_t want = (kFill + states - 1) / states, most = chunks / kLeastChunks;
   const int64_t count = want < most ? want : most, per = (chunks + count - 1) / count;
   return (chunks + per - 1) / per;

@@ -167,3 +167,19 @@ def test_distill_refusals(lib):
     assert both(rows=0, logits=None, ids=None) == (pkg.RDF2V_OK, pkg.RDF2V_OK)
     for sizes in ((-1, 1, 1), (1, 0, 1), (1, 1, 513), (2**31, 1, 1), (1, 2**31, 1)):
         assert pkg.rdf2v_distill_workspace_size(*sizes) == 0
+
+
+@pytest.mark.parametrize("length", [0, 1, 448, 449, 1024, 2**31 - 1])
+def test_attention_of_no_rows(lib, length):
+    """An empty batch of rows of any length needs nothing and does nothing."""
+    so, pkg = lib
+    for heads, kv, d in ((1, 1, 1), (4, 2, 32), (65535, 1, 128)):
+        sizes = (0, length, heads, kv, d, d)
+        assert pkg.rdf2v_decay_attention_workspace_size(*sizes) == 0
+        assert pkg.rdf2v_decay_attention_backward_workspace_size(*sizes) == 0
+        a = dict(rows=0, length=length, heads=heads, kv_heads=kv, dk=d, dv=d)
+        assert _forward(lib, **a) == pkg.RDF2V_OK and _forward(lib, ws=None, wsb=0, **a) == pkg.RDF2V_OK
+        c, v = _attention(pkg, **a), _view(pkg)
+        for ws, wsb in ((WS, 1 << 40), (None, 0)):
+            assert so.rdf2v_decay_attention_backward(c, v, v, v, v, None, None, FAKE, FAKE, FAKE, None, ws, wsb, None,
+                                                     None) == pkg.RDF2V_OK
