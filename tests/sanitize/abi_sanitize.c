@@ -22,6 +22,87 @@
 
 static void *fake(uintptr_t addr) { return (void *)addr; }
 
+/* The operators of a sequence model over walk tokens. */
+static size_t model_entries(const int64_t *big64, size_t n64, const int32_t *big32, size_t n32) {
+  size_t sink = 0;
+  void *F = fake((uintptr_t)1 << 40), *W = fake((uintptr_t)1 << 44);
+  float *FF = (float *)F, *WF = (float *)W;
+  int32_t *FI = (int32_t *)F, *WI = (int32_t *)W;
+  const int64_t lengths[] = {0, 1, 448, 449, 1024, ((int64_t)1 << 31) - 1, INT64_MAX, INT64_MIN};
+  for (size_t i = 0; i < n64; ++i) {
+    for (size_t j = 0; j < sizeof(lengths) / sizeof(lengths[0]); ++j)
+      for (size_t k = 0; k < n32; ++k)
+        for (size_t l = 0; l < n32; ++l) {
+          const rdf2v_attention a = {big64[i], lengths[j], big32[k], big32[l], 1 + (int32_t)(l % 128), 128, RDF2V_F32,
+                                     1.0f, NULL, NULL};
+          rdf2v_attention b = a;
+          b.kv_heads = b.heads;
+          b.dk = big32[l];
+          sink += rdf2v_decay_attention_workspace_size(&a) + rdf2v_decay_attention_backward_workspace_size(&a);
+          sink += rdf2v_decay_attention_workspace_size(&b) + rdf2v_decay_attention_backward_workspace_size(&b);
+        }
+    for (size_t j = 0; j < n64; ++j)
+      for (size_t k = 0; k < n32; ++k) {
+        sink += rdf2v_beam_select_workspace_size(big64[i], big32[k], big64[j], 64);
+        sink += rdf2v_beam_select_workspace_size(big64[i], 64, big64[j], big32[k]);
+        sink += rdf2v_distill_workspace_size(big64[i], big64[j], big32[k], RDF2V_BF16);
+        sink += rdf2v_distill_workspace_size(big64[i], big64[j], 512, big32[k]);
+      }
+  }
+
+  /* decay attention */
+  const rdf2v_attention ok = {4, 10, 4, 2, 16, 24, RDF2V_F32, 1.0f, FF, NULL};
+  const rdf2v_heads_view v = {F, 640, 64, 16}, none = {NULL, 640, 64, 16}, far = {F, INT64_MIN, INT64_MAX, INT64_MIN};
+  rdf2v_attention a = ok;
+  EXPECT(rdf2v_decay_attention(NULL, &v, &v, &v, NULL, W, NULL, NULL, 0, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_decay_attention(&ok, &v, &far, &v, NULL, W, NULL, NULL, 0, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_decay_attention(&ok, &v, &none, &v, NULL, W, NULL, NULL, 0, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_decay_attention_backward(&ok, &v, &v, &v, &v, NULL, NULL, W, W, W, NULL, NULL, 0, NULL, NULL) ==
+         RDF2V_ERR_WORKSPACE);
+  EXPECT(rdf2v_decay_attention_step(&ok, &v, &v, &v, FF, INT64_MAX, FI, W, WF, NULL, NULL) == RDF2V_ERR_TOO_LARGE);
+  EXPECT(rdf2v_decay_attention_step(&ok, &v, &v, &v, FF, INT64_MIN, FI, W, WF, NULL, NULL) ==
+         RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_decay_attention_step(&ok, &v, &v, &v, FF, 4, FI, W, FF, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  a.rows = ((int64_t)1 << 31) - 1;
+  a.length = a.rows;
+  EXPECT(rdf2v_decay_attention(&a, &v, &v, &v, NULL, W, NULL, NULL, 0, NULL, NULL) == RDF2V_ERR_TOO_LARGE);
+  for (size_t i = 0; i < sizeof(lengths) / sizeof(lengths[0]); ++i) {
+    a = ok;
+    a.rows = 0;
+    a.length = lengths[i];
+    const rdf2v_status want = a.length < 0                   ? RDF2V_ERR_INVALID_ARGUMENT
+                              : a.length >= (int64_t)1 << 31 ? RDF2V_ERR_TOO_LARGE
+                                                             : RDF2V_OK;
+    EXPECT(rdf2v_decay_attention(&a, &v, &v, &v, NULL, W, NULL, NULL, 0, NULL, NULL) == want);
+    EXPECT(rdf2v_decay_attention_backward(&a, &v, &v, &v, &v, NULL, NULL, W, W, W, NULL, NULL, 0, NULL, NULL) == want);
+  }
+
+  /* beam selection and reordering */
+  EXPECT(rdf2v_beam_select(F, INT64_MAX, RDF2V_F32, FF, NULL, 2, 3, 100, 4, WF, WI, WI, NULL, 0, NULL, NULL) ==
+         RDF2V_ERR_TOO_LARGE);
+  EXPECT(rdf2v_beam_select(F, INT64_MIN, RDF2V_F32, FF, NULL, 2, 3, 100, 4, WF, WI, WI, NULL, 0, NULL, NULL) ==
+         RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_beam_select(F, 100, RDF2V_F32, FF, NULL, 2, 3, 100, 4, WF, WI, WI, NULL, 0, NULL, NULL) ==
+         RDF2V_ERR_WORKSPACE);
+  EXPECT(rdf2v_beam_reorder(F, INT64_MAX, INT64_MAX, FI, 1, W, NULL, NULL) == RDF2V_ERR_TOO_LARGE);
+  EXPECT(rdf2v_beam_reorder(F, 1, INT64_MAX, FI, 1, W, NULL, NULL) == RDF2V_ERR_TOO_LARGE);
+  EXPECT(rdf2v_beam_reorder(F, 1, INT64_MIN, FI, 1, W, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_beam_reorder(F, 4, 64, FI, 4, (char *)F + 255, NULL, NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+
+  /* distillation */
+  EXPECT(rdf2v_distill_loss(F, INT64_MAX, RDF2V_F32, FI, FF, 8, 100, 4, 1.0f, WF, WF, NULL, NULL, 0, NULL, 0, NULL,
+                            NULL) == RDF2V_ERR_TOO_LARGE);
+  EXPECT(rdf2v_distill_loss(F, 100, RDF2V_F32, FI, FF, INT64_MIN, 100, 4, 1.0f, WF, WF, NULL, NULL, 0, NULL, 0, NULL,
+                            NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_distill_loss(F, (int64_t)1 << 30, RDF2V_F32, FI, FF, 8, (int64_t)1 << 30, 4, 1.0f, WF, WF, NULL, NULL,
+                            0, NULL, 0, NULL, NULL) == RDF2V_ERR_WORKSPACE);
+  EXPECT(rdf2v_distill_loss_backward(F, 100, RDF2V_F32, FI, FF, 8, 100, 4, 1.0f, FF, FF, W, INT64_MIN, NULL, 0, NULL,
+                                     NULL) == RDF2V_ERR_INVALID_ARGUMENT);
+  EXPECT(rdf2v_distill_loss_backward(F, 100, RDF2V_F32, FI, FF, 8, 100, 4, 1.0f, FF, FF, W, INT64_MAX, NULL, 0, NULL,
+                                     NULL) == RDF2V_ERR_TOO_LARGE);
+  return sink;
+}
+
 int main(void) {
   const int64_t big64[] = {0, 1, 4095, 4096, 4097, (int64_t)1 << 30, ((int64_t)1 << 31) - 1, (int64_t)1 << 31,
                            (int64_t)1 << 40, INT64_MAX, -1, INT64_MIN};
@@ -105,6 +186,8 @@ int main(void) {
                                 NULL) == RDF2V_ERR_INVALID_ARGUMENT);
   EXPECT(rdf2v_build_vocabulary(C, O, 10, C, O, 10, C, O, 10, 5, 10, 10, FI, FI, FI, counts, NULL, 0, NULL,
                                 NULL) == RDF2V_ERR_WORKSPACE);
+
+  sink += model_entries(big64, n64, big32, n32);
 
   for (int s = -1; s < 7; ++s) EXPECT(rdf2v_status_string(s) != NULL);
   printf("abi sanitize: ok (%zu)\n", sink % 7);
