@@ -456,8 +456,11 @@ rdf2v_status rdf2v_build_vocabulary(const uint8_t *subj_chars, const int64_t *su
  * sequence mixer (linear attention with a decay for each head), its loss
  * (distillation from a teacher's top logits) and its answers' search (beam
  * selection). Their arguments follow the conventions above; floating arrays
- * hold RDF2V_F32 or RDF2V_BF16 values, and everything in between is held in 32
- * bits.
+ * hold RDF2V_F32 or RDF2V_BF16 values. Sums, states and statistics are held in
+ * 32 bits. With RDF2V_BF16, decay attention over whole rows multiplies tokens
+ * with states, and values with the weights of their pairs of tokens, taken to 16
+ * bits: an output is off by up to 2^-15 of the sum of its terms' absolute values
+ * before it is rounded. The step takes them as they are.
  */
 typedef enum rdf2v_dtype {
   RDF2V_F32 = 0,

@@ -103,14 +103,14 @@ struct Vec<bf16> {
   typedef bf16x4 four;
   typedef bf16x8 eight;
   typedef bf16x8 load;  // 16 bytes
-  // Operands of the matrix products that are computed values. The weights of a
-  // chunk's pairs are fed as two bfloat16 pieces (16 bits). A state that earlier
-  // chunks have left is held in float32 and rounded once to be an operand: the
-  // outputs' error is then up to 1.4 times that of their own rounding; with two
-  // pieces it would be 1.0 times, and the scan take 1.05 times as long. What is
-  // added to a state keeps 24 bits, as three pieces, where the state is an
-  // output in float32, and 16 where only bfloat16 outputs are made of it.
-  static constexpr int kPieces = 2, kOperand = 1, kStatePieces = 3;
+  // Operands of the matrix products that are computed values: the weights of a chunk's pairs, and a float32
+  // state that tokens are multiplied with, are fed as two bfloat16 pieces, 16 bits, each off by at most 2^-16
+  // of itself. The outputs' error is then that of their own rounding, 1.66e-3 in the 2-norm for random inputs
+  // (one piece for the states: 2.05e-3, and far more where a state's large values cancel). Of four rows of
+  // 4,096 x 16 heads of 128, forward and backward, the states take 438, 458 and 485 us with one, two and three
+  // pieces; three for weights and states 576. What is added to a state keeps 24 bits, as three pieces, where
+  // the state is an output in float32, and 16 where only bfloat16 outputs are made of it.
+  static constexpr int kPieces = 2, kOperand = 2, kStatePieces = 3;
 };
 template <>
 struct Vec<float> {

@@ -360,3 +360,27 @@ def test_gradients_of_shared_heads_beyond_a_row():
         beyond = torch.arange(length, device=device()) >= x["lens"][:, None]
         for name, want in zip(("dq", "dk", "dv"), ref):
             assert torch.equal(outs[name], want) and bool((outs[name][beyond] == 0).all()), (length, type_, name)
+
+
+@pytest.mark.parametrize("size", [(4, 1, 2, 2, 32, 32), (2, 1, 2, 1, 64, 128), (3, 40, 2, 2, 32, 16),
+                                  (2, 70, 2, 1, 64, 64), (1, 700, 2, 2, 128, 128)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_states_that_cancel_in_bfloat16(size):
+    """States of 100 and a little, and tokens whose neighbouring values cancel: what is left of a state's
+    product is the little. States, and the weights of pairs, are operands of 16 bits (2^-16 each, of terms
+    that are disjoint), and a state may also be a sum of such terms: 2^-15 of the terms' absolute values,
+    beside float32's roundings and the result's own to bfloat16."""
+    say(f"[attention] states that cancel {size}")
+    x = _inputs(*size, BF16, 67, False, True)
+    for name in ("q", "k", "v", "dout"):
+        y = x[name].unflatten(-1, (-1, 2))
+        x[name] = torch.stack((y[..., 0], -y[..., 0]), -1).flatten(-2)
+    for name in ("state", "dstate_out"):
+        x[name] = x[name] + 100.0
+    x["log_decay"] = x["log_decay"] * 0.01
+    ref, sizes = _reference(x, size[4] ** -0.5)
+    b = attention_bounds(ref, sizes, F32, size[2] // size[3])
+    for name in b:
+        if "state" not in name:
+            b[name] = b[name] + 1.01 * 2.0 ** -15 * sizes[name] + 1.01 * UBF16 * ref[name].abs()
+    _check(_run(x), ref, b, f"cancel {size}")
