@@ -7,9 +7,10 @@
 // so the choice does not depend on the order of the work.
 //
 // Totals are rounded sums, so logits that differ can have equal totals, of
-// which the lowest token counts. The last entry of a slice bounds the totals of
-// what the slice left out: only where that bound reaches the last chosen total
-// is the beam's row read again and its best found by total.
+// which the lowest token counts. The last entry of a slice is the best of what
+// the slice left out: only where it or a smaller logit reaches the last chosen
+// total, and could win by its token, is the beam's row read again and its best
+// found by total.
 
 #include "logits.hpp"
 
@@ -330,7 +331,7 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p,
       if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
     }
     const float bound = block_bound<kMergeWaves>(head, p.num_out, fscratch);
-    // Descending logits have descending totals; the last entry only bounds what was left out.
+    // Descending logits have descending totals; the last entry is left out.
     for (int e = threadIdx.x; e < lists * k; e += kMergeThreads) {
       const int l = e / k, b = l / int(slices);
       const uint64_t key = counts[b] && e - l * k < p.num_out ? keys[e] : 0;
@@ -407,16 +408,22 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p,
     }
     __syncthreads();
     if (round > 0) break;
-    // Whether something that a slice left out could belong to the chosen: its logit is below the
-    // slice's last entry, or equal to it with a higher token, which loses to that entry.
+    // Whether something that a slice left out, or its last entry, could belong to the chosen. The slice has
+    // num_out entries of no smaller totals, so only at the last chosen total, and by a lower token than one of
+    // those has. Of the last entry's logit the lowest tokens are taken first, so then either a greater logit
+    // has the same total and a higher token, or a smaller logit the same total and any token.
     const uint64_t worst = chosen[p.num_out - 1];
-    const float least = worst != 0 ? key_value(worst) : -kInf;
+    const float least = worst != 0 ? key_value(worst) : kInf;  // fewer than num_out: nothing was left out
     for (int l = l0; l < lists; l += kMergeThreads) {
       const int b = l / int(slices);
       const uint64_t key = counts[b] ? keys[l * k + p.num_out] : 0;
-      if (key == 0) continue;
-      const float t = total_of(b, previous<T>(key_value(key)));
-      if (t >= least && t > -kInf) {
+      if (worst == 0 || key == 0 || !(total_of(b, key_value(key)) >= least)) continue;
+      bool look = total_of(b, previous<T>(key_value(key))) >= least;
+      for (int i = 0; i < p.num_out && !look; ++i) {
+        const uint64_t entry = keys[l * k + i];
+        look = key_index(entry) > key_index(key) && total_of(b, key_value(entry)) == least;
+      }
+      if (look) {
         again[b] = 1;
         any_again = 1;
       }

@@ -295,3 +295,84 @@ def test_more_entries_than_stay_on_the_chip(size, type_):
     logits, scores = _inputs(groups, beams, vocab, type_, 12)
     _check(logits, scores, num_out)
     _check(logits, scores * 0.0, num_out)
+
+
+def _totals(logits, scores):
+    """The totals that the definition gives in float32, on the CPU. The log-sum-exp is the kernel's own: a
+    token of logit 0 has at score 0 the total 0 + (0 - lse), which is exact. Every row has one, token 2,
+    among its 64 best."""
+    groups, beams, vocab = logits.shape
+    rows = logits.reshape(-1, 1, vocab)
+    got, tokens, _ = rd.rdf2v_beam_select(rows, torch.zeros(rows.shape[0], 1, device=device()), min(64, vocab))
+    lse = -got[tokens == 2].view(groups, beams, 1).cpu()
+    return scores.cpu()[..., None] + (logits.float().cpu() - lse)
+
+
+def _check_places(logits, scores, num_out):
+    want = _totals(logits, scores)
+    groups, beams, vocab = want.shape
+    got, tokens, parents = rd.rdf2v_beam_select(logits, scores, num_out)
+    first = torch.arange(groups)[:, None] * beams
+    best = want.flatten(1).sort(dim=1, descending=True, stable=True)
+    place = (parents.cpu() - first).long() * vocab + tokens.cpu()
+    wrong = (place != best.indices[:, :num_out]).any(1)
+    assert torch.equal(got.cpu(), best.values[:, :num_out])
+    assert not bool(wrong.any()), f"{int(wrong.sum())} of {groups} groups"
+
+
+def test_ties_of_neighbouring_logits():
+    """Logits whose totals are equal though they differ: the lowest token is chosen, be it the one that a
+    slice left out. Two examples, in which the next smaller float has a smaller total."""
+    say("[beam] ties of neighbouring logits: examples")
+    for score, row in ((-65.54468536376953, [-5.0, 3.113436222076416, -5.0, 3.1134371757507324]),
+                       (-6.0, [1.0000001192092896, 1.000000238418579])):
+        logits, scores = torch.tensor([[row]], device=device()), torch.tensor([[score]], device=device())
+        at = sorted(range(len(row)), key=lambda i: -row[i])[:2]
+        # the kernel's log-sum-exp, by a difference that is exact: the two are within a factor of two
+        lse = logits[0, 0, at[0]] - rd.rdf2v_beam_select(logits, scores * 0.0, 1)[0][0, 0]
+        total = (scores[0] + (logits[0, 0] - lse)).tolist()
+        below = float(scores + (torch.nextafter(logits[0, 0, at[1]], scores[0] - 9.0) - lse))
+        assert total[at[0]] == total[at[1]] > below
+        _, tokens, _ = rd.rdf2v_beam_select(logits, scores, 1)
+        assert tokens[0].tolist() == [min(at)]
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("num_out", [1, 2, 3, 7])
+@pytest.mark.parametrize("vocab", [13, 300])
+def test_ties_of_neighbouring_logits_over_many_values(vocab, num_out, type_):
+    """Tokens a few units of the type apart, in random order, with scores of any size."""
+    say(f"[beam] ties of neighbouring logits {vocab} {num_out} {type_}")
+    g = torch.Generator().manual_seed(vocab * 8 + num_out)
+    groups, unit = 4_000, 2.0 ** (-23 if type_ == F32 else -7)
+    for beams in (1, 3):
+        base = torch.rand(groups, 1, 1, generator=g) * 3 + 0.25
+        steps = torch.randint(0, 12, (groups, beams, vocab), generator=g).float()
+        logits = (base.to(type_).float() + steps * unit * 2.0 ** base.log2().floor()).to(type_)
+        logits[..., 16:] -= 5.0                            # a few of them at the top
+        logits[..., 2] = 0.0
+        if vocab > 64:
+            logits[..., 64:] -= 9.0                        # the logit of 0 is among the 64 best
+        scores = torch.rand(groups, 1, generator=g) * 8.0
+        scores = -torch.exp2(scores if type_ == F32 else scores + 13.0).expand(-1, beams).contiguous()
+        _check_places(logits.to(device()), scores.to(device()), num_out)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [9_000, 40_003, 150_001])
+def test_ties_across_slices(vocab, type_):
+    """The tied tokens lie all over a row of many slices, its last values among them, and there are more of
+    them than are chosen."""
+    say(f"[beam] ties across slices {vocab} {type_}")
+    unit = 2.0 ** (-23 if type_ == F32 else -7)
+    for seed in range(12):
+        g = torch.Generator().manual_seed(vocab + seed)
+        logits = torch.randn(4, 2, vocab, generator=g) - 8.0
+        for i in range(8):
+            n = (3, 20, 200, 3_000)[i % 4]
+            at = torch.cat((torch.randperm(vocab, generator=g)[:n], vocab - 1 - torch.arange(seed % 3)))
+            logits[i // 2, i % 2, at] = -1.0 - torch.randint(0, 16, (len(at),), generator=g) * unit
+        logits[..., 2] = 0.0
+        scores = -torch.exp2(torch.rand(4, 1, generator=g) * 8.0 + (0.0 if type_ == F32 else 13.0))
+        for num_out in (1, 2, 8, 64):
+            _check_places(logits.to(type_).to(device()), scores.expand(-1, 2).contiguous().to(device()), num_out)
