@@ -231,7 +231,7 @@ def test_refusals():
 
 @pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("vocab", [300, 5_000, 40_000])
-def test_totals_that_round_together(vocab, type_):
+def test_totals_that_round_together_at_powers_of_two(vocab, type_):
     """Scores so low that many logits have the same total: the lowest tokens of it are chosen, wherever
     their logits stand. The totals here are exact to predict: scores are powers of two whose float32
     step is far above the logits' spread, or at it."""
