@@ -9,8 +9,10 @@
 // Totals are rounded sums, so logits that differ can have equal totals, of
 // which the lowest token counts. The last entry of a slice is the best of what
 // the slice left out: only where it or a smaller logit reaches the last chosen
-// total, and could win by its token, is the beam's row read again and its best
-// found by total.
+// total, and could win by its token, is the slice read again for the lowest
+// tokens at that total.
+
+#include <climits>
 
 #include "logits.hpp"
 
@@ -23,11 +25,15 @@ constexpr int kVectors = 8;                    // 16-byte loads of a thread: 32 
 constexpr int kSlice = kVectors * kThreads;    // vectors of a slice
 constexpr int kList = 1024;                    // candidates of a slice that are ranked at once
 
+// Values in their order as unsigned numbers; that of -inf is below kLowest.
+constexpr uint32_t kLowest = 0x00800000u;
+__device__ __forceinline__ uint32_t order(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);  // -0 becomes +0
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
 // Descending (value, -index) as one unsigned number: larger is better, 0 is none.
 __device__ __forceinline__ uint64_t order_key(float x, uint32_t index) {
-  const uint32_t b = __float_as_uint(x + 0.0f);  // -0 becomes +0
-  const uint32_t o = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return uint64_t(o) << 32 | (0xffffffffu - index);
+  return uint64_t(order(x)) << 32 | (0xffffffffu - index);
 }
 __device__ __forceinline__ float key_value(uint64_t key) {
   const uint32_t o = uint32_t(key >> 32);
@@ -47,19 +53,46 @@ __device__ __forceinline__ V block_reduce(V x, V *scratch, Op op) {
   for (int i = 1; i < W; ++i) x = op(x, scratch[i]);
   return x;
 }
-template <int W = kWaves>
-__device__ __forceinline__ uint64_t block_max_key(uint64_t x, uint64_t *scratch) {
-  return block_reduce<W>(x, scratch, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+template <int W>
+__device__ __forceinline__ int block_sum(int x, int *scratch) {
+  return block_reduce<W>(x, scratch, [](int a, int b) { return a + b; });
+}
+
+// The largest number of [lo, hi] that reach(number) holds for, and the smallest. reach falls (rises) once. The
+// largest is often lo.
+template <class Reach>
+__device__ __forceinline__ uint32_t largest(uint32_t lo, uint32_t hi, Reach reach) {
+  if (lo < hi && !reach(lo + 1)) return lo;
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo - 1) / 2 + 1;
+    if (reach(mid))
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+template <class Reach>
+__device__ __forceinline__ uint32_t smallest(uint32_t lo, uint32_t hi, Reach reach) {
+  while (lo < hi) {
+    const uint32_t mid = lo + (hi - lo) / 2;
+    if (reach(mid))
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  return lo;
 }
 
 // A bound that at least k of the values that the threads' maxima x come from
-// reach: in each of the W waves the k / W-th of its lanes' distinct maxima, and the
-// least of those. -inf where the values are fewer. One barrier pair.
+// reach: in each of the W waves the k / W-th of its lanes' maxima, and the least of
+// those. -inf where the values are fewer. One barrier pair.
 template <int W = kWaves>
 __device__ __forceinline__ float block_bound(float x, int k, float *scratch) {
   float at = kInf;
-  for (int i = 0; i < (k + W - 1) / W; ++i) {
+  for (int left = (k + W - 1) / W; left > 0;) {
     at = wave_max(x);
+    left -= __popcll(__ballot(x == at));  // lanes of one maximum at once: where all are equal it is the bound
     if (x == at) x = -kInf;
   }
   __syncthreads();
@@ -115,8 +148,8 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64_t first) {
   constexpr int kPer = Row<T>::kPer;
   __shared__ float scratch[2 * kWaves];
-  __shared__ uint64_t list[kList], kscratch[kWaves];
-  __shared__ int count;
+  __shared__ uint64_t list[kList];
+  __shared__ int count, cscratch[kWaves];
   const int64_t block = first + blockIdx.x, row = block / p.slices, slice = block % p.slices;
   if (!row_counts(p, row)) return;
   const T *z = static_cast<const T *>(p.logits) + row * p.stride;
@@ -133,9 +166,10 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) x[i] = Row<T>::load(z, end, v0 + i * kThreads);
   }
-  // the values after the last vector, one to a thread of the first slice
+  // the values after the last vector, one to a thread of the last slice
   const int64_t rest_at = whole * kPer + threadIdx.x;
-  float rest = slice == 0 && rest_at < p.vocab ? to_f32(z[rest_at]) : -kInf;
+  const bool has_rest = slice == p.slices - 1 && rest_at < p.vocab;
+  float rest = has_rest ? to_f32(z[rest_at]) : -kInf;
   // Values are made from the words anew in each pass: kept, they would take the registers of other waves.
   auto each = [&](auto take) {
     if (whole > 0) {
@@ -205,26 +239,60 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(SelectArgs p, int64
     rank_list(list, n, k, [&](int rank, uint64_t key) { best[rank] = key; });
     return;
   }
-  // more ties at the bound than the list holds: one by one, from memory
-  uint64_t last = ~uint64_t(0);
-  for (int r = 0; r < k; ++r) {
-    uint64_t key = 0;
-    auto offer = [&](int64_t j) {
-      const float y = usable(to_f32(z[j]));
-      const uint64_t c = y > -kInf ? order_key(y, uint32_t(j)) : 0;
-      if (c < last && c > key) key = c;
+  // More at the bound than the list holds, as where all logits are equal: the k-th value by halving, then of
+  // that value as many tokens as are needed, in ascending order. The slice is read again for it: more code over
+  // the registers would take them from the other waves.
+  auto again = [&](auto take) {
+#pragma unroll 1
+    for (int64_t v = v0; v < end; v += kThreads) {
+      const Words w = Row<T>::load(z, end, v);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) take(usable(Row<T>::value(w, j)), uint32_t(v * kPer + j));
+    }
+    take(usable(rest), uint32_t(rest_at));
+  };
+  auto at_least = [&](uint32_t value) {
+    int c = 0;
+    again([&](float y, uint32_t) { c += order(y) >= value; });
+    return block_sum<kWaves>(c, cscratch);
+  };
+  const uint32_t most = order(fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3])));
+  const uint32_t value = largest(max(order(bound), kLowest), most, [&](uint32_t v) { return at_least(v) >= k; });
+  int need = k - (value < most ? at_least(value + 1) : 0);
+  uint32_t token = 0;
+#pragma unroll 1
+  for (int64_t step = begin;; step += kThreads) {
+    const bool last = step + kThreads >= end;
+    const Words w = Row<T>::load(z, end, step + threadIdx.x);
+    auto up_to = [&](uint32_t t) {
+      int c = last && order(usable(rest)) == value && uint32_t(rest_at) <= t;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        c += order(usable(Row<T>::value(w, j))) == value && uint32_t((step + threadIdx.x) * kPer + j) <= t;
+      return block_sum<kWaves>(c, cscratch);
     };
-    for (int64_t j = begin * kPer + threadIdx.x; j < end * kPer; j += kThreads) offer(j);
-    if (slice == 0 && rest_at < p.vocab) offer(rest_at);
-    last = block_max_key(key, kscratch);
-    if (threadIdx.x == 0) best[r] = last;
+    const int here = up_to(0xffffffffu);
+    if (here < need && !last) {
+      need -= here;
+      continue;
+    }
+    token = smallest(uint32_t(step * kPer), uint32_t(last ? p.vocab - 1 : (step + kThreads) * kPer - 1),
+                     [&](uint32_t t) { return up_to(t) >= need; });
+    break;
   }
+  if (threadIdx.x == 0) count = 0;
+  __syncthreads();
+  again([&](float y, uint32_t index) {
+    if (order(y) > value || (order(y) == value && index <= token)) list[atomicAdd(&count, 1)] = order_key(y, index);
+  });
+  __syncthreads();
+  rank_list(list, k, k, [&](int rank, uint64_t key) { best[rank] = key; });
 }
 
 constexpr int kOwn = 2;        // parts of a wave that are read ahead
 constexpr int kStaged = 5120;  // entries of all lists that LDS takes
-// Candidates of the merge that are ranked at once: all of them where there are fewer lists than places to fill.
-constexpr int kMergeList = RDF2V_MAX_BEAMS * (RDF2V_MAX_BEAMS + 1);
+// Candidates of the merge that are ranked at once, which takes as many steps as their square.
+constexpr int kMergeList = 768;
 
 // The next value of the element type below x, which is one.
 template <class T>
@@ -247,14 +315,15 @@ constexpr int kMergeWaves = kMergeThreads / kWave;
 template <class T>
 __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p, int64_t first) {
   __shared__ float lse[RDF2V_MAX_BEAMS], score[RDF2V_MAX_BEAMS];
-  __shared__ uint8_t counts[RDF2V_MAX_BEAMS], ended[RDF2V_MAX_BEAMS], again[RDF2V_MAX_BEAMS];
+  __shared__ uint8_t counts[RDF2V_MAX_BEAMS], ended[RDF2V_MAX_BEAMS];
   __shared__ float fscratch[kMergeWaves];
   __shared__ uint64_t kscratch[kMergeWaves];
   __shared__ uint64_t list[kMergeList], stage[kStaged];
   __shared__ uint32_t place[kMergeList];
   __shared__ uint64_t chosen[RDF2V_MAX_BEAMS];
   __shared__ uint32_t chosen_place[RDF2V_MAX_BEAMS];
-  __shared__ int count, any_again;
+  __shared__ uint32_t tied[kMergeWaves][RDF2V_MAX_BEAMS];
+  __shared__ int count, cscratch[kMergeWaves], tied_count[kMergeWaves];
   const int64_t group = first + blockIdx.x, row0 = group * p.beams;
   const int k = p.num_out + 1;
   const int64_t slices = p.slices;
@@ -286,7 +355,6 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p,
     score[threadIdx.x] = x;
     counts[threadIdx.x] = x > -kInf && !end;
     ended[threadIdx.x] = x > -kInf && end;
-    again[threadIdx.x] = 0;
   }
   __syncthreads();
   for (int b = wave, o = 0; b < p.beams; b += kMergeWaves, ++o) {
@@ -319,140 +387,175 @@ __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p,
   // the total of a beam's logit, in the order of the definition
   auto total_of = [&](int b, float x) { return score[b] + (x - lse[b]); };
   // candidates are compared by total, then by beam and token: (total, beam) is unique up to the token
-  for (int round = 0;; ++round) {
-    if (threadIdx.x == 0) count = any_again = 0;
-    // after a second look the lists are those in memory
-    const uint64_t *keys = staged && round == 0 ? stage : source;
-    // the lists' first entries: num_out of them bound the last chosen total
-    float head = -kInf;
-    for (int l = l0; l < lists; l += kMergeThreads) {
-      const int b = l / int(slices);
-      const uint64_t key = counts[b] ? keys[l * k] : 0;
-      if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
+  // a wave ranks one candidate of n at a time, its lanes a candidate each to set against it
+  auto rank_one = [&](int i, int n) {
+    const uint64_t key = list[i];
+    const uint32_t at = place[i];
+    int rank = 0;
+    for (int j = lane; j - lane < n; j += kWave) {
+      const uint64_t other = j < n ? list[j] : 0;
+      const uint32_t there = j < n ? place[j] : 0;
+      rank += __popcll(__ballot(other > key || (other == key && there < at)));
     }
-    const float bound = block_bound<kMergeWaves>(head, p.num_out, fscratch);
-    // Descending logits have descending totals; the last entry is left out.
-    for (int e = threadIdx.x; e < lists * k; e += kMergeThreads) {
-      const int l = e / k, b = l / int(slices);
-      const uint64_t key = counts[b] && e - l * k < p.num_out ? keys[e] : 0;
-      const float t = total_of(b, key_value(key));
-      if (key == 0 || !(t >= bound) || t == -kInf) continue;
-      const int at = atomicAdd(&count, 1);
-      if (at < kMergeList) {
-        list[at] = order_key(t, uint32_t(b) << 26);
-        place[at] = key_index(key);
-      }
+    if (lane == 0 && rank < p.num_out && key != 0) {
+      chosen[rank] = key;
+      chosen_place[rank] = at;
     }
+  };
+  if (threadIdx.x == 0) count = 0;
+  const uint64_t *keys = staged ? stage : source;
+  // the lists' first entries: num_out of them bound the last chosen total
+  float head = -kInf;
+  for (int l = l0; l < lists; l += kMergeThreads) {
+    const int b = l / int(slices);
+    const uint64_t key = counts[b] ? keys[l * k] : 0;
+    if (key != 0) head = fmaxf(head, total_of(b, key_value(key)));
+  }
+  const float bound = block_bound<kMergeWaves>(head, p.num_out, fscratch);
+  // take(total, list, beam, token, 1 for a beam that has ended) for this thread's candidates of the first
+  // `entries`. Descending logits have descending totals; the last entry of a list is left out.
+  auto one = [&](int e, auto take) {
+    const int l = e / k, b = l / int(slices);
+    const uint64_t key = counts[b] && e - l * k < p.num_out ? keys[e] : 0;
+    const float t = total_of(b, key_value(key));
+    if (key != 0 && t >= bound && t > -kInf) take(t, l, b, key_index(key), 0u);
+  };
+  auto each = [&](int entries, auto take, int most = INT_MAX) {
+    for (int e = threadIdx.x; e < entries && *static_cast<volatile int *>(&count) <= most; e += kMergeThreads) one(e, take);
     for (int b = threadIdx.x; b < p.beams; b += kMergeThreads)
-      if (ended[b]) {
-        const int at = atomicAdd(&count, 1);
-        if (at < kMergeList) {
-          list[at] = order_key(score[b], uint32_t(b) << 26 | 1u);
-          place[at] = 0;
-        }
-      }
+      if (ended[b]) take(score[b], 0, b, 0u, 1u);
+  };
+  auto put = [&](float t, int, int b, uint32_t token, uint32_t end) {
+    const int at = atomicAdd(&count, 1);
+    if (at < kMergeList) {
+      list[at] = order_key(t, uint32_t(b) << 26 | end);
+      place[at] = token;
+    }
+  };
+  each(lists * k, put, kMergeList);
+  __syncthreads();
+  int n = count;
+  if (n > kMergeList) {
+    // More at the bound than the list holds: the last total by halving, then of that total the first lists that
+    // have enough, since a list's tokens are all lower than the next one's. Those are less than a step's entries
+    // and a list too many, and fit.
+    auto at_least = [&](uint32_t value) {
+      int c = 0;
+      each(lists * k, [&](float t, int, int, uint32_t, uint32_t) { c += order(t) >= value; });
+      return block_sum<kMergeWaves>(c, cscratch);
+    };
+    uint32_t most = order(head);
+    if (int(threadIdx.x) < p.beams && ended[threadIdx.x]) most = max(most, order(score[threadIdx.x]));
+    most = block_reduce<kMergeWaves>(most, reinterpret_cast<uint32_t *>(cscratch), [](uint32_t a, uint32_t b) { return max(a, b); });
+    const uint32_t value =
+        largest(max(order(bound), kLowest), most, [&](uint32_t v) { return at_least(v) >= p.num_out; });
+    int need = p.num_out - (value < most ? at_least(value + 1) : 0), upto = lists - 1;
+    for (int step = 0; step < lists * k && need > 0; step += kMergeThreads) {
+      int c = 0;
+      if (step + int(threadIdx.x) < lists * k)
+        one(step + threadIdx.x, [&](float t, int, int, uint32_t, uint32_t) { c = order(t) == value; });
+      need -= block_sum<kMergeWaves>(c, cscratch);
+      upto = min(lists - 1, (step + kMergeThreads - 1) / k);
+    }
+    if (threadIdx.x == 0) count = 0;
     __syncthreads();
-    const int n = count;
-    if (n <= kMergeList) {
-      // a wave ranks one candidate at a time, its lanes a candidate each to set against it
-      for (int i = wave; i < n; i += kMergeWaves) {
-        const uint64_t key = list[i];
-        const uint32_t at = place[i];
-        int rank = 0;
-        for (int j = lane; j - lane < n; j += kWave) {
-          const uint64_t other = j < n ? list[j] : 0;
-          const uint32_t there = j < n ? place[j] : 0;
-          rank += __popcll(__ballot(other > key || (other == key && there < at)));
-        }
-        if (lane == 0 && rank < p.num_out) {
-          chosen[rank] = key;
-          chosen_place[rank] = at;
-        }
-      }
-      for (int i = n + threadIdx.x; i < p.num_out; i += kMergeThreads) chosen[i] = 0;
-    } else {
-      // one by one, from the lists
-      uint64_t last = ~uint64_t(0);
-      uint32_t last_place = 0;
-      for (int r = 0; r < p.num_out; ++r) {
-        uint64_t key = 0;
-        uint32_t at = 0xffffffffu;
-        auto offer = [&](uint64_t c, uint32_t token) {
-          const bool below = c < last || (c == last && token > last_place);
-          if (below && (c > key || (c == key && token < at))) {
-            key = c;
-            at = token;
+    each(value < most ? lists * k : (upto + 1) * k, [&](float t, int l, int b, uint32_t token, uint32_t end) {
+      if (order(t) > value || (order(t) == value && l <= upto)) put(t, l, b, token, end);
+    });
+    __syncthreads();
+    n = count;
+  }
+  for (int i = wave; i < n; i += kMergeWaves) rank_one(i, n);
+  for (int i = n + threadIdx.x; i < p.num_out; i += kMergeThreads) chosen[i] = 0;
+  __syncthreads();
+
+  // Whether something that a slice left out, its last entry among it, could belong to the chosen. The slice has
+  // num_out entries of no smaller totals, so only at the last chosen total, and by a lower token than one of
+  // those has. Of the last entry's logit the lowest tokens are taken first, so then either a greater logit
+  // has the same total and a higher token, or a smaller logit the same total and any token.
+  const uint64_t worst = chosen[p.num_out - 1];
+  const float least = worst != 0 ? key_value(worst) : kInf;  // fewer than num_out: nothing was left out
+  auto look_again = [&](int l) {
+    const int b = l / int(slices);
+    const uint64_t key = counts[b] ? keys[l * k + p.num_out] : 0;
+    if (key == 0 || !(total_of(b, key_value(key)) >= least)) return false;
+    bool look = total_of(b, previous<T>(key_value(key))) >= least;
+    for (int i = 0; i < p.num_out && !look; ++i) {
+      const uint64_t entry = keys[l * k + i];
+      look = key_index(entry) > key_index(key) && total_of(b, key_value(entry)) == least;
+    }
+    return look;
+  };
+  // Such slices are read again, in ascending order of beam and token, until they have given as many tokens at
+  // the last chosen total as it has places: what they give beyond is worse. Each gives one at least, its last
+  // entry, so few are read, be all logits equal. One of 100,050 float32 zeros takes 3 us more.
+  int places = RDF2V_MAX_BEAMS, found = 0;
+  if (worst != 0) {
+    for (int base = 0; base < lists && found < places; base += kMergeThreads) {
+      const int mine = base + int(threadIdx.x);
+      const bool look = mine < lists && look_again(mine);
+      if (!__syncthreads_or(look)) continue;
+      places = 0;
+      for (int i = 0; i < p.num_out; ++i) places += chosen[i] >> 32 == worst >> 32;
+      const uint64_t looks = __ballot(look);
+      if (lane == 0) kscratch[wave] = looks;
+      __syncthreads();
+      for (int w = 0; w < kMergeWaves && found < places; ++w) {
+        for (uint64_t left = kscratch[w]; left != 0 && found < places; left &= left - 1) {
+          const int l = base + w * kWave + __builtin_ctzll(left), b = l / int(slices);
+          const int64_t s = l - int64_t(b) * slices;
+          constexpr int kPer = Row<T>::kPer, kAhead = 8;
+          const int64_t whole = p.vocab / kPer, per = (whole + slices - 1) / slices;
+          const int64_t begin = min(whole, s * per) * kPer;
+          const int64_t end = s == slices - 1 ? p.vocab : min(whole, (s + 1) * per) * kPer;
+          // a wave takes an eighth of the slice, in order
+          const int64_t part = (end - begin + kMergeWaves - 1) / kMergeWaves;
+          const int64_t lo = min(end, begin + wave * part), hi = min(end, lo + part);
+          const T *z = static_cast<const T *>(p.logits) + (row0 + b) * p.stride;
+          int n = 0;
+          for (int64_t j0 = lo; j0 < hi && n < places; j0 += kAhead * kWave) {
+            float x[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) x[i] = to_f32(z[min(j0 + i * kWave + lane, hi - 1)]);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+              const int64_t j = j0 + i * kWave + lane;
+              const bool is = j < hi && total_of(b, usable(x[i])) == least;
+              const uint64_t all = __ballot(is);
+              const int at = n + __popcll(all & ((uint64_t(1) << lane) - 1));
+              if (is && at < places) tied[wave][at] = uint32_t(j);
+              n += __popcll(all);
+            }
           }
-        };
-        for (int l = threadIdx.x; l < lists; l += kMergeThreads) {
-          const int b = l / int(slices);
-          if (!counts[b]) continue;
-          for (int i = 0; i < p.num_out; ++i) {
-            const uint64_t c = keys[l * k + i];
-            if (c == 0) break;
-            const float t = total_of(b, key_value(c));
-            if (t > -kInf) offer(order_key(t, uint32_t(b) << 26), key_index(c));
+          if (lane == 0) tied_count[wave] = min(n, places);
+          __syncthreads();
+          int before = found;
+          for (int i = 0; i < wave; ++i) before += tied_count[i];
+          if (lane < tied_count[wave] && before + lane < places) {
+            list[p.num_out + before + lane] = order_key(least, uint32_t(b) << 26);
+            place[p.num_out + before + lane] = tied[wave][lane];
           }
-        }
-        for (int b = threadIdx.x; b < p.beams; b += kMergeThreads)
-          if (ended[b]) offer(order_key(score[b], uint32_t(b) << 26 | 1u), 0);
-        const uint64_t top = block_max_key<kMergeWaves>(key, kscratch);
-        const uint64_t low = block_max_key<kMergeWaves>(key == top && top != 0 ? uint64_t(0xffffffffu - at) + 1 : 0, kscratch);
-        last = top;
-        last_place = low == 0 ? 0 : 0xffffffffu - uint32_t(low - 1);
-        if (threadIdx.x == 0) {
-          chosen[r] = last;
-          chosen_place[r] = last_place;
+          for (int i = 0; i < kMergeWaves; ++i) found += tied_count[i];
+          found = min(found, places);
+          __syncthreads();
         }
       }
     }
-    __syncthreads();
-    if (round > 0) break;
-    // Whether something that a slice left out, or its last entry, could belong to the chosen. The slice has
-    // num_out entries of no smaller totals, so only at the last chosen total, and by a lower token than one of
-    // those has. Of the last entry's logit the lowest tokens are taken first, so then either a greater logit
-    // has the same total and a higher token, or a smaller logit the same total and any token.
-    const uint64_t worst = chosen[p.num_out - 1];
-    const float least = worst != 0 ? key_value(worst) : kInf;  // fewer than num_out: nothing was left out
-    for (int l = l0; l < lists; l += kMergeThreads) {
-      const int b = l / int(slices);
-      const uint64_t key = counts[b] ? keys[l * k + p.num_out] : 0;
-      if (worst == 0 || key == 0 || !(total_of(b, key_value(key)) >= least)) continue;
-      bool look = total_of(b, previous<T>(key_value(key))) >= least;
-      for (int i = 0; i < p.num_out && !look; ++i) {
-        const uint64_t entry = keys[l * k + i];
-        look = key_index(entry) > key_index(key) && total_of(b, key_value(entry)) == least;
-      }
-      if (look) {
-        again[b] = 1;
-        any_again = 1;
-      }
+  }
+  if (found > 0) {
+    // the chosen and the found, one of each
+    const int n = p.num_out + found;
+    for (int i = threadIdx.x; i < p.num_out; i += kMergeThreads) {
+      list[i] = chosen[i];
+      place[i] = chosen_place[i];
     }
     __syncthreads();
-    if (!any_again) break;
-    // such beams' best by total, from the whole row, in place of their lists
-    for (int b = 0; b < p.beams; ++b) {
-      if (!again[b]) continue;
-      const int64_t row = row0 + b;
-      const T *z = static_cast<const T *>(p.logits) + row * p.stride;
-      uint64_t last = ~uint64_t(0);
-      for (int r = 0; r < p.num_out; ++r) {
-        uint64_t key = 0;
-        float x_of = 0.0f;
-        for (int64_t j = threadIdx.x; j < p.vocab; j += kMergeThreads) {
-          const float x = usable(to_f32(z[j])), t = total_of(b, x);
-          const uint64_t c = x > -kInf && t > -kInf ? order_key(t, uint32_t(j)) : 0;
-          if (c < last && c > key) {
-            key = c;
-            x_of = x;
-          }
-        }
-        last = block_max_key<kMergeWaves>(key, kscratch);
-        if (last != 0 && key == last) p.best[row * slices * k + r] = order_key(x_of, key_index(last));
-        if (last == 0 && threadIdx.x == 0) p.best[row * slices * k + r] = 0;
-      }
-      for (int64_t i = k + threadIdx.x; i < slices * k; i += kMergeThreads) p.best[row * slices * k + i] = 0;
+    for (int i = p.num_out + wave; i < n; i += kMergeWaves) {
+      const bool same = lane < p.num_out && chosen[lane] == list[i] && chosen_place[lane] == place[i];
+      if (__ballot(same) != 0 && lane == 0) list[i] = 0;
     }
+    __syncthreads();
+    for (int i = wave; i < n; i += kMergeWaves) rank_one(i, n);
     __syncthreads();
   }
 

@@ -376,3 +376,22 @@ def test_ties_across_slices(vocab, type_):
         scores = -torch.exp2(torch.rand(4, 1, generator=g) * 8.0 + (0.0 if type_ == F32 else 13.0))
         for num_out in (1, 2, 8, 64):
             _check_places(logits.to(type_).to(device()), scores.expand(-1, 2).contiguous().to(device()), num_out)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("value", [0.0, -0.0, 1.0, -3.0e38])
+def test_equal_logits_everywhere(value, type_):
+    """What a model without training gives: the first tokens of the first beams, and before them a beam that
+    has ended. At -3e38 the vocabulary's logarithm is lost beside the logits in float32, as the definition has
+    it, and the living beam of score -6.5 stays before the ended one of -7."""
+    say(f"[beam] all logits {value} {type_}")
+    for vocab in (70, 20_001, 1_000_200):
+        logits = torch.full((2, 3, vocab), value, device=device(), dtype=type_)
+        scores = torch.tensor([[-7.0, -7.0, -7.0], [-9.0, -6.5, -7.0]], device=device())
+        finished = torch.tensor([[0, 0, 0], [0, 0, 1]], dtype=torch.int32, device=device())
+        for k in (1, 7, 64):
+            got, tokens, parents = rd.rdf2v_beam_select(logits, scores, k, finished=finished)
+            assert tokens[0].tolist() == list(range(k)) and parents[0].tolist() == [0] * k
+            ended = [] if value < -1.0e38 else [-1]
+            assert tokens[1].tolist() == ended + list(range(k - len(ended)))
+            assert parents[1].tolist() == [5] * len(ended) + [4] * (k - len(ended))
