@@ -649,6 +649,8 @@ size_t rdf2v_distill_workspace_size(int64_t rows, int64_t vocab, int32_t top, in
  *   loss = tau^2 * sum_k p_k (log p_k - log q[id_k])
  *   dlogits[j] = dloss * tau * (q[j] - sum of the p_k with id_k = j)
  *
+ * p is that of the differences of the t_k, wherever they lie; log q is z / tau
+ * less the row's lse in float32, off by up to 2^-24 of the two's size.
  * An entry whose id is negative, or whose t_k is -inf, is absent; a row without
  * entries (padding after a walk's end) has loss 0, lse 0 and gradient 0, and
  * its logits are not read. Logits of -inf have q = 0; a row of nothing else has

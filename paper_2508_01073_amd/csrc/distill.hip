@@ -38,11 +38,14 @@ struct Workspace {
   int64_t slices;
 };
 
-// A row's teacher entries: every wave computes their log-sum-exp for itself;
-// `each(k, id, t / tau)` is called by one lane of the calling wave for each.
+// A row's teacher entries: every wave computes their log-sum-exp for itself, as
+// the largest and the logarithm of the sum over it: their sum would lose the
+// latter, and the entries' differences, beside large logits. `each(k, id, t)` is
+// called by one lane of the calling wave for each.
 struct Teacher {
-  float lse;
+  float most, log_sum, inv_tau;
   bool valid;
+  __device__ __forceinline__ float log_p(float t) const { return fmaf(t - most, inv_tau, -log_sum); }
 };
 template <class Each>
 __device__ __forceinline__ Teacher read_teacher(const DistillArgs &a, int64_t row, float inv_tau, bool report,
@@ -51,7 +54,7 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs &a, int64_t ro
   bool any = false;
   for (int k = lane_id(); k < a.top; k += kWave) {
     int32_t id = a.ids[row * a.top + k];
-    const float t = a.teacher[row * a.top + k] * inv_tau;
+    const float t = a.teacher[row * a.top + k];
     if (int64_t(id) >= a.vocab) {
       if (report && a.status != nullptr) atomicOr(a.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
       id = -1;
@@ -61,12 +64,12 @@ __device__ __forceinline__ Teacher read_teacher(const DistillArgs &a, int64_t ro
     if (id < 0) continue;
     any = true;
     const float up = fmaxf(most, t);
-    sum = sum * (most == -kInf ? 0.0f : expf(most - up)) + expf(t - up);
+    sum = sum * (most == -kInf ? 0.0f : expf((most - up) * inv_tau)) + expf((t - up) * inv_tau);
     most = up;
   }
   const float top = wave_max(most);
-  sum = wave_sum(any ? sum * expf(most - top) : 0.0f);
-  return {top + logf(sum), __ballot(any) != 0};
+  sum = wave_sum(any ? sum * expf((most - top) * inv_tau) : 0.0f);
+  return {top, logf(sum), inv_tau, __ballot(any) != 0};
 }
 
 // Calls take(words, i, whether the vector is there) for the vectors of this thread.
@@ -155,16 +158,16 @@ __device__ __forceinline__ float log_sum(float2 x) { return x.x == -kInf && x.y 
 
 // What row_loss and the gradient at the ids read; ids that count are not negative.
 struct Entries {
-  const float *t, *zk;  // over tau
+  const float *t, *zk;  // zk is over tau
   const int32_t *id;
 };
 
 // The loss of a row, by one wave.
-__device__ __forceinline__ float row_loss(const DistillArgs &a, const Entries &e, float lse_t, float lse) {
+__device__ __forceinline__ float row_loss(const DistillArgs &a, const Entries &e, const Teacher &teacher, float lse) {
   float loss = 0.0f;
   for (int k = lane_id(); k < a.top; k += kWave) {
     if (e.id[k] < 0) continue;
-    const float log_p = e.t[k] - lse_t;
+    const float log_p = teacher.log_p(e.t[k]);
     loss += expf(log_p) * (log_p - (e.zk[k] == -kInf ? -kInf : e.zk[k] - lse));
   }
   return a.temperature * a.temperature * wave_sum(loss);
@@ -173,13 +176,13 @@ __device__ __forceinline__ float row_loss(const DistillArgs &a, const Entries &e
 // The gradient at the ids in [lo, hi).
 template <class T, int THREADS>
 __device__ __forceinline__ void store_entries(const DistillArgs &a, const Entries &e, T *dz, int64_t lo, int64_t hi,
-                                              float lse_t, float lse, float w) {
+                                              const Teacher &teacher, float lse, float w) {
   for (int k = threadIdx.x; k < a.top; k += THREADS) {
     const int32_t id = e.id[k];
     if (id < 0 || id < lo || id >= hi) continue;
     float p = 0.0f;
     for (int m = 0; m < a.top; ++m)
-      if (e.id[m] == id) p += expf(e.t[m] - lse_t);
+      if (e.id[m] == id) p += expf(teacher.log_p(e.t[m]));
     dz[id] = from_f32<T>(w * (__builtin_amdgcn_exp2f((e.zk[k] - lse) * kLog2e) - p));
   }
 }
@@ -215,7 +218,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
   if (a.loss != nullptr) {
     lse = log_sum(block_fold<THREADS>(slice.fold(0, whole, inv_tau), scratch));
     if (first_wave) {
-      const float loss = row_loss(a, {t, zk, id}, teacher.lse, lse);
+      const float loss = row_loss(a, {t, zk, id}, teacher, lse);
       if (threadIdx.x == 0) {
         a.loss[row] = loss;
         a.lse[row] = lse;
@@ -229,7 +232,7 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a, int
   const float w = a.dloss[row] * a.temperature, from = lse == -kInf ? 0.0f : lse;  // all masked: q = 0
   slice.store(dz, 0, whole, rest_at, a.vocab, inv_tau, from, w);
   __syncthreads();
-  store_entries<T, THREADS>(a, {t, zk, id}, dz, 0, a.vocab, teacher.lse, from, w);
+  store_entries<T, THREADS>(a, {t, zk, id}, dz, 0, a.vocab, teacher, from, w);
 }
 
 // One workgroup to a slice of a long row: its part of the log-sum-exp, and with
@@ -300,7 +303,7 @@ __global__ __launch_bounds__(kSliceThreads) void distill_grad_kernel(DistillArgs
     const float most = wave_max(x.x);
     lse = log_sum(make_float2(most, wave_sum(x.y * (x.x == most ? 1.0f : expf(x.x - most)))));
     if (at == 0 && first_wave) {
-      const float loss = row_loss(a, {t, zk, id}, teacher.lse, lse);
+      const float loss = row_loss(a, {t, zk, id}, teacher, lse);
       if (threadIdx.x == 0) {
         a.loss[row] = loss;
         a.lse[row] = lse;
@@ -314,8 +317,8 @@ __global__ __launch_bounds__(kSliceThreads) void distill_grad_kernel(DistillArgs
   slice.store(dz, begin, end, rest_at, a.vocab, inv_tau, from, w);
   __syncthreads();
   const Entries e{t, zk, id};
-  store_entries<T, kSliceThreads>(a, e, dz, begin * Row<T>::kPer, end * Row<T>::kPer, teacher.lse, from, w);
-  if (at == 0) store_entries<T, kSliceThreads>(a, e, dz, whole * Row<T>::kPer, a.vocab, teacher.lse, from, w);
+  store_entries<T, kSliceThreads>(a, e, dz, begin * Row<T>::kPer, end * Row<T>::kPer, teacher, from, w);
+  if (at == 0) store_entries<T, kSliceThreads>(a, e, dz, whole * Row<T>::kPer, a.vocab, teacher, from, w);
 }
 
 int64_t row_vectors(int64_t vocab, int32_t dtype) { return vocab / (dtype == RDF2V_BF16 ? 8 : 4); }

@@ -226,3 +226,28 @@ def test_refusals():
     big = torch.zeros(4, 60, device=device())
     with pytest.raises(rd.Rdf2vError):                     # overlapping, and not element by element
         call(big[:, :50], ids, t, dloss=d, dlogits=big[:, 5:55])
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("vocab", [600, 9_000, 120_000])
+def test_teachers_far_from_zero(vocab, tau):
+    """A teacher's distribution is that of its logits' differences, wherever they lie; entries that are all of
+    the type's lowest value weigh the same. The bounds are those of logits whose largest is 0, for their
+    differences are exact or rounded once."""
+    say(f"[distill] teachers far from zero, vocabulary of {vocab}, temperature {tau}")
+    z, ids, t, d = _inputs(8, vocab, 40, F32, 9)
+    low = torch.finfo(F32).min
+    for i, offset in enumerate((3.0e4, -3.0e4, 1.0e6, -1.0e6, 1.0e30, low, low, 0.0)):
+        t[i] += offset
+    t[6] = low
+    t[7, 3:] = low                                         # three entries and masked ones
+    loss, lse, grad = rd.rdf2v_distill_loss(z, ids, t, temperature=tau, dloss=d)
+    alone = rd.rdf2v_distill_loss_backward(z, ids, t, rd.rdf2v_distill_loss(z, ids, t, temperature=tau)[1], d,
+                                           temperature=tau)
+    ref = distill(z, ids, t, tau, d.cpu())
+    there = torch.where(ids >= 0, t.double(), -math.inf)
+    shift = (t.double() - there.amax(1, keepdim=True)).clamp(min=-1.0e3)    # beyond, an entry weighs nothing
+    bl, be, bg = _bounds(z, torch.where((ids >= 0) & (shift > -1.0e3), shift, 0.0), tau, *ref, d, F32)
+    assert _near(loss, ref[0], bl), (loss.double().cpu() - ref[0]).abs() / bl
+    assert _near(lse, ref[1], be)
+    assert _near(grad, ref[2], bg) and _near(alone, ref[2], bg)
