@@ -167,8 +167,12 @@ __device__ __forceinline__ float row_loss(const DistillArgs &a, const Entries &e
   float loss = 0.0f;
   for (int k = lane_id(); k < a.top; k += kWave) {
     if (e.id[k] < 0) continue;
-    const float log_p = teacher.log_p(e.t[k]);
-    loss += expf(log_p) * (log_p - (e.zk[k] == -kInf ? -kInf : e.zk[k] - lse));
+    const float log_p = teacher.log_p(e.t[k]), p = expf(log_p);
+    // a p that is too small for float32 is not 0: nothing times a number, infinite where q is 0
+    if (p == 0.0f)
+      loss += e.zk[k] == -kInf ? kInf : 0.0f;
+    else
+      loss += p * (log_p - (e.zk[k] == -kInf ? -kInf : e.zk[k] - lse));
   }
   return a.temperature * a.temperature * wave_sum(loss);
 }

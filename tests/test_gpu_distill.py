@@ -251,3 +251,23 @@ def test_teachers_far_from_zero(vocab, tau):
     assert _near(loss, ref[0], bl), (loss.double().cpu() - ref[0]).abs() / bl
     assert _near(lse, ref[1], be)
     assert _near(grad, ref[2], bg) and _near(alone, ref[2], bg)
+
+
+@pytest.mark.parametrize("vocab", [600, 9_000, 120_000])
+def test_entries_of_hardly_any_weight(vocab):
+    """An entry whose weight is too small for float32 adds nothing, and infinity where its token's q is 0."""
+    say(f"[distill] entries of hardly any weight, vocabulary of {vocab}")
+    z, ids, t, d = _inputs(6, vocab, 5, F32, 10)
+    ids[:] = torch.tensor([3, 5, 7, 11, vocab - 1], dtype=torch.int32)
+    t[:, 1] = -130.0                                       # exp(-130) is below float32's smallest
+    t[:, 2] = -500.0
+    z[1, 5] = -math.inf
+    z[2, 7] = -math.inf
+    z[3, 3] = -math.inf
+    t[4, 2], z[4, 7] = torch.finfo(F32).min, -300.0
+    z[5] = -math.inf
+    loss, lse, grad = _check(z, ids, t, d, 1.0)
+    assert [i for i in range(6) if float(loss[i]) == math.inf] == [1, 2, 3, 5]
+    assert not bool(torch.isnan(grad).any())
+    z[4, 7] = -math.inf                                    # beyond what 64 bits say: the same rule
+    assert float(rd.rdf2v_distill_loss(z, ids, t)[0][4]) == math.inf
