@@ -527,7 +527,8 @@ size_t rdf2v_decay_attention_backward_workspace_size(const rdf2v_attention *a);
  *   status_dev  device int32 or NULL (RDF2V_STATUS_BAD_VALUE,
  *               RDF2V_STATUS_BAD_LENGTH).
  *
- * Outputs may not overlap inputs, but for state_out. The same inputs give the
+ * Outputs may not overlap inputs or one another, but for state_out over state
+ * (RDF2V_ERR_INVALID_ARGUMENT; so too in the gradients). The same inputs give the
  * same bits on every call. A NaN or infinity in a token below L reaches, beyond
  * the outputs of the formula, those of up to 63 tokens before it, whose weights
  * for it are zeros.

@@ -4,6 +4,8 @@
 
 #include <climits>
 #include <cmath>
+#include <initializer_list>
+#include <utility>
 
 #include "model.hpp"
 
@@ -65,6 +67,82 @@ bool overlap(const void *a, size_t an, const void *b, size_t bn) {
   return x <= y ? y - x < an : x - y < bn;
 }
 
+// An array of a call: where it lies, of how many bytes. Null or empty: it overlaps nothing.
+struct Span {
+  const void *data;
+  size_t bytes;
+};
+bool overlap(const Span &a, const Span &b) {
+  return a.data != nullptr && b.data != nullptr && a.bytes != 0 && b.bytes != 0 &&
+         overlap(a.data, a.bytes, b.data, b.bytes);
+}
+bool same(const Span &a, const Span &b) { return a.data == b.data; }
+
+// The bytes of a view as boxes inside boxes: count[i] boxes every step[i] bytes, those of the last level
+// `bytes` long.
+struct Boxes {
+  __int128 step[3];
+  int64_t count[3];
+  __int128 bytes;
+};
+
+// Whether boxes of the levels from `level` on, the first of them at byte `at`, have a byte in [lo, hi).
+bool boxes_reach(const Boxes &x, int level, __int128 at, __int128 lo, __int128 hi) {
+  if (level == 3) return at < hi && at + x.bytes > lo;
+  if (x.count[level] == 1) return boxes_reach(x, level + 1, at, lo, hi);
+  __int128 size = x.bytes;  // from a box's first byte to its last
+  for (int i = level + 1; i < 3; ++i) size += x.step[i] * (x.count[i] - 1);
+  const __int128 all = size + x.step[level] * (x.count[level] - 1);
+  if (at >= hi || at + all <= lo) return false;
+  if (x.step[level] < size) return true;  // the boxes lie in one another: taken as one
+  // Of the boxes that reach into the interval all but the first and the last lie in it.
+  const __int128 first = at >= lo ? 0 : (lo - at) / x.step[level];
+  __int128 last = (hi - 1 - at) / x.step[level];
+  if (last > x.count[level] - 1) last = x.count[level] - 1;
+  if (last - first > 1) return true;
+  for (__int128 i = first; i <= last; ++i)
+    if (boxes_reach(x, level + 1, at + i * x.step[level], lo, hi)) return true;
+  return false;
+}
+
+// Whether a view of rows x tokens x heads of `size` values has a byte in an array. What lies between a view's
+// values is not its own: another slice of the projection, say.
+bool overlap(const rdf2v_heads_view &v, const rdf2v_attention &a, int heads, int size, const Span &out) {
+  if (out.data == nullptr || out.bytes == 0 || a.rows == 0 || a.length == 0) return false;
+  const int64_t value = int64_t(dtype_size(a.dtype));
+  const int64_t strides[3] = {v.row_stride, v.token_stride, v.head_stride}, counts[3] = {a.rows, a.length, heads};
+  Boxes x{};
+  x.bytes = __int128(size) * value;
+  __int128 at = __int128(reinterpret_cast<uintptr_t>(v.data));
+  for (int i = 0; i < 3; ++i) {
+    const __int128 step = __int128(strides[i]) * value;
+    if (step < 0) at += step * (counts[i] - 1);  // from the lowest byte upwards
+    x.step[i] = step < 0 ? -step : step;
+    x.count[i] = step == 0 ? 1 : counts[i];
+    if (x.count[i] == 1) x.step[i] = 0;
+  }
+  for (int i = 0; i < 2; ++i)  // the widest first
+    for (int j = 0; j < 2 - i; ++j)
+      if (x.step[j] < x.step[j + 1]) {
+        std::swap(x.step[j], x.step[j + 1]);
+        std::swap(x.count[j], x.count[j + 1]);
+      }
+  const __int128 lo = __int128(reinterpret_cast<uintptr_t>(out.data));
+  return boxes_reach(x, 0, at, lo, lo + __int128(out.bytes));
+}
+
+size_t state_bytes(const rdf2v_attention &a) { return size_t(a.rows) * a.heads * a.dk * a.dv * 4; }
+size_t head_bytes(const rdf2v_attention &a, int heads, int size) {
+  return size_t(a.rows) * a.length * heads * size * dtype_size(a.dtype);
+}
+
+// Whether a view has a byte in one of the outputs.
+bool reads(const rdf2v_heads_view &v, const rdf2v_attention &a, int heads, int size, std::initializer_list<Span> outs) {
+  for (const Span &out : outs)
+    if (overlap(v, a, heads, size, out)) return true;
+  return false;
+}
+
 }  // namespace
 
 RDF2V_API size_t rdf2v_decay_attention_workspace_size(const rdf2v_attention *a) {
@@ -90,6 +168,12 @@ RDF2V_API rdf2v_status rdf2v_decay_attention(const rdf2v_attention *a, const rdf
   st = check_workspace(workspace, workspace_bytes, rdf2v::decay_attention_workspace_bytes(*a, false));
   if (st != RDF2V_OK) return st;
   if (a->rows == 0) return RDF2V_OK;
+  const size_t states = state_bytes(*a);
+  const Span o = {out, head_bytes(*a, a->heads, a->dv)}, s = {state, states}, so = {state_out, states};
+  if (overlap(o, s) || overlap(o, so) || (overlap(s, so) && !same(s, so))) return RDF2V_ERR_INVALID_ARGUMENT;
+  if (reads(*q, *a, a->heads, a->dk, {o, so}) || reads(*k, *a, a->kv_heads, a->dk, {o, so}) ||
+      reads(*v, *a, a->kv_heads, a->dv, {o, so}))
+    return RDF2V_ERR_INVALID_ARGUMENT;
   return rdf2v::launch_decay_attention(*a, *q, *k, *v, state, out, state_out, workspace, status_dev,
                                        static_cast<hipStream_t>(stream));
 }
@@ -114,6 +198,18 @@ RDF2V_API rdf2v_status rdf2v_decay_attention_backward(const rdf2v_attention *a, 
   st = check_workspace(workspace, workspace_bytes, rdf2v::decay_attention_workspace_bytes(*a, true));
   if (st != RDF2V_OK) return st;
   if (a->rows == 0) return RDF2V_OK;
+  const size_t states = state_bytes(*a);
+  const Span s = {state, states}, dso = {dstate_out, states}, ds = {dstate, states},
+             gq = {dq, head_bytes(*a, a->heads, a->dk)}, gk = {dk, head_bytes(*a, a->kv_heads, a->dk)},
+             gv = {dv, head_bytes(*a, a->kv_heads, a->dv)};
+  if (overlap(gq, gk) || overlap(gq, gv) || overlap(gk, gv) || overlap(ds, s) ||
+      (overlap(ds, dso) && !same(ds, dso)))
+    return RDF2V_ERR_INVALID_ARGUMENT;
+  for (const Span *g : {&gq, &gk, &gv})
+    if (overlap(*g, s) || overlap(*g, dso) || overlap(*g, ds)) return RDF2V_ERR_INVALID_ARGUMENT;
+  if (reads(*q, *a, a->heads, a->dk, {gq, gk, gv, ds}) || reads(*k, *a, a->kv_heads, a->dk, {gq, gk, gv, ds}) ||
+      reads(*v, *a, a->kv_heads, a->dv, {gq, gk, gv, ds}) || reads(*dout, *a, a->heads, a->dv, {gq, gk, gv, ds}))
+    return RDF2V_ERR_INVALID_ARGUMENT;
   return rdf2v::launch_decay_attention_backward(*a, *q, *k, *v, *dout, state, dstate_out, dq, dk, dv, dstate,
                                                 workspace, status_dev, static_cast<hipStream_t>(stream));
 }

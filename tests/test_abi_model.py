@@ -183,3 +183,57 @@ def test_attention_of_no_rows(lib, length):
         for ws, wsb in ((WS, 1 << 40), (None, 0)):
             assert so.rdf2v_decay_attention_backward(c, v, v, v, v, None, None, FAKE, FAKE, FAKE, None, ws, wsb, None,
                                                      None) == pkg.RDF2V_OK
+
+
+def test_attention_refuses_overlaps(lib):
+    """Outputs over inputs or over one another, by as little as a value: rows x tokens x heads of 4 x 10 x 4
+    queries of 16 values and 4 x 10 x 2 keys and values of 16 and 24, float32, at places of their own."""
+    so, pkg = lib
+    inv = pkg.RDF2V_ERR_INVALID_ARGUMENT
+    sizes = dict(q=4 * 10 * 4 * 16 * 4, k=4 * 10 * 2 * 16 * 4, v=4 * 10 * 2 * 24 * 4, out=4 * 10 * 4 * 24 * 4,
+                 state=4 * 4 * 16 * 24 * 4)
+    places = {n: FAKE + (i << 24) for i, n in enumerate(
+        ("q", "k", "v", "dout", "out", "state", "state_out", "dstate_out", "dq", "dk", "dv", "dstate"))}
+    size = lambda n: sizes["out" if n == "dout" else "state" if "state" in n else n[-1] if n != "out" else n]  # noqa: E731
+
+    def forward(**moved):
+        at = dict(places, **moved)
+        views = [_view(pkg, at[n], *s) for n, s in (("q", (640, 64, 16)), ("k", (320, 32, 16)), ("v", (480, 48, 24)))]
+        return so.rdf2v_decay_attention(_attention(pkg), *views, at["state"], at["out"], at["state_out"], WS, 1 << 40,
+                                        None, None)
+
+    def backward(**moved):
+        at = dict(places, **moved)
+        views = [_view(pkg, at[n], *s) for n, s in (("q", (640, 64, 16)), ("k", (320, 32, 16)), ("v", (480, 48, 24)),
+                                                    ("dout", (960, 96, 24)))]
+        return so.rdf2v_decay_attention_backward(_attention(pkg), *views, at["state"], at["dstate_out"], at["dq"],
+                                                 at["dk"], at["dv"], at["dstate"], WS, 1 << 40, None, None)
+
+    for call, outs, ins in ((forward, ("out", "state_out"), ("q", "k", "v", "state")),
+                            (backward, ("dq", "dk", "dv", "dstate"), ("q", "k", "v", "dout", "state", "dstate_out"))):
+        for i, x in enumerate(outs):
+            for y in outs[:i] + ins:
+                for step in (4, size(y) // 8 * 4, size(y) - 4, 4 - size(x)):
+                    assert call(**{x: places[y] + step}) == inv, (x, y, step)
+                if (x, y) not in (("state_out", "state"), ("dstate", "dstate_out")):
+                    assert call(**{x: places[y]}) == inv, (x, y)
+
+
+def test_attention_refuses_overlaps_with_strided_inputs(lib):
+    """An output within the values of an input of any strides is refused: heads before tokens, negative
+    strides, keys shared by all rows, tokens far apart."""
+    so, pkg = lib
+    at = FAKE + (1 << 30)
+
+    def call(view, out):
+        far = _view(pkg, FAKE + (1 << 38))
+        return so.rdf2v_decay_attention(_attention(pkg, heads=2, kv_heads=2), view, far, far, None, out, None, WS,
+                                        1 << 40, None, None)
+
+    size = 4 * 10 * 2 * 24 * 4                                        # of the output
+    for row, token, head in ((2 * 10 * 16, 16, 160), (-320, 32, 16), (320, -32, -16), (0, 32, 16), (16, 64, 1 << 20),
+                             (1 << 20, 1 << 22, 1 << 18), (1, 2, 3)):
+        for r, t, h in ((0, 0, 0), (3, 9, 1), (1, 5, 1), (2, 0, 0)):
+            value = at + 4 * (r * row + t * token + h * head)
+            for out in (value, value + 60, value - size + 4):         # the first or last value of a head
+                assert call(_view(pkg, at, row, token, head), out) == pkg.RDF2V_ERR_INVALID_ARGUMENT, (row, token, head)

@@ -384,3 +384,22 @@ def test_states_that_cancel_in_bfloat16(size):
         if "state" not in name:
             b[name] = b[name] + 1.01 * 2.0 ** -15 * sizes[name] + 1.01 * UBF16 * ref[name].abs()
     _check(_run(x), ref, b, f"cancel {size}")
+
+
+def test_outputs_between_an_inputs_rows():
+    """An output that lies between the rows of an input shares nothing with it."""
+    say("[attention] outputs between the rows of an input")
+    x = _inputs(2, 20, 2, 2, 16, 16, F32, 71)
+    a, _ = rd.rdf2v_decay_attention(x["q"], x["k"], x["v"], x["log_decay"])
+    whole = torch.full((4096,), math.nan, device=device())
+    q = whole.as_strided((2, 20, 2, 16), (2048, 32, 16, 1))            # 640 values at 0 and at 2048
+    q.copy_(x["q"])
+    out = whole[640:640 + 1280].view(2, 20, 2, 16)
+    got, _ = rd.rdf2v_decay_attention(q, x["k"], x["v"], x["log_decay"], out=out)
+    assert got is out and torch.equal(out, a) and torch.equal(q, x["q"])
+    with pytest.raises(rd.Rdf2vError):
+        rd.rdf2v_decay_attention(q, x["k"], x["v"], x["log_decay"], out=whole[800:800 + 1280].view(2, 20, 2, 16))
+    with pytest.raises(rd.Rdf2vError):
+        rd.rdf2v_decay_attention(x["q"], x["k"], x["v"], x["log_decay"], out=x["v"])
+    with pytest.raises(rd.Rdf2vError):
+        rd.rdf2v_decay_attention_backward(x["q"], x["k"], x["v"], x["log_decay"], x["dout"], dk=x["k"])
