@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 from dataclasses import dataclass
 
 import torch
@@ -747,6 +748,46 @@ class _Attention:
                                   dk ** -0.5 if scale is None else scale, log_decay.data_ptr(), _ptr(lens))
 
 
+def _records(*tensors) -> bool:
+    """Whether autograd records what is done with any of these (None: not there)."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+    return False
+
+
+def _no_gradient(call: str, names: str) -> None:
+    """Said where a gradient is asked for that a call does not compute."""
+    warnings.warn(f"{call} computes no gradient for {names}: autograd does not record it. Detach it, or call under "
+                  "torch.no_grad()", stacklevel=3)
+
+
+class _DecayAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, state, scale, lens, want_state, workspace, status, stream):
+        out, state_out = rdf2v_decay_attention(q, k, v, log_decay, scale=scale, lens=lens, state=state,
+                                               want_state=want_state, workspace=workspace, status=status, stream=stream)
+        ctx.save_for_backward(q, k, v, log_decay, state, lens)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return (out, state_out) if want_state else out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dstate_out=None):
+        q, k, v, log_decay, state, lens = ctx.saved_tensors
+        if dout is None:                                   # the states alone were used
+            dout = q.new_zeros((*q.shape[:-1], v.shape[-1]))
+        elif dout.stride(-1) != 1:
+            dout = dout.contiguous()
+        if dstate_out is not None:
+            dstate_out = dstate_out.contiguous()
+        dq, dk, dv, dstate = rdf2v_decay_attention_backward(q, k, v, log_decay, dout, scale=ctx.scale, lens=lens,
+                                                            state=state, dstate_out=dstate_out)
+        return dq, dk, dv, None, dstate, None, None, None, None, None, None
+
+
 def rdf2v_decay_attention_workspace_size(rows: int, length: int, heads: int, kv_heads: int, dk: int, dv: int,
                                          dtype: torch.dtype = torch.float32) -> int:
     c = _AttentionStruct(rows, length, heads, kv_heads, dk, dv, _DTYPES.get(dtype, -1), 1.0, None, None)
@@ -772,9 +813,20 @@ def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     value head h // (heads // kv_heads). log_decay: float32 [heads], <= 0. scale defaults to dk ** -0.5.
     lens: int32 [rows], the tokens of each row that count (as the walk calls return them). state: float32
     [rows, heads, dk, dv] to begin from. Returns (out [rows, length, heads, dv], state_out), state_out
-    being None unless it is given or want_state is set."""
+    being None unless it is given or want_state is set.
+
+    Where q, k, v or state requires gradients, autograd records the call; out and state_out must then be left
+    to it, as in torch's own functions."""
     a = _Attention(q, k, v, log_decay, scale, lens, 4)
     dev, c = a.dev, a.c
+    if _records(log_decay):
+        _no_gradient("rdf2v_decay_attention", "log_decay")
+    if _records(q, k, v, state):
+        if out is not None or state_out is not None:
+            raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
+                             "gradients")
+        got = _DecayAttention.apply(q, k, v, log_decay, state, scale, lens, want_state, workspace, status, stream)
+        return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
         shape = (c.rows, c.heads, c.dk, c.dv)
         if out is None:
@@ -850,7 +902,7 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
 
     With parents (int32, one per row), row r continues state parents[r], as rdf2v_beam_select numbers
     them, and state_out must not overlap state. Without, row r continues state r, and state is updated
-    in place unless state_out is given."""
+    in place unless state_out is given. For answering: autograd does not record it."""
     a = _Attention(q, k, v, log_decay, scale, None, 3)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
@@ -873,6 +925,8 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
         else:
             _state(state_out, "state_out", shape, dev)
         _status(status, dev)
+        if _records(q, k, v, log_decay, state):
+            _no_gradient("rdf2v_decay_attention_step", "its inputs")
         vq, vk, vv = a.views
         st = _native().rdf2v_decay_attention_step(ctypes.byref(c), vq, vk, vv, _ptr(state), num_states,
                                                   _ptr(parents), _ptr(out), _ptr(state_out), _ptr(status), h)
@@ -896,7 +950,7 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
     Returns (scores, tokens, parents), each [groups, num_out]: totals in descending order, ties to the
     lowest (beam, token); parents are row numbers group * beams + beam, as rdf2v_beam_reorder and
     rdf2v_decay_attention_step take them. Places without a candidate hold -inf, -1 and the group's first
-    row."""
+    row. For answering: autograd does not record it."""
     dtype = _float_dtype(logits, "logits")
     if logits.dim() != 3:
         raise ValueError("logits must have shape [groups, beams, vocab]")
@@ -918,6 +972,8 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
         parents = (torch.empty(shape, dtype=torch.int32, device=dev) if parents is None else
                    _exact(parents, "parents", torch.int32, shape, dev))
         _status(status, dev)
+        if _records(logits, scores):
+            _no_gradient("rdf2v_beam_select", "logits and scores")
         lib = _native()
         if workspace is None:
             need = lib.rdf2v_beam_select_workspace_size(groups, beams, vocab, num_out)
@@ -984,6 +1040,24 @@ def _teacher(logits, ids, teacher):
     return dtype, stride, dev
 
 
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, ids, teacher, temperature, workspace, status, stream):
+        loss, lse = rdf2v_distill_loss(logits, ids, teacher, temperature=temperature, workspace=workspace,
+                                       status=status, stream=stream)
+        ctx.save_for_backward(logits, ids, teacher, lse)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(lse)
+        return loss, lse
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, _):
+        logits, ids, teacher, lse = ctx.saved_tensors
+        grad = rdf2v_distill_loss_backward(logits, ids, teacher, lse, dloss.contiguous(), temperature=ctx.temperature)
+        return grad, None, None, None, None, None, None
+
+
 def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, *, temperature: float = 1.0,
                        dloss: torch.Tensor | None = None, loss: torch.Tensor | None = None,
                        lse: torch.Tensor | None = None, dlogits: torch.Tensor | None = None,
@@ -994,8 +1068,17 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
     logits [rows, vocab] float32 or bfloat16, rows contiguous; ids int32 [rows, top] (negative: absent)
     and teacher float32 [rows, top]. Returns (loss, lse), float32 [rows]; with dloss (float32 [rows], the
     gradient of loss) the gradient of the logits is computed in the same pass and (loss, lse, dlogits) is
-    returned. dlogits may be logits itself."""
+    returned. dlogits may be logits itself.
+
+    Where logits requires gradients and dloss is not given, autograd records loss (not lse); loss and lse must
+    then be left to the call, as in torch's own functions."""
     dtype, stride, dev = _teacher(logits, ids, teacher)
+    if _records(teacher):
+        _no_gradient("rdf2v_distill_loss", "teacher")
+    if dloss is None and dlogits is None and _records(logits):
+        if loss is not None or lse is not None:
+            raise ValueError("loss and lse cannot be given where autograd records the call: logits requires gradients")
+        return _DistillLoss.apply(logits, ids, teacher, temperature, workspace, status, stream)
     with _on_stream(dev, stream) as h:
         rows, vocab = logits.shape
         loss = torch.empty(rows, dtype=torch.float32, device=dev) if loss is None else \
