@@ -529,9 +529,8 @@ size_t rdf2v_decay_attention_backward_workspace_size(const rdf2v_attention *a);
  *
  * Outputs may not overlap inputs or one another, but for state_out over state
  * (RDF2V_ERR_INVALID_ARGUMENT; so too in the gradients). The same inputs give the
- * same bits on every call. A NaN or infinity in a token below L reaches, beyond
- * the outputs of the formula, those of up to 63 tokens before it, whose weights
- * for it are zeros.
+ * same bits on every call. A NaN or infinity in a token below L reaches what the
+ * sum over s <= t has it in, where an infinity may be NaN, and nothing else.
  */
 rdf2v_status rdf2v_decay_attention(const rdf2v_attention *a, const rdf2v_heads_view *q, const rdf2v_heads_view *k,
                                    const rdf2v_heads_view *v, const float *state, void *out, float *state_out,

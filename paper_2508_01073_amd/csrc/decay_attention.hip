@@ -161,6 +161,44 @@ __device__ __forceinline__ F take_piece(F &x, float) {
   return x;
 }
 
+// Values that are no numbers have to stay where the sum over w <= u has them: a weight of 0 does not take them
+// out of a matrix product. So columns with any are products without them, and NaN from the first of them on.
+template <class E>
+__device__ __forceinline__ bool any_odd(const E &x) {  // an exponent of ones, to which a one carries
+  constexpr bool kHalf = sizeof(x[0]) == 2;
+  constexpr unsigned kExponent = kHalf ? 0x7f807f80u : 0x7f800000u, kOne = kHalf ? 0x00800080u : 0x00800000u,
+                     kCarry = kHalf ? 0x80008000u : 0x80000000u;
+  typedef unsigned words __attribute__((ext_vector_type(sizeof(E) / 4)));
+  const words w = __builtin_bit_cast(words, x);
+  unsigned any = 0;
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(E) / 4; ++i) any |= (w[i] & kExponent) + kOne;
+  return (any & kCarry) != 0;
+}
+// Takes them out of x, whose value j is that of place(j); returns the least place that had one, or `first`.
+template <class E, class Place>
+__device__ __forceinline__ int take_odd(E &x, int first, Place place) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (__builtin_isfinite(to_f32(x[j]))) continue;
+    first = min(first, place(j));
+    x[j] = 0.0f;
+  }
+  return first;
+}
+// The least place of column l % 16 over the lane groups.
+__device__ __forceinline__ int least_odd(int first) {
+  first = min(first, __shfl_xor(first, 16, kWave));
+  return min(first, __shfl_xor(first, 32, kWave));
+}
+// Result o holds columns 4 g + r of token u; `first` is that of column l % 16. NaN where u is at or behind its
+// column's first.
+__device__ __forceinline__ void spread_odd(f32x4 &o, int first, int u, int g) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (u >= __shfl(first, 4 * g + r, kWave)) o[r] = __builtin_nanf("");
+}
+
 // A tile of rows of W values in LDS. In bfloat16 the groups of four values of a
 // row are permuted by the row: the 16-byte reads of 16 rows at one place, and
 // the transposing reads of four neighbouring groups of eight rows, then meet
@@ -511,7 +549,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int d = d3 + 3 - r;
-              w[r] *= d >= 0 ? p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma) : 0.0f;
+              const float y = w[r] * (p.pscale * __builtin_amdgcn_exp2f(float(d) * log2_gamma));
+              w[r] = d >= 0 ? y : 0.0f;
             }
           }
         }
@@ -618,6 +657,19 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
     if (OUT && whole(u0 + kChunk)) fetch(thread, u0 + kChunk, 0);
 
     if (OUT) {
+      // a column of c that has NaN or infinities has made its column of S one, where S was computed
+      bool odd = !last || exact_state ? !__builtin_isfinite(s[0][0][0]) : any_odd(cv[0][0]) || any_odd(cv[0][1]);
+      if (__builtin_expect(__ballot(odd) != 0, 0)) {
+#pragma unroll
+        for (int n = 0; n < kTilesN; ++n) {
+          int first = kChunk;
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) first = take_odd(cv[n][kk], first, [&](int j) { return 32 * kk + 8 * g + j; });
+          first = least_odd(first);
+#pragma unroll
+          for (int t = 0; t < kTilesT; ++t) spread_odd(o[t][n], first, (wt * kTilesT + t) * kTile + l16, g);
+        }
+      }
       const int64_t out_at = ((row * p.length + t0) * p.heads + h) * int64_t(p.dout);
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk)
@@ -731,6 +783,54 @@ __device__ __forceinline__ typename Vec<T>::eight short_column(const T *base, co
   return x;
 }
 
+// Columns of a short row whose c has NaN or infinities: the outputs before the first of them, which the matrix
+// products have made none, one by one.
+template <class T, class TokenOf>
+__device__ __forceinline__ void short_odd(const ScanArgs &p, const T *a, const T *b, const T *c, const float *s0,
+                                          int64_t out_at, int64_t out_step, int len, float log2_gamma,
+                                          TokenOf token_of) {
+  int lane = lane_id();
+  asm volatile("" : "+v"(lane));  // nothing of this is kept for it
+  const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1, e = p.reverse ? 0 : 1;
+#pragma unroll 1
+  for (int n0 = 0; n0 < p.dout; n0 += kWave) {
+    const bool there = n0 + lane < p.dout;
+    const int col = there ? n0 + lane : 0;
+    int first = len;
+#pragma unroll 1
+    for (int u = len - 1; u >= 0; --u)
+      if (!__builtin_isfinite(to_f32(c[token_of(u) * p.c.token + col]))) first = u;
+    const bool mends = there && first < len;
+#pragma unroll 1
+    for (int u = 0; __ballot(mends && u < first) != 0; ++u) {
+      const T *au = a + token_of(u) * p.a.token;
+      float o = 0.0f;
+#pragma unroll 1
+      for (int w = 0; w <= u; ++w) {
+        const T *bw = b + token_of(w) * p.b.token;
+        float x = 0.0f;
+        for (int i = lane; i < p.di; i += kWave) x += to_f32(au[i]) * to_f32(bw[i]);
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) x += __shfl_xor(x, off, kWave);
+        x *= p.pscale * __builtin_amdgcn_exp2f(float(u - w) * log2_gamma);
+        o += x * to_f32(c[token_of(w) * p.c.token + col]);
+      }
+      if (s0 != nullptr) {
+        float x = 0.0f;
+#pragma unroll 1
+        for (int k = 0; k < p.di; ++k) x += to_f32(au[k]) * s0[unsigned(k * per_k + col * per_col)];
+        o += x * p.oscale * __builtin_amdgcn_exp2f(float(u + e) * log2_gamma);
+      }
+      if (!mends || u >= first) continue;
+      const int64_t at = out_at + token_of(u) * out_step + col;
+      if (p.out_f32)
+        static_cast<float *>(p.out)[at] = o;
+      else
+        static_cast<T *>(p.out)[at] = from_f32<T>(o);
+    }
+  }
+}
+
 template <class T, int DI, int TT>
 __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_scan_kernel(ScanRoles roles,
                                                                                           int64_t items,
@@ -819,6 +919,7 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
     const int per_k = p.transposed ? 1 : p.dout, per_col = p.transposed ? p.di : 1;
     const int64_t out_step = int64_t(p.heads) * p.dout, out_at = (row * p.length * p.heads + h) * p.dout;
     const float whole = __builtin_amdgcn_exp2f(float(len) * log2_gamma);
+    bool odd = false;
     for (int n0 = 0; n0 < p.dout; n0 += kTile) {
       const int col = min(n0 + l16, p.dout - 1);  // columns beyond the last are not stored
       eight cv[kBlocks];
@@ -867,10 +968,16 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
           for (int i = 0; i < kPieces; ++i)  // of the last block an even tile has the lower half
             o[t] = 2 * kk == t ? mma_low(cv[kk], w[t][kk][i], o[t]) : mma(cv[kk], w[t][kk][i], o[t]);
         const int u = t * kTile + l16;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) odd |= !__builtin_isfinite(o[t][r]);
         if (u < len) store_four<T>(p, out_at + token_of(u) * out_step + n0 + 4 * g, n0 + 4 * g, o[t]);
       }
-      if (p.s1 == nullptr) continue;
-      // S at the row's end, a tile at a time; what it needs besides is made here, not kept
+    }
+    if (__builtin_expect(__ballot(odd) != 0, 0))
+      short_odd<T>(p, a, b, c, s0, out_at, out_step, len, log2_gamma, token_of);
+    // S at the row's end, a tile at a time; what it needs is made here, not kept
+    for (int n0 = 0; p.s1 != nullptr && n0 < p.dout; n0 += kTile) {
+      const int col = min(n0 + l16, p.dout - 1);  // columns beyond the last are not stored
       int g = lane / 16;
       asm volatile("" : "+v"(g));
       unsigned b_at[kBlocks][8];
@@ -884,11 +991,12 @@ __global__ __launch_bounds__(kShortWaves * kWave, TT <= 2 ? 6 : 4) void short_sc
 #pragma unroll
       for (int kk = 0; kk < kBlocks; ++kk) {
         if (kk >= blocks) break;
+        const eight cv = short_column(c, c_at[kk], unsigned(col) * unsigned(sizeof(T)));
         f32x8 x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int u = kk * 32 + 16 * (j / 4) + 4 * g + j % 4;
-          const float y = to_f32(cv[kk][j]) * p.sscale * __builtin_amdgcn_exp2f(float(len - e - u) * log2_gamma);
+          const float y = to_f32(cv[j]) * p.sscale * __builtin_amdgcn_exp2f(float(len - e - u) * log2_gamma);
           x[j] = u < len ? y : 0.0f;
         }
 #pragma unroll

@@ -403,3 +403,37 @@ def test_outputs_between_an_inputs_rows():
         rd.rdf2v_decay_attention(x["q"], x["k"], x["v"], x["log_decay"], out=x["v"])
     with pytest.raises(rd.Rdf2vError):
         rd.rdf2v_decay_attention_backward(x["q"], x["k"], x["v"], x["log_decay"], x["dout"], dk=x["k"])
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 12, 2, 1, 16, 24), (2, 31, 2, 2, 40, 33), (1, 48, 4, 2, 32, 64), (2, 70, 2, 1, 64, 20),
+                                  (1, 130, 2, 2, 128, 128), (1, 200, 1, 1, 24, 64), (1, 700, 2, 1, 64, 64)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_no_numbers_stay_where_the_formula_has_them(size, type_):
+    """A NaN or an infinity in a token: what the formula makes no number of it is none, and all the rest is
+    what it is with a zero there: earlier tokens' outputs, later tokens' gradients, other columns. The same
+    bits, or within the bounds where a short row's columns are done again."""
+    n, t, heads, kv, dk, dv = size
+    say(f"[attention] no numbers {size} {type_}")
+    for state in (False, True):
+        x = _inputs(*size, type_, 73, False, state)
+        places = sorted({0, t // 2, t - 1, min(63, t - 1), min(64, t - 1), min(17, t - 1)})
+        for i, name in enumerate(("q", "k", "v", "dout")):
+            for place in places:
+                for bad in (math.nan, math.inf) if place == t // 2 else ((math.nan, -math.inf)[place % 2],):
+                    y, z = dict(x), dict(x)
+                    y[name], z[name] = x[name].clone(), x[name].clone()
+                    at = (n - 1, place, (place + i) % x[name].shape[2], (3 * place + i) % x[name].shape[3])
+                    y[name][at], z[name][at] = bad, 0.0
+                    a, b = _run(y), _run(z)
+                    ref = attention(y["q"], y["k"], y["v"], y["log_decay"], dk ** -0.5, state=y["state"],
+                                    dout=y["dout"], dstate_out=y["dstate_out"])
+                    near = {out: a[out].cpu() == b[out].cpu() for out in a}
+                    if t <= 48:
+                        clean, sizes = _reference(z, dk ** -0.5)
+                        bounds = attention_bounds(clean, sizes, type_, heads // kv)
+                        near = {out: x | ((a[out].cpu() - clean[out]).abs() <= bounds[out]) for out, x in near.items()}
+                    for out in a:
+                        none = ~torch.isfinite(ref[out])
+                        assert torch.equal(~torch.isfinite(a[out]).cpu(), none), (name, place, bad, out)
+                        assert bool(near[out][~none].all()), (name, place, bad, out)
