@@ -1153,17 +1153,27 @@ void finish(ScanArgs &p, bool short_rows, int64_t segments) {
   p.wide_out = p.dout % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (p.out_f32 || sizeof(T) == 4 ? 15 : 7)) == 0;
 }
 
-// Whether a wave to a row and head is the faster way. us with a wave / with a
-// workgroup and chunks, 8 heads, 256 MB of q, k, v and out:
-//              tokens  sizes 32   64         128        sizes 32, states   64         128
-//   bfloat16   16      56 / 356   61 / 282   63 / 218   310 / 546          659 / 543  1388 / 646
-//              32      53 / 182   71 / 146   93 / 123   216 / 288          464 / 283   999 / 341
-//              33      75 / 178  104 / 153  105 / 119   273 / 295          492 / 305   909 / 358
-//              48      64 / 126  101 / 111  106 / 88    205 / 210          424 / 221   867 / 259
-//   float32    16      44 / 316   47 / 320   46 / 402   201 / 445          373 / 497   743 / 763
-//              32      48 / 165   50 / 180   56 / 221   157 / 235          276 / 293   465 / 413
-//              33      58 / 174   55 / 184   61 / 226   161 / 263          263 / 325   514 / 460
-//              48      51 / 126   54 / 136   55 / 166   141 / 192          255 / 236   422 / 330
+// Whether a wave to a row and head is the faster way. us with a wave / with a workgroup and chunks, forward and
+// the three gradients, 8 heads; many rows are 256 MB of q, k, v and out:
+//                      tokens  sizes 32             64                    128
+//   bfloat16           16      57/366  200/1055     61/282   214/830      64/250    234/731
+//                      33      69/181   227/539     76/153   244/463      75/136    246/396
+//                      48      57/127   207/377     84/112   238/346      89/101    242/287
+//   with states        16      284/538  587/1351    679/535  1079/1263    1371/666  2060/1669
+//                      33      236/294  563/720     440/304  911/703      919/367   1683/896
+//                      48      197/209  448/509     436/223  714/507      827/268   1322/636
+//   float32            16      45/315   132/940     47/321   139/946      48/406    146/1213
+//                      33      59/176   180/546     57/188   173/563      56/227    175/665
+//                      48      52/128   150/396     56/136   151/406      51/167    162/485
+//   with states        16      208/451  340/1139    410/493  591/1231     780/759   1166/1979
+//                      33      175/266  365/650     277/328  582/722      539/460   1169/1049
+//                      48      160/193  286/468     278/236  450/518      489/331   874/754
+// With states a wave does in turn what a workgroup does side by side, so few rows are faster with workgroups:
+//   rows of 8 heads            64               128              256               512
+//   bfloat16, 33 tokens, 32    18/14   25/24    18/15   29/32    25/24   51/52     35/40    80/93
+//   float32, 33 tokens, 32     19/14   28/28    21/22   35/49    30/38   61/87     47/68    97/162
+//   float32, 16 tokens, 64     34/19   48/47    48/35   64/86    60/63   92/157    91/116   167/300
+//   float32, 48 tokens, 64     60/23   80/55    73/42   104/98   96/77   200/182   189/175  349/395
 // (states: float32 in and out). A wave's 32-bit places take tokens less than
 // 2^23 values apart, in ascending order.
 template <class T>
@@ -1172,7 +1182,10 @@ bool use_short(const ScanArgs *scans, int count) {
   for (int i = 0; i < count; ++i) {
     const ScanArgs &p = scans[i];
     if (p.length > 3 * kTile) return false;
-    if ((p.s0 != nullptr || p.s1 != nullptr) && (p.di > kStates || p.dout > kStates)) return false;
+    if (p.s0 != nullptr || p.s1 != nullptr) {
+      const int size = p.di > p.dout ? p.di : p.dout;
+      if (size > kStates || p.rows * p.heads < (size > 32 ? 2048 : 1024)) return false;
+    }
     for (const ScanOperand *x : {&p.a, &p.b, &p.c})
       if (x->token < 0 || x->token >= int64_t(1) << 23) return false;
   }

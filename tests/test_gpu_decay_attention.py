@@ -437,3 +437,34 @@ def test_no_numbers_stay_where_the_formula_has_them(size, type_):
                         none = ~torch.isfinite(ref[out])
                         assert torch.equal(~torch.isfinite(a[out]).cpu(), none), (name, place, bad, out)
                         assert bool(near[out][~none].all()), (name, place, bad, out)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [(256, 17, 4, 4, 32, 32), (350, 9, 6, 2, 20, 31), (130, 33, 8, 4, 32, 16),
+                                  (270, 48, 8, 8, 64, 40), (520, 20, 4, 2, 33, 64)], ids=lambda s: "x".join(map(str, s)))
+def test_many_short_rows_with_states(size, type_):
+    """As many rows as a wave each is taken for with states; the states also in place; and no numbers."""
+    say(f"[attention] many short rows with states {size} {type_}")
+    x = _inputs(*size, type_, 79, True, True)
+    ref, sizes = _reference(x, size[4] ** -0.5)
+    bounds = attention_bounds(ref, sizes, type_, size[2] // size[3])
+    got = _run(x)
+    _check(got, ref, bounds, f"{size}")
+    end, grad = x["state"].clone(), x["dstate_out"].clone()
+    out, _ = rd.rdf2v_decay_attention(x["q"], x["k"], x["v"], x["log_decay"], lens=x["lens"], state=end, state_out=end)
+    grads = rd.rdf2v_decay_attention_backward(x["q"], x["k"], x["v"], x["log_decay"], x["dout"], lens=x["lens"],
+                                              state=x["state"], dstate_out=grad, dstate=grad)
+    for y, name in zip((out, end, *grads), ("out", "state", "dq", "dk", "dv", "dstate")):
+        assert torch.equal(y, got[name]), name
+    place = size[1] // 2
+    for name in ("q", "k", "v", "dout"):
+        y = dict(x, **{name: x[name].clone()})
+        y[name][0, place, -1, 3] = math.nan                # the first row has all of its tokens
+        a = _run(y)
+        none = attention(*(y[n][:1] for n in "qkv"), y["log_decay"], size[4] ** -0.5, state=y["state"][:1],
+                         dout=y["dout"][:1], dstate_out=y["dstate_out"][:1])
+        for out in a:
+            assert torch.equal(a[out][1:], got[out][1:]), (name, out)
+            bad = ~torch.isfinite(none[out][0])
+            assert torch.equal(~torch.isfinite(a[out][0]).cpu(), bad), (name, out)
+            assert bool(((a[out][0].cpu() - ref[out][0]).abs() <= bounds[out][0])[~bad].all()), (name, out)
