@@ -307,6 +307,7 @@ __device__ __forceinline__ float previous(float x) {
 // 8 groups of 8 beams and 1,000,200 bfloat16 logits 45, 42 and 40 us.
 constexpr int kMergeThreads = 512;
 constexpr int kMergeWaves = kMergeThreads / kWave;
+static_assert(kMergeThreads + 4 * RDF2V_MAX_BEAMS <= kMergeList, "a step's entries, and what goes with them, are ranked at once");
 
 // One workgroup to a group: its beams' candidates by total. Bound by the latency of its steps, not by what it
 // reads: one trip to memory for all lists (2.4 us of 11), the beams' log-sum-exps (2), a bound from the lists'
