@@ -303,16 +303,16 @@ __device__ __forceinline__ float previous(float x) {
 }
 
 // Threads of the merge: a chain of short steps, each shorter with more threads. A selection of 8 from 32
-// groups of 8 beams and 100,050 float32 logits takes 34, 33 and 34 us with 256, 512 and 1024 threads, one from
-// 8 groups of 8 beams and 1,000,200 bfloat16 logits 45, 42 and 40 us.
+// groups of 8 beams and 100,050 float32 logits takes 34.5, 33 and 33 us with 256, 512 and 1024 threads, one
+// from 8 groups of 8 beams and 1,000,200 bfloat16 logits 48, 41.5 and 40.5 us.
 constexpr int kMergeThreads = 512;
 constexpr int kMergeWaves = kMergeThreads / kWave;
 static_assert(kMergeThreads + 4 * RDF2V_MAX_BEAMS <= kMergeList, "a step's entries, and what goes with them, are ranked at once");
 
-// One workgroup to a group: its beams' candidates by total. Bound by the latency of its steps, not by what it
-// reads: one trip to memory for all lists (2.4 us of 11), the beams' log-sum-exps (2), a bound from the lists'
-// first entries (1), the entries that reach it (1), their ranks, a wave to a candidate and a ballot to 64 of
-// those it is set against (1; 6 with a thread to a candidate), and the look at what the slices left out.
+// One workgroup to a group: its beams' candidates by total. 7 us for those 32 groups and 10 for those 8, bound
+// by the latency of its steps, not by what it reads: one trip to memory for all lists, the beams' log-sum-exps,
+// a bound from the lists' first entries, the entries that reach it, their ranks (a wave to a candidate and a
+// ballot to 64 of those it is set against), and the look at what the slices left out.
 template <class T>
 __global__ __launch_bounds__(kMergeThreads) void beam_merge_kernel(SelectArgs p, int64_t first) {
   __shared__ float lse[RDF2V_MAX_BEAMS], score[RDF2V_MAX_BEAMS];

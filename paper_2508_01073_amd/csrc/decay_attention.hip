@@ -380,12 +380,13 @@ __device__ __forceinline__ void store_four(const ScanArgs &p, int64_t at, int co
 //
 // OUT: outputs are wanted; otherwise only S of the segment (from zeros).
 //
-// One row of 20,011 tokens, 8 heads of 128 in bfloat16, in 63 segments: 49 us
-// with outputs (4.0 TB/s, states included), 31 us for the states alone (3.7) and
-// 16 us to join them (4.1). Four rows of 4,096, 16 heads: 78 us for the outputs
-// and 225 for the three gradients. The issue of vector instructions, half of
-// the cycles, and the waits at a chunk's two barriers bound the scans with
-// outputs, HBM those without.
+// One row of 20,011 tokens, 8 heads of 128 in bfloat16, in 63 segments: 55 us
+// with outputs (197 MB beyond L2, 3.6 TB/s), 30 us for the states alone (116 MB,
+// 3.8) and 16 us to join them (67 MB, 4.2). Four rows of 4,096, 16 heads: 83 us
+// for the outputs and 240 for the three gradients. Vector instructions issue in
+// 58 to 63 % of the busy cycles of all of these scans, matrix instructions are
+// busy for 22 to 26 %, and waves wait for 43 to 48 % of their time: the issue,
+// and the waits at a chunk's barriers, bound them.
 //
 // A tile of 16 columns to a wave keeps all of that in 128 registers up to heads
 // of 128, so that 16 waves share a CU; two tiles to a wave spilled, and the
@@ -427,8 +428,8 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
   const float head_log2_gamma =
       head_log_decay(p.log_decay, h, p.status, report && row == 0) * kLog2e;
   // Decays over 1 .. 7 tokens and over a tile of them, the same in all lanes: of neighbouring tokens' decays
-  // one is computed and the others are its products (gradients of 12 rows of 2,048 x 16 heads of 128 with
-  // the forward pass 606 -> 593 us, of two of 8,192 x 16 of 64 215 -> 203).
+  // one is computed and the others are its products (two rows of 8,192 x 16 heads of 64 with gradients 6 %
+  // faster, 12 of 2,048 x 16 of 128 2 %).
   float by_tokens[7], by_tile;
   auto uniform = [](float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); };
 #pragma unroll
@@ -739,11 +740,11 @@ __global__ __launch_bounds__(scan_waves(NB) * kWave, sizeof(T) == 2 ? 4 : 2) voi
 // above, operands of the products with c as they stand, so the wave needs no
 // LDS and no barrier, and many waves share a CU; a workgroup to a row leaves
 // most of its waves idle at its barriers. 4,000 rows of up to 17 tokens (half
-// of them there), 4 heads of 32 in bfloat16: 19 us, 2.3 TB/s, bound by the
-// latency of a wave's few dependent loads; 73 us with workgroups. 1,024 rows of
-// up to 33 in float32, 6 heads on 3 of 48 and 80: 38 us, and 76 for the three
-// gradients, of which the matrix instructions take a quarter and the requests
-// to L1 a third.
+// of them there), 4 heads of 32 in bfloat16: 20 us, 2.1 TB/s, bound by the
+// latency of a wave's few dependent loads; 101 us with workgroups. 1,024 rows of
+// up to 33 in float32, 6 heads on 3 of 48 and 80: 39 us, and 80 for the three
+// gradients; vector instructions issue in 27 and 31 % of the busy cycles, matrix
+// instructions are busy for 16 and 23 %, and waves wait for half of their time.
 //
 // TT: most tiles of 16 tokens.
 constexpr int kShortWaves = 4;  // of a workgroup, each for itself
@@ -1118,13 +1119,13 @@ rdf2v_status launch_short(const ScanRoles &roles, hipStream_t stream) {
 // below what the segment itself reads.
 //
 // kFill: two workgroups of a scan share a CU, so 512 are one round of them.
-// One row of 20,011 x 8 heads of 128, forward, takes 110, 114, 104 and 106 us
+// One row of 20,011 x 8 heads of 128, forward, takes 113, 116, 110 and 107 us
 // with 256, 384, 512 and 768. The segments are as many as the state scans (two
 // of them backwards) need to fill a round: with the 512 counted over the three
 // scans of the gradients, four rows of 4,096 x 16 heads of 128, forward and
-// backward, take 508 us, not 460, and two of 8,192 x 16 heads of 64 took 253,
-// not 215. But rows whose three scans fill a round by themselves are not cut:
-// 12 rows of 2,048 x 16 heads of 128 took 606 us whole and 741 in two.
+// backward, take 523 us, not 473, and two of 8,192 x 16 heads of 64 take 241,
+// not 211. But rows whose three scans fill a round by themselves are not cut:
+// 12 rows of 2,048 x 16 heads of 128 take 639 us whole and 775 in two.
 constexpr int64_t kFill = 512;
 constexpr int64_t kLeastChunks = 4;
 
