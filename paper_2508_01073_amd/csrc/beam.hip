@@ -92,7 +92,8 @@ __device__ __forceinline__ float block_bound(float x, int k, float *scratch) {
   float at = kInf;
   for (int left = (k + W - 1) / W; left > 0;) {
     at = wave_max(x);
-    left -= __popcll(__ballot(x == at));  // lanes of one maximum at once: where all are equal it is the bound
+    // lanes of one maximum at once: where all are equal it is the bound
+    left -= max(1, __popcll(__ballot(x == at)));
     if (x == at) x = -kInf;
   }
   __syncthreads();

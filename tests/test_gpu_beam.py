@@ -395,3 +395,17 @@ def test_equal_logits_everywhere(value, type_):
             ended = [] if value < -1.0e38 else [-1]
             assert tokens[1].tolist() == ended + list(range(k - len(ended)))
             assert parents[1].tolist() == [5] * len(ended) + [4] * (k - len(ended))
+
+
+@pytest.mark.parametrize("vocab", [50, 30_000])
+def test_scores_of_infinity(vocab):
+    """A beam of score +inf: all of its totals are, and its lowest tokens are chosen, but for masked ones."""
+    say(f"[beam] scores of infinity, vocabulary of {vocab}")
+    logits, scores = _inputs(2, 3, vocab, F32, 14)
+    scores[0, 1] = math.inf
+    scores[1, 0] = scores[1, 2] = math.inf
+    logits[0, 1, 4] = -math.inf
+    got, tokens, parents = rd.rdf2v_beam_select(logits, scores, 9)
+    assert bool((got == math.inf).all())
+    assert tokens[0].tolist() == [0, 1, 2, 3, 5, 6, 7, 8, 9] and parents[0].tolist() == [1] * 9
+    assert tokens[1].tolist() == list(range(9)) and parents[1].tolist() == [3] * 9
