@@ -55,7 +55,7 @@ typedef enum rdf2v_status {
 #define RDF2V_STATUS_ID_OUT_OF_RANGE 0x1 /* a subject/object/start id >= num_entities or < 0, or a predicate id out of range */
 #define RDF2V_STATUS_BAD_CSR 0x2         /* row_ptr not non-decreasing within [0, num_edges] */
 #define RDF2V_STATUS_BAD_LENGTH 0x4      /* a walk length outside [0, row_width] (treated as clamped), or a bad string offset */
-#define RDF2V_STATUS_BAD_VALUE 0x10      /* a log decay that is NaN or positive, or a logit of rdf2v_beam_select that is NaN or +inf */
+#define RDF2V_STATUS_BAD_VALUE 0x10      /* a log decay that is NaN or positive, a scan's rate that is not finite or positive, or a logit of rdf2v_beam_select that is NaN or +inf */
 #define RDF2V_STATUS_CAPACITY 0x8        /* more results than the output holds (the rest are not written), or more distinct strings than a vocabulary bound */
 
 /* Longest walk, in hops. A walk row holds 2 * depth + 1 tokens. */
@@ -686,6 +686,270 @@ rdf2v_status rdf2v_distill_loss_backward(const void *logits, int64_t logits_stri
                                          int32_t top, float temperature, const float *lse, const float *dloss,
                                          void *dlogits, int64_t dlogits_stride, void *workspace,
                                          size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/*
+ * Operators of a model's layers over walk tokens.
+ *
+ * What a layer needs beside its matrix products: rdf2v_residual_norm joins the
+ * last layer's output to the residual stream and norms it, rdf2v_causal_conv
+ * looks at the tokens just before, rdf2v_selective_scan mixes a row with decays
+ * that its tokens give. Activations hold RDF2V_F32 or RDF2V_BF16 values,
+ * parameters and their gradients float32. Everything between inputs and outputs
+ * is float32. The conventions of the calls above hold: outputs may not overlap
+ * inputs or one another where nothing else is said (RDF2V_ERR_INVALID_ARGUMENT);
+ * tokens at and beyond a row's length are not used, whatever they hold, and
+ * outputs and gradients are zeros there; the same inputs give the same bits on
+ * every call; a NaN or infinity reaches what the formulas have it in, and
+ * nothing else.
+ */
+
+/* An input of rows of tokens: value (row, token, channel) lies at
+ * data[row * row_stride + token * token_stride + channel]. Strides count
+ * elements and may be anything that keeps the offsets inside the caller's
+ * memory. */
+typedef struct rdf2v_tokens_view {
+  const void *data; /* device; aligned to its element type */
+  int64_t row_stride, token_stride;
+} rdf2v_tokens_view;
+
+/* Widest causal convolution, in tokens. */
+#define RDF2V_MAX_CONV_WIDTH 8
+
+/* Sizes and parameters that the causal convolution calls share. */
+typedef struct rdf2v_conv {
+  int64_t rows, length;  /* 0 .. 2^31 - 1 each; the step does not read length and len */
+  int32_t channels;      /* 1 .. 2^31 - 1 */
+  int32_t width;         /* 1 .. RDF2V_MAX_CONV_WIDTH */
+  int32_t dtype;         /* rdf2v_dtype of inputs, outputs, states and their gradients */
+  int32_t silu;          /* nonzero: the outputs go through u * sigmoid(u) */
+  const float *weight;   /* [channels][width] float32 (device) */
+  const float *bias;     /* [channels] float32 (device) or NULL */
+  /* [rows] int32 (device) or NULL, as in rdf2v_attention */
+  const int32_t *len;
+} rdf2v_conv;
+
+/* Bytes of device workspace rdf2v_causal_conv_backward needs (0 for sizes it
+ * rejects). Pure host function of the sizes. */
+size_t rdf2v_causal_conv_backward_workspace_size(const rdf2v_conv *a);
+
+/*
+ * Causal convolution of each channel by itself. With x_{-1}, x_{-2}, .. from the
+ * state (zeros if NULL) and L the row's length, for t = 0 .. L-1 and every channel:
+ *
+ *   u_t = bias + sum_{j < width} weight[j] x_{t - width + 1 + j},   out_t = u_t or u_t sigmoid(u_t)
+ *
+ *   x          view of channels values, rows x length.
+ *   state      [rows][width - 1][channels] of the dtype (device) or NULL: the
+ *              inputs before the row's first token, the oldest first.
+ *   out        [rows][length][channels] of the dtype (device), written.
+ *   state_out  [rows][width - 1][channels] of the dtype (device) or NULL,
+ *              written: the last width - 1 of the state's and the row's inputs.
+ *   status_dev device int32 or NULL (RDF2V_STATUS_BAD_LENGTH).
+ */
+rdf2v_status rdf2v_causal_conv(const rdf2v_conv *a, const rdf2v_tokens_view *x, const void *state, void *out,
+                               void *state_out, int32_t *status_dev, void *stream);
+
+/*
+ * Gradients of rdf2v_causal_conv from those of its outputs, dout (a view) and
+ * dstate_out (as state_out; NULL: zeros).
+ *
+ *   dx         [rows][length][channels] of the dtype, written.
+ *   dweight    [channels][width] float32, written; dbias [channels] float32 or
+ *              NULL, written.
+ *   dstate     [rows][width - 1][channels] of the dtype or NULL, written.
+ *   workspace  rdf2v_causal_conv_backward_workspace_size() bytes of device
+ *              scratch, 256-byte aligned.
+ */
+rdf2v_status rdf2v_causal_conv_backward(const rdf2v_conv *a, const rdf2v_tokens_view *x,
+                                        const rdf2v_tokens_view *dout, const void *state, const void *dstate_out,
+                                        void *dx, float *dweight, float *dbias, void *dstate, void *workspace,
+                                        size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/*
+ * One more token for each row: rdf2v_causal_conv at length 1 (a->length and
+ * a->len are not read), with the states taken from other rows.
+ *
+ *   x          view whose token_stride is not read.
+ *   state      [num_states][width - 1][channels] of the dtype (device).
+ *   parents    as in rdf2v_decay_attention_step.
+ *   out        [rows][channels] of the dtype (device), written.
+ *   state_out  [rows][width - 1][channels] of the dtype (device), written.
+ *              Without parents it may be `state` itself.
+ */
+rdf2v_status rdf2v_causal_conv_step(const rdf2v_conv *a, const rdf2v_tokens_view *x, const void *state,
+                                    int64_t num_states, const int32_t *parents, void *out, void *state_out,
+                                    int32_t *status_dev, void *stream);
+
+/* Most states of a channel in the selective scan calls. */
+#define RDF2V_MAX_SCAN_STATES 64
+
+/* Sizes and parameters that the selective scan calls share. */
+typedef struct rdf2v_scan {
+  int64_t rows, length;  /* 0 .. 2^31 - 1 each; the step does not read length and len */
+  int32_t channels;      /* 1 .. 2^31 - 1: a multiple of groups */
+  int32_t groups;        /* 1 .. 65535: channel d reads b and c of group d / (channels / groups) */
+  int32_t states;        /* of a channel, 1 .. RDF2V_MAX_SCAN_STATES */
+  int32_t dtype;         /* rdf2v_dtype of x, dt, b, c, gate, out and their gradients */
+  /* [channels][states] float32 (device): rates, finite and <= 0. Others raise
+   * RDF2V_STATUS_BAD_VALUE and are taken as 0 (no decay). */
+  const float *a;
+  const float *dt_bias;  /* [channels] float32 (device) or NULL: zeros */
+  const float *skip;     /* [channels] float32 (device) or NULL: zeros */
+  /* [rows] int32 (device) or NULL, as in rdf2v_attention */
+  const int32_t *len;
+} rdf2v_scan;
+
+/* Bytes of device workspace the two calls need (0 for sizes that they reject).
+ * Pure host functions of the sizes: pointers are not read. */
+size_t rdf2v_selective_scan_workspace_size(const rdf2v_scan *a);
+size_t rdf2v_selective_scan_backward_workspace_size(const rdf2v_scan *a);
+
+/*
+ * Selective scan over whole rows of tokens. For each row and channel, with L the
+ * row's length and h_{-1} = state (zeros if NULL), for t = 0 .. L-1:
+ *
+ *   delta_t = log(1 + exp(dt_t + dt_bias))
+ *   h_t[n]  = exp(delta_t a[n]) h_{t-1}[n] + delta_t x_t b_t[n]     n < states
+ *   y_t     = sum_n c_t[n] h_t[n] + skip x_t
+ *   out_t   = y_t, or with a gate y_t gate_t sigmoid(gate_t)
+ *
+ *   x, dt      views of channels values, rows x length; gate likewise or NULL.
+ *   b, c       views with `groups` heads of `states` values.
+ *   state      [rows][channels][states] float32 (device) or NULL.
+ *   out        [rows][length][channels] of the dtype (device), written.
+ *   state_out  [rows][channels][states] float32 (device) or NULL: h_{L-1} is
+ *              written. May be `state` itself.
+ *   workspace  rdf2v_selective_scan_workspace_size() bytes of device scratch,
+ *              256-byte aligned.
+ *   status_dev device int32 or NULL (RDF2V_STATUS_BAD_VALUE,
+ *              RDF2V_STATUS_BAD_LENGTH).
+ */
+rdf2v_status rdf2v_selective_scan(const rdf2v_scan *a, const rdf2v_tokens_view *x, const rdf2v_tokens_view *dt,
+                                  const rdf2v_heads_view *b, const rdf2v_heads_view *c,
+                                  const rdf2v_tokens_view *gate, const float *state, void *out, float *state_out,
+                                  void *workspace, size_t workspace_bytes, int32_t *status_dev, void *stream);
+
+/* Where rdf2v_selective_scan_backward writes (device). */
+typedef struct rdf2v_scan_gradients {
+  void *dx, *ddt;   /* [rows][length][channels] of the dtype */
+  void *db, *dc;    /* [rows][length][groups][states] of the dtype: sums over the group's channels, rounded once */
+  void *dgate;      /* [rows][length][channels] of the dtype; NULL where there is no gate, and only there */
+  float *da;        /* [channels][states] float32 */
+  float *ddt_bias;  /* [channels] float32 or NULL */
+  float *dskip;     /* [channels] float32 or NULL */
+  float *dstate;    /* [rows][channels][states] float32 or NULL; may be dstate_out itself */
+} rdf2v_scan_gradients;
+
+/*
+ * Gradients of rdf2v_selective_scan from those of its outputs, dout (a view) and
+ * dstate_out (as state_out; NULL: zeros). With g_t the gradient of y_t and r_t
+ * that of h_t,
+ *
+ *   r_t = c_t g_t + exp(delta_{t+1} a) r_{t+1},   r_{L-1} = c g + dstate_out
+ *   ddelta_t = sum_n r_t[n] (a[n] exp(delta_t a[n]) h_{t-1}[n] + x_t b_t[n]),   ddt_t = ddelta_t sigmoid(dt_t + dt_bias)
+ *   dx_t = delta_t sum_n r_t[n] b_t[n] + skip g_t,   dgate_t = dout_t y_t times the slope of u sigmoid(u)
+ *   db_t[n] = sum over channels of r_t[n] delta_t x_t,   dc_t[n] = sum over channels of g_t h_t[n]
+ *   da[n] = sum_t r_t[n] delta_t exp(delta_t a[n]) h_{t-1}[n],   dskip = sum_t g_t x_t,   ddt_bias = sum_t ddt_t
+ *   dstate = exp(delta_0 a) r_0
+ *
+ * (dstate = dstate_out for a row of length 0). A rate that was taken as 0 has
+ * the gradient at 0.
+ */
+rdf2v_status rdf2v_selective_scan_backward(const rdf2v_scan *a, const rdf2v_tokens_view *x,
+                                           const rdf2v_tokens_view *dt, const rdf2v_heads_view *b,
+                                           const rdf2v_heads_view *c, const rdf2v_tokens_view *gate,
+                                           const rdf2v_tokens_view *dout, const float *state,
+                                           const float *dstate_out, const rdf2v_scan_gradients *grads,
+                                           void *workspace, size_t workspace_bytes, int32_t *status_dev,
+                                           void *stream);
+
+/*
+ * One more token for each row: rdf2v_selective_scan at length 1 (a->length and
+ * a->len are not read), with the states taken from other rows.
+ *
+ *   x, dt, b, c, gate  views whose token_stride is not read.
+ *   state      [num_states][channels][states] float32 (device).
+ *   parents    as in rdf2v_decay_attention_step.
+ *   out        [rows][channels] of the dtype (device), written.
+ *   state_out  [rows][channels][states] float32 (device), written. Without
+ *              parents it may be `state` itself.
+ */
+rdf2v_status rdf2v_selective_scan_step(const rdf2v_scan *a, const rdf2v_tokens_view *x, const rdf2v_tokens_view *dt,
+                                       const rdf2v_heads_view *b, const rdf2v_heads_view *c,
+                                       const rdf2v_tokens_view *gate, const float *state, int64_t num_states,
+                                       const int32_t *parents, void *out, float *state_out, int32_t *status_dev,
+                                       void *stream);
+
+/* Most channels of the residual norm calls. */
+#define RDF2V_MAX_NORM_CHANNELS 16384
+
+/* Sizes and parameters that the residual norm calls share. */
+typedef struct rdf2v_norm {
+  int64_t rows, length;    /* 0 .. 2^31 - 1 each */
+  int32_t channels;        /* 1 .. RDF2V_MAX_NORM_CHANNELS */
+  int32_t dtype;           /* rdf2v_dtype of x, out and their gradients */
+  int32_t residual_dtype;  /* of residual, hidden and their gradients: the same, or RDF2V_F32 */
+  int32_t center;          /* nonzero: the mean is taken off before the norm */
+  float eps;               /* finite, >= 0 */
+  const float *weight;     /* [channels] float32 (device) */
+  const float *bias;       /* [channels] float32 (device) or NULL */
+  const float *scale;      /* [channels] float32 (device) or NULL: ones */
+  /* Share of x's values that are dropped, 0 <= drop < 1 - 2^-32. The others are
+   * multiplied by 1 / (1 - drop). Value (row, token, channel) is dropped where
+   * word [channel mod 4] of the Philox4x32-10 block of key (seed + seed_offset)
+   * and counter (channel / 4, token + 1, row_begin + row as low and high word)
+   * is below round(drop 2^32): the mask is a function of these alone, whatever
+   * the batch, and none of a walk's words of the same seed. */
+  double drop;
+  uint64_t seed;
+  /* One int64 (device) or NULL: added to the seed by the kernels, so that a
+   * captured graph draws other masks when the caller changes it. */
+  const int64_t *seed_offset;
+  int64_t row_begin;       /* >= 0 */
+  /* [rows] int32 (device) or NULL, as in rdf2v_attention */
+  const int32_t *len;
+} rdf2v_norm;
+
+/* Bytes of device workspace rdf2v_residual_norm_backward needs (0 for sizes it
+ * rejects). Pure host function of the sizes. */
+size_t rdf2v_residual_norm_backward_workspace_size(const rdf2v_norm *a);
+
+/*
+ * Residual connection and norm, token by token:
+ *
+ *   hidden = residual + scale * dropout(x)
+ *   out    = weight * (hidden - mean) / sqrt(mean of (hidden - mean)^2 + eps) + bias
+ *
+ * with mean 0 where center is 0. The norm is that of hidden before it is rounded.
+ *
+ *   x         view of channels values, rows x length.
+ *   residual  view of residual_dtype or NULL: zeros.
+ *   out       [rows][length][channels] of the dtype (device), written.
+ *   hidden    [rows][length][channels] of residual_dtype (device) or NULL, written.
+ *   stats     [rows][length][2] float32 (device) or NULL, written: the mean and
+ *             1 / sqrt(..), for the backward call; zeros beyond a row's length.
+ *   status_dev  device int32 or NULL (RDF2V_STATUS_BAD_LENGTH).
+ */
+rdf2v_status rdf2v_residual_norm(const rdf2v_norm *a, const rdf2v_tokens_view *x, const rdf2v_tokens_view *residual,
+                                 void *out, void *hidden, float *stats, int32_t *status_dev, void *stream);
+
+/*
+ * Gradients of rdf2v_residual_norm from those of its outputs, dout and dhidden
+ * (views; dhidden of residual_dtype or NULL: zeros), with the stats that it wrote.
+ *
+ *   dx         [rows][length][channels] of the dtype, written.
+ *   dresidual  [rows][length][channels] of residual_dtype or NULL, written.
+ *   dweight    [channels] float32, written; dbias, dscale [channels] float32 or
+ *              NULL, written.
+ *   workspace  rdf2v_residual_norm_backward_workspace_size() bytes of device
+ *              scratch, 256-byte aligned.
+ */
+rdf2v_status rdf2v_residual_norm_backward(const rdf2v_norm *a, const rdf2v_tokens_view *x,
+                                          const rdf2v_tokens_view *residual, const float *stats,
+                                          const rdf2v_tokens_view *dout, const rdf2v_tokens_view *dhidden, void *dx,
+                                          void *dresidual, float *dweight, float *dbias, float *dscale,
+                                          void *workspace, size_t workspace_bytes, int32_t *status_dev,
+                                          void *stream);
 
 /* Static, human-readable name of a status code (any int: values that are not
  * an rdf2v_status give "RDF2V_UNKNOWN_STATUS"). */

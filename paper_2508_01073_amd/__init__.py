@@ -19,6 +19,7 @@ import ctypes
 import os
 import warnings
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -39,6 +40,12 @@ __all__ = [
     "rdf2v_decay_attention_backward_workspace_size", "rdf2v_decay_attention_backward",
     "rdf2v_decay_attention_step", "rdf2v_beam_select_workspace_size", "rdf2v_beam_select", "rdf2v_beam_reorder",
     "rdf2v_distill_workspace_size", "rdf2v_distill_loss", "rdf2v_distill_loss_backward",
+    "RDF2V_MAX_CONV_WIDTH", "RDF2V_MAX_SCAN_STATES", "RDF2V_MAX_NORM_CHANNELS",
+    "rdf2v_causal_conv", "rdf2v_causal_conv_backward_workspace_size", "rdf2v_causal_conv_backward",
+    "rdf2v_causal_conv_step", "rdf2v_selective_scan_workspace_size", "rdf2v_selective_scan",
+    "rdf2v_selective_scan_backward_workspace_size", "rdf2v_selective_scan_backward", "ScanGradients",
+    "rdf2v_selective_scan_step", "rdf2v_residual_norm", "rdf2v_residual_norm_backward_workspace_size",
+    "rdf2v_residual_norm_backward", "NormGradients",
     "rdf2v_status_string", "check_device_status",
     "library_path",
 ]
@@ -67,6 +74,9 @@ RDF2V_BF16 = 1
 RDF2V_MAX_HEAD_SIZE = 128
 RDF2V_MAX_BEAMS = 64
 RDF2V_MAX_TEACHER_TOP = 512
+RDF2V_MAX_CONV_WIDTH = 8
+RDF2V_MAX_SCAN_STATES = 64
+RDF2V_MAX_NORM_CHANNELS = 16384
 
 _lib = None
 
@@ -91,6 +101,36 @@ class _AttentionStruct(ctypes.Structure):
 class _HeadsViewStruct(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
+
+
+class _TokensViewStruct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
+class _ConvStruct(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("length", ctypes.c_int64), ("channels", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("silu", ctypes.c_int32),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("len", ctypes.c_void_p)]
+
+
+class _ScanStruct(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("length", ctypes.c_int64), ("channels", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("states", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("a", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p), ("skip", ctypes.c_void_p),
+                ("len", ctypes.c_void_p)]
+
+
+class _ScanGradientsStruct(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("dx", "ddt", "db", "dc", "dgate", "da", "ddt_bias", "dskip",
+                                                     "dstate")]
+
+
+class _NormStruct(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("length", ctypes.c_int64), ("channels", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("center", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("drop", ctypes.c_double), ("seed", ctypes.c_uint64),
+                ("seed_offset", ctypes.c_void_p), ("row_begin", ctypes.c_int64), ("len", ctypes.c_void_p)]
 
 
 def _native():
@@ -167,6 +207,23 @@ def _native():
     lib.rdf2v_distill_loss_backward.argtypes = [vp, i64, i32, vp, vp, i64, i64, i32, f32, vp, vp, vp, i64, vp, sz,
                                                 vp, vp]
     lib.rdf2v_distill_loss_backward.restype = ctypes.c_int
+    conv_p, tok_p = ctypes.POINTER(_ConvStruct), ctypes.POINTER(_TokensViewStruct)
+    scan_p, norm_p = ctypes.POINTER(_ScanStruct), ctypes.POINTER(_NormStruct)
+    for name, args in (("causal_conv", [conv_p, tok_p] + [vp] * 5),
+                       ("causal_conv_backward", [conv_p, tok_p, tok_p] + [vp] * 7 + [sz, vp, vp]),
+                       ("causal_conv_step", [conv_p, tok_p, vp, i64] + [vp] * 5),
+                       ("selective_scan", [scan_p, tok_p, tok_p, view_p, view_p, tok_p] + [vp] * 4 + [sz, vp, vp]),
+                       ("selective_scan_backward", [scan_p, tok_p, tok_p, view_p, view_p, tok_p, tok_p, vp, vp,
+                                                    ctypes.POINTER(_ScanGradientsStruct), vp, sz, vp, vp]),
+                       ("selective_scan_step", [scan_p, tok_p, tok_p, view_p, view_p, tok_p, vp, i64] + [vp] * 5),
+                       ("residual_norm", [norm_p, tok_p, tok_p] + [vp] * 5),
+                       ("residual_norm_backward", [norm_p, tok_p, tok_p, vp, tok_p, tok_p] + [vp] * 6 + [sz, vp, vp])):
+        call = getattr(lib, "rdf2v_" + name)
+        call.argtypes, call.restype = args, ctypes.c_int
+    for name, arg in (("causal_conv_backward", conv_p), ("selective_scan", scan_p), ("selective_scan_backward", scan_p),
+                      ("residual_norm_backward", norm_p)):
+        call = getattr(lib, f"rdf2v_{name}_workspace_size")
+        call.argtypes, call.restype = [arg], sz
     lib.rdf2v_status_string.argtypes = [ctypes.c_int]
     lib.rdf2v_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -1131,6 +1188,539 @@ def rdf2v_distill_loss_backward(logits: torch.Tensor, ids: torch.Tensor, teacher
                                              dstride, _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_distill_loss_backward")
         return dlogits
+
+
+def _tokens_view(t: torch.Tensor, name: str, dtype: torch.dtype, dev: torch.device, shape) -> _TokensViewStruct:
+    """A [rows, tokens, channels] (or [rows, channels]) input in any layout whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev:
+        raise TypeError(f"{name} must be a {dtype} tensor on {dev}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; this call needs {tuple(shape)}")
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return _TokensViewStruct(t.data_ptr(), stride[0], stride[1] if len(stride) == 3 else 0)
+
+
+def _parameter(t: torch.Tensor | None, name: str, shape, dev: torch.device):
+    """Pointer of an optional float32 parameter of exactly this shape."""
+    return None if t is None else _exact(t, name, torch.float32, shape, dev).data_ptr()
+
+
+def _new(t: torch.Tensor | None, name: str, dtype: torch.dtype, shape, dev: torch.device) -> torch.Tensor:
+    """An output of exactly this shape: the caller's, or a new one."""
+    return torch.empty(shape, dtype=dtype, device=dev) if t is None else _exact(t, name, dtype, shape, dev)
+
+
+def _workspace(need: int, dev: torch.device) -> torch.Tensor | None:
+    return torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+
+
+def _gradient(t: torch.Tensor | None, like) -> torch.Tensor:
+    """What autograd hands a backward call for an output, as the calls take it; zeros for an output that was not used."""
+    if t is None:
+        return torch.zeros(like[0], dtype=like[1], device=like[2])
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+def _lens(t: torch.Tensor | None, rows: int, dev: torch.device):
+    return None if t is None else _ptr(_exact(t, "lens", torch.int32, (rows,), dev))
+
+
+def _parents_and_states(parents, state, rows: int, tail, dtype: torch.dtype, dev: torch.device) -> int:
+    """Checks a step's parents and states; returns how many states there are."""
+    num_states = rows
+    if parents is not None:
+        _out(parents, "parents", torch.int32, 0, dev)
+        if parents.numel() != rows:
+            raise ValueError(f"parents holds {parents.numel()} elements; this call needs {rows}")
+        if isinstance(state, torch.Tensor) and state.dim() == len(tail) + 1:
+            num_states = state.shape[0]
+    if state is None:
+        raise TypeError("state must be a CUDA (HIP) tensor")
+    _exact(state, "state", dtype, (num_states, *tail), dev)
+    return num_states
+
+
+class _Conv:
+    """The checked arguments that the causal convolution calls share."""
+
+    __slots__ = ("c", "view", "dev", "dtype", "shape", "states")
+
+    def __init__(self, x, weight, bias, silu, lens, ndim):
+        dtype = _float_dtype(x, "x")
+        shape = self.shape = x.shape
+        if len(shape) != ndim:
+            raise ValueError(f"x must have {ndim} dimensions")
+        dev, self.dtype = x.device, x.dtype
+        self.dev = dev
+        rows, channels = shape[0], shape[-1]
+        if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+            raise ValueError("weight must have shape [channels, width]")
+        width = weight.shape[1]
+        if not 1 <= width <= RDF2V_MAX_CONV_WIDTH:
+            raise ValueError(f"width {width}: 1 to {RDF2V_MAX_CONV_WIDTH} are supported")
+        if channels < 1:
+            raise ValueError("x must have channels")
+        self.view = _tokens_view(x, "x", x.dtype, dev, shape)
+        self.states = (rows, width - 1, channels)
+        self.c = _ConvStruct(rows, shape[1] if ndim == 3 else 1, channels, width, dtype, bool(silu),
+                             _parameter(weight, "weight", (channels, width), dev),
+                             _parameter(bias, "bias", (channels,), dev), _lens(lens, rows, dev))
+
+
+class _CausalConv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, state, silu, lens, want_state, status, stream):
+        out, state_out = rdf2v_causal_conv(x, weight, bias, silu=silu, lens=lens, state=state, want_state=want_state,
+                                           status=status, stream=stream)
+        ctx.save_for_backward(x, weight, bias, state, lens)
+        ctx.silu = silu
+        ctx.set_materialize_grads(False)
+        return (out, state_out) if want_state else out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dstate_out=None):
+        x, weight, bias, state, lens = ctx.saved_tensors
+        if dstate_out is not None:
+            dstate_out = dstate_out.contiguous()
+        dx, dweight, dbias, dstate = rdf2v_causal_conv_backward(
+            x, weight, bias, _gradient(dout, (x.shape, x.dtype, x.device)), silu=ctx.silu, lens=lens, state=state,
+            dstate_out=dstate_out)
+        return dx, dweight, dbias, dstate, None, None, None, None, None
+
+
+def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None, *, silu: bool = True,
+                      lens: torch.Tensor | None = None, state: torch.Tensor | None = None, want_state: bool = False,
+                      out: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                      status: torch.Tensor | None = None, stream=None):
+    """Causal convolution of each channel by itself: u_t = bias + sum_j weight[:, j] x_{t - width + 1 + j}, out_t = u_t
+    sigmoid(u_t), or u_t where silu is False.
+
+    x [rows, length, channels] is float32 or bfloat16 in any layout whose last dimension is contiguous; weight
+    [channels, width] and bias [channels] are float32. lens: int32 [rows], the tokens of each row that count. state
+    [rows, width - 1, channels] in x's type: the inputs before the row's first (None: zeros). Returns (out, state_out),
+    state_out (the last width - 1 inputs) being None unless it is given or want_state is set.
+
+    Where x, weight, bias or state requires gradients, autograd records the call; out and state_out must then be left
+    to it, as in torch's own functions."""
+    a = _Conv(x, weight, bias, silu, lens, 3)
+    dev, c = a.dev, a.c
+    if _records(x, weight, bias, state):
+        if out is not None or state_out is not None:
+            raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
+                             "gradients")
+        got = _CausalConv.apply(x, weight, bias, state, silu, lens, want_state, status, stream)
+        return got if want_state else (got, None)
+    with _on_stream(dev, stream) as h:
+        out = _new(out, "out", a.dtype, a.shape, dev)
+        if want_state or state_out is not None:
+            state_out = _new(state_out, "state_out", a.dtype, a.states, dev)
+        if state is not None:
+            _exact(state, "state", a.dtype, a.states, dev)
+        _status(status, dev)
+        st = _native().rdf2v_causal_conv(c, a.view, _ptr(state), _ptr(out), _ptr(state_out), _ptr(status), h)
+        _check(st, "rdf2v_causal_conv")
+        return out, state_out
+
+
+def rdf2v_causal_conv_backward_workspace_size(rows: int, length: int, channels: int, width: int,
+                                              dtype: torch.dtype = torch.float32) -> int:
+    c = _ConvStruct(rows, length, channels, width, _DTYPES.get(dtype, -1), 1, None, None, None)
+    return int(_native().rdf2v_causal_conv_backward_workspace_size(c))
+
+
+def rdf2v_causal_conv_backward(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None, dout: torch.Tensor, *,
+                               silu: bool = True, lens: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                               dstate_out: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                               dweight: torch.Tensor | None = None, dbias: torch.Tensor | None = None,
+                               dstate: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                               status: torch.Tensor | None = None, stream=None):
+    """Gradients of rdf2v_causal_conv for its inputs, from dout (that of out) and dstate_out (that of state_out; None:
+    zeros). Returns (dx, dweight, dbias, dstate); dbias is None unless bias or dbias is given, dstate unless state or
+    dstate is."""
+    a = _Conv(x, weight, bias, silu, lens, 3)
+    dev, c = a.dev, a.c
+    with _on_stream(dev, stream) as h:
+        view = _tokens_view(dout, "dout", a.dtype, dev, a.shape)
+        dx = _new(dx, "dx", a.dtype, a.shape, dev)
+        dweight = _new(dweight, "dweight", torch.float32, weight.shape, dev)
+        if bias is not None or dbias is not None:
+            dbias = _new(dbias, "dbias", torch.float32, (c.channels,), dev)
+        if state is not None or dstate is not None:
+            dstate = _new(dstate, "dstate", a.dtype, a.states, dev)
+        for t, name in ((state, "state"), (dstate_out, "dstate_out")):
+            if t is not None:
+                _exact(t, name, a.dtype, a.states, dev)
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            workspace = _workspace(lib.rdf2v_causal_conv_backward_workspace_size(c), dev)
+        st = lib.rdf2v_causal_conv_backward(c, a.view, view, _ptr(state), _ptr(dstate_out), _ptr(dx), _ptr(dweight),
+                                            _ptr(dbias), _ptr(dstate), _ptr(workspace), _ws_bytes(workspace),
+                                            _ptr(status), h)
+        _check(st, "rdf2v_causal_conv_backward")
+        return dx, dweight, dbias, dstate
+
+
+def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None, state: torch.Tensor, *,
+                           silu: bool = True, parents: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                           state_out: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """rdf2v_causal_conv for one more token of each row: x [rows, channels], state [num_states, width - 1, channels] in
+    x's type. Returns (out [rows, channels], state_out [rows, width - 1, channels]). parents and state_out are as in
+    rdf2v_decay_attention_step. For answering: autograd does not record it."""
+    a = _Conv(x, weight, bias, silu, None, 2)
+    dev, c = a.dev, a.c
+    with _on_stream(dev, stream) as h:
+        num_states = _parents_and_states(parents, state, c.rows, a.states[1:], a.dtype, dev)
+        out = _new(out, "out", a.dtype, a.shape, dev)
+        if state_out is None and parents is None:
+            state_out = state
+        state_out = _new(state_out, "state_out", a.dtype, a.states, dev)
+        _status(status, dev)
+        if _records(x, weight, bias, state):
+            _no_gradient("rdf2v_causal_conv_step", "its inputs")
+        st = _native().rdf2v_causal_conv_step(c, a.view, _ptr(state), num_states, _ptr(parents), _ptr(out),
+                                              _ptr(state_out), _ptr(status), h)
+        _check(st, "rdf2v_causal_conv_step")
+        return out, state_out
+
+
+class ScanGradients(NamedTuple):
+    """Gradients of rdf2v_selective_scan's inputs; None for an input that was not given."""
+
+    dx: torch.Tensor
+    ddt: torch.Tensor
+    da: torch.Tensor
+    db: torch.Tensor
+    dc: torch.Tensor
+    ddt_bias: torch.Tensor | None
+    dskip: torch.Tensor | None
+    dgate: torch.Tensor | None
+    dstate: torch.Tensor | None
+
+
+class _Scan:
+    """The checked arguments that the selective scan calls share."""
+
+    __slots__ = ("c", "views", "dev", "dtype", "shape", "heads", "states")
+
+    def __init__(self, x, dt, a, b, c, dt_bias, skip, gate, lens, ndim):
+        dtype = _float_dtype(x, "x")
+        shape = self.shape = x.shape
+        if len(shape) != ndim:
+            raise ValueError(f"x must have {ndim} dimensions")
+        dev, kind = x.device, x.dtype
+        self.dev, self.dtype = dev, kind
+        rows, channels = shape[0], shape[-1]
+        if not isinstance(b, torch.Tensor) or b.dim() != ndim + 1:
+            raise ValueError(f"b and c must have {ndim + 1} dimensions")
+        groups, states = b.shape[-2:]
+        if channels < 1 or groups < 1 or channels % groups:
+            raise ValueError(f"{channels} channels are no multiple of {groups} groups")
+        if not 1 <= states <= RDF2V_MAX_SCAN_STATES:
+            raise ValueError(f"{states} states: 1 to {RDF2V_MAX_SCAN_STATES} are supported")
+        self.heads = (*shape[:-1], groups, states)
+        self.states = (rows, channels, states)
+        self.views = (_tokens_view(x, "x", kind, dev, shape), _tokens_view(dt, "dt", kind, dev, shape),
+                      _heads_view(b, "b", kind, dev, self.heads), _heads_view(c, "c", kind, dev, self.heads),
+                      None if gate is None else _tokens_view(gate, "gate", kind, dev, shape))
+        if a is None:
+            raise TypeError("a must be a CUDA (HIP) tensor")
+        self.c = _ScanStruct(rows, shape[1] if ndim == 3 else 1, channels, groups, states, dtype,
+                             _parameter(a, "a", (channels, states), dev),
+                             _parameter(dt_bias, "dt_bias", (channels,), dev),
+                             _parameter(skip, "skip", (channels,), dev), _lens(lens, rows, dev))
+
+
+class _SelectiveScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, dt, a, b, c, dt_bias, skip, gate, state, lens, want_state, workspace, status, stream):
+        out, state_out = rdf2v_selective_scan(x, dt, a, b, c, dt_bias=dt_bias, skip=skip, gate=gate, lens=lens,
+                                              state=state, want_state=want_state, workspace=workspace, status=status,
+                                              stream=stream)
+        ctx.save_for_backward(x, dt, a, b, c, dt_bias, skip, gate, state, lens)
+        ctx.set_materialize_grads(False)
+        return (out, state_out) if want_state else out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dstate_out=None):
+        x, dt, a, b, c, dt_bias, skip, gate, state, lens = ctx.saved_tensors
+        if dstate_out is not None:
+            dstate_out = dstate_out.contiguous()
+        g = rdf2v_selective_scan_backward(x, dt, a, b, c, _gradient(dout, (x.shape, x.dtype, x.device)),
+                                          dt_bias=dt_bias, skip=skip, gate=gate, lens=lens, state=state,
+                                          dstate_out=dstate_out)
+        return g.dx, g.ddt, g.da, g.db, g.dc, g.ddt_bias, g.dskip, g.dgate, g.dstate, None, None, None, None, None
+
+
+def rdf2v_selective_scan_workspace_size(rows: int, length: int, channels: int, groups: int, states: int,
+                                        dtype: torch.dtype = torch.float32) -> int:
+    c = _ScanStruct(rows, length, channels, groups, states, _DTYPES.get(dtype, -1), None, None, None, None)
+    return int(_native().rdf2v_selective_scan_workspace_size(c))
+
+
+def rdf2v_selective_scan_backward_workspace_size(rows: int, length: int, channels: int, groups: int, states: int,
+                                                 dtype: torch.dtype = torch.float32) -> int:
+    c = _ScanStruct(rows, length, channels, groups, states, _DTYPES.get(dtype, -1), None, None, None, None)
+    return int(_native().rdf2v_selective_scan_backward_workspace_size(c))
+
+
+def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor, *,
+                         dt_bias: torch.Tensor | None = None, skip: torch.Tensor | None = None,
+                         gate: torch.Tensor | None = None, lens: torch.Tensor | None = None,
+                         state: torch.Tensor | None = None, want_state: bool = False, out: torch.Tensor | None = None,
+                         state_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                         status: torch.Tensor | None = None, stream=None):
+    """Selective scan over rows of tokens, channel by channel: delta_t = softplus(dt_t + dt_bias), h_t = exp(delta_t a)
+    h_{t-1} + delta_t x_t b_t, y_t = c_t . h_t + skip x_t, out_t = y_t gate_t sigmoid(gate_t) (y_t without a gate).
+
+    x, dt and gate [rows, length, channels] and b and c [rows, length, groups, states] are float32 or bfloat16 in any
+    layout whose last dimension is contiguous; channel d reads group d // (channels // groups). a [channels, states]
+    (finite, <= 0), dt_bias and skip [channels] are float32. lens: int32 [rows], the tokens of each row that count.
+    state: float32 [rows, channels, states] to begin from. Returns (out, state_out), state_out being None unless it is
+    given or want_state is set.
+
+    Where an input requires gradients, autograd records the call; out and state_out must then be left to it, as in
+    torch's own functions."""
+    s = _Scan(x, dt, a, b, c, dt_bias, skip, gate, lens, 3)
+    dev = s.dev
+    if _records(x, dt, a, b, c, dt_bias, skip, gate, state):
+        if out is not None or state_out is not None:
+            raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
+                             "gradients")
+        got = _SelectiveScan.apply(x, dt, a, b, c, dt_bias, skip, gate, state, lens, want_state, workspace, status,
+                                   stream)
+        return got if want_state else (got, None)
+    with _on_stream(dev, stream) as h:
+        out = _new(out, "out", s.dtype, s.shape, dev)
+        if want_state or state_out is not None:
+            state_out = _new(state_out, "state_out", torch.float32, s.states, dev)
+        _state(state, "state", s.states, dev)
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            workspace = _workspace(lib.rdf2v_selective_scan_workspace_size(s.c), dev)
+        st = lib.rdf2v_selective_scan(s.c, *s.views, _ptr(state), _ptr(out), _ptr(state_out), _ptr(workspace),
+                                      _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_selective_scan")
+        return out, state_out
+
+
+def rdf2v_selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
+                                  dout: torch.Tensor, *, dt_bias: torch.Tensor | None = None,
+                                  skip: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                                  lens: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                                  dstate_out: torch.Tensor | None = None, out: ScanGradients | None = None,
+                                  workspace: torch.Tensor | None = None, status: torch.Tensor | None = None,
+                                  stream=None) -> ScanGradients:
+    """Gradients of rdf2v_selective_scan for its inputs, from dout (that of out) and dstate_out (that of state_out;
+    None: zeros), each in its input's shape and type. `out`: tensors to write them to, with None for those of inputs
+    that are not given (dstate may be there without a state)."""
+    s = _Scan(x, dt, a, b, c, dt_bias, skip, gate, lens, 3)
+    dev, kind, f32 = s.dev, s.dtype, torch.float32
+    with _on_stream(dev, stream) as h:
+        view = _tokens_view(dout, "dout", kind, dev, s.shape)
+        given = (None,) * 9 if out is None else out
+        channels = (s.c.channels,)
+        wanted = ((True, kind, s.shape), (True, kind, s.shape), (True, f32, a.shape), (True, kind, s.heads),
+                  (True, kind, s.heads), (dt_bias is not None, f32, channels), (skip is not None, f32, channels),
+                  (gate is not None, kind, s.shape), (state is not None, f32, s.states))
+        g = ScanGradients(*[_new(t, name, type_, shape, dev) if want or t is not None else None
+                            for t, name, (want, type_, shape) in zip(given, ScanGradients._fields, wanted)])
+        _state(state, "state", s.states, dev)
+        _state(dstate_out, "dstate_out", s.states, dev)
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            workspace = _workspace(lib.rdf2v_selective_scan_backward_workspace_size(s.c), dev)
+        to = _ScanGradientsStruct(_ptr(g.dx), _ptr(g.ddt), _ptr(g.db), _ptr(g.dc), _ptr(g.dgate), _ptr(g.da),
+                                  _ptr(g.ddt_bias), _ptr(g.dskip), _ptr(g.dstate))
+        st = lib.rdf2v_selective_scan_backward(s.c, *s.views, view, _ptr(state), _ptr(dstate_out), to,
+                                               _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_selective_scan_backward")
+        return g
+
+
+def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: torch.Tensor, c: torch.Tensor,
+                              state: torch.Tensor, *, dt_bias: torch.Tensor | None = None,
+                              skip: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                              parents: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                              state_out: torch.Tensor | None = None, status: torch.Tensor | None = None, stream=None):
+    """rdf2v_selective_scan for one more token of each row: x, dt, gate [rows, channels], b, c [rows, groups, states],
+    state float32 [num_states, channels, states]. Returns (out [rows, channels], state_out [rows, channels, states]).
+    parents and state_out are as in rdf2v_decay_attention_step. For answering: autograd does not record it."""
+    s = _Scan(x, dt, a, b, c, dt_bias, skip, gate, None, 2)
+    dev = s.dev
+    with _on_stream(dev, stream) as h:
+        num_states = _parents_and_states(parents, state, s.c.rows, s.states[1:], torch.float32, dev)
+        out = _new(out, "out", s.dtype, s.shape, dev)
+        if state_out is None and parents is None:
+            state_out = state
+        state_out = _new(state_out, "state_out", torch.float32, s.states, dev)
+        _status(status, dev)
+        if _records(x, dt, a, b, c, dt_bias, skip, gate, state):
+            _no_gradient("rdf2v_selective_scan_step", "its inputs")
+        st = _native().rdf2v_selective_scan_step(s.c, *s.views, _ptr(state), num_states, _ptr(parents), _ptr(out),
+                                                 _ptr(state_out), _ptr(status), h)
+        _check(st, "rdf2v_selective_scan_step")
+        return out, state_out
+
+
+class NormGradients(NamedTuple):
+    """Gradients of rdf2v_residual_norm's inputs; None for an input that was not given."""
+
+    dx: torch.Tensor
+    dresidual: torch.Tensor | None
+    dweight: torch.Tensor
+    dbias: torch.Tensor | None
+    dscale: torch.Tensor | None
+
+
+class _Norm:
+    """The checked arguments that the residual norm calls share."""
+
+    __slots__ = ("c", "views", "dev", "dtype", "shape", "hidden_dtype", "stats")
+
+    def __init__(self, x, residual, weight, bias, scale, drop, seed, seed_offset, row_begin, center, eps, lens,
+                 hidden_dtype):
+        dtype = _float_dtype(x, "x")
+        shape = self.shape = x.shape
+        if len(shape) not in (2, 3):
+            raise ValueError("x must have shape [rows, length, channels] or [rows, channels]")
+        dev, self.dtype = x.device, x.dtype
+        self.dev = dev
+        rows, channels = shape[0], shape[-1]
+        if not 1 <= channels <= RDF2V_MAX_NORM_CHANNELS:
+            raise ValueError(f"{channels} channels: 1 to {RDF2V_MAX_NORM_CHANNELS} are supported")
+        if residual is not None:
+            hidden_dtype = residual.dtype if isinstance(residual, torch.Tensor) else None
+        elif hidden_dtype is None:
+            hidden_dtype = x.dtype
+        if hidden_dtype not in (x.dtype, torch.float32):
+            raise TypeError(f"residual must be {x.dtype} or float32, got {hidden_dtype}")
+        if not 0.0 <= drop < 1.0 - 2.0 ** -32:
+            raise ValueError(f"drop must be in [0, 1), got {drop}")
+        if row_begin < 0:
+            raise ValueError("row_begin must not be negative")
+        self.hidden_dtype = hidden_dtype
+        self.views = (_tokens_view(x, "x", x.dtype, dev, shape),
+                      None if residual is None else _tokens_view(residual, "residual", hidden_dtype, dev, shape))
+        self.stats = (*shape[:-1], 2)
+        if weight is None:
+            raise TypeError("weight must be a CUDA (HIP) tensor")
+        if seed_offset is not None:
+            seed_offset = _out(seed_offset, "seed_offset", torch.int64, 1, dev).data_ptr()
+        each = (channels,)
+        self.c = _NormStruct(rows, shape[1] if len(shape) == 3 else 1, channels, dtype, _DTYPES[hidden_dtype],
+                             bool(center), eps, _parameter(weight, "weight", each, dev),
+                             _parameter(bias, "bias", each, dev), _parameter(scale, "scale", each, dev), drop,
+                             seed & 0xFFFFFFFFFFFFFFFF, seed_offset, row_begin, _lens(lens, rows, dev))
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, scale, seed_offset, lens, given, status, stream):
+        out, hidden, stats = rdf2v_residual_norm(x, residual, weight, bias, scale=scale, seed_offset=seed_offset,
+                                                 lens=lens, status=status, stream=stream, **given)
+        ctx.save_for_backward(x, residual, weight, bias, scale, seed_offset, lens, stats)
+        ctx.given = given
+        ctx.hidden_dtype = hidden.dtype
+        ctx.mark_non_differentiable(stats)
+        ctx.set_materialize_grads(False)
+        return out, hidden, stats
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dhidden, _):
+        x, residual, weight, bias, scale, seed_offset, lens, stats = ctx.saved_tensors
+        if dhidden is not None:
+            dhidden = _gradient(dhidden, None)
+        g = rdf2v_residual_norm_backward(x, residual, weight, bias, stats, _gradient(dout, (x.shape, x.dtype, x.device)),
+                                         dhidden=dhidden, scale=scale, seed_offset=seed_offset, lens=lens, **ctx.given)
+        return g.dx, g.dresidual, g.dweight, g.dbias, g.dscale, None, None, None, None, None
+
+
+def rdf2v_residual_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: torch.Tensor,
+                        bias: torch.Tensor | None = None, *, scale: torch.Tensor | None = None, drop: float = 0.0,
+                        seed: int = 0, seed_offset: torch.Tensor | None = None, row_begin: int = 0,
+                        center: bool = False, eps: float = 1e-5, lens: torch.Tensor | None = None,
+                        hidden_dtype: torch.dtype | None = None, out: torch.Tensor | None = None,
+                        hidden: torch.Tensor | None = None, stats: torch.Tensor | None = None,
+                        status: torch.Tensor | None = None, stream=None):
+    """Residual connection and norm of each token: hidden = residual + scale * dropout(x), out = weight * (hidden -
+    mean) / sqrt(mean of (hidden - mean)^2 + eps) + bias, the mean being taken off only where center is set.
+
+    x [rows, length, channels] (or [rows, channels]) is float32 or bfloat16, residual the same or float32, in any layout
+    whose last dimension is contiguous; None stands for zeros, and hidden is of residual's type (hidden_dtype, or x's,
+    without one). weight, bias and scale [channels] are float32. lens: int32 [rows], the tokens of each row that count.
+    Returns (out, hidden, stats): stats, float32 [..., 2], is for the backward call.
+
+    A share `drop` of x's values is dropped, by random words of (seed + seed_offset; row_begin + row, token, channel)
+    that are made where they are needed: nothing is stored, and the backward call, given the same, drops the same.
+    seed_offset: int64 [1] on the device, read by the kernels, so that a captured graph draws new masks when it is
+    changed.
+
+    Where an input requires gradients, autograd records out and hidden; they must then be left to the call, as in
+    torch's own functions."""
+    n = _Norm(x, residual, weight, bias, scale, drop, seed, seed_offset, row_begin, center, eps, lens, hidden_dtype)
+    dev = n.dev
+    if _records(x, residual, weight, bias, scale):
+        if out is not None or hidden is not None or stats is not None:
+            raise ValueError("out, hidden and stats cannot be given where autograd records the call: an input requires "
+                             "gradients")
+        given = dict(drop=drop, seed=seed, row_begin=row_begin, center=center, eps=eps, hidden_dtype=hidden_dtype)
+        return _ResidualNorm.apply(x, residual, weight, bias, scale, seed_offset, lens, given, status, stream)
+    with _on_stream(dev, stream) as h:
+        out = _new(out, "out", n.dtype, n.shape, dev)
+        hidden = _new(hidden, "hidden", n.hidden_dtype, n.shape, dev)
+        stats = _new(stats, "stats", torch.float32, n.stats, dev)
+        _status(status, dev)
+        st = _native().rdf2v_residual_norm(n.c, *n.views, _ptr(out), _ptr(hidden), _ptr(stats), _ptr(status), h)
+        _check(st, "rdf2v_residual_norm")
+        return out, hidden, stats
+
+
+def rdf2v_residual_norm_backward_workspace_size(rows: int, length: int, channels: int,
+                                                dtype: torch.dtype = torch.float32,
+                                                hidden_dtype: torch.dtype | None = None) -> int:
+    c = _NormStruct(rows, length, channels, _DTYPES.get(dtype, -1), _DTYPES.get(hidden_dtype or dtype, -1))
+    return int(_native().rdf2v_residual_norm_backward_workspace_size(c))
+
+
+def rdf2v_residual_norm_backward(x: torch.Tensor, residual: torch.Tensor | None, weight: torch.Tensor,
+                                 bias: torch.Tensor | None, stats: torch.Tensor, dout: torch.Tensor, *,
+                                 dhidden: torch.Tensor | None = None, scale: torch.Tensor | None = None,
+                                 drop: float = 0.0, seed: int = 0, seed_offset: torch.Tensor | None = None,
+                                 row_begin: int = 0, center: bool = False, eps: float = 1e-5,
+                                 lens: torch.Tensor | None = None, hidden_dtype: torch.dtype | None = None,
+                                 out: NormGradients | None = None, workspace: torch.Tensor | None = None,
+                                 status: torch.Tensor | None = None, stream=None) -> NormGradients:
+    """Gradients of rdf2v_residual_norm for its inputs, from dout (that of out), dhidden (that of hidden; None: zeros)
+    and the stats that it returned; the other arguments as there. `out`: tensors to write them to, with None for those
+    of inputs that are not given."""
+    n = _Norm(x, residual, weight, bias, scale, drop, seed, seed_offset, row_begin, center, eps, lens, hidden_dtype)
+    dev, f32, each = n.dev, torch.float32, weight.shape
+    with _on_stream(dev, stream) as h:
+        views = (_tokens_view(dout, "dout", n.dtype, dev, n.shape),
+                 None if dhidden is None else _tokens_view(dhidden, "dhidden", n.hidden_dtype, dev, n.shape))
+        _exact(stats, "stats", f32, n.stats, dev)
+        given = (None,) * 5 if out is None else out
+        wanted = ((True, n.dtype, n.shape), (residual is not None, n.hidden_dtype, n.shape), (True, f32, each),
+                  (bias is not None, f32, each), (scale is not None, f32, each))
+        g = NormGradients(*[_new(t, name, type_, shape, dev) if want or t is not None else None
+                            for t, name, (want, type_, shape) in zip(given, NormGradients._fields, wanted)])
+        _status(status, dev)
+        lib = _native()
+        if workspace is None:
+            workspace = _workspace(lib.rdf2v_residual_norm_backward_workspace_size(n.c), dev)
+        st = lib.rdf2v_residual_norm_backward(n.c, *n.views, _ptr(stats), *views, _ptr(g.dx), _ptr(g.dresidual),
+                                              _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dscale), _ptr(workspace),
+                                              _ws_bytes(workspace), _ptr(status), h)
+        _check(st, "rdf2v_residual_norm_backward")
+        return g
 
 
 def check_device_status(status: torch.Tensor, where: str = "device", stream=None) -> None:

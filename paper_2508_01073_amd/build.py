@@ -16,7 +16,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librdf2v.so")
 SOURCES = ["api.hip", "csr_build.hip", "random_walk.hip", "walk_edges.hip", "skipgram.hip", "unique_walks.hip", "bfs_walks.hip",
-           "vocab.hip", "noalloc.hip", "model_api.hip", "decay_attention.hip", "beam.hip", "distill.hip"]
+           "vocab.hip", "noalloc.hip", "model_api.hip", "decay_attention.hip", "beam.hip", "distill.hip", "layer_api.hip", "causal_conv.hip", "selective_scan.hip",
+           "residual_norm.hip", "part_sums.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

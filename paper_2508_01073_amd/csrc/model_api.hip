@@ -2,28 +2,12 @@
 // checks, then the launchers. The declarations, argument meanings and error
 // behaviour are in rdf2v.h.
 
-#include <climits>
-#include <cmath>
-#include <initializer_list>
-#include <utility>
-
+#include "checks.hpp"
 #include "model.hpp"
 
+using namespace rdf2v;
+
 namespace {
-
-constexpr int64_t kInt32Limit = int64_t(1) << 31;
-// Most elements of one array of a call: keeps every byte offset and size exact
-// in 64 bits, and is far beyond any device memory.
-constexpr int64_t kMaxElements = int64_t(1) << 56;
-constexpr int64_t kMaxStride = int64_t(1) << 56;
-
-bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-
-bool dtype_ok(int32_t dtype) { return dtype == RDF2V_F32 || dtype == RDF2V_BF16; }
-size_t dtype_size(int32_t dtype) { return dtype == RDF2V_BF16 ? 2 : 4; }
-
-// a * b for non-negative a and b, at most `most`; -1 beyond.
-int64_t product(int64_t a, int64_t b, int64_t most) { return a >= 0 && (b == 0 || a <= most / b) ? a * b : -1; }
 
 rdf2v_status check_sizes(const rdf2v_attention *a, bool step) {
   if (a == nullptr || a->rows < 0 || (!step && a->length < 0)) return RDF2V_ERR_INVALID_ARGUMENT;
@@ -48,89 +32,6 @@ rdf2v_status check_attention(const rdf2v_attention *a, bool step) {
   return RDF2V_OK;
 }
 
-bool stride_ok(int64_t s) { return s > -kMaxStride && s < kMaxStride; }
-
-bool view_ok(const rdf2v_heads_view *v, int32_t dtype, bool empty) {
-  if (v == nullptr) return false;
-  if (!stride_ok(v->row_stride) || !stride_ok(v->token_stride) || !stride_ok(v->head_stride)) return false;
-  return (empty || v->data != nullptr) && aligned(v->data, dtype_size(dtype));
-}
-
-rdf2v_status check_workspace(const void *workspace, size_t bytes, size_t need) {
-  if (need == 0) return RDF2V_OK;
-  return workspace == nullptr || bytes < need || !aligned(workspace, 256) ? RDF2V_ERR_WORKSPACE : RDF2V_OK;
-}
-
-// Whether [a, a + an) and [b, b + bn) share a byte.
-bool overlap(const void *a, size_t an, const void *b, size_t bn) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x <= y ? y - x < an : x - y < bn;
-}
-
-// An array of a call: where it lies, of how many bytes. Null or empty: it overlaps nothing.
-struct Span {
-  const void *data;
-  size_t bytes;
-};
-bool overlap(const Span &a, const Span &b) {
-  return a.data != nullptr && b.data != nullptr && a.bytes != 0 && b.bytes != 0 &&
-         overlap(a.data, a.bytes, b.data, b.bytes);
-}
-bool same(const Span &a, const Span &b) { return a.data == b.data; }
-
-// The bytes of a view as boxes inside boxes: count[i] boxes every step[i] bytes, those of the last level
-// `bytes` long.
-struct Boxes {
-  __int128 step[3];
-  int64_t count[3];
-  __int128 bytes;
-};
-
-// Whether boxes of the levels from `level` on, the first of them at byte `at`, have a byte in [lo, hi).
-bool boxes_reach(const Boxes &x, int level, __int128 at, __int128 lo, __int128 hi) {
-  if (level == 3) return at < hi && at + x.bytes > lo;
-  if (x.count[level] == 1) return boxes_reach(x, level + 1, at, lo, hi);
-  __int128 size = x.bytes;  // from a box's first byte to its last
-  for (int i = level + 1; i < 3; ++i) size += x.step[i] * (x.count[i] - 1);
-  const __int128 all = size + x.step[level] * (x.count[level] - 1);
-  if (at >= hi || at + all <= lo) return false;
-  if (x.step[level] < size) return true;  // the boxes lie in one another: taken as one
-  // Of the boxes that reach into the interval all but the first and the last lie in it.
-  const __int128 first = at >= lo ? 0 : (lo - at) / x.step[level];
-  __int128 last = (hi - 1 - at) / x.step[level];
-  if (last > x.count[level] - 1) last = x.count[level] - 1;
-  if (last - first > 1) return true;
-  for (__int128 i = first; i <= last; ++i)
-    if (boxes_reach(x, level + 1, at + i * x.step[level], lo, hi)) return true;
-  return false;
-}
-
-// Whether a view of rows x tokens x heads of `size` values has a byte in an array. What lies between a view's
-// values is not its own: another slice of the projection, say.
-bool overlap(const rdf2v_heads_view &v, const rdf2v_attention &a, int heads, int size, const Span &out) {
-  if (out.data == nullptr || out.bytes == 0 || a.rows == 0 || a.length == 0) return false;
-  const int64_t value = int64_t(dtype_size(a.dtype));
-  const int64_t strides[3] = {v.row_stride, v.token_stride, v.head_stride}, counts[3] = {a.rows, a.length, heads};
-  Boxes x{};
-  x.bytes = __int128(size) * value;
-  __int128 at = __int128(reinterpret_cast<uintptr_t>(v.data));
-  for (int i = 0; i < 3; ++i) {
-    const __int128 step = __int128(strides[i]) * value;
-    if (step < 0) at += step * (counts[i] - 1);  // from the lowest byte upwards
-    x.step[i] = step < 0 ? -step : step;
-    x.count[i] = step == 0 ? 1 : counts[i];
-    if (x.count[i] == 1) x.step[i] = 0;
-  }
-  for (int i = 0; i < 2; ++i)  // the widest first
-    for (int j = 0; j < 2 - i; ++j)
-      if (x.step[j] < x.step[j + 1]) {
-        std::swap(x.step[j], x.step[j + 1]);
-        std::swap(x.count[j], x.count[j + 1]);
-      }
-  const __int128 lo = __int128(reinterpret_cast<uintptr_t>(out.data));
-  return boxes_reach(x, 0, at, lo, lo + __int128(out.bytes));
-}
-
 size_t state_bytes(const rdf2v_attention &a) { return size_t(a.rows) * a.heads * a.dk * a.dv * 4; }
 size_t head_bytes(const rdf2v_attention &a, int heads, int size) {
   return size_t(a.rows) * a.length * heads * size * dtype_size(a.dtype);
@@ -138,8 +39,9 @@ size_t head_bytes(const rdf2v_attention &a, int heads, int size) {
 
 // Whether a view has a byte in one of the outputs.
 bool reads(const rdf2v_heads_view &v, const rdf2v_attention &a, int heads, int size, std::initializer_list<Span> outs) {
+  const ViewBoxes boxes(v, a.rows, a.length, heads, size, a.dtype);
   for (const Span &out : outs)
-    if (overlap(v, a, heads, size, out)) return true;
+    if (boxes.reach(out)) return true;
   return false;
 }
 

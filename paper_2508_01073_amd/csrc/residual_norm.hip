@@ -1,0 +1,457 @@
+// Residual connection, dropout and norm on gfx950, and their gradients.
+//
+// hidden = residual + scale * dropout(x), out = weight * (hidden - mean) / std + bias: HBM-bound, the floor is
+// each array read or written once. A token's channels stay in the registers of a team of threads between the
+// sums and what needs them; a team takes tokens in turn and holds the parameters, and in the gradients their
+// sums, in registers too. The dropout mask is made from counters where it is needed and never stored: ten
+// rounds for four channels, in the shadow of the loads.
+//
+// Gradients are computed from x and residual again, not from hidden as it was rounded: the parameters'
+// gradients have 32 bits, and would have lost them.
+
+#include "vectors.hpp"
+
+#include "layer.hpp"
+#include "logits.hpp"
+
+namespace rdf2v {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int V = 4;  // channels of a vector: what a block of the generator serves
+
+struct Norm {
+  const void *x, *residual, *dout, *dhidden;
+  void *out, *hidden;  // dx and dresidual in the gradients
+  const float *weight, *bias, *scale, *stats_in;
+  float *stats, *partial;
+  const int32_t *len;
+  const int64_t *seed_offset;
+  int32_t *status;
+  int64_t x_row, x_token, residual_row, residual_token, dout_row, dout_token, dhidden_row, dhidden_token;
+  int64_t length, tokens, row_begin, workgroups;
+  uint64_t seed;
+  int32_t channels;
+  uint32_t threshold;
+  float keep, eps;
+};
+
+// Four words of Philox4x32-10 (Salmon, Moraes, Dror & Shaw, SC'11).
+struct Words4 {
+  uint32_t w[4];
+};
+__device__ __forceinline__ Words4 philox(uint32_t x0, uint32_t x1, uint64_t row, uint64_t key) {
+  uint32_t x2 = uint32_t(row), x3 = uint32_t(row >> 32), k0 = uint32_t(key), k1 = uint32_t(key >> 32);
+#pragma unroll
+  for (int round = 0; round < 10; ++round) {
+    const uint64_t a = uint64_t(x0) * 0xD2511F53u, b = uint64_t(x2) * 0xCD9E8D57u;
+    x0 = uint32_t(b >> 32) ^ x1 ^ k0;
+    x1 = uint32_t(b);
+    x2 = uint32_t(a >> 32) ^ x3 ^ k1;
+    x3 = uint32_t(a);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return {{x0, x1, x2, x3}};
+}
+
+// Sums over a team of TEAM threads, in each of them. Teams of more than a wave: a barrier, `scratch` of a sum
+// for each wave and two calls before it is used again.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sum(float (&x)[N], float (*scratch)[N]) {
+  if constexpr (TEAM < kWave) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int m = TEAM / 2; m > 0; m /= 2) x[i] += __shfl_xor(x[i], m, kWave);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
+    if constexpr (TEAM > kWave) {
+      if (lane_id() == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) scratch[threadIdx.x / kWave][i] = x[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        x[i] = scratch[0][i];
+        for (int w = 1; w < TEAM / kWave; ++w) x[i] += scratch[w][i];
+      }
+    }
+  }
+}
+
+// What of a token's channels a thread has: vectors lane, lane + TEAM, ...
+template <int TEAM, int PER>
+struct Own {
+  int lane;
+  int channels;
+  __device__ __forceinline__ int at(int i) const { return (lane + i * TEAM) * V; }
+  __device__ __forceinline__ int count(int i) const { return min(V, channels - at(i)); }  // 0 or less: nothing there
+};
+
+template <class T, int TEAM, int PER>
+__device__ __forceinline__ void load_token(const T *p, const Own<TEAM, PER> &own, float (&x)[PER][V]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) load_values<T, V>(p + own.at(i), own.count(i), x[i]);
+}
+template <class T, int TEAM, int PER>
+__device__ __forceinline__ void store_token(T *p, const Own<TEAM, PER> &own, const float (&x)[PER][V]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) store_values<T, V>(p + own.at(i), own.count(i), x[i]);
+}
+
+// x after dropout, and the factors that it was multiplied with (0: dropped, whatever x holds).
+template <bool DROP, int TEAM, int PER>
+__device__ __forceinline__ void dropout(const Norm &a, const Own<TEAM, PER> &own, int64_t row, int64_t token,
+                                        uint64_t key, float (&x)[PER][V], uint64_t &kept) {
+  kept = ~uint64_t(0);
+  if constexpr (DROP) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const Words4 r = philox(uint32_t(own.at(i) / V), uint32_t(token + 1), uint64_t(a.row_begin + row), key);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const bool keep = r.w[j] >= a.threshold;
+        x[i][j] = keep ? x[i][j] * a.keep : 0.0f;
+        if (!keep) kept &= ~(uint64_t(1) << (i * V + j));
+      }
+    }
+  }
+}
+
+constexpr int workgroup_of(int team) { return team < kThreads ? kThreads : team; }
+
+template <class T, class R, bool DROP, bool CENTER, int TEAM, int PER>
+__global__ __launch_bounds__(workgroup_of(TEAM)) void norm_kernel(Norm a) {
+  constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
+  __shared__ float scratch[2][kBlock / kWave][1];
+  const Own<TEAM, PER> own{int(threadIdx.x) % TEAM, a.channels};
+  const uint64_t key = a.seed + (DROP && a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
+  const float inverse = 1.0f / float(a.channels);
+  float weight[PER][V];
+  load_token(a.weight, own, weight);
+  int turn = 0;
+  for (int64_t at = int64_t(blockIdx.x) * kTeams; at < a.tokens; at += a.workgroups * kTeams) {
+    // a team without a token goes along: it has lanes in common with those that have one
+    const bool mine = at + int(threadIdx.x) / TEAM < a.tokens;
+    const int64_t id = mine ? at + int(threadIdx.x) / TEAM : a.tokens - 1;
+    const int64_t row = id / a.length, token = id % a.length;
+    const bool live = token < row_length(a.len, row, a.length, mine && token == 0 && own.lane == 0, a.status);
+    float h[PER][V] = {};
+    if (live) {
+      load_token(static_cast<const T *>(a.x) + row * a.x_row + token * a.x_token, own, h);
+      float from[PER][V] = {};
+      if (a.residual != nullptr)
+        load_token(static_cast<const R *>(a.residual) + row * a.residual_row + token * a.residual_token, own, from);
+      uint64_t kept;
+      dropout<DROP>(a, own, row, token, key, h, kept);
+      if (a.scale != nullptr) {
+        float scale[PER][V];
+        load_token(a.scale, own, scale);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+          for (int j = 0; j < V; ++j) h[i][j] *= scale[i][j];
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[i][j] += from[i][j];
+    }
+    if (mine && a.hidden != nullptr) store_token(static_cast<R *>(a.hidden) + id * a.channels, own, h);
+    float mean = 0.0f, sum[1] = {0.0f};
+    if constexpr (CENTER) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[0] += h[i][j];
+      team_sum<TEAM>(sum, scratch[turn]);
+      turn ^= 1;
+      mean = sum[0] * inverse;
+      sum[0] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[i][j] = j < own.count(i) ? h[i][j] - mean : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] = fmaf(h[i][j], h[i][j], sum[0]);
+    team_sum<TEAM>(sum, scratch[turn]);
+    turn ^= 1;
+    const float inv = live ? 1.0f / sqrtf(fmaf(sum[0], inverse, a.eps)) : 0.0f;
+    if (!mine) continue;
+    if (a.stats != nullptr && own.lane == 0) {
+      a.stats[2 * id] = mean;
+      a.stats[2 * id + 1] = inv;
+    }
+    if (live) {
+      float bias[PER][V] = {};
+      if (a.bias != nullptr) load_token(a.bias, own, bias);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[i][j] = fmaf(h[i][j] * inv, weight[i][j], bias[i][j]);
+    }
+    store_token(static_cast<T *>(a.out) + id * a.channels, own, h);
+  }
+}
+
+// The teams' sums of one parameter's gradient, in order, to the workgroup's part.
+template <int TEAM, int PER>
+__device__ __forceinline__ void store_part(float *part, const Own<TEAM, PER> &own, const float (&x)[PER][V],
+                                           float (*scratch)[V]) {
+  constexpr int kTeams = workgroup_of(TEAM) / TEAM;
+  if constexpr (kTeams == 1) {
+    store_token(part, own, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < V; ++j) scratch[threadIdx.x][j] = x[i][j];
+      __syncthreads();
+      if (threadIdx.x >= TEAM) continue;
+      float sum[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        sum[j] = x[i][j];
+        for (int t = 1; t < kTeams; ++t) sum[j] += scratch[t * TEAM + threadIdx.x][j];
+      }
+      store_values<float, V>(part + own.at(i), own.count(i), sum);
+    }
+  }
+}
+
+// With n = (hidden - mean) / std and dn = dout * weight, a token's gradient is
+//   dhidden + (dn - n mean(dn n) - mean(dn)) / std        (the last mean where the norm is centred)
+// MORE: there is a scale, or gradients of the bias or the scale are wanted.
+template <class T, class R, bool DROP, bool CENTER, bool MORE, int TEAM, int PER>
+__global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm a) {
+  constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
+  __shared__ float scratch[2][kBlock / kWave][2];
+  __shared__ float parts[kTeams > 1 ? kBlock : 1][V];
+  const Own<TEAM, PER> own{int(threadIdx.x) % TEAM, a.channels};
+  const uint64_t key = a.seed + (DROP && a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
+  const float inverse = 1.0f / float(a.channels);
+  float weight[PER][V], scale[PER][V];
+  load_token(a.weight, own, weight);
+  if (MORE && a.scale != nullptr) {
+    load_token(a.scale, own, scale);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) scale[i][j] = 1.0f;
+  }
+  float dweight[PER][V] = {}, dbias[PER][V] = {}, dscale[PER][V] = {};
+  int turn = 0;
+  for (int64_t at = int64_t(blockIdx.x) * kTeams; at < a.tokens; at += a.workgroups * kTeams) {
+    const bool mine = at + int(threadIdx.x) / TEAM < a.tokens;
+    const int64_t id = mine ? at + int(threadIdx.x) / TEAM : a.tokens - 1;
+    const int64_t row = id / a.length, token = id % a.length;
+    const bool live =
+        token < row_length(a.len, row, a.length, mine && token == 0 && own.lane == 0, a.status) && mine;
+    float x[PER][V] = {}, h[PER][V] = {}, d[PER][V] = {}, dh[PER][V] = {};
+    uint64_t kept = 0;
+    float inv = 0.0f, sums[2] = {0.0f, 0.0f};
+    if (live) {
+      load_token(static_cast<const T *>(a.x) + row * a.x_row + token * a.x_token, own, x);
+      if (a.residual != nullptr)
+        load_token(static_cast<const R *>(a.residual) + row * a.residual_row + token * a.residual_token, own, h);
+      load_token(static_cast<const T *>(a.dout) + row * a.dout_row + token * a.dout_token, own, d);
+      if (a.dhidden != nullptr)
+        load_token(static_cast<const R *>(a.dhidden) + row * a.dhidden_row + token * a.dhidden_token, own, dh);
+      const float mean = CENTER ? a.stats_in[2 * id] : 0.0f;
+      inv = a.stats_in[2 * id + 1];
+      dropout<DROP>(a, own, row, token, key, x, kept);
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float n = ((MORE ? x[i][j] * scale[i][j] : x[i][j]) + h[i][j] - mean) * inv;
+          h[i][j] = n;
+          dweight[i][j] = fmaf(d[i][j], n, dweight[i][j]);
+          if (MORE) dbias[i][j] += d[i][j];
+          d[i][j] *= weight[i][j];
+          if (j < own.count(i)) sums[0] = fmaf(d[i][j], n, sums[0]);
+          if (CENTER) sums[1] += d[i][j];
+        }
+    }
+    if constexpr (CENTER) {
+      team_sum<TEAM>(sums, scratch[turn]);
+    } else {
+      float one[1] = {sums[0]};
+      team_sum<TEAM>(one, reinterpret_cast<float(*)[1]>(&scratch[turn][0][0]));
+      sums[0] = one[0];
+    }
+    turn ^= 1;
+    if (!mine) continue;
+    if (live) {
+      const float along = sums[0] * inverse, level = CENTER ? sums[1] * inverse : 0.0f;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float g = fmaf(d[i][j] - fmaf(h[i][j], along, level), inv, dh[i][j]);
+          dh[i][j] = g;
+          if (MORE) dscale[i][j] = fmaf(g, x[i][j], dscale[i][j]);
+          d[i][j] = MORE ? g * scale[i][j] : g;
+          if (DROP) d[i][j] = kept >> (i * V + j) & 1 ? d[i][j] * a.keep : 0.0f;
+        }
+    }
+    store_token(static_cast<T *>(a.out) + id * a.channels, own, d);
+    if (a.hidden != nullptr) store_token(static_cast<R *>(a.hidden) + id * a.channels, own, dh);
+  }
+  float *part = a.partial + int64_t(blockIdx.x) * a.channels * (MORE ? 3 : 1);
+  store_part(part, own, dweight, parts);
+  if constexpr (MORE) {
+    store_part(part + a.channels, own, dbias, parts);
+    store_part(part + 2 * a.channels, own, dscale, parts);
+  }
+}
+
+// Calls launch with constants for the size of a team and the vectors of a thread: the fewest threads that leave
+// each at most four vectors.
+template <class Launch>
+rdf2v_status with_team(int channels, Launch launch) {
+#define RDF2V_TEAM(TEAM, PER) \
+  if (channels <= TEAM * PER * V) return launch(std::integral_constant<int, TEAM>{}, std::integral_constant<int, PER>{});
+  RDF2V_TEAM(16, 1)
+  RDF2V_TEAM(64, 1)
+  RDF2V_TEAM(64, 2)
+  RDF2V_TEAM(64, 4)
+  RDF2V_TEAM(256, 2)
+  RDF2V_TEAM(256, 4)
+  RDF2V_TEAM(1024, 2)
+  RDF2V_TEAM(1024, 4)
+#undef RDF2V_TEAM
+  return RDF2V_ERR_INVALID_ARGUMENT;
+}
+
+template <class Launch>
+rdf2v_status with_types(int dtype, int residual_dtype, Launch launch) {
+  if (dtype == RDF2V_F32) return launch(float{}, float{});
+  if (residual_dtype == RDF2V_F32) return launch(bf16{}, float{});
+  return launch(bf16{}, bf16{});
+}
+
+template <class Launch>
+rdf2v_status with_flag(bool flag, Launch launch) {
+  return flag ? launch(std::true_type{}) : launch(std::false_type{});
+}
+
+int teams_of_workgroup(int channels) {
+  int teams = 1;
+  with_team(channels, [&](auto team, auto) {
+    teams = workgroup_of(team()) / team();
+    return RDF2V_OK;
+  });
+  return teams;
+}
+
+// Workgroups that fill the chip, each with tokens to hold the parameters for.
+int64_t workgroups_of(int64_t tokens, int channels, int64_t most) {
+  const int64_t teams = teams_of_workgroup(channels);
+  return std::max<int64_t>(1, std::min((tokens + teams - 1) / teams, most));
+}
+constexpr int64_t kForward = 2048, kBackward = 1024;
+
+Norm base(const rdf2v_norm &a, const rdf2v_tokens_view &x, const rdf2v_tokens_view &residual, int32_t *status) {
+  Norm n{};
+  n.x = x.data;
+  n.x_row = x.row_stride;
+  n.x_token = x.token_stride;
+  n.residual = residual.data;
+  n.residual_row = residual.row_stride;
+  n.residual_token = residual.token_stride;
+  n.weight = a.weight;
+  n.bias = a.bias;
+  n.scale = a.scale;
+  n.len = a.len;
+  n.seed_offset = a.seed_offset;
+  n.status = status;
+  n.length = a.length;
+  n.tokens = a.rows * a.length;
+  n.row_begin = a.row_begin;
+  n.seed = a.seed;
+  n.channels = a.channels;
+  n.threshold = uint32_t(std::nearbyint(a.drop * 0x1p32));
+  n.keep = float(1.0 / (1.0 - a.drop));
+  n.eps = a.eps;
+  return n;
+}
+
+}  // namespace
+
+size_t residual_norm_backward_workspace_bytes(const rdf2v_norm &a) {
+  if (a.rows == 0 || a.length == 0) return 0;
+  return align_up(size_t(workgroups_of(a.rows * a.length, a.channels, kBackward)) * a.channels * 3 * sizeof(float),
+                  256);
+}
+
+rdf2v_status launch_residual_norm(const rdf2v_norm &a, const rdf2v_tokens_view &x, const rdf2v_tokens_view &residual,
+                                  void *out, void *hidden, float *stats, int32_t *status_dev, hipStream_t stream) {
+  Norm n = base(a, x, residual, status_dev);
+  n.out = out;
+  n.hidden = hidden;
+  n.stats = stats;
+  n.workgroups = workgroups_of(n.tokens, a.channels, kForward);
+  return with_types(a.dtype, a.residual_dtype, [&](auto t, auto r) {
+    return with_flag(n.threshold != 0, [&](auto drop) {
+      return with_flag(a.center != 0, [&](auto center) {
+        return with_team(a.channels, [&](auto team, auto per) {
+          norm_kernel<decltype(t), decltype(r), drop(), center(), team(), per()>
+              <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
+          RDF2V_LAUNCH_CHECK();
+          return RDF2V_OK;
+        });
+      });
+    });
+  });
+}
+
+rdf2v_status launch_residual_norm_backward(const rdf2v_norm &a, const rdf2v_tokens_view &x,
+                                           const rdf2v_tokens_view &residual, const float *stats,
+                                           const rdf2v_tokens_view &dout, const rdf2v_tokens_view &dhidden, void *dx,
+                                           void *dresidual, float *dweight, float *dbias, float *dscale,
+                                           void *workspace, int32_t *status_dev, hipStream_t stream) {
+  Norm n = base(a, x, residual, status_dev);
+  n.stats_in = stats;
+  n.dout = dout.data;
+  n.dout_row = dout.row_stride;
+  n.dout_token = dout.token_stride;
+  n.dhidden = dhidden.data;
+  n.dhidden_row = dhidden.row_stride;
+  n.dhidden_token = dhidden.token_stride;
+  n.out = dx;
+  n.hidden = dresidual;
+  n.partial = static_cast<float *>(workspace);
+  n.workgroups = n.tokens > 0 ? workgroups_of(n.tokens, a.channels, kBackward) : 0;
+  const bool more = a.scale != nullptr || dbias != nullptr || dscale != nullptr;
+  if (n.tokens > 0) {
+    const rdf2v_status st = with_types(a.dtype, a.residual_dtype, [&](auto t, auto r) {
+      return with_flag(n.threshold != 0, [&](auto drop) {
+        return with_flag(a.center != 0, [&](auto center) {
+          return with_flag(more, [&](auto has) {
+            return with_team(a.channels, [&](auto team, auto per) {
+              norm_backward_kernel<decltype(t), decltype(r), drop(), center(), has(), team(), per()>
+                  <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
+              RDF2V_LAUNCH_CHECK();
+              return RDF2V_OK;
+            });
+          });
+        });
+      });
+    });
+    if (st != RDF2V_OK) return st;
+  }
+  const int64_t rest = more ? a.channels : 0;
+  const rdf2v_status st =
+      launch_part_sums({n.partial, n.workgroups, {a.channels, rest, rest}, {dweight, dbias, dscale}}, stream);
+  return st;
+}
+
+}  // namespace rdf2v
