@@ -5,11 +5,10 @@
 // for every channel by itself: per token, channel and state one exponential and three multiply-adds, so with 16
 // states vector instructions bound it, the exponentials (a quarter of the rate) half of them; memory comes next.
 //
-// A workgroup takes 64 channels (a lane each) of a row, or of a segment of it, 16 tokens at a time. The channels'
-// states are dealt to its four waves: what is made of a token once (delta and delta x) goes through LDS to all of
-// them, and their parts of y come back the same way. A wave takes its states in turn, each through the chunk's 16
-// tokens, whose values stay in registers meanwhile: the number of states is a loop's, not a register file's.
-// b and c of the chunk lie in LDS and are read by all lanes at once.
+// A wave takes 64 channels (a lane each) of a row, or of a segment of it, 16 tokens at a time, and nothing is
+// shared with other waves: no barrier, no value made twice. It takes the channels' states in turn, each through
+// the chunk's 16 tokens, whose values stay in registers meanwhile: the number of states is a loop's, not a
+// register file's. b and c of the chunk lie in LDS and are read by all lanes at once.
 //
 // Rows too few to fill the chip are cut into segments: every segment's state from zeros (scan_states_kernel), the
 // states' way through the segments (scan_join_kernel), then all segments at once. That costs the exponentials
@@ -17,7 +16,7 @@
 //
 // Gradients go backwards through the chunks: a chunk's states are made again from the one before it, which
 // scan_states_kernel has left in memory, and stay in registers for the way back. The sums over states (for x and
-// dt) are a lane's own; the sums over channels (for b and c) are taken by matrix instructions, see channel_sums.
+// dt) are a lane's own; the sums over channels (for b and c) are taken by matrix instructions, see ChannelSums.
 
 #include "vectors.hpp"
 
@@ -28,8 +27,7 @@ namespace rdf2v {
 namespace {
 
 constexpr int kTokens = 16;  // of a chunk
-constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kOwn = kTokens / kWaves;  // tokens of a chunk that a wave prepares and finishes
+constexpr int kThreads = 256;  // of a workgroup where waves need not be alone
 
 struct Scan {
   rdf2v_tokens_view x, dt, gate, dout;
@@ -49,8 +47,9 @@ struct Scan {
   float *bc;      // [blocks of a group][rows][length][groups][2 states]: parts of the gradients of b and c
   int64_t rows, length, num_states;
   int64_t segments, segment, chunks;  // segments of a row, tokens of a segment, chunks of a row
-  int64_t blocks, parts;              // workgroups side by side in a group's channels; gradients: along rows and segments
+  int64_t blocks, parts;              // waves side by side in a group's channels, and along rows and segments
   int32_t channels, groups, states, per_group;
+  uint32_t by_states;                 // 2^16 / states, rounded up: i / states = i by_states / 2^16 for i < 1024
 };
 
 // The part of the work that a workgroup has.
@@ -68,7 +67,9 @@ __device__ __forceinline__ Place place_of(const Scan &p, int64_t column, int64_t
   w.seg = row_and_seg % p.segments;
   w.c0 = w.group * p.per_group + int32_t(w.block) * kWave;
   w.count = min(int32_t(kWave), p.per_group - int32_t(w.block) * kWave);
-  const int64_t length = row_length(p.len, w.row, p.length, report && column == 0 && w.seg == 0, p.status);
+  // the same in all lanes, and the compiler is to know
+  const int64_t length = __builtin_amdgcn_readfirstlane(
+      int32_t(row_length(p.len, w.row, p.length, report && column == 0 && w.seg == 0, p.status)));
   w.begin = w.seg * p.segment;
   w.end = min(w.begin + p.segment, p.length);
   w.stop = max(w.begin, min(w.end, length));
@@ -96,278 +97,318 @@ __device__ __forceinline__ float checked_rate(float a, int32_t *status) {
   return 0.0f;
 }
 
+// put(i, load(i)) for i = 0 .. count - 1, eight loads in flight at a time.
+template <class Load, class Put>
+__device__ __forceinline__ void in_batches(int count, Load load, Put put) {
+  constexpr int kBatch = 8;
+  for (int first = 0; first < count; first += kBatch) {
+    decltype(load(0)) x[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) x[k] = load(min(first + k, count - 1));
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k)
+      if (first + k < count) put(first + k, x[k]);
+  }
+}
+
 // The rates over ln 2, [states][64], and zeros for channels that are not there.
 __device__ __forceinline__ void load_rates(const Scan &p, const Place &w, float *rates, bool report) {
-  for (int i = threadIdx.x; i < kWave * p.states; i += kThreads) {
-    const int channel = i / p.states, n = i % p.states;
-    rates[n * kWave + channel] =
-        channel < w.count
-            ? checked_rate(p.a[int64_t(w.c0) * p.states + i], report ? p.status : nullptr) * kLog2e
-            : 0.0f;
-  }
+  const float *from = p.a + int64_t(w.c0) * p.states;
+  in_batches(
+      p.states, [&](int k) { return from[min(k * kWave + int(threadIdx.x), w.count * p.states - 1)]; },
+      [&](int k, float a) {
+        const int i = k * kWave + threadIdx.x, channel = i / p.states, n = i - channel * p.states;
+        rates[n * kWave + channel] =
+            channel < w.count ? checked_rate(a, report ? p.status : nullptr) * kLog2e : 0.0f;
+      });
 }
 
 // States [channels][states] of memory from or to [states][64]; null: zeros.
 __device__ __forceinline__ void load_states(const Scan &p, const Place &w, const float *from, float *to) {
-  for (int i = threadIdx.x; i < kWave * p.states; i += kThreads) {
-    const int channel = i / p.states, n = i % p.states;
-    to[n * kWave + channel] = from != nullptr && channel < w.count
-                                  ? from[(w.row * p.channels + w.c0) * p.states + i]
-                                  : 0.0f;
+  if (from == nullptr) {
+    for (int n = 0; n < p.states; ++n) to[n * kWave + threadIdx.x] = 0.0f;
+    return;
   }
+  from += (w.row * p.channels + w.c0) * p.states;
+  in_batches(
+      p.states, [&](int k) { return from[min(k * kWave + int(threadIdx.x), w.count * p.states - 1)]; },
+      [&](int k, float h) {
+        const int i = k * kWave + threadIdx.x, channel = i / p.states, n = i - channel * p.states;
+        to[n * kWave + channel] = channel < w.count ? h : 0.0f;
+      });
 }
 __device__ __forceinline__ void store_states(const Scan &p, const Place &w, const float *from, float *to) {
-  for (int i = threadIdx.x; i < w.count * p.states; i += kThreads)
+  for (int i = threadIdx.x; i < w.count * p.states; i += kWave)
     to[(w.row * p.channels + w.c0) * p.states + i] = from[i % p.states * kWave + i / p.states];
 }
-
-// A wave's tokens of a chunk, the lane's channel: values in flight as they lie in memory.
-template <class T>
-struct Ahead {
-  T v[kOwn];
-  __device__ __forceinline__ void load(const rdf2v_tokens_view &view, const Place &w, int64_t t0, int wave, int lane) {
-    const T *at = static_cast<const T *>(view.data) + w.row * view.row_stride + w.c0 + lane;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int64_t t = t0 + wave * kOwn + i;
-      v[i] = T(0.0f);
-      if (t < w.stop && lane < w.count) v[i] = at[t * view.token_stride];
-    }
-  }
-};
-
-// b or c of a chunk: a thread's values in flight, then [states][16] in LDS; zeros for tokens that do not count.
-template <class T, int NMAX>
-struct AheadHeads {
-  static constexpr int kEach = kTokens * NMAX / kThreads;
-  T v[kEach];
-  __device__ __forceinline__ void load(const Scan &p, const rdf2v_heads_view &view, const Place &w, int64_t t0) {
-    const T *at = static_cast<const T *>(view.data) + w.row * view.row_stride + w.group * view.head_stride;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int i = threadIdx.x + k * kThreads, token = i / p.states, n = i % p.states;
-      v[k] = T(0.0f);
-      if (token < kTokens && t0 + token < w.stop) v[k] = at[(t0 + token) * view.token_stride + n];
-    }
-  }
-  __device__ __forceinline__ void put(const Scan &p, float *lds) const {
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int i = threadIdx.x + k * kThreads, token = i / p.states, n = i % p.states;
-      if (token < kTokens) lds[n * kTokens + token] = to_f32(v[k]);
-    }
-  }
-};
-
-// A lane's values of a chunk's tokens, [16][64] in LDS.
-__device__ __forceinline__ void read_tokens(const float (*lds)[kWave], int lane, float (&x)[kTokens]) {
-#pragma unroll
-  for (int t = 0; t < kTokens; ++t) x[t] = lds[t][lane];
+// The same of the workspace, [states][channels].
+__device__ __forceinline__ void load_carry(const Scan &p, const Place &w, const float *from, int channel, float *to) {
+  in_batches(
+      p.states, [&](int n) { return from[int64_t(n) * p.channels + channel]; },
+      [&](int n, float h) { to[n * kWave + threadIdx.x] = int(threadIdx.x) < w.count ? h : 0.0f; });
 }
+
+// A chunk's work is written for N = 4, 8, 12 or 16 tokens, the fewest that hold those that count: rows of a few
+// tokens leave most of a chunk out, and no token has a branch of its own.
+template <class Chunk>
+__device__ __forceinline__ void with_tokens(int count, Chunk chunk) {
+  if (count > 12)
+    chunk(std::integral_constant<int, 16>{});
+  else if (count > 8)
+    chunk(std::integral_constant<int, 12>{});
+  else if (count > 4)
+    chunk(std::integral_constant<int, 8>{});
+  else
+    chunk(std::integral_constant<int, 4>{});
+}
+
+// The lane's channel of a chunk's first `count` tokens; what follows is the last of them again. Addresses are made
+// one after the other: all at once they would not fit the scalar registers.
+template <class T, int N>
+__device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const Place &w, int channel, int64_t t0,
+                                            int count, T (&x)[N]) {
+  const T *base = static_cast<const T *>(view.data);
+  int64_t at = w.row * view.row_stride + t0 * view.token_stride;
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    x[t] = (base + at)[uint32_t(channel)];
+    at += t + 1 < N - 3 || t + 1 < count ? view.token_stride : 0;
+    asm volatile("" : "+s"(at));
+  }
+}
+
+// The same of an output, from token `first` of all rows on.
+template <class T, int N>
+__device__ __forceinline__ void store_tokens(void *out, int64_t first, int64_t channels, int channel, int count,
+                                             const float (&x)[N]) {
+  T *base = static_cast<T *>(out);
+  int64_t at = first * channels;
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    if (t < N - 3 || t < count) (base + at)[uint32_t(channel)] = from_f32<T>(x[t]);
+    at += channels;
+    asm volatile("" : "+s"(at));
+  }
+}
+
+// b or c of a chunk to [states][16] in LDS; zeros for tokens that do not count.
+template <class T, int NMAX>
+__device__ __forceinline__ void load_heads(const Scan &p, const rdf2v_heads_view &view, const Place &w, int64_t t0,
+                                           int count, float *lds) {
+  const T *at = static_cast<const T *>(view.data) + w.row * view.row_stride + t0 * view.token_stride +
+                w.group * view.head_stride;
+  constexpr int kEach = kTokens * NMAX / kWave;
+  T x[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = threadIdx.x + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
+    x[k] = T(0.0f);
+    if (token < count) x[k] = at[token * view.token_stride + n];
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = threadIdx.x + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
+    if (token < kTokens) lds[n * kTokens + token] = to_f32(x[k]);
+  }
+}
+
 // A state's values of a chunk's tokens, the same in every lane.
-__device__ __forceinline__ void read_head(const float *lds, int n, float (&x)[kTokens]) {
+template <int N>
+__device__ __forceinline__ void read_head(const float *lds, int n, float (&x)[N]) {
   typedef float Four __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int i = 0; i < kTokens / 4; ++i) {
+  for (int i = 0; i < N / 4; ++i) {
     const Four v = reinterpret_cast<const Four *>(lds + n * kTokens)[i];
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j];
   }
 }
 
+// delta and delta x of a chunk's tokens; 0 beyond the last that counts: nothing decays and nothing is added.
+template <class T, int N>
+__device__ __forceinline__ void make_steps(const T (&x)[N], const T (&dt)[N], float bias, int count, bool there,
+                                           float (&delta)[N], float (&u)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    const bool on = there && t < count;
+    const float d = softplus(to_f32(dt[t]) + bias);
+    delta[t] = on ? d : 0.0f;
+    u[t] = on ? d * to_f32(x[t]) : 0.0f;
+  }
+}
+
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
+
+// The gradients of y of a chunk's tokens.
+template <class T, int N>
+__device__ __forceinline__ void make_gradients(const T (&dout)[N], const T (&gate)[N], bool gated, int count,
+                                               bool there, float (&g)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) g[t] = there && t < count ? to_f32(dout[t]) : 0.0f;
+  if (!gated) return;
+#pragma unroll
+  for (int t = 0; t < N; ++t) g[t] = there && t < count ? g[t] * silu(to_f32(gate[t])) : 0.0f;
+}
+
 template <class T>
 __device__ __forceinline__ void store_zeros(void *out, int64_t from, int64_t to, int64_t row, int64_t length,
                                             int64_t width, int64_t at, int count) {
   T *p = static_cast<T *>(out) + row * length * width + at;
-  for (int64_t t = from + threadIdx.x / kWave; t < to; t += kWaves)
-    for (int i = threadIdx.x % kWave; i < count; i += kWave) p[t * width + i] = from_f32<T>(0.0f);
+  for (int64_t t = from; t < to; ++t)
+    for (int i = threadIdx.x; i < count; i += kWave) p[t * width + i] = from_f32<T>(0.0f);
 }
 
-// The outputs of a segment.
+// What a wave keeps for its channels.
+struct Lane {
+  int lane, channel;
+  bool there, gated;
+  float bias, skip;
+  __device__ __forceinline__ Lane(const Scan &p, const Place &w)
+      : lane(threadIdx.x), channel(w.c0 + (int(threadIdx.x) < w.count ? threadIdx.x : 0)),
+        there(int(threadIdx.x) < w.count), gated(p.gate.data != nullptr),
+        bias(p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f), skip(p.skip != nullptr ? p.skip[channel] : 0.0f) {}
+};
+
+// The outputs of a segment. A wave's barriers cost nothing: it is alone in its workgroup.
 template <class T, int NMAX>
-__global__ __launch_bounds__(kThreads) void scan_out_kernel(Scan p, int64_t first) {
+__global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) {
   __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens], c[NMAX * kTokens];
-  __shared__ float delta[kTokens][kWave], u[kTokens][kWave], sums[kWaves][kTokens][kWave];
-  const int64_t item = first + blockIdx.x, columns = p.blocks * p.groups;
-  const Place w = place_of(p, item % columns, item / columns, threadIdx.x == 0);
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const bool there = lane < w.count;
-  const int channel = w.c0 + (there ? lane : 0);
-  load_rates(p, w, rates, w.row == 0 && w.seg == 0);
-  if (p.segments == 1) {
-    load_states(p, w, p.state, held);
-  } else {
-    const float *from = p.carry + (w.row * p.segments + w.seg) * p.states * p.channels + channel;
-    for (int n = wave; n < p.states; n += kWaves) held[n * kWave + lane] = there ? from[int64_t(n) * p.channels] : 0.0f;
-  }
-  const float bias = p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f;
-  const float skip = p.skip != nullptr ? p.skip[channel] : 0.0f;
-  const bool gated = p.gate.data != nullptr;
-  T *out = static_cast<T *>(p.out) + w.row * p.length * p.channels + w.c0 + lane;
-  Ahead<T> x, dt, gate;
-  AheadHeads<T, NMAX> bs, cs;
-  const auto load = [&](int64_t t0) {
-    x.load(p.x, w, t0, wave, lane);
-    dt.load(p.dt, w, t0, wave, lane);
-    if (gated) gate.load(p.gate, w, t0, wave, lane);
-    bs.load(p, p.b, w, t0);
-    cs.load(p, p.c, w, t0);
-  };
-  load(w.begin);
-  for (int64_t t0 = w.begin; t0 < w.stop; t0 += kTokens) {
-    float kept[kOwn], open[kOwn];
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int t = wave * kOwn + i;
-      const bool on = there && t0 + t < w.stop;
-      const float d = on ? softplus(to_f32(dt.v[i]) + bias) : 0.0f, xv = to_f32(x.v[i]);
-      delta[t][lane] = d;
-      u[t][lane] = on ? d * xv : 0.0f;
-      kept[i] = skip * xv;
-      const float z = gated ? to_f32(gate.v[i]) : 0.0f;
-      open[i] = z * sigmoid(z);
-    }
-    bs.put(p, b);
-    cs.put(p, c);
+  const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
+                part = (first + blockIdx.x) / columns;
+  Place w = place_of(p, column, 0, false);
+  const Lane me(p, w);
+  load_rates(p, w, rates, part == 0);
+  for (int64_t item = part; item < p.rows * p.segments; item += p.parts) {
+    w = place_of(p, column, item, me.lane == 0);
     __syncthreads();
-    load(t0 + kTokens);
-    const int count = int(min(int64_t(kTokens), w.stop - t0));
-    float dl[kTokens], ul[kTokens], y[kTokens] = {};
-    read_tokens(delta, lane, dl);
-    read_tokens(u, lane, ul);
-    for (int n = wave; n < p.states; n += kWaves) {
-      const float rate = rates[n * kWave + lane];
-      float h = held[n * kWave + lane], bn[kTokens], cn[kTokens];
-      read_head(b, n, bn);
-      read_head(c, n, cn);
-#pragma unroll
-      for (int t = 0; t < kTokens; ++t) {
-        if (t % 4 == 0 && t >= count) break;
-        h = fmaf(exp2_fast(dl[t] * rate), h, ul[t] * bn[t]);
-        y[t] = fmaf(h, cn[t], y[t]);
-      }
-      held[n * kWave + lane] = h;
+    if (p.segments == 1) {
+      load_states(p, w, p.state, held);
+    } else {
+      load_carry(p, w, p.carry + item * p.states * p.channels, me.channel, held);
     }
+    for (int64_t t0 = w.begin; t0 < w.stop; t0 += kTokens) {
+      const int count = int(min(int64_t(kTokens), w.stop - t0));
+      with_tokens(count, [&](auto tokens) {
+        constexpr int N = tokens();
+        T x[N], dt[N], gate[N];
+        load_tokens(p.x, w, me.channel, t0, count, x);
+        load_tokens(p.dt, w, me.channel, t0, count, dt);
+        if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
+        __syncthreads();
+        load_heads<T, NMAX>(p, p.b, w, t0, count, b);
+        load_heads<T, NMAX>(p, p.c, w, t0, count, c);
+        float delta[N], u[N], y[N];
+        make_steps(x, dt, me.bias, count, me.there, delta, u);
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t) sums[wave][t][lane] = y[t];
+        for (int t = 0; t < N; ++t) y[t] = me.skip * to_f32(x[t]);
+        __syncthreads();
+        for (int n = 0; n < p.states; ++n) {
+          const float rate = rates[n * kWave + me.lane];
+          float h = held[n * kWave + me.lane], bn[N], cn[N];
+          read_head(b, n, bn);
+          read_head(c, n, cn);
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            h = fmaf(exp2_fast(delta[t] * rate), h, u[t] * bn[t]);
+            y[t] = fmaf(h, cn[t], y[t]);
+          }
+          held[n * kWave + me.lane] = h;
+        }
+        if (me.gated)
+#pragma unroll
+          for (int t = 0; t < N; ++t) y[t] *= silu(to_f32(gate[t]));
+        if (me.there) store_tokens<T>(p.out, w.row * p.length + t0, p.channels, me.channel, count, y);
+      });
+    }
+    store_zeros<T>(p.out, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
+    if (p.segments > 1 || p.state_out == nullptr) continue;
     __syncthreads();
-    if (!there) continue;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int t = wave * kOwn + i;
-      if (t >= count) break;
-      float sum = kept[i];
-#pragma unroll
-      for (int v = 0; v < kWaves; ++v) sum += sums[v][t][lane];
-      out[(t0 + t) * p.channels] = from_f32<T>(gated ? sum * open[i] : sum);
-    }
+    store_states(p, w, held, p.state_out);
   }
-  store_zeros<T>(p.out, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
-  if (p.segments > 1 || p.state_out == nullptr) return;
-  __syncthreads();
-  store_states(p, w, held, p.state_out);
 }
 
 // The states that a segment ends with, from zeros; BACK, for the gradients: the states before its chunks (from the
 // row's own state where there is one segment), and the gradient that its outputs give the state before it,
 // sum_t (product of the decays up to t) c_t g_t, which needs no second way through the tokens.
-template <class T, int NMAX, bool BACK>
-__global__ __launch_bounds__(kThreads) void scan_states_kernel(Scan p, int64_t first) {
+template <class T, int NMAX, bool BACK, bool CUT>
+__global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t first) {
+  constexpr bool kBoth = BACK && CUT;
   __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens];
-  __shared__ float decay[BACK ? NMAX * kWave : 1], grad[BACK ? NMAX * kWave : 1], c[BACK ? NMAX * kTokens : 1];
-  __shared__ float delta[kTokens][kWave], u[kTokens][kWave], g[BACK ? kTokens : 1][kWave];
-  const int64_t item = first + blockIdx.x, columns = p.blocks * p.groups;
-  const Place w = place_of(p, item % columns, item / columns, false);
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const bool there = lane < w.count, cut = p.segments > 1, gated = p.gate.data != nullptr;
-  const int channel = w.c0 + (there ? lane : 0);
+  __shared__ float decay[kBoth ? NMAX * kWave : 1], grad[kBoth ? NMAX * kWave : 1], c[kBoth ? NMAX * kTokens : 1];
+  const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
+                part = (first + blockIdx.x) / columns;
+  Place w = place_of(p, column, 0, false);
+  const Lane me(p, w);
+  const int lane = me.lane;
   load_rates(p, w, rates, false);
-  load_states(p, w, cut ? nullptr : p.state, held);
-  if (BACK && cut)
-    for (int n = wave; n < p.states; n += kWaves) {
-      decay[n * kWave + lane] = 1.0f;
-      grad[n * kWave + lane] = 0.0f;
-    }
-  const float bias = p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f;
-  Ahead<T> x, dt, gate, dout;
-  AheadHeads<T, NMAX> bs, cs;
-  const auto load = [&](int64_t t0) {
-    x.load(p.x, w, t0, wave, lane);
-    dt.load(p.dt, w, t0, wave, lane);
-    bs.load(p, p.b, w, t0);
-    if (!BACK || !cut) return;
-    if (gated) gate.load(p.gate, w, t0, wave, lane);
-    dout.load(p.dout, w, t0, wave, lane);
-    cs.load(p, p.c, w, t0);
-  };
-  float sum = 0.0f;  // of delta
-  // without segments the state after the last chunk is not needed
-  const int64_t stop = cut ? w.stop : w.stop - kTokens;
-  if (w.begin < stop) load(w.begin);
-  for (int64_t t0 = w.begin; t0 < stop; t0 += kTokens) {
-    __syncthreads();  // the chunk before has been read
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int t = wave * kOwn + i;
-      const bool on = there && t0 + t < w.stop;
-      const float d = on ? softplus(to_f32(dt.v[i]) + bias) : 0.0f;
-      delta[t][lane] = d;
-      u[t][lane] = on ? d * to_f32(x.v[i]) : 0.0f;
-      if (BACK && cut) {
-        const float z = gated ? to_f32(gate.v[i]) : 0.0f, o = to_f32(dout.v[i]);
-        g[BACK ? t : 0][lane] = gated ? o * (z * sigmoid(z)) : o;
-      }
-    }
-    bs.put(p, b);
-    if (BACK && cut) cs.put(p, c);
+  for (int64_t item = part; item < p.rows * p.segments; item += p.parts) {
+    w = place_of(p, column, item, false);
     __syncthreads();
-    load(t0 + kTokens);
-    const int count = int(min(int64_t(kTokens), w.stop - t0));
-    float dl[kTokens], ul[kTokens], gl[kTokens];
-    read_tokens(delta, lane, dl);
-    read_tokens(u, lane, ul);
-    if (BACK && cut) read_tokens(g, lane, gl);
-    if (BACK && cut && wave == 0 && there)
-      p.until[(w.row * p.chunks + t0 / kTokens) * p.channels + channel] = sum;
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t) sum += dl[t];
-    for (int n = wave; n < p.states; n += kWaves) {
-      const float rate = rates[n * kWave + lane];
-      float h = held[n * kWave + lane], bn[kTokens], cn[kTokens];
-      if (BACK && cut && there)
-        p.starts[((w.row * p.chunks + t0 / kTokens) * p.states + n) * p.channels + channel] = h;
-      read_head(b, n, bn);
-      if (BACK && cut) {
-        read_head(c, n, cn);
-        float most = decay[n * kWave + lane], r = grad[n * kWave + lane];
-#pragma unroll
-        for (int t = 0; t < kTokens; ++t) {
-          if (t % 4 == 0 && t >= count) break;
-          const float e = exp2_fast(dl[t] * rate);
-          h = fmaf(e, h, ul[t] * bn[t]);
-          most *= e;
-          r = fmaf(most, gl[t] * cn[t], r);
-        }
-        decay[n * kWave + lane] = most;
-        grad[n * kWave + lane] = r;
-      } else {
-#pragma unroll
-        for (int t = 0; t < kTokens; ++t) {
-          if (t % 4 == 0 && t >= count) break;
-          h = fmaf(exp2_fast(dl[t] * rate), h, ul[t] * bn[t]);
-        }
+    load_states(p, w, CUT ? nullptr : p.state, held);
+    if (kBoth)
+      for (int n = 0; n < p.states; ++n) {
+        decay[n * kWave + lane] = 1.0f;
+        grad[n * kWave + lane] = 0.0f;
       }
-      held[n * kWave + lane] = h;
-      if (BACK && !cut && there)
-        p.starts[((w.row * p.chunks + t0 / kTokens + 1) * p.states + n) * p.channels + channel] = h;
+    float sum = 0.0f;  // of delta
+    // without segments the state after the last chunk is not needed
+    const int64_t stop = CUT ? w.stop : w.stop - kTokens;
+    for (int64_t t0 = w.begin; t0 < stop; t0 += kTokens) {
+      const int count = int(min(int64_t(kTokens), w.stop - t0));
+      const int64_t chunk = w.row * p.chunks + t0 / kTokens;
+      with_tokens(count, [&](auto tokens) {
+        constexpr int N = tokens();
+        T x[N], dt[N];
+        float delta[N], u[N], g[N];
+        load_tokens(p.x, w, me.channel, t0, count, x);
+        load_tokens(p.dt, w, me.channel, t0, count, dt);
+        __syncthreads();
+        load_heads<T, NMAX>(p, p.b, w, t0, count, b);
+        if constexpr (kBoth) {
+          T o[N], gate[N];
+          load_tokens(p.dout, w, me.channel, t0, count, o);
+          if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
+          load_heads<T, NMAX>(p, p.c, w, t0, count, c);
+          make_gradients(o, gate, me.gated, count, me.there, g);
+        }
+        make_steps(x, dt, me.bias, count, me.there, delta, u);
+        __syncthreads();
+        if (kBoth && me.there) p.until[chunk * p.channels + me.channel] = sum;
+        if constexpr (CUT)
+#pragma unroll
+          for (int t = 0; t < N; ++t) sum += delta[t];
+        for (int n = 0; n < p.states; ++n) {
+          const float rate = rates[n * kWave + lane];
+          float h = held[n * kWave + lane], bn[N];
+          if (kBoth && me.there) p.starts[(chunk * p.states + n) * p.channels + me.channel] = h;
+          read_head(b, n, bn);
+          if constexpr (kBoth) {
+            float cn[N], most = decay[n * kWave + lane], r = grad[n * kWave + lane];
+            read_head(c, n, cn);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+              const float e = exp2_fast(delta[t] * rate);
+              h = fmaf(e, h, u[t] * bn[t]);
+              most *= e;
+              r = fmaf(most, g[t] * cn[t], r);
+            }
+            decay[n * kWave + lane] = most;
+            grad[n * kWave + lane] = r;
+          } else {
+#pragma unroll
+            for (int t = 0; t < N; ++t) h = fmaf(exp2_fast(delta[t] * rate), h, u[t] * bn[t]);
+          }
+          held[n * kWave + lane] = h;
+          if (BACK && !CUT && me.there) p.starts[((chunk + 1) * p.states + n) * p.channels + me.channel] = h;
+        }
+      });
     }
-  }
-  if (!cut || !there) return;
-  const int64_t at = w.row * p.segments + w.seg;
-  if (wave == 0) p.steps[at * p.channels + channel] = sum;
-  for (int n = wave; n < p.states; n += kWaves) {
-    p.carry[(at * p.states + n) * p.channels + channel] = held[n * kWave + lane];
-    if (BACK) p.back[(at * p.states + n) * p.channels + channel] = grad[n * kWave + lane];
+    if (!CUT || !me.there) continue;
+    p.steps[item * p.channels + me.channel] = sum;
+    for (int n = 0; n < p.states; ++n) {
+      p.carry[(item * p.states + n) * p.channels + me.channel] = held[n * kWave + lane];
+      if (kBoth) p.back[(item * p.states + n) * p.channels + me.channel] = grad[n * kWave + lane];
+    }
   }
 }
 
@@ -409,8 +450,9 @@ typedef float Four __attribute__((ext_vector_type(4)));
 // 64 lanes, at most 2 instructions a value instead of 7.
 struct ChannelSums {
   Four sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  __device__ __forceinline__ void add(float value, int t, int lane) {
-    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(value, lane % kTokens == t ? 1.0f : 0.0f, sum, 0, 0, 0);
+  // `unit`: 1 in the lanes of column t, from unit_column
+  __device__ __forceinline__ void add(float value, float unit) {
+    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(value, unit, sum, 0, 0, 0);
   }
   // token lane % 16's, in every lane
   __device__ __forceinline__ float total() const {
@@ -420,182 +462,178 @@ struct ChannelSums {
   }
 };
 
-// Gradients of a segment, chunk after chunk from its end; a workgroup takes several segments of its channels in
-// turn and holds the parameters' gradients meanwhile.
+// `first`, 1 in lanes 0, 16, 32 and 48 and 0 in the others, moved up by T lanes in its rows of 16.
+template <int T>
+__device__ __forceinline__ float unit_column(float first) {
+  if constexpr (T == 0)
+    return first;
+  else
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(first), 0x110 + T, 0xf, 0xf, true));
+}
+
+// Calls each(constant) for N - 1, N - 2, .. 0.
+template <int N, class Each>
+__device__ __forceinline__ void backwards(Each each) {
+  if constexpr (N > 0) {
+    each(std::integral_constant<int, N - 1>{});
+    backwards<N - 1>(each);
+  }
+}
+
+// Gradients of a segment, chunk after chunk from its end; a wave takes several segments of its channels in turn
+// and holds the parameters' gradients meanwhile. Inputs are read twice, before the states' loop and after it:
+// what is made of them would not fit the registers beside it.
 template <class T, int NMAX>
-__global__ __launch_bounds__(kThreads, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
-  __shared__ float rates[NMAX * kWave], grads[NMAX * kWave], da[NMAX * kWave];
+__global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
+  __shared__ float rates[NMAX * kWave], grads[NMAX * kWave], da[NMAX * kWave], held[NMAX * kWave];
   __shared__ float b[NMAX * kTokens], c[NMAX * kTokens], db[kTokens * NMAX], dc[kTokens * NMAX];
-  __shared__ float delta[kTokens][kWave], u[kTokens][kWave], g[kTokens][kWave];
-  __shared__ float ys[kWaves][kTokens][kWave], dus[kWaves][kTokens][kWave], dds[kWaves][kTokens][kWave];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
                 part = (first + blockIdx.x) / columns;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const bool gated = p.gate.data != nullptr, cut = p.segments > 1, direct = p.blocks == 1;
+  const bool cut = p.segments > 1, direct = p.blocks == 1;
   Place w = place_of(p, column, 0, false);
-  const bool there = lane < w.count;
-  const int channel = w.c0 + (there ? lane : 0);
-  const float bias = p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f;
-  const float skip = p.skip != nullptr ? p.skip[channel] : 0.0f;
+  const Lane me(p, w);
+  const int lane = me.lane;
   load_rates(p, w, rates, part == 0);
-  for (int i = threadIdx.x; i < NMAX * kWave; i += kThreads) da[i] = 0.0f;
+  for (int n = 0; n < p.states; ++n) da[n * kWave + lane] = 0.0f;
   float ddt_bias = 0.0f, dskip = 0.0f;
   for (int64_t item = part; item < p.rows * p.segments; item += p.parts) {
-    w = place_of(p, column, item, threadIdx.x == 0);
-    const int64_t at = w.row * p.segments + w.seg, tokens = w.row * p.length * p.channels + w.c0 + lane;
+    w = place_of(p, column, item, lane == 0);
     __syncthreads();
     if (!cut) {
       load_states(p, w, p.dstate_out, grads);
     } else {
-      for (int n = wave; n < p.states; n += kWaves)
-        grads[n * kWave + lane] = there ? p.back[(at * p.states + n) * p.channels + channel] : 0.0f;
+      load_carry(p, w, p.back + item * p.states * p.channels, me.channel, grads);
     }
-    Ahead<T> x, dt, gate, dout;
-    AheadHeads<T, NMAX> bs, cs;
-    const auto load = [&](int64_t t0) {
-      x.load(p.x, w, t0, wave, lane);
-      dt.load(p.dt, w, t0, wave, lane);
-      if (gated) gate.load(p.gate, w, t0, wave, lane);
-      dout.load(p.dout, w, t0, wave, lane);
-      bs.load(p, p.b, w, t0);
-      cs.load(p, p.c, w, t0);
-    };
     const int64_t last = w.begin + (w.stop - w.begin - 1) / kTokens * kTokens;  // chunk
-    if (w.begin < w.stop) load(last);
     for (int64_t t0 = last; t0 >= w.begin && w.begin < w.stop; t0 -= kTokens) {
-      float xv[kOwn], dv[kOwn], raw[kOwn], z[kOwn], sig[kOwn], o[kOwn], gv[kOwn];
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i) {
-        const int t = wave * kOwn + i;
-        const bool on = there && t0 + t < w.stop;
-        xv[i] = to_f32(x.v[i]);
-        raw[i] = to_f32(dt.v[i]) + bias;
-        dv[i] = on ? softplus(raw[i]) : 0.0f;
-        o[i] = to_f32(dout.v[i]);
-        z[i] = gated ? to_f32(gate.v[i]) : 0.0f;
-        sig[i] = gated ? sigmoid(z[i]) : 0.0f;
-        gv[i] = gated ? o[i] * (z[i] * sig[i]) : o[i];
-        delta[t][lane] = dv[i];
-        u[t][lane] = on ? dv[i] * xv[i] : 0.0f;
-        g[t][lane] = on ? gv[i] : 0.0f;
-      }
-      bs.put(p, b);
-      cs.put(p, c);
-      __syncthreads();
-      if (t0 > w.begin) load(t0 - kTokens);
       const int count = int(min(int64_t(kTokens), w.stop - t0));
-      float dl[kTokens], ul[kTokens], gl[kTokens], y[kTokens] = {}, du[kTokens] = {}, dd[kTokens] = {};
-      read_tokens(delta, lane, dl);
-      read_tokens(u, lane, ul);
-      read_tokens(g, lane, gl);
-      const int64_t chunk = w.row * p.chunks + t0 / kTokens;
-      const float until = cut && there ? p.until[chunk * p.channels + channel] : 0.0f;
-      for (int n = wave; n < p.states; n += kWaves) {
-        const float rate = rates[n * kWave + lane];
-        float h = 0.0f;
-        if (there) {
-          if (cut)
-            h = fmaf(exp2_fast(until * rate), p.carry[(at * p.states + n) * p.channels + channel],
-                     p.starts[(chunk * p.states + n) * p.channels + channel]);
-          else if (t0 > w.begin)
-            h = p.starts[(chunk * p.states + n) * p.channels + channel];
-          else if (p.state != nullptr)
-            h = p.state[(w.row * p.channels + channel) * p.states + n];
-        }
-        float bn[kTokens], cn[kTokens], e[kTokens], kept[kTokens];
-        read_head(b, n, bn);
-        read_head(c, n, cn);
+      const int64_t chunk = w.row * p.chunks + t0 / kTokens, token = w.row * p.length + t0;
+      // the states before the chunk: the row's, or its own and what the segment begins with
+      const float *starts = p.starts + chunk * p.states * p.channels + me.channel;
+      if (cut) {
+        const float *carry = p.carry + item * p.states * p.channels + me.channel;
+        const float until = p.until[chunk * p.channels + me.channel];
+        in_batches(
+            p.states,
+            [&](int n) { return make_float2(starts[int64_t(n) * p.channels], carry[int64_t(n) * p.channels]); },
+            [&](int n, float2 h) {
+              held[n * kWave + lane] =
+                  me.there ? fmaf(exp2_fast(until * rates[n * kWave + lane]), h.y, h.x) : 0.0f;
+            });
+      } else if (t0 > w.begin) {
+        load_carry(p, w, starts - me.channel, me.channel, held);
+      } else {
+        load_states(p, w, p.state, held);
+      }
+      with_tokens(count, [&](auto tokens) {
+        constexpr int N = tokens();
+        float delta[N], u[N], g[N], y[N], du[N] = {}, dd[N] = {};
+        __syncthreads();
+        {
+          T x[N], dt[N], gate[N], o[N];
+          load_tokens(p.x, w, me.channel, t0, count, x);
+          load_tokens(p.dt, w, me.channel, t0, count, dt);
+          if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
+          load_tokens(p.dout, w, me.channel, t0, count, o);
+          load_heads<T, NMAX>(p, p.b, w, t0, count, b);
+          load_heads<T, NMAX>(p, p.c, w, t0, count, c);
+          make_steps(x, dt, me.bias, count, me.there, delta, u);
+          make_gradients(o, gate, me.gated, count, me.there, g);
 #pragma unroll
-        for (int t = 0; t < kTokens; ++t) {
-          if (t % 4 == 0 && t >= count) break;
-          e[t] = exp2_fast(dl[t] * rate);
-          kept[t] = e[t] * h;
-          h = fmaf(ul[t], bn[t], kept[t]);
-          y[t] = fmaf(h, cn[t], y[t]);
-        }
-        const float after = grads[n * kWave + lane];
-        float r = after, rates_sum = 0.0f;
-        ChannelSums sb, sc;
-#pragma unroll
-        for (int t = kTokens - 1; t >= 0; --t) {
-          if (t / 4 * 4 >= count) continue;
-          r = fmaf(gl[t], cn[t], r);
-          sb.add(r * ul[t], t, lane);
-          sc.add(gl[t] * fmaf(ul[t], bn[t], kept[t]), t, lane);
-          du[t] = fmaf(r, bn[t], du[t]);
-          const float q = r * kept[t];
-          dd[t] = fmaf(q, rate, dd[t]);
-          rates_sum = fmaf(q, dl[t], rates_sum);
-          r *= e[t];
-        }
-        grads[n * kWave + lane] = r;
-        da[n * kWave + lane] += rates_sum;
-        float tb = sb.total(), tc = sc.total();
-        if (__builtin_expect(__ballot(!(fabsf(tb) < kInf) || !(fabsf(tc) < kInf)) != 0, 0)) {
-          // What is no number has spread over the unit columns' zeros: the same sums token by token.
-          r = after;
-          for (int t = kTokens - 1; t >= 0; --t) {
-            if (t >= count) continue;
-            const float ct = c[n * kTokens + t], bt = b[n * kTokens + t], ut = u[t][lane], gt = g[t][lane];
-            float et = 0.0f, kt = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kTokens; ++k) {
-              et = k == t ? e[k] : et;
-              kt = k == t ? kept[k] : kt;
-            }
-            r = fmaf(gt, ct, r);
-            ChannelSums ob, oc;
-            ob.add(there ? r * ut : 0.0f, t, lane);
-            oc.add(there ? gt * fmaf(ut, bt, kt) : 0.0f, t, lane);
-            r *= et;
-            const float one = ob.total(), two = oc.total();
-            if (lane % kTokens == t) {
-              tb = one;
-              tc = two;
-            }
+          for (int t = 0; t < N; ++t) {
+            const float xv = to_f32(x[t]);
+            dskip = t < count ? fmaf(g[t], xv, dskip) : dskip;
+            y[t] = me.skip * xv;
           }
         }
-        if (lane < kTokens) {
-          db[lane * p.states + n] = tb;
-          dc[lane * p.states + n] = tc;
-        }
-      }
+        __syncthreads();
+        float first = lane % kTokens == 0 ? 1.0f : 0.0f;
+        for (int n = 0; n < p.states; ++n) {
+          asm volatile("" : "+v"(first));  // its columns are made anew: kept, they would cost 16 registers
+          const float rate = rates[n * kWave + lane], h0 = held[n * kWave + lane], after = grads[n * kWave + lane];
+          float bn[N], cn[N], e[N], h[N];
+          read_head(b, n, bn);
+          read_head(c, n, cn);
 #pragma unroll
-      for (int t = 0; t < kTokens; ++t) {
-        ys[wave][t][lane] = y[t];
-        dus[wave][t][lane] = du[t];
-        dds[wave][t][lane] = dd[t];
-      }
+          for (int t = 0; t < N; ++t) {
+            e[t] = exp2_fast(delta[t] * rate);
+            h[t] = fmaf(e[t], t > 0 ? h[t > 0 ? t - 1 : 0] : h0, u[t] * bn[t]);
+            y[t] = fmaf(h[t], cn[t], y[t]);
+          }
+          float r = after, rates_sum = 0.0f;
+          ChannelSums sb, sc;
+          backwards<N>([&](auto token) {
+            constexpr int t = token();
+            const float unit = unit_column<t>(first);
+            r = fmaf(g[t], cn[t], r);
+            sb.add(r * u[t], unit);
+            sc.add(g[t] * h[t], unit);
+            du[t] = fmaf(r, bn[t], du[t]);
+            r *= e[t];
+            const float q = r * (t > 0 ? h[t > 0 ? t - 1 : 0] : h0);
+            dd[t] = fmaf(q, rate, dd[t]);
+            rates_sum = fmaf(q, delta[t], rates_sum);
+          });
+          grads[n * kWave + lane] = r;
+          da[n * kWave + lane] += rates_sum;
+          float tb = sb.total(), tc = sc.total();
+          if (__builtin_expect(__ballot(!(fabsf(tb) < kInf) || !(fabsf(tc) < kInf)) != 0, 0)) {
+            // What is no number has spread over the unit columns' zeros: the same sums token by token.
+            r = after;
+            backwards<N>([&](auto token) {
+              constexpr int t = token();
+              const float unit = unit_column<t>(first);
+              r = fmaf(g[t], cn[t], r);
+              ChannelSums ob, oc;
+              ob.add(me.there ? r * u[t] : 0.0f, unit);
+              oc.add(me.there ? g[t] * h[t] : 0.0f, unit);
+              r *= e[t];
+              const float one = ob.total(), two = oc.total();
+              if (lane % kTokens == t) {
+                tb = one;
+                tc = two;
+              }
+            });
+          }
+          if (lane < kTokens) {
+            db[lane * p.states + n] = tb;
+            dc[lane * p.states + n] = tc;
+          }
+        }
+        T x[N], dt[N], gate[N], o[N];
+        load_tokens(p.x, w, me.channel, t0, count, x);
+        load_tokens(p.dt, w, me.channel, t0, count, dt);
+        if (me.gated) {
+          load_tokens(p.gate, w, me.channel, t0, count, gate);
+          load_tokens(p.dout, w, me.channel, t0, count, o);
+        }
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+          dd[t] = fmaf(dd[t], kLn2, to_f32(x[t]) * du[t]) * sigmoid(to_f32(dt[t]) + me.bias);
+          du[t] = fmaf(delta[t], du[t], me.skip * g[t]);
+          if (t < count) ddt_bias += dd[t];
+        }
+        if (me.there) {
+          store_tokens<T>(p.dx, token, p.channels, me.channel, count, du);
+          store_tokens<T>(p.ddt, token, p.channels, me.channel, count, dd);
+        }
+        if (!me.gated) return;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+          const float z = to_f32(gate[t]);
+          y[t] = to_f32(o[t]) * y[t] * silu_slope(z, sigmoid(z));
+        }
+        if (me.there) store_tokens<T>(p.dgate, token, p.channels, me.channel, count, y);
+      });
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kOwn; ++i) {
-        const int t = wave * kOwn + i;
-        if (t >= count) break;
-        if (!there) break;
-        float sy = skip * xv[i], su = 0.0f, sd = 0.0f;
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-          sy += ys[v][t][lane];
-          su += dus[v][t][lane];
-          sd += dds[v][t][lane];
-        }
-        const float dstep = fmaf(sd, kLn2, xv[i] * su) * sigmoid(raw[i]);
-        ddt_bias += dstep;
-        dskip = fmaf(gv[i], xv[i], dskip);
-        const int64_t to = tokens + (t0 + t) * p.channels;
-        static_cast<T *>(p.dx)[to] = from_f32<T>(fmaf(dv[i], su, skip * gv[i]));
-        static_cast<T *>(p.ddt)[to] = from_f32<T>(dstep);
-        if (gated) static_cast<T *>(p.dgate)[to] = from_f32<T>(o[i] * sy * silu_slope(z[i], sig[i]));
-      }
-      for (int i = threadIdx.x; i < count * p.states; i += kThreads) {
-        const int64_t token = w.row * p.length + t0 + i / p.states;
-        const int n = i % p.states;
+      for (int i = lane; i < count * p.states; i += kWave) {
+        const int t = i * p.by_states >> 16, n = i - t * p.states;
         if (direct) {
-          const int64_t to = (token * p.groups + w.group) * p.states + n;
+          const int64_t to = ((token + t) * p.groups + w.group) * p.states + n;
           static_cast<T *>(p.db)[to] = from_f32<T>(db[i]);
           static_cast<T *>(p.dc)[to] = from_f32<T>(dc[i]);
         } else {
-          float *to = p.bc + ((w.block * p.rows * p.length + token) * p.groups + w.group) * 2 * p.states + n;
+          float *to = p.bc + ((w.block * p.rows * p.length + token + t) * p.groups + w.group) * 2 * p.states + n;
           to[0] = db[i];
           to[p.states] = dc[i];
         }
@@ -603,7 +641,7 @@ __global__ __launch_bounds__(kThreads, NMAX <= 16 ? 2 : 1) void scan_backward_ke
     }
     store_zeros<T>(p.dx, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
     store_zeros<T>(p.ddt, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
-    if (gated) store_zeros<T>(p.dgate, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
+    if (me.gated) store_zeros<T>(p.dgate, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
     if (direct) {
       store_zeros<T>(p.db, w.stop, w.end, w.row, p.length, int64_t(p.groups) * p.states, w.group * p.states, p.states);
       store_zeros<T>(p.dc, w.stop, w.end, w.row, p.length, int64_t(p.groups) * p.states, w.group * p.states, p.states);
@@ -615,15 +653,11 @@ __global__ __launch_bounds__(kThreads, NMAX <= 16 ? 2 : 1) void scan_backward_ke
   }
   float *partial = p.partial + part * p.channels * (p.states + 2);
   __syncthreads();
-  for (int i = threadIdx.x; i < w.count * p.states; i += kThreads)
+  for (int i = lane; i < w.count * p.states; i += kWave)
     partial[int64_t(w.c0) * p.states + i] = da[i % p.states * kWave + i / p.states];
-  ys[wave][0][lane] = ddt_bias;
-  ys[wave][1][lane] = dskip;
-  __syncthreads();
-  if (wave >= 2 || !there) return;
-  float sum = 0.0f;
-  for (int v = 0; v < kWaves; ++v) sum += ys[v][wave][lane];
-  partial[int64_t(p.channels) * (p.states + wave) + channel] = sum;
+  if (!me.there) return;
+  partial[int64_t(p.channels) * p.states + me.channel] = ddt_bias;
+  partial[int64_t(p.channels) * (p.states + 1) + me.channel] = dskip;
 }
 
 // Gradients of b and c: the sums over a group's workgroups, in order.
@@ -695,19 +729,22 @@ Scan base(const rdf2v_scan &a, const ScanInputs &in, int32_t *status) {
   p.states = a.states;
   p.per_group = a.channels / a.groups;
   p.blocks = (p.per_group + kWave - 1) / kWave;
+  p.by_states = (65536u + uint32_t(a.states) - 1) / uint32_t(a.states);
   return p;
 }
 
-// Segments of a row, chunks, the gradients' workgroups, and where the workspace's arrays lie; its bytes.
+// Segments of a row, chunks, the waves along rows and segments, and where the workspace's arrays lie; its bytes.
 size_t plan(Scan &p, bool backward, void *workspace) {
-  constexpr int64_t kFill = 512, kShortest = 4 * kTokens;
+  // Waves that fill the chip are 1,024 times two or three.
+  constexpr int64_t kFew = 1024, kFill = 2048, kMost = 8192, kShortest = 2 * kTokens;
   const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
   int64_t segments = 1;
-  if (whole < kFill) segments = std::max<int64_t>(1, std::min((2 * kFill) / whole, p.length / kShortest));
+  if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
   p.segment = std::max<int64_t>(1, (p.length + segments - 1) / segments);
   p.segment = (p.segment + kTokens - 1) / kTokens * kTokens;
   p.segments = std::max<int64_t>(1, (p.length + p.segment - 1) / p.segment);
   p.chunks = (p.length + kTokens - 1) / kTokens;
+  p.parts = std::max<int64_t>(1, std::min(p.rows * p.segments, (backward ? kMost / 2 : kMost) / columns));
   size_t bytes = 0;
   const auto take = [&](float *&at, int64_t count) {
     at = workspace != nullptr ? reinterpret_cast<float *>(static_cast<char *>(workspace) + bytes) : nullptr;
@@ -724,7 +761,6 @@ size_t plan(Scan &p, bool backward, void *workspace) {
     take(p.until, p.rows * p.chunks * p.channels);
   }
   if (p.chunks > 1) take(p.starts, p.rows * p.chunks * p.states * p.channels);
-  p.parts = std::max<int64_t>(1, std::min(p.rows * p.segments, 4096 / columns));
   if (p.rows > 0) take(p.partial, p.parts * p.channels * (p.states + 2));
   if (p.blocks > 1) take(p.bc, p.blocks * p.rows * p.length * p.groups * 2 * p.states);
   return bytes;
@@ -739,13 +775,21 @@ rdf2v_status with_types(int dtype, int states, Launch launch) {
   return dtype == RDF2V_BF16 ? sized(bf16{}) : sized(float{});
 }
 
-template <bool BACK>
+// Calls launch for the waves of a call.
+template <class Launch>
+rdf2v_status for_waves(const Scan &p, Launch launch) {
+  return for_each_launch(p.parts * p.blocks * p.groups, kWave, 1, [&](int64_t first, int64_t count) {
+    launch(first, dim3(unsigned(count)));
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
+}
+
+template <bool BACK, bool CUT>
 rdf2v_status launch_states(const Scan &p, int dtype, hipStream_t stream) {
   return with_types(dtype, p.states, [&](auto t, auto most) {
-    return for_each_launch(p.rows * p.segments * p.blocks * p.groups, kThreads, 1, [&](int64_t first, int64_t count) {
-      scan_states_kernel<decltype(t), most(), BACK><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
-      RDF2V_LAUNCH_CHECK();
-      return RDF2V_OK;
+    return for_waves(p, [&](int64_t first, dim3 grid) {
+      scan_states_kernel<decltype(t), most(), BACK, CUT><<<grid, dim3(kWave), 0, stream>>>(p, first);
     });
   });
 }
@@ -775,15 +819,13 @@ rdf2v_status launch_selective_scan(const rdf2v_scan &a, const ScanInputs &in, co
   p.state_out = state_out;
   plan(p, false, workspace);
   if (p.segments > 1) {
-    rdf2v_status st = launch_states<false>(p, a.dtype, stream);
+    rdf2v_status st = launch_states<false, true>(p, a.dtype, stream);
     if (st == RDF2V_OK) st = launch_join<false>(p, stream);
     if (st != RDF2V_OK) return st;
   }
   return with_types(a.dtype, p.states, [&](auto t, auto most) {
-    return for_each_launch(p.rows * p.segments * p.blocks * p.groups, kThreads, 1, [&](int64_t first, int64_t count) {
-      scan_out_kernel<decltype(t), most()><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
-      RDF2V_LAUNCH_CHECK();
-      return RDF2V_OK;
+    return for_waves(p, [&](int64_t first, dim3 grid) {
+      scan_out_kernel<decltype(t), most()><<<grid, dim3(kWave), 0, stream>>>(p, first);
     });
   });
 }
@@ -805,14 +847,16 @@ rdf2v_status launch_selective_scan_backward(const rdf2v_scan &a, const ScanInput
   plan(p, true, workspace);
   rdf2v_status st = RDF2V_OK;
   if (p.rows > 0) {
-    if (p.chunks > 1) st = launch_states<true>(p, a.dtype, stream);
-    if (st == RDF2V_OK && p.segments > 1) st = launch_join<true>(p, stream);
+    if (p.segments > 1) {
+      st = launch_states<true, true>(p, a.dtype, stream);
+      if (st == RDF2V_OK) st = launch_join<true>(p, stream);
+    } else if (p.chunks > 1) {
+      st = launch_states<true, false>(p, a.dtype, stream);
+    }
     if (st != RDF2V_OK) return st;
     st = with_types(a.dtype, p.states, [&](auto t, auto most) {
-      return for_each_launch(p.parts * p.blocks * p.groups, kThreads, 1, [&](int64_t first, int64_t count) {
-        scan_backward_kernel<decltype(t), most()><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
-        RDF2V_LAUNCH_CHECK();
-        return RDF2V_OK;
+      return for_waves(p, [&](int64_t first, dim3 grid) {
+        scan_backward_kernel<decltype(t), most()><<<grid, dim3(kWave), 0, stream>>>(p, first);
       });
     });
     if (st != RDF2V_OK) return st;
