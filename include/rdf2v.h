@@ -786,7 +786,7 @@ rdf2v_status rdf2v_causal_conv_step(const rdf2v_conv *a, const rdf2v_tokens_view
 /* Sizes and parameters that the selective scan calls share. */
 typedef struct rdf2v_scan {
   int64_t rows, length;  /* 0 .. 2^31 - 1 each; the step does not read length and len */
-  int32_t channels;      /* 1 .. 2^31 - 1: a multiple of groups */
+  int32_t channels;      /* 1 .. 2^28: a multiple of groups */
   int32_t groups;        /* 1 .. 65535: channel d reads b and c of group d / (channels / groups) */
   int32_t states;        /* of a channel, 1 .. RDF2V_MAX_SCAN_STATES */
   int32_t dtype;         /* rdf2v_dtype of x, dt, b, c, gate, out and their gradients */

@@ -74,7 +74,7 @@ __device__ __forceinline__ float tap_sum(const Taps<W, V> &taps, const float (&x
 // Whole rows: a thread to a vector of channels and a tile of tokens.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
-  constexpr int V = 16 / sizeof(T), kAhead = 4;
+  constexpr int V = 4, kAhead = 4;
   const int64_t item = (first + blockIdx.x) * kThreads + threadIdx.x;
   if (item >= a.rows * a.tiles * a.vectors) return;
   const int64_t vector = item % a.vectors, rest = item / a.vectors, tile = rest % a.tiles, row = rest / a.tiles;
@@ -327,7 +327,7 @@ rdf2v_status launch_causal_conv(const rdf2v_conv &a, const rdf2v_tokens_view &x,
   c.out = out;
   c.state_out = state_out;
   tile_rows(c);
-  const int per = a.dtype == RDF2V_BF16 ? 8 : 4;
+  const int per = 4;
   c.vectors = (int64_t(a.channels) + per - 1) / per;
   const int64_t blocks = (a.rows * c.tiles * c.vectors + kThreads - 1) / kThreads;
   return with_width(a.width, a.silu != 0, [&](auto width, auto silu) {

@@ -94,6 +94,7 @@ rdf2v_status check_scan_sizes(const rdf2v_scan *a, bool step) {
   if (a == nullptr || a->channels < 1 || a->groups < 1 || a->groups > 65535 || a->channels % a->groups != 0 ||
       a->states < 1 || a->states > RDF2V_MAX_SCAN_STATES || !dtype_ok(a->dtype))
     return RDF2V_ERR_INVALID_ARGUMENT;
+  if (a->channels > 1 << 28) return RDF2V_ERR_TOO_LARGE;
   return check_rows(a->rows, step ? 1 : a->length, int64_t(a->channels) * RDF2V_MAX_SCAN_STATES * 8);
 }
 

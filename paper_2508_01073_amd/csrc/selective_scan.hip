@@ -162,6 +162,13 @@ __device__ __forceinline__ void with_tokens(int count, Chunk chunk) {
     chunk(std::integral_constant<int, 4>{});
 }
 
+// The lane's channel of a token: 32 bits of offset beside an address that all lanes have in common.
+template <class T>
+__device__ __forceinline__ T *lane_of(T *token, int channel) {
+  typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
+  return reinterpret_cast<T *>(reinterpret_cast<Byte *>(token) + uint32_t(channel) * uint32_t(sizeof(T)));
+}
+
 // The lane's channel of a chunk's first `count` tokens; what follows is the last of them again. Addresses are made
 // one after the other: all at once they would not fit the scalar registers.
 template <class T, int N>
@@ -171,7 +178,7 @@ __device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const
   int64_t at = w.row * view.row_stride + t0 * view.token_stride;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    x[t] = (base + at)[uint32_t(channel)];
+    x[t] = *lane_of(base + at, channel);
     at += t + 1 < N - 3 || t + 1 < count ? view.token_stride : 0;
     asm volatile("" : "+s"(at));
   }
@@ -185,7 +192,7 @@ __device__ __forceinline__ void store_tokens(void *out, int64_t first, int64_t c
   int64_t at = first * channels;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    if (t < N - 3 || t < count) (base + at)[uint32_t(channel)] = from_f32<T>(x[t]);
+    if (t < N - 3 || t < count) *lane_of(base + at, channel) = from_f32<T>(x[t]);
     at += channels;
     asm volatile("" : "+s"(at));
   }
@@ -412,9 +419,11 @@ __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t firs
   }
 }
 
-// A row's states from segment to segment, a thread to a channel's state; BACK: also their gradients, backwards.
+// A row's states from segment to segment, a thread to a channel's state; BACK: also their gradients, backwards. Each
+// segment's values are read ahead of the chain that needs them.
 template <bool BACK>
 __global__ __launch_bounds__(kThreads) void scan_join_kernel(Scan p, int64_t first) {
+  constexpr int kAhead = 16;
   const int64_t item = (first + blockIdx.x) * kThreads + threadIdx.x;
   if (item >= p.rows * p.states * p.channels) return;
   const int64_t channel = item % p.channels, n = item / p.channels % p.states, row = item / p.channels / p.states;
@@ -422,24 +431,32 @@ __global__ __launch_bounds__(kThreads) void scan_join_kernel(Scan p, int64_t fir
   const int64_t held = (row * p.channels + channel) * p.states + n;
   const float *steps = p.steps + row * p.segments * p.channels + channel;
   const int64_t stride = int64_t(p.states) * p.channels, at = row * p.segments * stride + n * p.channels + channel;
-  float h = p.state != nullptr ? p.state[held] : 0.0f;
-#pragma unroll 8
-  for (int64_t s = 0; s < p.segments; ++s) {
-    const float mine = p.carry[at + s * stride];
-    p.carry[at + s * stride] = h;
-    h = fmaf(exp2_fast(steps[s * p.channels] * rate), h, mine);
-  }
-  if (!BACK) {
-    if (p.state_out != nullptr) p.state_out[held] = h;
-    return;
-  }
-  float r = p.dstate_out != nullptr ? p.dstate_out[held] : 0.0f;
-#pragma unroll 8
-  for (int64_t s = p.segments - 1; s >= 0; --s) {
-    const float mine = p.back[at + s * stride];
-    p.back[at + s * stride] = r;
-    r = fmaf(exp2_fast(steps[s * p.channels] * rate), r, mine);
-  }
+  // From x on through the segments s, s + by, ..: `values` holds what each adds, and then what each begins with.
+  const auto chain = [&](float x, float *values, int64_t s, int64_t by) {
+    for (int64_t left = p.segments; left > 0; left -= kAhead) {
+      const int count = int(min(left, int64_t(kAhead)));
+      float mine[kAhead], decay[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int64_t from = s + by * min(k, count - 1);
+        mine[k] = values[from * stride];
+        decay[k] = steps[from * p.channels];
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (k >= count) break;
+        values[(s + by * k) * stride] = x;
+        x = fmaf(exp2_fast(decay[k] * rate), x, mine[k]);
+      }
+      s += by * kAhead;
+    }
+    return x;
+  };
+  const float h = chain(p.state != nullptr ? p.state[held] : 0.0f, p.carry + at, 0, 1);
+  if (BACK)
+    chain(p.dstate_out != nullptr ? p.dstate_out[held] : 0.0f, p.back + at, p.segments - 1, -1);
+  else if (p.state_out != nullptr)
+    p.state_out[held] = h;
 }
 
 typedef float Four __attribute__((ext_vector_type(4)));
@@ -454,13 +471,18 @@ struct ChannelSums {
   __device__ __forceinline__ void add(float value, float unit) {
     sum = __builtin_amdgcn_mfma_f32_16x16x4f32(value, unit, sum, 0, 0, 0);
   }
-  // token lane % 16's, in every lane
-  __device__ __forceinline__ float total() const {
-    float x = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    x += __shfl_xor(x, 16, kWave);
-    return x + __shfl_xor(x, 32, kWave);
-  }
+  // of the lane's column
+  __device__ __forceinline__ float part() const { return (sum[0] + sum[1]) + (sum[2] + sum[3]); }
 };
+
+// The columns' totals of two sums: lane t has token t's of the first, lane 32 + t of the second.
+__device__ __forceinline__ float two_totals(const ChannelSums &one, const ChannelSums &two) {
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(one.part()), __float_as_uint(two.part()), false,
+                                                       false);
+  const uint32_t x = __float_as_uint(__uint_as_float(halves[0]) + __uint_as_float(halves[1]));
+  const auto rows = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+}
 
 // `first`, 1 in lanes 0, 16, 32 and 48 and 0 in the others, moved up by T lanes in its rows of 16.
 template <int T>
@@ -576,8 +598,8 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kerne
           });
           grads[n * kWave + lane] = r;
           da[n * kWave + lane] += rates_sum;
-          float tb = sb.total(), tc = sc.total();
-          if (__builtin_expect(__ballot(!(fabsf(tb) < kInf) || !(fabsf(tc) < kInf)) != 0, 0)) {
+          float total = two_totals(sb, sc);
+          if (__builtin_expect(__ballot(!(fabsf(total) < kInf)) != 0, 0)) {
             // What is no number has spread over the unit columns' zeros: the same sums token by token.
             r = after;
             backwards<N>([&](auto token) {
@@ -588,17 +610,11 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kerne
               ob.add(me.there ? r * u[t] : 0.0f, unit);
               oc.add(me.there ? g[t] * h[t] : 0.0f, unit);
               r *= e[t];
-              const float one = ob.total(), two = oc.total();
-              if (lane % kTokens == t) {
-                tb = one;
-                tc = two;
-              }
+              const float one = two_totals(ob, oc);
+              if (lane % kTokens == t) total = one;
             });
           }
-          if (lane < kTokens) {
-            db[lane * p.states + n] = tb;
-            dc[lane * p.states + n] = tc;
-          }
+          if (lane % 32 < kTokens) (lane < 32 ? db : dc)[lane % kTokens * p.states + n] = total;
         }
         T x[N], dt[N], gate[N], o[N];
         load_tokens(p.x, w, me.channel, t0, count, x);
@@ -677,37 +693,73 @@ __global__ __launch_bounds__(kThreads) void scan_bc_kernel(Scan p, int64_t first
     static_cast<T *>(p.dc)[head * p.states + n - p.states] = from_f32<T>(sum);
 }
 
-// One token more: `lanes` threads, a power of two, to a row's channel, its states dealt to them.
-template <class T>
-__global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, int64_t first) {
-  const int64_t item = ((first + blockIdx.x) * kThreads + threadIdx.x) / lanes;
+// One token more. `lanes` threads, a power of two, take a channel's states, V neighbouring ones at a time; a
+// workgroup takes a tile of channels of kStepRows rows, whose loads are all in flight at once, and the rates once
+// for them. HBM-bound: states are read and written.
+constexpr int kStepRows = 4;
+template <class T, int V>
+__global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, int64_t tiles, int64_t first) {
+  const int64_t block = first + blockIdx.x, row0 = block / tiles * kStepRows;
   const int lane = threadIdx.x % lanes;
-  if (item >= p.rows * p.channels) return;  // whole teams leave
-  const int64_t channel = item % p.channels, row = item / p.channels, group = channel / p.per_group;
-  const int64_t from = p.parents != nullptr ? p.parents[row] : row;
-  const bool known = from >= 0 && from < p.num_states;
-  if (!known && channel == 0 && lane == 0 && p.status != nullptr) atomicOr(p.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
-  const float x = to_f32(static_cast<const T *>(p.x.data)[row * p.x.row_stride + channel]);
-  const float raw = to_f32(static_cast<const T *>(p.dt.data)[row * p.dt.row_stride + channel]);
-  const float d = softplus(raw + (p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f)), u = d * x;
-  const T *b = static_cast<const T *>(p.b.data) + row * p.b.row_stride + group * p.b.head_stride;
-  const T *c = static_cast<const T *>(p.c.data) + row * p.c.row_stride + group * p.c.head_stride;
-  float y = 0.0f;
-  for (int n = lane; n < p.states; n += lanes) {
-    const float rate = checked_rate(p.a[channel * p.states + n], row == 0 ? p.status : nullptr) * kLog2e;
-    const float old = known ? p.state[(from * p.channels + channel) * p.states + n] : 0.0f;
-    const float h = fmaf(exp2_fast(d * rate), old, u * to_f32(b[n]));
-    p.state_out[item * p.states + n] = h;
-    y = fmaf(h, to_f32(c[n]), y);
+  const int64_t at = block % tiles * (kThreads / lanes) + threadIdx.x / lanes;
+  const bool there = at < p.channels;
+  const int64_t channel = there ? at : p.channels - 1, group = channel / p.per_group;
+  const int rows = int(min(int64_t(kStepRows), p.rows - row0));
+  const float bias = p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f;
+  const float skip = p.skip != nullptr ? p.skip[channel] : 0.0f;
+  int64_t from[kStepRows];
+  float x[kStepRows], d[kStepRows], z[kStepRows], y[kStepRows] = {};
+#pragma unroll
+  for (int r = 0; r < kStepRows; ++r) {
+    const int64_t row = row0 + min(r, rows - 1);
+    from[r] = p.parents != nullptr ? p.parents[row] : row;
+    x[r] = to_f32(static_cast<const T *>(p.x.data)[row * p.x.row_stride + channel]);
+    d[r] = to_f32(static_cast<const T *>(p.dt.data)[row * p.dt.row_stride + channel]);
+    z[r] = p.gate.data != nullptr
+               ? to_f32(static_cast<const T *>(p.gate.data)[row * p.gate.row_stride + channel])
+               : 0.0f;
   }
-  for (int m = lanes / 2; m > 0; m /= 2) y += __shfl_xor(y, m, kWave);
-  if (lane != 0) return;
-  y = fmaf(p.skip != nullptr ? p.skip[channel] : 0.0f, x, y);
-  if (p.gate.data != nullptr) {
-    const float z = to_f32(static_cast<const T *>(p.gate.data)[row * p.gate.row_stride + channel]);
-    y *= z * sigmoid(z);
+  for (int n = lane * V; n < p.states; n += lanes * V) {
+    float rate[V], h[kStepRows][V], b[kStepRows][V], c[kStepRows][V];
+    load_values<float, V>(p.a + channel * p.states + n, V, rate);
+#pragma unroll
+    for (int r = 0; r < kStepRows; ++r) {
+      const int64_t row = row0 + min(r, rows - 1);
+      const bool known = from[r] >= 0 && from[r] < p.num_states;
+      load_values<float, V>(p.state + ((known ? from[r] : 0) * p.channels + channel) * p.states + n,
+                            p.num_states > 0 ? V : 0, h[r]);
+      load_values<T, V>(static_cast<const T *>(p.b.data) + row * p.b.row_stride + group * p.b.head_stride + n, V, b[r]);
+      load_values<T, V>(static_cast<const T *>(p.c.data) + row * p.c.row_stride + group * p.c.head_stride + n, V, c[r]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) h[r][i] = known ? h[r][i] : 0.0f;
+    }
+    if (n == lane * V)
+#pragma unroll
+      for (int r = 0; r < kStepRows; ++r) d[r] = softplus(d[r] + bias);
+#pragma unroll
+    for (int i = 0; i < V; ++i) rate[i] = checked_rate(rate[i], row0 == 0 ? p.status : nullptr) * kLog2e;
+#pragma unroll
+    for (int r = 0; r < kStepRows; ++r) {
+      const float u = d[r] * x[r];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        h[r][i] = fmaf(exp2_fast(d[r] * rate[i]), h[r][i], u * b[r][i]);
+        y[r] = fmaf(h[r][i], c[r][i], y[r]);
+      }
+      if (there && r < rows)
+        store_values<float, V>(p.state_out + ((row0 + r) * p.channels + channel) * p.states + n, V, h[r]);
+    }
   }
-  static_cast<T *>(p.out)[item] = from_f32<T>(y);
+#pragma unroll
+  for (int r = 0; r < kStepRows; ++r) {
+    for (int m = lanes / 2; m > 0; m /= 2) y[r] += __shfl_xor(y[r], m, kWave);
+    if (r >= rows || lane != 0 || !there) continue;
+    if (channel == 0 && p.status != nullptr && (from[r] < 0 || from[r] >= p.num_states))
+      atomicOr(p.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
+    y[r] = fmaf(skip, x[r], y[r]);
+    if (p.gate.data != nullptr) y[r] *= silu(z[r]);
+    static_cast<T *>(p.out)[(row0 + r) * p.channels + channel] = from_f32<T>(y[r]);
+  }
 }
 
 Scan base(const rdf2v_scan &a, const ScanInputs &in, int32_t *status) {
@@ -736,7 +788,7 @@ Scan base(const rdf2v_scan &a, const ScanInputs &in, int32_t *status) {
 // Segments of a row, chunks, the waves along rows and segments, and where the workspace's arrays lie; its bytes.
 size_t plan(Scan &p, bool backward, void *workspace) {
   // Waves that fill the chip are 1,024 times two or three.
-  constexpr int64_t kFew = 1024, kFill = 2048, kMost = 8192, kShortest = 2 * kTokens;
+  constexpr int64_t kFew = 1024, kFill = 4096, kMost = 8192, kShortest = 2 * kTokens;
   const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
   int64_t segments = 1;
   if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
@@ -887,14 +939,21 @@ rdf2v_status launch_selective_scan_step(const rdf2v_scan &a, const ScanInputs &i
   p.parents = parents;
   p.out = out;
   p.state_out = state_out;
+  // whole vectors of four states where there are no others
+  const int each = p.states % 4 == 0 ? 4 : 1;
   int lanes = 1;
-  while (lanes < kWave && lanes < p.states) lanes *= 2;
-  const int64_t blocks = (p.rows * p.channels + kThreads / lanes - 1) / (kThreads / lanes);
-  return for_each_launch(blocks, kThreads, 1, [&](int64_t first, int64_t count) {
-    if (a.dtype == RDF2V_BF16)
-      scan_step_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, lanes, first);
+  while (lanes < kWave && lanes * each < p.states) lanes *= 2;
+  const int64_t per = kThreads / lanes, tiles = (p.channels + per - 1) / per;
+  return for_each_launch((p.rows + kStepRows - 1) / kStepRows * tiles, kThreads, 1, [&](int64_t first, int64_t count) {
+    const dim3 grid(static_cast<unsigned>(count)), block(kThreads);
+    if (a.dtype == RDF2V_BF16 && each == 4)
+      scan_step_kernel<bf16, 4><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+    else if (a.dtype == RDF2V_BF16)
+      scan_step_kernel<bf16, 1><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+    else if (each == 4)
+      scan_step_kernel<float, 4><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
     else
-      scan_step_kernel<float><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, lanes, first);
+      scan_step_kernel<float, 1><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });
