@@ -28,6 +28,10 @@ struct Conv {
   int32_t channels, lanes;       // gradients: threads side by side in the channels
 };
 
+// Channels of a vector in the gradients: what is held of each, 5 width + 8 values, sets how many waves there are.
+template <class T>
+constexpr int kBackwardVector = sizeof(T) == 2 ? 4 : 2;
+
 template <int W, int V>
 struct Taps {
   float w[W][V], bias[V];
@@ -89,13 +93,18 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
     float x[W][V];
 #pragma unroll
     for (int j = 0; j + 1 < W; ++j) load_input<T, W, V>(a, row, begin - (W - 1) + j, c, n, x[j + 1]);
-    for (int64_t t = begin; t < stop; t += kAhead) {
+    const T *from = static_cast<const T *>(a.x) + row * a.row_stride + begin * a.token_stride + c;
+    T *to = out + begin * a.channels;
+    for (int left = int(stop - begin); left > 0; left -= kAhead) {
       float next[kAhead][V];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) load_input<T, W, V>(a, row, min(t + k, stop - 1), c, n, next[k]);
+      for (int k = 0; k < kAhead; ++k) {
+        load_values<T, V>(from, n, next[k]);
+        if (k + 1 < left) from += a.token_stride;
+      }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        if (t + k >= stop) break;
+        if (k >= left) break;
         shift<W, V>(x);
         float y[V];
 #pragma unroll
@@ -104,7 +113,8 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
           const float u = tap_sum<W, V>(taps, x, i);
           y[i] = SILU ? u * sigmoid(u) : u;
         }
-        store_values<T, V>(out + (t + k) * a.channels, n, y);
+        store_values<T, V>(to, n, y);
+        to += a.channels;
       }
     }
   }
@@ -118,18 +128,18 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
   }
 }
 
-// Gradients. `lanes` threads side by side take vectors of channels, the workgroup's others and the `parts`
-// workgroups the tiles of tokens in turn; the parameters' gradients stay in registers until the end. dx_p is a
+// Gradients. `lanes` threads side by side take vectors of channels, the workgroup's others (what is left of them has
+// nothing to do) and the `parts` workgroups the tiles of tokens in turn; the parameters' gradients stay in registers until the end. dx_p is a
 // sum over the `width` tokens from p on, so a tile goes width - 1 tokens beyond its end; the first tile begins
 // with the state's inputs.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t first) {
-  constexpr int V = 4, kAhead = 4;
+  constexpr int V = kBackwardVector<T>, kAhead = 4;
   __shared__ float scratch[kThreads][V];
   const int64_t block = first + blockIdx.x, part = block / a.blocks;
   const int subs = kThreads / a.lanes, sub = threadIdx.x / a.lanes, lane = threadIdx.x % a.lanes;
   const int64_t vector = block % a.blocks * a.lanes + lane, c = vector * V;
-  const bool there = vector < a.vectors;
+  const bool there = vector < a.vectors && sub < subs;
   const int n = there ? int(min(int64_t(V), a.channels - c)) : 0;
   float dw[W][V] = {}, db[V] = {};
   if (there) {
@@ -139,66 +149,71 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
       const int64_t row = item / a.tiles, tile = item % a.tiles;
       const int64_t length = row_length(a.len, row, a.length, vector == 0 && tile == 0, a.status);
       const int64_t begin = tile * a.tile, end = min(begin + a.tile, a.length), stop = min(end, length);
-      const int64_t from = tile == 0 && a.dstate != nullptr ? -(W - 1) : begin;  // first input with a gradient here
-      const T *dout = static_cast<const T *>(a.dout) + row * a.dout_row_stride + c;
-      T *dx = static_cast<T *>(a.out) + row * a.length * a.channels + c;
-      const int64_t to = min(end, length) + W - 1;  // tokens whose gradients reach an input of the tile
-      if (from < stop || (from < 0 && a.dstate != nullptr)) {
+      const bool states = tile == 0 && a.dstate != nullptr;  // the state's inputs are the tile's too
+      T *dx = static_cast<T *>(a.out) + (row * a.length + begin) * a.channels + c;
+      int zeros = int(end - begin);
+      if (begin < stop || states) {
         float x[W][V], du[W][V] = {};  // inputs of the tokens up to t; gradients of u of the tokens up to t
 #pragma unroll
         for (int j = 0; j + 1 < W; ++j) load_input<T, W, V>(a, row, begin - (W - 1) + j, c, n, x[j + 1]);
-        for (int64_t t = begin; t < to; t += kAhead) {
+        const T *px = static_cast<const T *>(a.x) + row * a.row_stride + begin * a.token_stride + c;
+        const T *pd = static_cast<const T *>(a.dout) + row * a.dout_row_stride + begin * a.dout_token_stride + c;
+        // counted from `begin`: tokens of the row, of the tile, and those whose gradients reach an input of the tile
+        const int64_t rest = length - begin;
+        const int own = int(stop - begin), to = own + W - 1, real = int(min(rest, int64_t(to)));
+        zeros -= own;
+        for (int t = 0; t < to; t += kAhead) {
           float nx[kAhead][V], nd[kAhead][V];
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) {
-            const int64_t s = min(t + k, length - 1);
-            if (t + k < length) {
-              load_input<T, W, V>(a, row, s, c, n, nx[k]);
-              load_values<T, V>(dout + s * a.dout_token_stride, n, nd[k]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < V; ++i) nx[k][i] = nd[k][i] = 0.0f;
+            load_values<T, V>(px, t + k < real ? n : 0, nx[k]);
+            load_values<T, V>(pd, t + k < real ? n : 0, nd[k]);
+            if (t + k + 1 < real) {
+              px += a.token_stride;
+              pd += a.dout_token_stride;
             }
           }
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) {
-            const int64_t s = t + k, p = s - (W - 1);
+            const int s = t + k, p = s - (W - 1);
             if (s >= to) break;
             shift<W, V>(x);
             shift<W, V>(du);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
               x[W - 1][i] = nx[k][i];
-              float d = s < length ? nd[k][i] : 0.0f;
-              if (SILU && s < length) {
+              float d = nd[k][i];
+              if (SILU && s < real) {
                 const float u = tap_sum<W, V>(taps, x, i);
                 d *= silu_slope(u, sigmoid(u));
               }
               du[W - 1][i] = d;
-              if (s < stop) {
+              if (s < own) {
                 db[i] += d;
 #pragma unroll
                 for (int j = 0; j < W; ++j) dw[j][i] = fmaf(d, x[j][i], dw[j][i]);
               }
             }
-            if (p < from) continue;
+            if (p < 0 && !states) continue;
             float g[V] = {};
-            const int64_t slot = p - (length - (W - 1));  // of the state that the row leaves
+            const int64_t slot = p - (rest - (W - 1));  // of the state that the row leaves
             if (slot >= 0 && a.dstate_out != nullptr)
               load_values<T, V>(static_cast<const T *>(a.dstate_out) + (row * (W - 1) + slot) * a.channels + c, n, g);
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
               for (int j = 0; j < W; ++j) g[i] = fmaf(taps.w[j][i], du[W - 1 - j][i], g[i]);
-            if (p >= 0)
-              store_values<T, V>(dx + p * a.channels, n, g);
-            else
+            if (p >= 0) {
+              store_values<T, V>(dx, n, g);
+              dx += a.channels;
+            } else {
               store_values<T, V>(static_cast<T *>(a.dstate) + (row * (W - 1) + p + W - 1) * a.channels + c, n, g);
+            }
           }
         }
       }
-      const float zeros[V] = {};
-      for (int64_t t = max(begin, stop); t < end; ++t) store_values<T, V>(dx + t * a.channels, n, zeros);
+      const float zero[V] = {};
+      for (; zeros > 0; --zeros, dx += a.channels) store_values<T, V>(dx, n, zero);
     }
   }
   // the workgroup's threads of one vector, in order
@@ -292,21 +307,22 @@ Conv base(const rdf2v_conv &a, const rdf2v_tokens_view &x, int32_t *status) {
   return c;
 }
 
-// Tiles of about 16 tokens, of one size but for the last; one also for rows without tokens.
-void tile_rows(Conv &c) {
-  constexpr int64_t kTile = 16;
-  c.tiles = c.length == 0 ? 1 : (c.length + kTile - 1) / kTile;
+// Tiles of at most `most` tokens, of one size but for the last; one also for rows without tokens.
+void tile_rows(Conv &c, int64_t most) {
+  c.tiles = c.length == 0 ? 1 : (c.length + most - 1) / most;
   c.tile = c.length == 0 ? 1 : (c.length + c.tiles - 1) / c.tiles;
   c.tiles = c.length == 0 ? 1 : (c.length + c.tile - 1) / c.tile;
 }
 
-// The gradients' workgroups.
-void plan_backward(Conv &c) {
-  tile_rows(c);
-  c.vectors = (int64_t(c.channels) + 3) / 4;
-  c.lanes = 1;
-  while (c.lanes < kWave && c.lanes < c.vectors) c.lanes *= 2;
-  c.blocks = (c.vectors + c.lanes - 1) / c.lanes;
+// The gradients' workgroups. A tile reads width - 1 tokens more at either end, so tiles are long where there are
+// enough of them.
+void plan_backward(Conv &c, int32_t dtype) {
+  const int64_t each = dtype == RDF2V_BF16 ? kBackwardVector<bf16> : kBackwardVector<float>;
+  c.vectors = (int64_t(c.channels) + each - 1) / each;
+  c.blocks = (c.vectors + kWave - 1) / kWave;
+  c.lanes = int32_t((c.vectors + c.blocks - 1) / c.blocks);
+  tile_rows(c, 64);
+  if (c.rows * c.tiles * c.vectors < (int64_t(1) << 18)) tile_rows(c, 16);
   const int64_t subs = kThreads / c.lanes, most = (c.rows * c.tiles + subs - 1) / subs;
   c.parts = std::max<int64_t>(1, std::min(most, 2048 / c.blocks));
 }
@@ -316,7 +332,7 @@ void plan_backward(Conv &c) {
 size_t causal_conv_backward_workspace_bytes(const rdf2v_conv &a) {
   if (a.rows == 0) return 0;
   Conv c = base(a, {}, nullptr);
-  plan_backward(c);
+  plan_backward(c, a.dtype);
   return align_up(size_t(c.parts) * a.channels * (a.width + 1) * sizeof(float), 256);
 }
 
@@ -326,7 +342,7 @@ rdf2v_status launch_causal_conv(const rdf2v_conv &a, const rdf2v_tokens_view &x,
   c.state = state;
   c.out = out;
   c.state_out = state_out;
-  tile_rows(c);
+  tile_rows(c, 16);
   const int per = 4;
   c.vectors = (int64_t(a.channels) + per - 1) / per;
   const int64_t blocks = (a.rows * c.tiles * c.vectors + kThreads - 1) / kThreads;
@@ -355,7 +371,7 @@ rdf2v_status launch_causal_conv_backward(const rdf2v_conv &a, const rdf2v_tokens
   c.out = dx;
   c.dstate = a.width > 1 ? dstate : nullptr;
   c.partial = static_cast<float *>(workspace);
-  plan_backward(c);
+  plan_backward(c, a.dtype);
   if (a.rows > 0) {
     const rdf2v_status st = with_width(a.width, a.silu != 0, [&](auto width, auto silu) {
       return for_each_launch(c.blocks * c.parts, kThreads, 1, [&](int64_t first, int64_t count) {

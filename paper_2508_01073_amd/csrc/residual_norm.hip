@@ -33,7 +33,8 @@ struct Norm {
   uint64_t seed;
   int32_t channels;
   uint32_t threshold;
-  float keep, eps;
+  float keep, eps;  // keep: 1 without dropout
+  bool center;
 };
 
 // Four words of Philox4x32-10 (Salmon, Moraes, Dror & Shaw, SC'11).
@@ -55,28 +56,39 @@ __device__ __forceinline__ Words4 philox(uint32_t x0, uint32_t x1, uint64_t row,
   return {{x0, x1, x2, x3}};
 }
 
-// Sums over a team of TEAM threads, in each of them. Teams of more than a wave: a barrier, `scratch` of a sum
-// for each wave and two calls before it is used again.
+// Sums over a team of TEAM threads, in each of them: over rows of 16 lanes with DPP rotations, over the rows of a
+// wave with swaps, over a team's waves through LDS. Teams of more than a wave: one barrier, and `scratch`, a place
+// for each wave, is not used in the call that follows.
 template <int TEAM, int N>
 __device__ __forceinline__ void team_sum(float (&x)[N], float (*scratch)[N]) {
-  if constexpr (TEAM < kWave) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+  for (int i = 0; i < N; ++i) {
+#define RDF2V_ROTATE(BY) \
+  x[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x[i]), 0x120 + BY, 0xf, 0xf, false));
+    RDF2V_ROTATE(8)
+    RDF2V_ROTATE(4)
+    RDF2V_ROTATE(2)
+    RDF2V_ROTATE(1)
+#undef RDF2V_ROTATE
+    if constexpr (TEAM > 16) {
+      const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[i]), __float_as_uint(x[i]), false, false);
+      x[i] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+    if constexpr (TEAM > 32) {
+      const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[i]), __float_as_uint(x[i]), false, false);
+      x[i] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+    }
+  }
+  if constexpr (TEAM > kWave) {
+    if (lane_id() == 0)
 #pragma unroll
-      for (int m = TEAM / 2; m > 0; m /= 2) x[i] += __shfl_xor(x[i], m, kWave);
-  } else {
+      for (int i = 0; i < N; ++i) scratch[threadIdx.x / kWave][i] = x[i];
+    __syncthreads();
+    const int first = threadIdx.x / TEAM * (TEAM / kWave);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = wave_sum(x[i]);
-    if constexpr (TEAM > kWave) {
-      if (lane_id() == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) scratch[threadIdx.x / kWave][i] = x[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        x[i] = scratch[0][i];
-        for (int w = 1; w < TEAM / kWave; ++w) x[i] += scratch[w][i];
-      }
+    for (int i = 0; i < N; ++i) {
+      x[i] = scratch[first][i];
+      for (int w = 1; w < TEAM / kWave; ++w) x[i] += scratch[first + w][i];
     }
   }
 }
@@ -101,42 +113,69 @@ __device__ __forceinline__ void store_token(T *p, const Own<TEAM, PER> &own, con
   for (int i = 0; i < PER; ++i) store_values<T, V>(p + own.at(i), own.count(i), x[i]);
 }
 
-// x after dropout, and the factors that it was multiplied with (0: dropped, whatever x holds).
-template <bool DROP, int TEAM, int PER>
+// The residual's scale: ones where there is none.
+template <int TEAM, int PER>
+__device__ __forceinline__ void load_scale(const Norm &a, const Own<TEAM, PER> &own, float (&scale)[PER][V]) {
+  if (a.scale != nullptr) {
+    load_token(a.scale, own, scale);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+#pragma unroll
+    for (int j = 0; j < V; ++j) scale[i][j] = 1.0f;
+}
+
+// x after dropout, where there is any, and what is kept, a bit for each value. What is dropped counts as 0, whatever
+// it holds.
+template <int TEAM, int PER>
 __device__ __forceinline__ void dropout(const Norm &a, const Own<TEAM, PER> &own, int64_t row, int64_t token,
-                                        uint64_t key, float (&x)[PER][V], uint64_t &kept) {
-  kept = ~uint64_t(0);
-  if constexpr (DROP) {
+                                        uint64_t key, float (&x)[PER][V], uint32_t &kept) {
+  kept = ~uint32_t(0);
+  if (a.threshold == 0) return;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const Words4 r = philox(uint32_t(own.at(i) / V), uint32_t(token + 1), uint64_t(a.row_begin + row), key);
+  for (int i = 0; i < PER; ++i) {
+    const Words4 r = philox(uint32_t(own.at(i) / V), uint32_t(token + 1), uint64_t(a.row_begin + row), key);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const bool keep = r.w[j] >= a.threshold;
-        x[i][j] = keep ? x[i][j] * a.keep : 0.0f;
-        if (!keep) kept &= ~(uint64_t(1) << (i * V + j));
-      }
+    for (int j = 0; j < V; ++j) {
+      const bool keep = r.w[j] >= a.threshold;
+      x[i][j] = keep ? x[i][j] * a.keep : 0.0f;
+      if (!keep) kept &= ~(uint32_t(1) << (i * V + j));
     }
+  }
+}
+
+// Row and token of one of all tokens.
+__device__ __forceinline__ void locate(const Norm &a, int64_t id, int64_t &row, int64_t &token) {
+  if (a.tokens <= 0xffffffffll) {  // a division of 32 bits is a fifth of one of 64
+    row = uint32_t(id) / uint32_t(a.length);
+    token = uint32_t(id) - uint32_t(row) * uint32_t(a.length);
+  } else {
+    row = id / a.length;
+    token = id % a.length;
   }
 }
 
 constexpr int workgroup_of(int team) { return team < kThreads ? kThreads : team; }
 
-template <class T, class R, bool DROP, bool CENTER, int TEAM, int PER>
+template <class T, class R, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
   __shared__ float scratch[2][kBlock / kWave][1];
   const Own<TEAM, PER> own{int(threadIdx.x) % TEAM, a.channels};
-  const uint64_t key = a.seed + (DROP && a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
+  const uint64_t key = a.seed + (a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
   const float inverse = 1.0f / float(a.channels);
-  float weight[PER][V];
+  float weight[PER][V], scale[PER][V], bias[PER][V] = {};
   load_token(a.weight, own, weight);
+  if (a.bias != nullptr) load_token(a.bias, own, bias);
+  load_scale(a, own, scale);
   int turn = 0;
   for (int64_t at = int64_t(blockIdx.x) * kTeams; at < a.tokens; at += a.workgroups * kTeams) {
     // a team without a token goes along: it has lanes in common with those that have one
     const bool mine = at + int(threadIdx.x) / TEAM < a.tokens;
     const int64_t id = mine ? at + int(threadIdx.x) / TEAM : a.tokens - 1;
-    const int64_t row = id / a.length, token = id % a.length;
+    int64_t row, token;
+    locate(a, id, row, token);
     const bool live = token < row_length(a.len, row, a.length, mine && token == 0 && own.lane == 0, a.status);
     float h[PER][V] = {};
     if (live) {
@@ -144,24 +183,16 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_kernel(Norm a) {
       float from[PER][V] = {};
       if (a.residual != nullptr)
         load_token(static_cast<const R *>(a.residual) + row * a.residual_row + token * a.residual_token, own, from);
-      uint64_t kept;
-      dropout<DROP>(a, own, row, token, key, h, kept);
-      if (a.scale != nullptr) {
-        float scale[PER][V];
-        load_token(a.scale, own, scale);
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-#pragma unroll
-          for (int j = 0; j < V; ++j) h[i][j] *= scale[i][j];
-      }
+      uint32_t kept;
+      dropout(a, own, row, token, key, h, kept);
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) h[i][j] += from[i][j];
+        for (int j = 0; j < V; ++j) h[i][j] = fmaf(h[i][j], scale[i][j], from[i][j]);
     }
     if (mine && a.hidden != nullptr) store_token(static_cast<R *>(a.hidden) + id * a.channels, own, h);
     float mean = 0.0f, sum[1] = {0.0f};
-    if constexpr (CENTER) {
+    if (a.center) {
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -188,8 +219,6 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_kernel(Norm a) {
       a.stats[2 * id + 1] = inv;
     }
     if (live) {
-      float bias[PER][V] = {};
-      if (a.bias != nullptr) load_token(a.bias, own, bias);
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -228,34 +257,28 @@ __device__ __forceinline__ void store_part(float *part, const Own<TEAM, PER> &ow
 // With n = (hidden - mean) / std and dn = dout * weight, a token's gradient is
 //   dhidden + (dn - n mean(dn n) - mean(dn)) / std        (the last mean where the norm is centred)
 // MORE: there is a scale, or gradients of the bias or the scale are wanted.
-template <class T, class R, bool DROP, bool CENTER, bool MORE, int TEAM, int PER>
+template <class T, class R, bool MORE, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
   __shared__ float scratch[2][kBlock / kWave][2];
   __shared__ float parts[kTeams > 1 ? kBlock : 1][V];
   const Own<TEAM, PER> own{int(threadIdx.x) % TEAM, a.channels};
-  const uint64_t key = a.seed + (DROP && a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
+  const uint64_t key = a.seed + (a.seed_offset != nullptr ? uint64_t(*a.seed_offset) : 0);
   const float inverse = 1.0f / float(a.channels);
   float weight[PER][V], scale[PER][V];
   load_token(a.weight, own, weight);
-  if (MORE && a.scale != nullptr) {
-    load_token(a.scale, own, scale);
-  } else {
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-#pragma unroll
-      for (int j = 0; j < V; ++j) scale[i][j] = 1.0f;
-  }
+  load_scale(a, own, scale);
   float dweight[PER][V] = {}, dbias[PER][V] = {}, dscale[PER][V] = {};
   int turn = 0;
   for (int64_t at = int64_t(blockIdx.x) * kTeams; at < a.tokens; at += a.workgroups * kTeams) {
     const bool mine = at + int(threadIdx.x) / TEAM < a.tokens;
     const int64_t id = mine ? at + int(threadIdx.x) / TEAM : a.tokens - 1;
-    const int64_t row = id / a.length, token = id % a.length;
+    int64_t row, token;
+    locate(a, id, row, token);
     const bool live =
         token < row_length(a.len, row, a.length, mine && token == 0 && own.lane == 0, a.status) && mine;
     float x[PER][V] = {}, h[PER][V] = {}, d[PER][V] = {}, dh[PER][V] = {};
-    uint64_t kept = 0;
+    uint32_t kept = 0;
     float inv = 0.0f, sums[2] = {0.0f, 0.0f};
     if (live) {
       load_token(static_cast<const T *>(a.x) + row * a.x_row + token * a.x_token, own, x);
@@ -264,9 +287,9 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm 
       load_token(static_cast<const T *>(a.dout) + row * a.dout_row + token * a.dout_token, own, d);
       if (a.dhidden != nullptr)
         load_token(static_cast<const R *>(a.dhidden) + row * a.dhidden_row + token * a.dhidden_token, own, dh);
-      const float mean = CENTER ? a.stats_in[2 * id] : 0.0f;
+      const float mean = a.stats_in[2 * id];
       inv = a.stats_in[2 * id + 1];
-      dropout<DROP>(a, own, row, token, key, x, kept);
+      dropout(a, own, row, token, key, x, kept);
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -277,20 +300,14 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm 
           if (MORE) dbias[i][j] += d[i][j];
           d[i][j] *= weight[i][j];
           if (j < own.count(i)) sums[0] = fmaf(d[i][j], n, sums[0]);
-          if (CENTER) sums[1] += d[i][j];
+          sums[1] += d[i][j];
         }
     }
-    if constexpr (CENTER) {
-      team_sum<TEAM>(sums, scratch[turn]);
-    } else {
-      float one[1] = {sums[0]};
-      team_sum<TEAM>(one, reinterpret_cast<float(*)[1]>(&scratch[turn][0][0]));
-      sums[0] = one[0];
-    }
+    team_sum<TEAM>(sums, scratch[turn]);
     turn ^= 1;
     if (!mine) continue;
     if (live) {
-      const float along = sums[0] * inverse, level = CENTER ? sums[1] * inverse : 0.0f;
+      const float along = sums[0] * inverse, level = a.center ? sums[1] * inverse : 0.0f;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -299,7 +316,7 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm 
           dh[i][j] = g;
           if (MORE) dscale[i][j] = fmaf(g, x[i][j], dscale[i][j]);
           d[i][j] = MORE ? g * scale[i][j] : g;
-          if (DROP) d[i][j] = kept >> (i * V + j) & 1 ? d[i][j] * a.keep : 0.0f;
+          d[i][j] = kept >> (i * V + j) & 1 ? d[i][j] * a.keep : 0.0f;
         }
     }
     store_token(static_cast<T *>(a.out) + id * a.channels, own, d);
@@ -313,18 +330,27 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm 
   }
 }
 
-// Calls launch with constants for the size of a team and the vectors of a thread: the fewest threads that leave
-// each at most four vectors.
-template <class Launch>
+// Calls launch with constants for the size of a team and the vectors of a thread: the smallest team that needs two
+// at most, three in the forward call: the generator works for all lanes, with channels or without. In the gradients
+// a third costs more in waves than idle lanes do (69,632 tokens of 301 channels: teams of 32 with three vectors and
+// of 64 with two take 72 and 80 us forward, 115 and 94 us backward).
+template <bool BACKWARD, class Launch>
 rdf2v_status with_team(int channels, Launch launch) {
 #define RDF2V_TEAM(TEAM, PER) \
   if (channels <= TEAM * PER * V) return launch(std::integral_constant<int, TEAM>{}, std::integral_constant<int, PER>{});
   RDF2V_TEAM(16, 1)
-  RDF2V_TEAM(64, 1)
+  RDF2V_TEAM(16, 2)
+  RDF2V_TEAM(32, 2)
+  if constexpr (!BACKWARD) {
+    RDF2V_TEAM(32, 3)
+  }
   RDF2V_TEAM(64, 2)
-  RDF2V_TEAM(64, 4)
+  if constexpr (!BACKWARD) {
+    RDF2V_TEAM(64, 3)
+  }
+  RDF2V_TEAM(128, 2)
   RDF2V_TEAM(256, 2)
-  RDF2V_TEAM(256, 4)
+  RDF2V_TEAM(512, 2)
   RDF2V_TEAM(1024, 2)
   RDF2V_TEAM(1024, 4)
 #undef RDF2V_TEAM
@@ -343,21 +369,20 @@ rdf2v_status with_flag(bool flag, Launch launch) {
   return flag ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
-int teams_of_workgroup(int channels) {
-  int teams = 1;
-  with_team(channels, [&](auto team, auto) {
-    teams = workgroup_of(team()) / team();
+// As many workgroups as the chip holds at once with 16 or 24 waves on each of its 256 compute units, at most one for
+// each workgroup's teams of tokens: they take tokens in turn, and a second round of some would leave units idle
+// (16,384 tokens of 4,096 channels, gradients: 349 us with 1,024 workgroups where 768 fit).
+template <bool BACKWARD>
+int64_t workgroups_of(int64_t tokens, int channels) {
+  constexpr int64_t waves = BACKWARD ? 16 : 24;
+  int64_t count = 1;
+  with_team<BACKWARD>(channels, [&](auto team, auto) {
+    const int64_t teams = workgroup_of(team()) / team();
+    count = std::min((tokens + teams - 1) / teams, 256 * std::max<int64_t>(1, waves * kWave / workgroup_of(team())));
     return RDF2V_OK;
   });
-  return teams;
+  return std::max<int64_t>(1, count);
 }
-
-// Workgroups that fill the chip, each with tokens to hold the parameters for.
-int64_t workgroups_of(int64_t tokens, int channels, int64_t most) {
-  const int64_t teams = teams_of_workgroup(channels);
-  return std::max<int64_t>(1, std::min((tokens + teams - 1) / teams, most));
-}
-constexpr int64_t kForward = 2048, kBackward = 1024;
 
 Norm base(const rdf2v_norm &a, const rdf2v_tokens_view &x, const rdf2v_tokens_view &residual, int32_t *status) {
   Norm n{};
@@ -379,7 +404,8 @@ Norm base(const rdf2v_norm &a, const rdf2v_tokens_view &x, const rdf2v_tokens_vi
   n.seed = a.seed;
   n.channels = a.channels;
   n.threshold = uint32_t(std::nearbyint(a.drop * 0x1p32));
-  n.keep = float(1.0 / (1.0 - a.drop));
+  n.keep = n.threshold != 0 ? float(1.0 / (1.0 - a.drop)) : 1.0f;
+  n.center = a.center != 0;
   n.eps = a.eps;
   return n;
 }
@@ -388,7 +414,7 @@ Norm base(const rdf2v_norm &a, const rdf2v_tokens_view &x, const rdf2v_tokens_vi
 
 size_t residual_norm_backward_workspace_bytes(const rdf2v_norm &a) {
   if (a.rows == 0 || a.length == 0) return 0;
-  return align_up(size_t(workgroups_of(a.rows * a.length, a.channels, kBackward)) * a.channels * 3 * sizeof(float),
+  return align_up(size_t(workgroups_of<true>(a.rows * a.length, a.channels)) * a.channels * 3 * sizeof(float),
                   256);
 }
 
@@ -398,17 +424,13 @@ rdf2v_status launch_residual_norm(const rdf2v_norm &a, const rdf2v_tokens_view &
   n.out = out;
   n.hidden = hidden;
   n.stats = stats;
-  n.workgroups = workgroups_of(n.tokens, a.channels, kForward);
+  n.workgroups = workgroups_of<false>(n.tokens, a.channels);
   return with_types(a.dtype, a.residual_dtype, [&](auto t, auto r) {
-    return with_flag(n.threshold != 0, [&](auto drop) {
-      return with_flag(a.center != 0, [&](auto center) {
-        return with_team(a.channels, [&](auto team, auto per) {
-          norm_kernel<decltype(t), decltype(r), drop(), center(), team(), per()>
-              <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
-          RDF2V_LAUNCH_CHECK();
-          return RDF2V_OK;
-        });
-      });
+    return with_team<false>(a.channels, [&](auto team, auto per) {
+      norm_kernel<decltype(t), decltype(r), team(), per()>
+          <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
+      RDF2V_LAUNCH_CHECK();
+      return RDF2V_OK;
     });
   });
 }
@@ -429,29 +451,23 @@ rdf2v_status launch_residual_norm_backward(const rdf2v_norm &a, const rdf2v_toke
   n.out = dx;
   n.hidden = dresidual;
   n.partial = static_cast<float *>(workspace);
-  n.workgroups = n.tokens > 0 ? workgroups_of(n.tokens, a.channels, kBackward) : 0;
+  n.workgroups = n.tokens > 0 ? workgroups_of<true>(n.tokens, a.channels) : 0;
   const bool more = a.scale != nullptr || dbias != nullptr || dscale != nullptr;
   if (n.tokens > 0) {
     const rdf2v_status st = with_types(a.dtype, a.residual_dtype, [&](auto t, auto r) {
-      return with_flag(n.threshold != 0, [&](auto drop) {
-        return with_flag(a.center != 0, [&](auto center) {
-          return with_flag(more, [&](auto has) {
-            return with_team(a.channels, [&](auto team, auto per) {
-              norm_backward_kernel<decltype(t), decltype(r), drop(), center(), has(), team(), per()>
-                  <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
-              RDF2V_LAUNCH_CHECK();
-              return RDF2V_OK;
-            });
-          });
+      return with_flag(more, [&](auto has) {
+        return with_team<true>(a.channels, [&](auto team, auto per) {
+          norm_backward_kernel<decltype(t), decltype(r), has(), team(), per()>
+              <<<dim3(unsigned(n.workgroups)), dim3(workgroup_of(team())), 0, stream>>>(n);
+          RDF2V_LAUNCH_CHECK();
+          return RDF2V_OK;
         });
       });
     });
     if (st != RDF2V_OK) return st;
   }
   const int64_t rest = more ? a.channels : 0;
-  const rdf2v_status st =
-      launch_part_sums({n.partial, n.workgroups, {a.channels, rest, rest}, {dweight, dbias, dscale}}, stream);
-  return st;
+  return launch_part_sums({n.partial, n.workgroups, {a.channels, rest, rest}, {dweight, dbias, dscale}}, stream);
 }
 
 }  // namespace rdf2v
