@@ -16,7 +16,7 @@
 //
 // Gradients go backwards through the chunks: a chunk's states are made again from the one before it, which
 // scan_states_kernel has left in memory, and stay in registers for the way back. The sums over states (for x and
-// dt) are a lane's own; the sums over channels (for b and c) are taken by matrix instructions, see ChannelSums.
+// dt) are a lane's own; the sums over channels (for b and c) are taken for sixteen values at once, see sixteen_sums.
 
 #include "vectors.hpp"
 
@@ -27,6 +27,8 @@ namespace rdf2v {
 namespace {
 
 constexpr int kTokens = 16;  // of a chunk
+constexpr int kBackTokens = 8;  // of a chunk in the gradients: what is held of each sets how many waves there are
+constexpr int kGang = 4;        // waves of a workgroup in the gradients, which have the rates in common
 constexpr int kThreads = 256;  // of a workgroup where waves need not be alone
 
 struct Scan {
@@ -44,7 +46,7 @@ struct Scan {
   float *starts;  // [rows][chunks][states]: the state before a chunk, from zeros at the segment's begin
   float *until;   // [rows][chunks]: sum of delta from the segment's begin to the chunk
   float *partial; // [parts]: gradients of a, dt_bias and skip
-  float *bc;      // [blocks of a group][rows][length][groups][2 states]: parts of the gradients of b and c
+  float *bc;      // [blocks of a group][rows][chunks][groups][states][2][tokens]: parts of the gradients of b and c
   int64_t rows, length, num_states;
   int64_t segments, segment, chunks;  // segments of a row, tokens of a segment, chunks of a row
   int64_t blocks, parts;              // waves side by side in a group's channels, and along rows and segments
@@ -65,7 +67,7 @@ __device__ __forceinline__ Place place_of(const Scan &p, int64_t column, int64_t
   w.group = int32_t(column / p.blocks);
   w.row = row_and_seg / p.segments;
   w.seg = row_and_seg % p.segments;
-  w.c0 = w.group * p.per_group + int32_t(w.block) * kWave;
+  w.c0 = __builtin_amdgcn_readfirstlane(w.group * p.per_group + int32_t(w.block) * kWave);
   w.count = min(int32_t(kWave), p.per_group - int32_t(w.block) * kWave);
   // the same in all lanes, and the compiler is to know
   const int64_t length = __builtin_amdgcn_readfirstlane(
@@ -78,8 +80,8 @@ __device__ __forceinline__ Place place_of(const Scan &p, int64_t column, int64_t
 
 // delta, from dt + dt_bias: log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|. The logarithm as
 // 2 artanh(e / (2 + e)), whose series in squares of at most 1 / 9 keeps the relative precision of small steps.
-__device__ __forceinline__ float softplus(float v) {
-  const float e = exp_negative(-fabsf(v)), s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
+__device__ __forceinline__ float log1p_series(float e) {
+  const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
   float r = 1.0f / 15.0f;
   r = fmaf(r, q, 1.0f / 13.0f);
   r = fmaf(r, q, 1.0f / 11.0f);
@@ -87,7 +89,16 @@ __device__ __forceinline__ float softplus(float v) {
   r = fmaf(r, q, 1.0f / 7.0f);
   r = fmaf(r, q, 1.0f / 5.0f);
   r = fmaf(r, q, 1.0f / 3.0f);
-  const float log1 = 2.0f * fmaf(r * q, s, s);
+  return 2.0f * fmaf(r * q, s, s);
+}
+__device__ __forceinline__ float softplus(float v) {
+  const float log1 = log1p_series(exp_negative(-fabsf(v)));
+  return v > 0.0f ? v + log1 : log1;
+}
+// The same with its slope, 1 / (1 + e^-v).
+__device__ __forceinline__ float softplus(float v, float &slope) {
+  const float e = exp_negative(-fabsf(v)), log1 = log1p_series(e), d = __builtin_amdgcn_rcpf(1.0f + e);
+  slope = v < 0.0f ? e * d : d;
   return v > 0.0f ? v + log1 : log1;
 }
 
@@ -95,6 +106,13 @@ __device__ __forceinline__ float checked_rate(float a, int32_t *status) {
   if (a <= 0.0f && a > -kInf) return a;
   if (status != nullptr) atomicOr(status, RDF2V_STATUS_BAD_VALUE);
   return 0.0f;
+}
+
+// Element `offset` of an array: 32 bits of a lane's own beside an address that all lanes have in common.
+template <class T>
+__device__ __forceinline__ T &lane_of(T *common, uint32_t offset) {
+  typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
+  return *reinterpret_cast<T *>(reinterpret_cast<Byte *>(common) + offset * uint32_t(sizeof(T)));
 }
 
 // put(i, load(i)) for i = 0 .. count - 1, eight loads in flight at a time.
@@ -115,9 +133,9 @@ __device__ __forceinline__ void in_batches(int count, Load load, Put put) {
 __device__ __forceinline__ void load_rates(const Scan &p, const Place &w, float *rates, bool report) {
   const float *from = p.a + int64_t(w.c0) * p.states;
   in_batches(
-      p.states, [&](int k) { return from[min(k * kWave + int(threadIdx.x), w.count * p.states - 1)]; },
+      p.states, [&](int k) { return from[min(k * kWave + lane_id(), w.count * p.states - 1)]; },
       [&](int k, float a) {
-        const int i = k * kWave + threadIdx.x, channel = i / p.states, n = i - channel * p.states;
+        const int i = k * kWave + lane_id(), channel = i / p.states, n = i - channel * p.states;
         rates[n * kWave + channel] =
             channel < w.count ? checked_rate(a, report ? p.status : nullptr) * kLog2e : 0.0f;
       });
@@ -126,59 +144,58 @@ __device__ __forceinline__ void load_rates(const Scan &p, const Place &w, float 
 // States [channels][states] of memory from or to [states][64]; null: zeros.
 __device__ __forceinline__ void load_states(const Scan &p, const Place &w, const float *from, float *to) {
   if (from == nullptr) {
-    for (int n = 0; n < p.states; ++n) to[n * kWave + threadIdx.x] = 0.0f;
+    for (int n = 0; n < p.states; ++n) to[n * kWave + lane_id()] = 0.0f;
     return;
   }
   from += (w.row * p.channels + w.c0) * p.states;
   in_batches(
-      p.states, [&](int k) { return from[min(k * kWave + int(threadIdx.x), w.count * p.states - 1)]; },
+      p.states, [&](int k) { return from[min(k * kWave + lane_id(), w.count * p.states - 1)]; },
       [&](int k, float h) {
-        const int i = k * kWave + threadIdx.x, channel = i / p.states, n = i - channel * p.states;
+        const int i = k * kWave + lane_id(), channel = i / p.states, n = i - channel * p.states;
         to[n * kWave + channel] = channel < w.count ? h : 0.0f;
       });
 }
 __device__ __forceinline__ void store_states(const Scan &p, const Place &w, const float *from, float *to) {
-  for (int i = threadIdx.x; i < w.count * p.states; i += kWave)
+  for (int i = lane_id(); i < w.count * p.states; i += kWave)
     to[(w.row * p.channels + w.c0) * p.states + i] = from[i % p.states * kWave + i / p.states];
 }
 // The same of the workspace, [states][channels].
-__device__ __forceinline__ void load_carry(const Scan &p, const Place &w, const float *from, int channel, float *to) {
+__device__ __forceinline__ void load_carry(const Scan &p, const Place &w, const float *from, uint32_t near, float *to) {
   in_batches(
-      p.states, [&](int n) { return from[int64_t(n) * p.channels + channel]; },
-      [&](int n, float h) { to[n * kWave + threadIdx.x] = int(threadIdx.x) < w.count ? h : 0.0f; });
+      p.states, [&](int n) { return lane_of(from + int64_t(n) * p.channels + w.c0, near); },
+      [&](int n, float h) { to[n * kWave + lane_id()] = lane_id() < w.count ? h : 0.0f; });
 }
 
-// A chunk's work is written for N = 4, 8, 12 or 16 tokens, the fewest that hold those that count: rows of a few
-// tokens leave most of a chunk out, and no token has a branch of its own.
-template <class Chunk>
+// A chunk's work is written for N = 4, 8, .. K tokens, the fewest that hold those that count: rows of a few tokens
+// leave most of a chunk out, and no token has a branch of its own.
+template <int K, class Chunk>
 __device__ __forceinline__ void with_tokens(int count, Chunk chunk) {
-  if (count > 12)
-    chunk(std::integral_constant<int, 16>{});
-  else if (count > 8)
-    chunk(std::integral_constant<int, 12>{});
-  else if (count > 4)
-    chunk(std::integral_constant<int, 8>{});
-  else
-    chunk(std::integral_constant<int, 4>{});
+  if constexpr (K > 4) {
+    if (count <= K - 4) {
+      with_tokens<K - 4>(count, chunk);
+      return;
+    }
+  }
+  chunk(std::integral_constant<int, K>{});
 }
 
-// The lane's channel of a token: 32 bits of offset beside an address that all lanes have in common.
-template <class T>
-__device__ __forceinline__ T *lane_of(T *token, int channel) {
-  typedef std::conditional_t<std::is_const_v<T>, const char, char> Byte;
-  return reinterpret_cast<T *>(reinterpret_cast<Byte *>(token) + uint32_t(channel) * uint32_t(sizeof(T)));
+// What the lanes of a wave hand to one another through LDS is there after this: a wave's accesses are made in order.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 
-// The lane's channel of a chunk's first `count` tokens; what follows is the last of them again. Addresses are made
+// The lane's channel (`near` the block's first) of a chunk's first `count` tokens; what follows is the last of them
+// again. Addresses are made
 // one after the other: all at once they would not fit the scalar registers.
 template <class T, int N>
-__device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const Place &w, int channel, int64_t t0,
+__device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const Place &w, uint32_t near, int64_t t0,
                                             int count, T (&x)[N]) {
   const T *base = static_cast<const T *>(view.data);
-  int64_t at = w.row * view.row_stride + t0 * view.token_stride;
+  int64_t at = w.row * view.row_stride + t0 * view.token_stride + w.c0;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    x[t] = *lane_of(base + at, channel);
+    x[t] = lane_of(base + at, near);
     at += t + 1 < N - 3 || t + 1 < count ? view.token_stride : 0;
     asm volatile("" : "+s"(at));
   }
@@ -186,46 +203,47 @@ __device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const
 
 // The same of an output, from token `first` of all rows on.
 template <class T, int N>
-__device__ __forceinline__ void store_tokens(void *out, int64_t first, int64_t channels, int channel, int count,
-                                             const float (&x)[N]) {
+__device__ __forceinline__ void store_tokens(void *out, int64_t first, int64_t channels, const Place &w, uint32_t near,
+                                             int count, const float (&x)[N]) {
   T *base = static_cast<T *>(out);
-  int64_t at = first * channels;
+  int64_t at = first * channels + w.c0;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    if (t < N - 3 || t < count) *lane_of(base + at, channel) = from_f32<T>(x[t]);
+    if (t < N - 3 || t < count) lane_of(base + at, near) = from_f32<T>(x[t]);
     at += channels;
     asm volatile("" : "+s"(at));
   }
 }
 
-// b or c of a chunk to [states][16] in LDS; zeros for tokens that do not count.
-template <class T, int NMAX>
-__device__ __forceinline__ void load_heads(const Scan &p, const rdf2v_heads_view &view, const Place &w, int64_t t0,
-                                           int count, float *lds) {
+// b or c of a chunk of K tokens to [states][K] in LDS; zeros for tokens that do not count.
+template <class T, int NMAX, int K>
+__device__ __forceinline__ void load_heads(const Scan &p, const rdf2v_heads_view &view, const Place &w, int lane,
+                                           int64_t t0, int count, float *lds) {
   const T *at = static_cast<const T *>(view.data) + w.row * view.row_stride + t0 * view.token_stride +
                 w.group * view.head_stride;
-  constexpr int kEach = kTokens * NMAX / kWave;
+  constexpr int kEach = K * NMAX / kWave;
   T x[kEach];
+  asm volatile("" : "+v"(lane));  // offsets are made anew for each chunk: kept, they would cost the registers of four
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int i = threadIdx.x + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
+    const int i = lane + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
     x[k] = T(0.0f);
     if (token < count) x[k] = at[token * view.token_stride + n];
   }
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
-    const int i = threadIdx.x + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
-    if (token < kTokens) lds[n * kTokens + token] = to_f32(x[k]);
+    const int i = lane + k * kWave, token = i * p.by_states >> 16, n = i - token * p.states;
+    if (token < K) lds[n * K + token] = to_f32(x[k]);
   }
 }
 
 // A state's values of a chunk's tokens, the same in every lane.
-template <int N>
+template <int K, int N>
 __device__ __forceinline__ void read_head(const float *lds, int n, float (&x)[N]) {
   typedef float Four __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {
-    const Four v = reinterpret_cast<const Four *>(lds + n * kTokens)[i];
+    const Four v = reinterpret_cast<const Four *>(lds + n * K)[i];
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j];
   }
@@ -262,17 +280,18 @@ __device__ __forceinline__ void store_zeros(void *out, int64_t from, int64_t to,
                                             int64_t width, int64_t at, int count) {
   T *p = static_cast<T *>(out) + row * length * width + at;
   for (int64_t t = from; t < to; ++t)
-    for (int i = threadIdx.x; i < count; i += kWave) p[t * width + i] = from_f32<T>(0.0f);
+    for (int i = lane_id(); i < count; i += kWave) p[t * width + i] = from_f32<T>(0.0f);
 }
 
 // What a wave keeps for its channels.
 struct Lane {
   int lane, channel;
+  uint32_t near;  // what the channel is beyond the block's first
   bool there, gated;
   float bias, skip;
   __device__ __forceinline__ Lane(const Scan &p, const Place &w)
-      : lane(threadIdx.x), channel(w.c0 + (int(threadIdx.x) < w.count ? threadIdx.x : 0)),
-        there(int(threadIdx.x) < w.count), gated(p.gate.data != nullptr),
+      : lane(lane_id()), channel(w.c0 + (lane < w.count ? lane : 0)), near(lane < w.count ? lane : 0),
+        there(lane < w.count), gated(p.gate.data != nullptr),
         bias(p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f), skip(p.skip != nullptr ? p.skip[channel] : 0.0f) {}
 };
 
@@ -291,19 +310,19 @@ __global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) 
     if (p.segments == 1) {
       load_states(p, w, p.state, held);
     } else {
-      load_carry(p, w, p.carry + item * p.states * p.channels, me.channel, held);
+      load_carry(p, w, p.carry + item * p.states * p.channels, me.near, held);
     }
     for (int64_t t0 = w.begin; t0 < w.stop; t0 += kTokens) {
       const int count = int(min(int64_t(kTokens), w.stop - t0));
-      with_tokens(count, [&](auto tokens) {
+      with_tokens<kTokens>(count, [&](auto tokens) {
         constexpr int N = tokens();
         T x[N], dt[N], gate[N];
-        load_tokens(p.x, w, me.channel, t0, count, x);
-        load_tokens(p.dt, w, me.channel, t0, count, dt);
-        if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
+        load_tokens(p.x, w, me.near, t0, count, x);
+        load_tokens(p.dt, w, me.near, t0, count, dt);
+        if (me.gated) load_tokens(p.gate, w, me.near, t0, count, gate);
         __syncthreads();
-        load_heads<T, NMAX>(p, p.b, w, t0, count, b);
-        load_heads<T, NMAX>(p, p.c, w, t0, count, c);
+        load_heads<T, NMAX, kTokens>(p, p.b, w, me.lane, t0, count, b);
+        load_heads<T, NMAX, kTokens>(p, p.c, w, me.lane, t0, count, c);
         float delta[N], u[N], y[N];
         make_steps(x, dt, me.bias, count, me.there, delta, u);
 #pragma unroll
@@ -312,8 +331,8 @@ __global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) 
         for (int n = 0; n < p.states; ++n) {
           const float rate = rates[n * kWave + me.lane];
           float h = held[n * kWave + me.lane], bn[N], cn[N];
-          read_head(b, n, bn);
-          read_head(c, n, cn);
+          read_head<kTokens>(b, n, bn);
+          read_head<kTokens>(c, n, cn);
 #pragma unroll
           for (int t = 0; t < N; ++t) {
             h = fmaf(exp2_fast(delta[t] * rate), h, u[t] * bn[t]);
@@ -324,7 +343,7 @@ __global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) 
         if (me.gated)
 #pragma unroll
           for (int t = 0; t < N; ++t) y[t] *= silu(to_f32(gate[t]));
-        if (me.there) store_tokens<T>(p.out, w.row * p.length + t0, p.channels, me.channel, count, y);
+        if (me.there) store_tokens<T>(p.out, w.row * p.length + t0, p.channels, w, me.near, count, y);
       });
     }
     store_zeros<T>(p.out, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
@@ -340,8 +359,9 @@ __global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) 
 template <class T, int NMAX, bool BACK, bool CUT>
 __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t first) {
   constexpr bool kBoth = BACK && CUT;
-  __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens];
-  __shared__ float decay[kBoth ? NMAX * kWave : 1], grad[kBoth ? NMAX * kWave : 1], c[kBoth ? NMAX * kTokens : 1];
+  constexpr int K = BACK ? kBackTokens : kTokens;
+  __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * K];
+  __shared__ float grad[kBoth ? NMAX * kWave : 1], c[kBoth ? NMAX * K : 1];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
                 part = (first + blockIdx.x) / columns;
   Place w = place_of(p, column, 0, false);
@@ -353,45 +373,43 @@ __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t firs
     __syncthreads();
     load_states(p, w, CUT ? nullptr : p.state, held);
     if (kBoth)
-      for (int n = 0; n < p.states; ++n) {
-        decay[n * kWave + lane] = 1.0f;
-        grad[n * kWave + lane] = 0.0f;
-      }
+      for (int n = 0; n < p.states; ++n) grad[n * kWave + lane] = 0.0f;
     float sum = 0.0f;  // of delta
     // without segments the state after the last chunk is not needed
-    const int64_t stop = CUT ? w.stop : w.stop - kTokens;
-    for (int64_t t0 = w.begin; t0 < stop; t0 += kTokens) {
-      const int count = int(min(int64_t(kTokens), w.stop - t0));
-      const int64_t chunk = w.row * p.chunks + t0 / kTokens;
-      with_tokens(count, [&](auto tokens) {
+    const int64_t stop = CUT ? w.stop : w.stop - K;
+    for (int64_t t0 = w.begin; t0 < stop; t0 += K) {
+      const int count = int(min(int64_t(K), w.stop - t0));
+      const int64_t chunk = w.row * p.chunks + t0 / K;
+      with_tokens<K>(count, [&](auto tokens) {
         constexpr int N = tokens();
         T x[N], dt[N];
         float delta[N], u[N], g[N];
-        load_tokens(p.x, w, me.channel, t0, count, x);
-        load_tokens(p.dt, w, me.channel, t0, count, dt);
+        load_tokens(p.x, w, me.near, t0, count, x);
+        load_tokens(p.dt, w, me.near, t0, count, dt);
         __syncthreads();
-        load_heads<T, NMAX>(p, p.b, w, t0, count, b);
+        load_heads<T, NMAX, K>(p, p.b, w, lane, t0, count, b);
         if constexpr (kBoth) {
           T o[N], gate[N];
-          load_tokens(p.dout, w, me.channel, t0, count, o);
-          if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
-          load_heads<T, NMAX>(p, p.c, w, t0, count, c);
+          load_tokens(p.dout, w, me.near, t0, count, o);
+          if (me.gated) load_tokens(p.gate, w, me.near, t0, count, gate);
+          load_heads<T, NMAX, K>(p, p.c, w, lane, t0, count, c);
           make_gradients(o, gate, me.gated, count, me.there, g);
         }
         make_steps(x, dt, me.bias, count, me.there, delta, u);
         __syncthreads();
-        if (kBoth && me.there) p.until[chunk * p.channels + me.channel] = sum;
+        if (kBoth && me.there) lane_of(p.until + chunk * p.channels + w.c0, me.near) = sum;
+        const float before = sum;
         if constexpr (CUT)
 #pragma unroll
           for (int t = 0; t < N; ++t) sum += delta[t];
         for (int n = 0; n < p.states; ++n) {
           const float rate = rates[n * kWave + lane];
           float h = held[n * kWave + lane], bn[N];
-          if (kBoth && me.there) p.starts[(chunk * p.states + n) * p.channels + me.channel] = h;
-          read_head(b, n, bn);
+          if (kBoth && me.there) lane_of(p.starts + (chunk * p.states + n) * p.channels + w.c0, me.near) = h;
+          read_head<K>(b, n, bn);
           if constexpr (kBoth) {
-            float cn[N], most = decay[n * kWave + lane], r = grad[n * kWave + lane];
-            read_head(c, n, cn);
+            float cn[N], most = exp2_fast(before * rate), r = grad[n * kWave + lane];
+            read_head<K>(c, n, cn);
 #pragma unroll
             for (int t = 0; t < N; ++t) {
               const float e = exp2_fast(delta[t] * rate);
@@ -399,22 +417,23 @@ __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t firs
               most *= e;
               r = fmaf(most, g[t] * cn[t], r);
             }
-            decay[n * kWave + lane] = most;
             grad[n * kWave + lane] = r;
           } else {
 #pragma unroll
             for (int t = 0; t < N; ++t) h = fmaf(exp2_fast(delta[t] * rate), h, u[t] * bn[t]);
           }
           held[n * kWave + lane] = h;
-          if (BACK && !CUT && me.there) p.starts[((chunk + 1) * p.states + n) * p.channels + me.channel] = h;
+          if (BACK && !CUT && me.there)
+            lane_of(p.starts + ((chunk + 1) * p.states + n) * p.channels + w.c0, me.near) = h;
         }
       });
     }
     if (!CUT || !me.there) continue;
-    p.steps[item * p.channels + me.channel] = sum;
+    lane_of(p.steps + item * p.channels + w.c0, me.near) = sum;
     for (int n = 0; n < p.states; ++n) {
-      p.carry[(item * p.states + n) * p.channels + me.channel] = held[n * kWave + lane];
-      if (kBoth) p.back[(item * p.states + n) * p.channels + me.channel] = grad[n * kWave + lane];
+      const int64_t at = (item * p.states + n) * p.channels + w.c0;
+      lane_of(p.carry + at, me.near) = held[n * kWave + lane];
+      if (kBoth) lane_of(p.back + at, me.near) = grad[n * kWave + lane];
     }
   }
 }
@@ -459,38 +478,37 @@ __global__ __launch_bounds__(kThreads) void scan_join_kernel(Scan p, int64_t fir
     p.state_out[held] = h;
 }
 
-typedef float Four __attribute__((ext_vector_type(4)));
-
-// Sums over a wave's channels of a value for each of 16 tokens, by matrix products with a unit column: with A the
-// value of lane 16 k + i at (i, k) and B ones in column t, a product adds the sums over k to column t of its
-// accumulator. Sixteen products of 32 cycles beside the vector instructions take the place of sixteen sums over
-// 64 lanes, at most 2 instructions a value instead of 7.
-struct ChannelSums {
-  Four sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  // `unit`: 1 in the lanes of column t, from unit_column
-  __device__ __forceinline__ void add(float value, float unit) {
-    sum = __builtin_amdgcn_mfma_f32_16x16x4f32(value, unit, sum, 0, 0, 0);
+// Sums over a wave's lanes of sixteen values at once: value lane / 4's in each lane. Every step adds two lanes of
+// each value and leaves half as many values in a lane, so that 35 instructions do: two values meet in a swap of the
+// wave's halves, then of rows, then (a lane's bit chooses what it keeps) of halves and quarters of rows, and quarters
+// are added up. Matrix products with unit columns take 3 instructions a value less, but the f32 ones keep the vector
+// instructions waiting, 8 for each product, and spread what is no number over all of the columns.
+__device__ __forceinline__ float sixteen_sums(const float (&v)[16]) {
+  const int lane = lane_id();
+  float w[8], x[4], y[2];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
+    w[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
   }
-  // of the lane's column
-  __device__ __forceinline__ float part() const { return (sum[0] + sum[1]) + (sum[2] + sum[3]); }
-};
-
-// The columns' totals of two sums: lane t has token t's of the first, lane 32 + t of the second.
-__device__ __forceinline__ float two_totals(const ChannelSums &one, const ChannelSums &two) {
-  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(one.part()), __float_as_uint(two.part()), false,
-                                                       false);
-  const uint32_t x = __float_as_uint(__uint_as_float(halves[0]) + __uint_as_float(halves[1]));
-  const auto rows = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  return __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
-}
-
-// `first`, 1 in lanes 0, 16, 32 and 48 and 0 in the others, moved up by T lanes in its rows of 16.
-template <int T>
-__device__ __forceinline__ float unit_column(float first) {
-  if constexpr (T == 0)
-    return first;
-  else
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(first), 0x110 + T, 0xf, 0xf, true));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[i]), __float_as_uint(w[i + 4]), false, false);
+    x[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  }
+#define RDF2V_DPP(VALUE, CTRL) \
+  __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(VALUE), CTRL, 0xf, 0xf, false))
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float keep = lane & 8 ? x[i + 2] : x[i], give = lane & 8 ? x[i] : x[i + 2];
+    y[i] = keep + RDF2V_DPP(give, 0x128);  // row_ror:8
+  }
+  const float keep = lane & 4 ? y[1] : y[0], give = lane & 4 ? y[0] : y[1];
+  float z = keep + RDF2V_DPP(give, 0x141);  // row_half_mirror
+  z += RDF2V_DPP(z, 0xb1);                  // quad_perm:[1,0,3,2]
+  z += RDF2V_DPP(z, 0x4e);                  // quad_perm:[2,3,0,1]
+#undef RDF2V_DPP
+  return z;
 }
 
 // Calls each(constant) for N - 1, N - 2, .. 0.
@@ -503,93 +521,105 @@ __device__ __forceinline__ void backwards(Each each) {
 }
 
 // Gradients of a segment, chunk after chunk from its end; a wave takes several segments of its channels in turn
-// and holds the parameters' gradients meanwhile. Inputs are read twice, before the states' loop and after it:
-// what is made of them would not fit the registers beside it.
+// and holds the parameters' gradients meanwhile.
 template <class T, int NMAX>
-__global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
-  __shared__ float rates[NMAX * kWave], grads[NMAX * kWave], da[NMAX * kWave], held[NMAX * kWave];
-  __shared__ float b[NMAX * kTokens], c[NMAX * kTokens], db[kTokens * NMAX], dc[kTokens * NMAX];
+__global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
+  constexpr int K = kBackTokens;
+  __shared__ float rates[NMAX * kWave], all_grads[kGang][NMAX * kWave], all_da[kGang][NMAX * kWave];
+  __shared__ float all_b[kGang][NMAX * K], all_c[kGang][NMAX * K];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  float *grads = all_grads[wave], *da = all_da[wave], *b = all_b[wave], *c = all_c[wave];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
-                part = (first + blockIdx.x) / columns;
-  const bool cut = p.segments > 1, direct = p.blocks == 1;
+                part = (first + blockIdx.x) / columns * kGang + wave;
+  const bool cut = p.segments > 1;
   Place w = place_of(p, column, 0, false);
   const Lane me(p, w);
   const int lane = me.lane;
-  load_rates(p, w, rates, part == 0);
+  const bool whole = w.count == kWave;  // lanes without a channel make products of zeros, which an infinity spoils
+  if (wave == 0) load_rates(p, w, rates, part == 0);
+  __syncthreads();
+  if (part >= p.parts) return;
   for (int n = 0; n < p.states; ++n) da[n * kWave + lane] = 0.0f;
   float ddt_bias = 0.0f, dskip = 0.0f;
   for (int64_t item = part; item < p.rows * p.segments; item += p.parts) {
     w = place_of(p, column, item, lane == 0);
-    __syncthreads();
-    if (!cut) {
+    wave_sync();
+    if (!cut)
       load_states(p, w, p.dstate_out, grads);
-    } else {
-      load_carry(p, w, p.back + item * p.states * p.channels, me.channel, grads);
-    }
-    const int64_t last = w.begin + (w.stop - w.begin - 1) / kTokens * kTokens;  // chunk
-    for (int64_t t0 = last; t0 >= w.begin && w.begin < w.stop; t0 -= kTokens) {
-      const int count = int(min(int64_t(kTokens), w.stop - t0));
-      const int64_t chunk = w.row * p.chunks + t0 / kTokens, token = w.row * p.length + t0;
+    else
+      load_carry(p, w, p.back + item * p.states * p.channels, me.near, grads);
+    const float *carry = p.carry + item * p.states * p.channels + w.c0;
+    const int64_t last = w.begin + (w.stop - w.begin - 1) / K * K;  // chunk
+    for (int64_t t0 = last; t0 >= w.begin && w.begin < w.stop; t0 -= K) {
+      const int count = int(min(int64_t(K), w.stop - t0));
+      const int64_t chunk = w.row * p.chunks + t0 / K, token = w.row * p.length + t0;
       // the states before the chunk: the row's, or its own and what the segment begins with
-      const float *starts = p.starts + chunk * p.states * p.channels + me.channel;
-      if (cut) {
-        const float *carry = p.carry + item * p.states * p.channels + me.channel;
-        const float until = p.until[chunk * p.channels + me.channel];
-        in_batches(
-            p.states,
-            [&](int n) { return make_float2(starts[int64_t(n) * p.channels], carry[int64_t(n) * p.channels]); },
-            [&](int n, float2 h) {
-              held[n * kWave + lane] =
-                  me.there ? fmaf(exp2_fast(until * rates[n * kWave + lane]), h.y, h.x) : 0.0f;
-            });
-      } else if (t0 > w.begin) {
-        load_carry(p, w, starts - me.channel, me.channel, held);
-      } else {
-        load_states(p, w, p.state, held);
-      }
-      with_tokens(count, [&](auto tokens) {
+      const bool own = cut || t0 > w.begin;
+      const float *starts = own ? p.starts + chunk * p.states * p.channels + w.c0
+                            : p.state != nullptr ? p.state + (w.row * p.channels + w.c0) * p.states
+                                                 : nullptr;
+      const int64_t stride = own ? p.channels : 1;
+      const uint32_t near = own ? me.near : me.near * uint32_t(p.states);
+      const float until = cut ? lane_of(p.until + chunk * p.channels + w.c0, me.near) : 0.0f;
+      float *sums = p.bc + (((w.block * p.rows * p.chunks + chunk) * p.groups + w.group) * p.states) * (2 * K);
+      with_tokens<K>(count, [&](auto tokens) {
         constexpr int N = tokens();
-        float delta[N], u[N], g[N], y[N], du[N] = {}, dd[N] = {};
-        __syncthreads();
+        float from = starts != nullptr ? lane_of(starts, near) : 0.0f, begin = cut ? lane_of(carry, me.near) : 0.0f;
+        float xs[N], delta[N], slope[N], u[N], g[N], y[N], dgate[N], du[N] = {}, dd[N] = {};
+        wave_sync();
         {
           T x[N], dt[N], gate[N], o[N];
-          load_tokens(p.x, w, me.channel, t0, count, x);
-          load_tokens(p.dt, w, me.channel, t0, count, dt);
-          if (me.gated) load_tokens(p.gate, w, me.channel, t0, count, gate);
-          load_tokens(p.dout, w, me.channel, t0, count, o);
-          load_heads<T, NMAX>(p, p.b, w, t0, count, b);
-          load_heads<T, NMAX>(p, p.c, w, t0, count, c);
-          make_steps(x, dt, me.bias, count, me.there, delta, u);
-          make_gradients(o, gate, me.gated, count, me.there, g);
+          load_tokens(p.x, w, me.near, t0, count, x);
+          load_tokens(p.dt, w, me.near, t0, count, dt);
+          if (me.gated) load_tokens(p.gate, w, me.near, t0, count, gate);
+          load_tokens(p.dout, w, me.near, t0, count, o);
+          load_heads<T, NMAX, K>(p, p.b, w, lane, t0, count, b);
+          load_heads<T, NMAX, K>(p, p.c, w, lane, t0, count, c);
 #pragma unroll
           for (int t = 0; t < N; ++t) {
-            const float xv = to_f32(x[t]);
-            dskip = t < count ? fmaf(g[t], xv, dskip) : dskip;
-            y[t] = me.skip * xv;
+            const bool on = me.there && t < count;
+            const float d = softplus(to_f32(dt[t]) + me.bias, slope[t]);
+            xs[t] = to_f32(x[t]);
+            delta[t] = on ? d : 0.0f;
+            u[t] = on ? d * xs[t] : 0.0f;
+            g[t] = on ? to_f32(o[t]) : 0.0f;
+            dgate[t] = 0.0f;
+          }
+          if (me.gated)
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+              const float z = to_f32(gate[t]), s = sigmoid(z);
+              dgate[t] = g[t] * silu_slope(z, s);
+              g[t] = me.there && t < count ? g[t] * (z * s) : 0.0f;
+            }
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            dskip = t < count ? fmaf(g[t], xs[t], dskip) : dskip;
+            y[t] = me.skip * xs[t];
           }
         }
-        __syncthreads();
-        float first = lane % kTokens == 0 ? 1.0f : 0.0f;
+        wave_sync();
         for (int n = 0; n < p.states; ++n) {
-          asm volatile("" : "+v"(first));  // its columns are made anew: kept, they would cost 16 registers
-          const float rate = rates[n * kWave + lane], h0 = held[n * kWave + lane], after = grads[n * kWave + lane];
+          const float rate = rates[n * kWave + lane];
+          const float h0 = me.there ? (cut ? fmaf(exp2_fast(until * rate), begin, from) : from) : 0.0f;
+          const int next = min(n + 1, p.states - 1);
+          if (starts != nullptr) from = lane_of(starts + next * stride, near);
+          if (cut) begin = lane_of(carry + int64_t(next) * p.channels, me.near);
           float bn[N], cn[N], e[N], h[N];
-          read_head(b, n, bn);
-          read_head(c, n, cn);
+          read_head<K>(b, n, bn);
+          read_head<K>(c, n, cn);
 #pragma unroll
           for (int t = 0; t < N; ++t) {
             e[t] = exp2_fast(delta[t] * rate);
             h[t] = fmaf(e[t], t > 0 ? h[t > 0 ? t - 1 : 0] : h0, u[t] * bn[t]);
             y[t] = fmaf(h[t], cn[t], y[t]);
           }
-          float r = after, rates_sum = 0.0f;
-          ChannelSums sb, sc;
+          float r = grads[n * kWave + lane], rates_sum = 0.0f, each[2 * K] = {};
           backwards<N>([&](auto token) {
             constexpr int t = token();
-            const float unit = unit_column<t>(first);
             r = fmaf(g[t], cn[t], r);
-            sb.add(r * u[t], unit);
-            sc.add(g[t] * h[t], unit);
+            each[t] = r * u[t];
+            each[K + t] = g[t] * h[t];
             du[t] = fmaf(r, bn[t], du[t]);
             r *= e[t];
             const float q = r * (t > 0 ? h[t > 0 ? t - 1 : 0] : h0);
@@ -598,77 +628,37 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kerne
           });
           grads[n * kWave + lane] = r;
           da[n * kWave + lane] += rates_sum;
-          float total = two_totals(sb, sc);
-          if (__builtin_expect(__ballot(!(fabsf(total) < kInf)) != 0, 0)) {
-            // What is no number has spread over the unit columns' zeros: the same sums token by token.
-            r = after;
-            backwards<N>([&](auto token) {
-              constexpr int t = token();
-              const float unit = unit_column<t>(first);
-              r = fmaf(g[t], cn[t], r);
-              ChannelSums ob, oc;
-              ob.add(me.there ? r * u[t] : 0.0f, unit);
-              oc.add(me.there ? g[t] * h[t] : 0.0f, unit);
-              r *= e[t];
-              const float one = two_totals(ob, oc);
-              if (lane % kTokens == t) total = one;
-            });
+          if (!whole) {
+            asm volatile("");  // a branch, not selects for all
+#pragma unroll
+            for (int i = 0; i < 2 * K; ++i) each[i] = me.there ? each[i] : 0.0f;
           }
-          if (lane % 32 < kTokens) (lane < 32 ? db : dc)[lane % kTokens * p.states + n] = total;
-        }
-        T x[N], dt[N], gate[N], o[N];
-        load_tokens(p.x, w, me.channel, t0, count, x);
-        load_tokens(p.dt, w, me.channel, t0, count, dt);
-        if (me.gated) {
-          load_tokens(p.gate, w, me.channel, t0, count, gate);
-          load_tokens(p.dout, w, me.channel, t0, count, o);
+          const float total = sixteen_sums(each);
+          if (lane % 4 == 0) lane_of(sums + n * 2 * K, uint32_t(lane) / 4) = total;
         }
 #pragma unroll
         for (int t = 0; t < N; ++t) {
-          dd[t] = fmaf(dd[t], kLn2, to_f32(x[t]) * du[t]) * sigmoid(to_f32(dt[t]) + me.bias);
+          dd[t] = fmaf(dd[t], kLn2, xs[t] * du[t]) * slope[t];
           du[t] = fmaf(delta[t], du[t], me.skip * g[t]);
+          y[t] *= dgate[t];
           if (t < count) ddt_bias += dd[t];
         }
-        if (me.there) {
-          store_tokens<T>(p.dx, token, p.channels, me.channel, count, du);
-          store_tokens<T>(p.ddt, token, p.channels, me.channel, count, dd);
-        }
-        if (!me.gated) return;
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-          const float z = to_f32(gate[t]);
-          y[t] = to_f32(o[t]) * y[t] * silu_slope(z, sigmoid(z));
-        }
-        if (me.there) store_tokens<T>(p.dgate, token, p.channels, me.channel, count, y);
+        if (!me.there) return;
+        store_tokens<T>(p.dx, token, p.channels, w, me.near, count, du);
+        store_tokens<T>(p.ddt, token, p.channels, w, me.near, count, dd);
+        if (me.gated) store_tokens<T>(p.dgate, token, p.channels, w, me.near, count, y);
       });
-      __syncthreads();
-      for (int i = lane; i < count * p.states; i += kWave) {
-        const int t = i * p.by_states >> 16, n = i - t * p.states;
-        if (direct) {
-          const int64_t to = ((token + t) * p.groups + w.group) * p.states + n;
-          static_cast<T *>(p.db)[to] = from_f32<T>(db[i]);
-          static_cast<T *>(p.dc)[to] = from_f32<T>(dc[i]);
-        } else {
-          float *to = p.bc + ((w.block * p.rows * p.length + token + t) * p.groups + w.group) * 2 * p.states + n;
-          to[0] = db[i];
-          to[p.states] = dc[i];
-        }
-      }
     }
     store_zeros<T>(p.dx, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
     store_zeros<T>(p.ddt, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
     if (me.gated) store_zeros<T>(p.dgate, w.stop, w.end, w.row, p.length, p.channels, w.c0, w.count);
-    if (direct) {
-      store_zeros<T>(p.db, w.stop, w.end, w.row, p.length, int64_t(p.groups) * p.states, w.group * p.states, p.states);
-      store_zeros<T>(p.dc, w.stop, w.end, w.row, p.length, int64_t(p.groups) * p.states, w.group * p.states, p.states);
-    }
     if (w.seg == 0 && p.dstate != nullptr) {
-      __syncthreads();
+      wave_sync();
       store_states(p, w, grads, p.dstate);
     }
   }
   float *partial = p.partial + part * p.channels * (p.states + 2);
-  __syncthreads();
+  wave_sync();
   for (int i = lane; i < w.count * p.states; i += kWave)
     partial[int64_t(w.c0) * p.states + i] = da[i % p.states * kWave + i / p.states];
   if (!me.there) return;
@@ -676,21 +666,27 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kerne
   partial[int64_t(p.channels) * (p.states + 1) + me.channel] = dskip;
 }
 
-// Gradients of b and c: the sums over a group's workgroups, in order.
+// Gradients of b and c: the sums over a group's blocks of channels, in order, from [states][2][tokens of a chunk] to
+// [tokens][states]. A thread to a value of the output.
 template <class T>
 __global__ __launch_bounds__(kThreads) void scan_bc_kernel(Scan p, int64_t first) {
-  const int64_t width = int64_t(p.groups) * 2 * p.states, all = p.rows * p.length * width;
+  constexpr int K = kBackTokens;
   const int64_t item = (first + blockIdx.x) * kThreads + threadIdx.x;
-  if (item >= all) return;
-  const int64_t token = item / width, row = token / p.length, n = item % (2 * p.states);
-  float sum = 0.0f;
-  if (token % p.length < row_length(p.len, row, p.length, false, nullptr))
-    for (int64_t k = 0; k < p.blocks; ++k) sum += p.bc[k * all + item];
-  const int64_t head = item / (2 * p.states);
-  if (n < p.states)
-    static_cast<T *>(p.db)[head * p.states + n] = from_f32<T>(sum);
-  else
-    static_cast<T *>(p.dc)[head * p.states + n - p.states] = from_f32<T>(sum);
+  if (item >= p.rows * p.length * p.groups * p.states) return;
+  const int64_t n = item % p.states, head = item / p.states, group = head % p.groups, token = head / p.groups;
+  const int64_t row = token / p.length, t = token % p.length;
+  float db = 0.0f, dc = 0.0f;
+  if (t < row_length(p.len, row, p.length, false, nullptr)) {
+    const int64_t all = p.rows * p.chunks * p.groups * p.states * (2 * K);
+    const float *from =
+        p.bc + (((row * p.chunks + t / K) * p.groups + group) * p.states + n) * (2 * K) + t % K;
+    for (int64_t k = 0; k < p.blocks; ++k) {
+      db += from[k * all];
+      dc += from[k * all + K];
+    }
+  }
+  static_cast<T *>(p.db)[item] = from_f32<T>(db);
+  static_cast<T *>(p.dc)[item] = from_f32<T>(dc);
 }
 
 // One token more. `lanes` threads, a power of two, take a channel's states, V neighbouring ones at a time; a
@@ -785,18 +781,25 @@ Scan base(const rdf2v_scan &a, const ScanInputs &in, int32_t *status) {
   return p;
 }
 
+// Waves along rows and segments, of at most `most` in all.
+int64_t parts_of(const Scan &p, int64_t most) {
+  return std::max<int64_t>(1, std::min(p.rows * p.segments, most / (p.blocks * p.groups)));
+}
+
 // Segments of a row, chunks, the waves along rows and segments, and where the workspace's arrays lie; its bytes.
 size_t plan(Scan &p, bool backward, void *workspace) {
-  // Waves that fill the chip are 1,024 times two or three.
-  constexpr int64_t kFew = 1024, kFill = 4096, kMost = 8192, kShortest = 2 * kTokens;
+  // Waves of a column of channels beside those of the others: with fewer than one to each of 1,024 SIMDs rows are cut
+  // into segments, as many as the kernels' registers let them have at once.
+  constexpr int64_t kFew = 1024, kShortest = 2 * kTokens;
+  const int64_t kFill = backward ? 2048 : 4096;
   const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
   int64_t segments = 1;
   if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
   p.segment = std::max<int64_t>(1, (p.length + segments - 1) / segments);
   p.segment = (p.segment + kTokens - 1) / kTokens * kTokens;
   p.segments = std::max<int64_t>(1, (p.length + p.segment - 1) / p.segment);
-  p.chunks = (p.length + kTokens - 1) / kTokens;
-  p.parts = std::max<int64_t>(1, std::min(p.rows * p.segments, (backward ? kMost / 2 : kMost) / columns));
+  p.chunks = (p.length + kBackTokens - 1) / kBackTokens;
+  p.parts = parts_of(p, backward ? 2048 : 8192);
   size_t bytes = 0;
   const auto take = [&](float *&at, int64_t count) {
     at = workspace != nullptr ? reinterpret_cast<float *>(static_cast<char *>(workspace) + bytes) : nullptr;
@@ -814,7 +817,7 @@ size_t plan(Scan &p, bool backward, void *workspace) {
   }
   if (p.chunks > 1) take(p.starts, p.rows * p.chunks * p.states * p.channels);
   if (p.rows > 0) take(p.partial, p.parts * p.channels * (p.states + 2));
-  if (p.blocks > 1) take(p.bc, p.blocks * p.rows * p.length * p.groups * 2 * p.states);
+  take(p.bc, p.blocks * p.rows * p.chunks * p.groups * p.states * 2 * kBackTokens);
   return bytes;
 }
 
@@ -838,7 +841,8 @@ rdf2v_status for_waves(const Scan &p, Launch launch) {
 }
 
 template <bool BACK, bool CUT>
-rdf2v_status launch_states(const Scan &p, int dtype, hipStream_t stream) {
+rdf2v_status launch_states(Scan p, int dtype, hipStream_t stream) {
+  p.parts = parts_of(p, 8192);
   return with_types(dtype, p.states, [&](auto t, auto most) {
     return for_waves(p, [&](int64_t first, dim3 grid) {
       scan_states_kernel<decltype(t), most(), BACK, CUT><<<grid, dim3(kWave), 0, stream>>>(p, first);
@@ -907,13 +911,16 @@ rdf2v_status launch_selective_scan_backward(const rdf2v_scan &a, const ScanInput
     }
     if (st != RDF2V_OK) return st;
     st = with_types(a.dtype, p.states, [&](auto t, auto most) {
-      return for_waves(p, [&](int64_t first, dim3 grid) {
-        scan_backward_kernel<decltype(t), most()><<<grid, dim3(kWave), 0, stream>>>(p, first);
+      const int64_t gangs = (p.parts + kGang - 1) / kGang * p.blocks * p.groups;
+      return for_each_launch(gangs, kGang * kWave, 1, [&](int64_t first, int64_t count) {
+        scan_backward_kernel<decltype(t), most()><<<dim3(unsigned(count)), dim3(kGang * kWave), 0, stream>>>(p, first);
+        RDF2V_LAUNCH_CHECK();
+        return RDF2V_OK;
       });
     });
     if (st != RDF2V_OK) return st;
-    if (p.blocks > 1 && p.length > 0) {
-      const int64_t blocks = (p.rows * p.length * p.groups * 2 * p.states + kThreads - 1) / kThreads;
+    if (p.length > 0) {
+      const int64_t blocks = (p.rows * p.length * p.groups * p.states + kThreads - 1) / kThreads;
       st = for_each_launch(blocks, kThreads, 1, [&](int64_t first, int64_t count) {
         if (a.dtype == RDF2V_BF16)
           scan_bc_kernel<bf16><<<dim3(unsigned(count)), dim3(kThreads), 0, stream>>>(p, first);
