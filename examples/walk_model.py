@@ -7,6 +7,7 @@ extends start entities token by token, the attention's states following the beam
 
     python examples/walk_model.py                 # 1,000 entities, 5,000 triples, a few seconds
     python examples/walk_model.py --steps 400
+    python examples/walk_model.py --mixer scan    # two layers of convolution and selective scan instead
 """
 
 import argparse
@@ -69,6 +70,19 @@ class WalkModel:
     def logits(self, x, attended):
         return (x + attended.flatten(-2) @ self.out) @ self.embed.T / SIZE
 
+    def begin(self, rows):
+        """The states of `rows` walks without tokens, and as much memory for those after a token."""
+        state = torch.zeros(rows, HEADS, SIZE, SIZE, device=self.embed.device)
+        return state, torch.empty_like(state)
+
+    def step(self, last, states, parents):
+        """(logits, states) of one token more for each row, from the states of the parents' rows."""
+        state, other = states
+        x = self.embed[last.clamp(min=0).long()]
+        q, k, v = self.split(x)
+        attended, new = rd.rdf2v_decay_attention_step(q, k, v, self.log_decay, state, parents=parents, state_out=other)
+        return self.logits(x, attended), (new, state)
+
     def train_step(self, tokens, lens, ids, weights):
         """Mean loss over the positions that something follows, and the gradients in .grad."""
         at = tokens.clamp(min=0).long()                        # rows are padded with -1; lens says where they end
@@ -94,6 +108,79 @@ class WalkModel:
         return (loss * dloss).sum()
 
 
+class ScanModel:
+    """Embeddings, layers of a causal convolution and a selective scan joined by residual norms, logits by the
+    embeddings. Autograd records the operators."""
+
+    def __init__(self, vocab, dev, seed=0, layers=2, size=HEADS * SIZE, states=8, width=4, drop=0.1):
+        g = torch.Generator(device=dev).manual_seed(seed)
+        r = lambda *s: torch.randn(*s, device=dev, generator=g)  # noqa: E731
+        self.size, self.states, self.width, self.drop, self.seed, self.steps = size, states, width, drop, seed, 0
+        self.embed = r(vocab, size)
+        rates = torch.arange(1.0, states + 1, device=dev).repeat(size, 1)
+        self.layers = [dict(norm=torch.ones(size, device=dev), enter=r(size, 2 * size) / math.sqrt(size),
+                            taps=r(size, width) / math.sqrt(width), taps_bias=torch.zeros(size, device=dev),
+                            select=r(size, size + 2 * states) / math.sqrt(size), log_rates=rates.log(),
+                            dt_bias=torch.full((size,), -2.0, device=dev), skip=torch.ones(size, device=dev),
+                            leave=r(size, size) / math.sqrt(size)) for _ in range(layers)]
+        self.last = torch.ones(size, device=dev)
+        self.params = [self.embed, self.last, *(p for layer in self.layers for p in layer.values())]
+        for p in self.params:
+            p.requires_grad_()
+
+    def select(self, layer, x):
+        """dt, b and c of the convolution's outputs."""
+        dt, b, c = (x @ layer["select"]).split([self.size, self.states, self.states], dim=-1)
+        return dt, b.unsqueeze(-2), c.unsqueeze(-2)
+
+    def __call__(self, tokens, lens, drop=0.0):
+        """Logits of whole rows."""
+        part, hidden = self.embed[tokens.clamp(min=0).long()], None
+        for i, layer in enumerate(self.layers):
+            given = dict(drop=drop if i else 0.0, seed=self.seed + 1000 * self.steps + i, lens=lens)
+            normed, hidden, _ = rd.rdf2v_residual_norm(part, hidden, layer["norm"], **given)
+            x, gate = (normed @ layer["enter"]).split(self.size, dim=-1)
+            x, _ = rd.rdf2v_causal_conv(x, layer["taps"], layer["taps_bias"], lens=lens)
+            dt, b, c = self.select(layer, x)
+            y, _ = rd.rdf2v_selective_scan(x, dt, -layer["log_rates"].exp(), b, c, dt_bias=layer["dt_bias"],
+                                           skip=layer["skip"], gate=gate, lens=lens)
+            part = y @ layer["leave"]
+        given = dict(drop=drop, seed=self.seed + 1000 * self.steps + len(self.layers), lens=lens)
+        return rd.rdf2v_residual_norm(part, hidden, self.last, **given)[0] @ self.embed.T / SIZE
+
+    def train_step(self, tokens, lens, ids, weights):
+        """Mean loss over the positions that something follows, and the gradients in .grad."""
+        z = self(tokens, lens, self.drop)
+        self.steps += 1
+        loss, _ = rd.rdf2v_distill_loss(z.flatten(0, 1), ids.flatten(0, 1), weights.flatten(0, 1))
+        mean = loss.sum() / (ids >= 0).any(-1).sum()
+        for p in self.params:
+            p.grad = None
+        mean.backward()
+        return mean.detach()
+
+    def begin(self, rows):
+        """The states of `rows` walks without tokens."""
+        new = lambda *s: torch.zeros(rows, *s, device=self.embed.device)  # noqa: E731
+        return [(new(self.width - 1, self.size), new(self.size, self.states)) for _ in self.layers]
+
+    @torch.no_grad()
+    def step(self, last, states, parents):
+        """(logits, states) of one token more for each row, from the states of the parents' rows."""
+        part, hidden, after = self.embed[last.clamp(min=0).long()], None, []
+        for layer, (near, far) in zip(self.layers, states):
+            normed, hidden, _ = rd.rdf2v_residual_norm(part, hidden, layer["norm"])
+            x, gate = (normed @ layer["enter"]).split(self.size, dim=-1)
+            x, near = rd.rdf2v_causal_conv_step(x, layer["taps"], layer["taps_bias"], near, parents=parents)
+            dt, b, c = self.select(layer, x)
+            y, far = rd.rdf2v_selective_scan_step(x, dt, -layer["log_rates"].exp(), b, c, far,
+                                                  dt_bias=layer["dt_bias"], skip=layer["skip"], gate=gate,
+                                                  parents=parents)
+            part = y @ layer["leave"]
+            after.append((near, far))
+        return rd.rdf2v_residual_norm(part, hidden, self.last)[0] @ self.embed.T / SIZE, after
+
+
 def search(model, csr, starts, hops, beams):
     """Likely walks of `hops` hops from each start: (tokens [starts, beams, 2 * hops + 1], scores). A walk
     that reaches an entity without out-edges ends there and is padded with -1."""
@@ -102,8 +189,7 @@ def search(model, csr, starts, hops, beams):
     is_pred = torch.arange(vocab, device=dev) >= csr.num_entities
     degree = csr.row_ptr[1:] - csr.row_ptr[:-1]
     rows = groups * beams
-    state = torch.zeros(rows, HEADS, SIZE, SIZE, device=dev)
-    other = torch.empty_like(state)
+    states = model.begin(rows)
     walks = torch.full((rows, 2 * hops + 1), -1, dtype=torch.int32, device=dev)
     walks[:, 0] = starts.repeat_interleave(beams)
     scores = torch.full((groups, beams), -math.inf, device=dev)
@@ -114,11 +200,8 @@ def search(model, csr, starts, hops, beams):
         last = walks[:, i]
         if i % 2 == 0:
             finished |= ((last < 0) | (degree[last.clamp(min=0).long()] == 0)).int().view(groups, beams)
-        x = model.embed[last.clamp(min=0).long()]
-        q, k, v = model.split(x)
-        attended, new = rd.rdf2v_decay_attention_step(q, k, v, model.log_decay, state, parents=parents, state_out=other)
-        state, other = new, state
-        z = model.logits(x, attended).masked_fill_(is_pred if i % 2 else ~is_pred, -math.inf)
+        z, states = model.step(last, states, parents)
+        z = z.masked_fill_(is_pred if i % 2 else ~is_pred, -math.inf)
         scores, tokens, parents = rd.rdf2v_beam_select(z.view(groups, beams, vocab), scores, beams, finished=finished)
         parents = parents.flatten()
         walks = rd.rdf2v_beam_reorder(walks, parents)          # the states follow in the next step
@@ -141,11 +224,12 @@ def main(argv=None):
     ap.add_argument("--batch", type=int, default=256, help="walks of a step")
     ap.add_argument("--beams", type=int, default=4)
     ap.add_argument("--hops", type=int, default=4)
+    ap.add_argument("--mixer", choices=["decay", "scan"], default="decay", help="decay attention, or selective scan")
     a = ap.parse_args(argv)
     dev = torch.device("cuda:0")
     csr, starts = load_graph(dev)
     vocab = csr.num_entities + csr.num_predicates
-    model = WalkModel(vocab, dev)
+    model = (WalkModel if a.mixer == "decay" else ScanModel)(vocab, dev)
     optimizer = torch.optim.Adam(model.params, lr=0.01)
     n = starts.shape[0]
     torch.manual_seed(0)

@@ -790,8 +790,7 @@ int64_t parts_of(const Scan &p, int64_t most) {
 size_t plan(Scan &p, bool backward, void *workspace) {
   // Waves of a column of channels beside those of the others: with fewer than one to each of 1,024 SIMDs rows are cut
   // into segments, as many as the kernels' registers let them have at once.
-  constexpr int64_t kFew = 1024, kShortest = 2 * kTokens;
-  const int64_t kFill = backward ? 2048 : 4096;
+  constexpr int64_t kFew = 1024, kFill = 4096, kShortest = 2 * kTokens;
   const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
   int64_t segments = 1;
   if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
