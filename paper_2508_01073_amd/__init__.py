@@ -1209,7 +1209,14 @@ def _parameter(t: torch.Tensor | None, name: str, shape, dev: torch.device):
 
 def _new(t: torch.Tensor | None, name: str, dtype: torch.dtype, shape, dev: torch.device) -> torch.Tensor:
     """An output of exactly this shape: the caller's, or a new one."""
-    return torch.empty(shape, dtype=dtype, device=dev) if t is None else _exact(t, name, dtype, shape, dev)
+    return torch.empty(tuple(shape), dtype=dtype, device=dev) if t is None else _exact(t, name, dtype, shape, dev)
+
+
+def _new_like(t: torch.Tensor | None, name: str, like: torch.Tensor, dtype: torch.dtype | None = None) -> torch.Tensor:
+    """The same in an input's shape, and type unless another is given; half of _new's time."""
+    if t is not None:
+        return _exact(t, name, dtype or like.dtype, like.shape, like.device)
+    return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
 
 
 def _workspace(need: int, dev: torch.device) -> torch.Tensor | None:
@@ -1314,7 +1321,7 @@ def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
         got = _CausalConv.apply(x, weight, bias, state, silu, lens, want_state, status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
-        out = _new(out, "out", a.dtype, a.shape, dev)
+        out = _new_like(out, "out", x)
         if want_state or state_out is not None:
             state_out = _new(state_out, "state_out", a.dtype, a.states, dev)
         if state is not None:
@@ -1344,7 +1351,7 @@ def rdf2v_causal_conv_backward(x: torch.Tensor, weight: torch.Tensor, bias: torc
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
         view = _tokens_view(dout, "dout", a.dtype, dev, a.shape)
-        dx = _new(dx, "dx", a.dtype, a.shape, dev)
+        dx = _new_like(dx, "dx", x)
         dweight = _new(dweight, "dweight", torch.float32, weight.shape, dev)
         if bias is not None or dbias is not None:
             dbias = _new(dbias, "dbias", torch.float32, (c.channels,), dev)
@@ -1374,7 +1381,7 @@ def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Te
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
         num_states = _parents_and_states(parents, state, c.rows, a.states[1:], a.dtype, dev)
-        out = _new(out, "out", a.dtype, a.shape, dev)
+        out = _new_like(out, "out", x)
         if state_out is None and parents is None:
             state_out = state
         state_out = _new(state_out, "state_out", a.dtype, a.states, dev)
@@ -1495,7 +1502,7 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
                                    stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
-        out = _new(out, "out", s.dtype, s.shape, dev)
+        out = _new_like(out, "out", x)
         if want_state or state_out is not None:
             state_out = _new(state_out, "state_out", torch.float32, s.states, dev)
         _state(state, "state", s.states, dev)
@@ -1556,7 +1563,7 @@ def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor
     dev = s.dev
     with _on_stream(dev, stream) as h:
         num_states = _parents_and_states(parents, state, s.c.rows, s.states[1:], torch.float32, dev)
-        out = _new(out, "out", s.dtype, s.shape, dev)
+        out = _new_like(out, "out", x)
         if state_out is None and parents is None:
             state_out = state
         state_out = _new(state_out, "state_out", torch.float32, s.states, dev)
@@ -1674,8 +1681,8 @@ def rdf2v_residual_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: 
         given = dict(drop=drop, seed=seed, row_begin=row_begin, center=center, eps=eps, hidden_dtype=hidden_dtype)
         return _ResidualNorm.apply(x, residual, weight, bias, scale, seed_offset, lens, given, status, stream)
     with _on_stream(dev, stream) as h:
-        out = _new(out, "out", n.dtype, n.shape, dev)
-        hidden = _new(hidden, "hidden", n.hidden_dtype, n.shape, dev)
+        out = _new_like(out, "out", x)
+        hidden = _new_like(hidden, "hidden", x, n.hidden_dtype)
         stats = _new(stats, "stats", torch.float32, n.stats, dev)
         _status(status, dev)
         st = _native().rdf2v_residual_norm(n.c, *n.views, _ptr(out), _ptr(hidden), _ptr(stats), _ptr(status), h)

@@ -96,10 +96,10 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
     const T *from = static_cast<const T *>(a.x) + row * a.row_stride + begin * a.token_stride + c;
     T *to = out + begin * a.channels;
     for (int left = int(stop - begin); left > 0; left -= kAhead) {
-      float next[kAhead][V];
+      Values<T, V> next[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        load_values<T, V>(from, n, next[k]);
+        next[k].load(from, n);
         if (k + 1 < left) from += a.token_stride;
       }
 #pragma unroll
@@ -163,11 +163,11 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
         const int own = int(stop - begin), to = own + W - 1, real = int(min(rest, int64_t(to)));
         zeros -= own;
         for (int t = 0; t < to; t += kAhead) {
-          float nx[kAhead][V], nd[kAhead][V];
+          Values<T, V> nx[kAhead], nd[kAhead];
 #pragma unroll
           for (int k = 0; k < kAhead; ++k) {
-            load_values<T, V>(px, t + k < real ? n : 0, nx[k]);
-            load_values<T, V>(pd, t + k < real ? n : 0, nd[k]);
+            nx[k].load(px, t + k < real ? n : 0);
+            nd[k].load(pd, t + k < real ? n : 0);
             if (t + k + 1 < real) {
               px += a.token_stride;
               pd += a.dout_token_stride;

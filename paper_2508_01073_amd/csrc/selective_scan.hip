@@ -78,28 +78,28 @@ __device__ __forceinline__ Place place_of(const Scan &p, int64_t column, int64_t
   return w;
 }
 
-// delta, from dt + dt_bias: log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|. The logarithm as
-// 2 artanh(e / (2 + e)), whose series in squares of at most 1 / 9 keeps the relative precision of small steps.
+// delta, from dt + dt_bias: log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|. The logarithm as 2 artanh(s / 2),
+// s = e / (1 + e / 2), whose series in s^2 / 4, 1 / 9 at most, keeps the relative precision of small steps: the first
+// term that is left out is 2^-25.
 __device__ __forceinline__ float log1p_series(float e) {
-  const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-  float r = 1.0f / 15.0f;
-  r = fmaf(r, q, 1.0f / 13.0f);
-  r = fmaf(r, q, 1.0f / 11.0f);
-  r = fmaf(r, q, 1.0f / 9.0f);
-  r = fmaf(r, q, 1.0f / 7.0f);
-  r = fmaf(r, q, 1.0f / 5.0f);
-  r = fmaf(r, q, 1.0f / 3.0f);
-  return 2.0f * fmaf(r * q, s, s);
+  const float s = e * __builtin_amdgcn_rcpf(fmaf(e, 0.5f, 1.0f)), q = s * s;
+  float r = 1.0f / (13.0f * 4096.0f);
+  r = fmaf(r, q, 1.0f / (11.0f * 1024.0f));
+  r = fmaf(r, q, 1.0f / (9.0f * 256.0f));
+  r = fmaf(r, q, 1.0f / (7.0f * 64.0f));
+  r = fmaf(r, q, 1.0f / (5.0f * 16.0f));
+  r = fmaf(r, q, 1.0f / (3.0f * 4.0f));
+  return fmaf(r * q, s, s);
 }
 __device__ __forceinline__ float softplus(float v) {
   const float log1 = log1p_series(exp_negative(-fabsf(v)));
-  return v > 0.0f ? v + log1 : log1;
+  return v <= 0.0f ? log1 : v + log1;  // and what is no number stays that
 }
 // The same with its slope, 1 / (1 + e^-v).
 __device__ __forceinline__ float softplus(float v, float &slope) {
   const float e = exp_negative(-fabsf(v)), log1 = log1p_series(e), d = __builtin_amdgcn_rcpf(1.0f + e);
   slope = v < 0.0f ? e * d : d;
-  return v > 0.0f ? v + log1 : log1;
+  return v <= 0.0f ? log1 : v + log1;
 }
 
 __device__ __forceinline__ float checked_rate(float a, int32_t *status) {
@@ -185,6 +185,13 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Whether token t of N is known to count, or does. Lanes without a channel go along with the block's first channel's
+// values and write nothing.
+template <int N>
+__device__ __forceinline__ bool counts(int t, int count) {
+  return t < N - 3 || t < count;
+}
+
 // The lane's channel (`near` the block's first) of a chunk's first `count` tokens; what follows is the last of them
 // again. Addresses are made
 // one after the other: all at once they would not fit the scalar registers.
@@ -196,7 +203,7 @@ __device__ __forceinline__ void load_tokens(const rdf2v_tokens_view &view, const
 #pragma unroll
   for (int t = 0; t < N; ++t) {
     x[t] = lane_of(base + at, near);
-    at += t + 1 < N - 3 || t + 1 < count ? view.token_stride : 0;
+    at += counts<N>(t + 1, count) ? view.token_stride : 0;
     asm volatile("" : "+s"(at));
   }
 }
@@ -209,7 +216,7 @@ __device__ __forceinline__ void store_tokens(void *out, int64_t first, int64_t c
   int64_t at = first * channels + w.c0;
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    if (t < N - 3 || t < count) lane_of(base + at, near) = from_f32<T>(x[t]);
+    if (counts<N>(t, count)) lane_of(base + at, near) = from_f32<T>(x[t]);
     at += channels;
     asm volatile("" : "+s"(at));
   }
@@ -251,14 +258,13 @@ __device__ __forceinline__ void read_head(const float *lds, int n, float (&x)[N]
 
 // delta and delta x of a chunk's tokens; 0 beyond the last that counts: nothing decays and nothing is added.
 template <class T, int N>
-__device__ __forceinline__ void make_steps(const T (&x)[N], const T (&dt)[N], float bias, int count, bool there,
-                                           float (&delta)[N], float (&u)[N]) {
+__device__ __forceinline__ void make_steps(const T (&x)[N], const T (&dt)[N], float bias, int count, float (&delta)[N],
+                                           float (&u)[N]) {
 #pragma unroll
   for (int t = 0; t < N; ++t) {
-    const bool on = there && t < count;
     const float d = softplus(to_f32(dt[t]) + bias);
-    delta[t] = on ? d : 0.0f;
-    u[t] = on ? d * to_f32(x[t]) : 0.0f;
+    delta[t] = counts<N>(t, count) ? d : 0.0f;
+    u[t] = counts<N>(t, count) ? d * to_f32(x[t]) : 0.0f;
   }
 }
 
@@ -267,12 +273,12 @@ __device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
 // The gradients of y of a chunk's tokens.
 template <class T, int N>
 __device__ __forceinline__ void make_gradients(const T (&dout)[N], const T (&gate)[N], bool gated, int count,
-                                               bool there, float (&g)[N]) {
+                                               float (&g)[N]) {
 #pragma unroll
-  for (int t = 0; t < N; ++t) g[t] = there && t < count ? to_f32(dout[t]) : 0.0f;
+  for (int t = 0; t < N; ++t) g[t] = counts<N>(t, count) ? to_f32(dout[t]) : 0.0f;
   if (!gated) return;
 #pragma unroll
-  for (int t = 0; t < N; ++t) g[t] = there && t < count ? g[t] * silu(to_f32(gate[t])) : 0.0f;
+  for (int t = 0; t < N; ++t) g[t] = counts<N>(t, count) ? g[t] * silu(to_f32(gate[t])) : 0.0f;
 }
 
 template <class T>
@@ -297,7 +303,7 @@ struct Lane {
 
 // The outputs of a segment. A wave's barriers cost nothing: it is alone in its workgroup.
 template <class T, int NMAX>
-__global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) {
+__global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Scan p, int64_t first) {
   __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens], c[NMAX * kTokens];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
                 part = (first + blockIdx.x) / columns;
@@ -324,7 +330,7 @@ __global__ __launch_bounds__(kWave) void scan_out_kernel(Scan p, int64_t first) 
         load_heads<T, NMAX, kTokens>(p, p.b, w, me.lane, t0, count, b);
         load_heads<T, NMAX, kTokens>(p, p.c, w, me.lane, t0, count, c);
         float delta[N], u[N], y[N];
-        make_steps(x, dt, me.bias, count, me.there, delta, u);
+        make_steps(x, dt, me.bias, count, delta, u);
 #pragma unroll
         for (int t = 0; t < N; ++t) y[t] = me.skip * to_f32(x[t]);
         __syncthreads();
@@ -393,9 +399,9 @@ __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t firs
           load_tokens(p.dout, w, me.near, t0, count, o);
           if (me.gated) load_tokens(p.gate, w, me.near, t0, count, gate);
           load_heads<T, NMAX, K>(p, p.c, w, lane, t0, count, c);
-          make_gradients(o, gate, me.gated, count, me.there, g);
+          make_gradients(o, gate, me.gated, count, g);
         }
-        make_steps(x, dt, me.bias, count, me.there, delta, u);
+        make_steps(x, dt, me.bias, count, delta, u);
         __syncthreads();
         if (kBoth && me.there) lane_of(p.until + chunk * p.channels + w.c0, me.near) = sum;
         const float before = sum;
@@ -535,7 +541,7 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
   Place w = place_of(p, column, 0, false);
   const Lane me(p, w);
   const int lane = me.lane;
-  const bool whole = w.count == kWave;  // lanes without a channel make products of zeros, which an infinity spoils
+  const bool whole = w.count == kWave;
   if (wave == 0) load_rates(p, w, rates, part == 0);
   __syncthreads();
   if (part >= p.parts) return;
@@ -577,7 +583,7 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
           load_heads<T, NMAX, K>(p, p.c, w, lane, t0, count, c);
 #pragma unroll
           for (int t = 0; t < N; ++t) {
-            const bool on = me.there && t < count;
+            const bool on = counts<N>(t, count);
             const float d = softplus(to_f32(dt[t]) + me.bias, slope[t]);
             xs[t] = to_f32(x[t]);
             delta[t] = on ? d : 0.0f;
@@ -590,18 +596,18 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
             for (int t = 0; t < N; ++t) {
               const float z = to_f32(gate[t]), s = sigmoid(z);
               dgate[t] = g[t] * silu_slope(z, s);
-              g[t] = me.there && t < count ? g[t] * (z * s) : 0.0f;
+              g[t] = counts<N>(t, count) ? g[t] * (z * s) : 0.0f;
             }
 #pragma unroll
           for (int t = 0; t < N; ++t) {
-            dskip = t < count ? fmaf(g[t], xs[t], dskip) : dskip;
+            dskip = counts<N>(t, count) ? fmaf(g[t], xs[t], dskip) : dskip;
             y[t] = me.skip * xs[t];
           }
         }
         wave_sync();
         for (int n = 0; n < p.states; ++n) {
           const float rate = rates[n * kWave + lane];
-          const float h0 = me.there ? (cut ? fmaf(exp2_fast(until * rate), begin, from) : from) : 0.0f;
+          const float h0 = cut ? fmaf(exp2_fast(until * rate), begin, from) : from;
           const int next = min(n + 1, p.states - 1);
           if (starts != nullptr) from = lane_of(starts + next * stride, near);
           if (cut) begin = lane_of(carry + int64_t(next) * p.channels, me.near);
@@ -641,7 +647,7 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
           dd[t] = fmaf(dd[t], kLn2, xs[t] * du[t]) * slope[t];
           du[t] = fmaf(delta[t], du[t], me.skip * g[t]);
           y[t] *= dgate[t];
-          if (t < count) ddt_bias += dd[t];
+          if (counts<N>(t, count)) ddt_bias += dd[t];
         }
         if (!me.there) return;
         store_tokens<T>(p.dx, token, p.channels, w, me.near, count, du);
