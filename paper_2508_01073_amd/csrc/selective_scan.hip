@@ -28,7 +28,9 @@ namespace {
 
 constexpr int kTokens = 16;  // of a chunk
 constexpr int kBackTokens = 8;  // of a chunk in the gradients: what is held of each sets how many waves there are
-constexpr int kGang = 4;        // waves of a workgroup in the gradients, which have the rates in common
+// Waves of a workgroup in the gradients, which have the rates in common: what 64 states need of shared memory (120 KB)
+// leaves room for two.
+constexpr int gang_of(int most) { return most <= 16 ? 4 : 2; }
 constexpr int kThreads = 256;  // of a workgroup where waves need not be alone
 
 struct Scan {
@@ -529,12 +531,13 @@ __device__ __forceinline__ void backwards(Each each) {
 // Gradients of a segment, chunk after chunk from its end; a wave takes several segments of its channels in turn
 // and holds the parameters' gradients meanwhile.
 template <class T, int NMAX>
-__global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
-  constexpr int K = kBackTokens;
+__global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p,
+                                                                                                   int64_t first) {
+  constexpr int K = kBackTokens, kGang = gang_of(NMAX), kStarts = 4;
   __shared__ float rates[NMAX * kWave], all_grads[kGang][NMAX * kWave], all_da[kGang][NMAX * kWave];
-  __shared__ float all_b[kGang][NMAX * K], all_c[kGang][NMAX * K];
+  __shared__ float all_held[kGang][NMAX * kWave], all_b[kGang][NMAX * K], all_c[kGang][NMAX * K];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  float *grads = all_grads[wave], *da = all_da[wave], *b = all_b[wave], *c = all_c[wave];
+  float *grads = all_grads[wave], *da = all_da[wave], *held = all_held[wave], *b = all_b[wave], *c = all_c[wave];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
                 part = (first + blockIdx.x) / columns * kGang + wave;
   const bool cut = p.segments > 1;
@@ -550,11 +553,12 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
   for (int64_t item = part; item < p.rows * p.segments; item += p.parts) {
     w = place_of(p, column, item, lane == 0);
     wave_sync();
-    if (!cut)
+    if (!cut) {
       load_states(p, w, p.dstate_out, grads);
-    else
+    } else {
       load_carry(p, w, p.back + item * p.states * p.channels, me.near, grads);
-    const float *carry = p.carry + item * p.states * p.channels + w.c0;
+      load_carry(p, w, p.carry + item * p.states * p.channels, me.near, held);
+    }
     const int64_t last = w.begin + (w.stop - w.begin - 1) / K * K;  // chunk
     for (int64_t t0 = last; t0 >= w.begin && w.begin < w.stop; t0 -= K) {
       const int count = int(min(int64_t(K), w.stop - t0));
@@ -570,7 +574,14 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
       float *sums = p.bc + (((w.block * p.rows * p.chunks + chunk) * p.groups + w.group) * p.states) * (2 * K);
       with_tokens<K>(count, [&](auto tokens) {
         constexpr int N = tokens();
-        float from = starts != nullptr ? lane_of(starts, near) : 0.0f, begin = cut ? lane_of(carry, me.near) : 0.0f;
+        // four states' at a time, read while the four before are worked on
+        const auto load_starts = [&](int n0, float (&from)[kStarts]) {
+#pragma unroll
+          for (int k = 0; k < kStarts; ++k)
+            from[k] = starts != nullptr ? lane_of(starts + min(n0 + k, p.states - 1) * stride, near) : 0.0f;
+        };
+        float from[kStarts];
+        load_starts(0, from);
         float xs[N], delta[N], slope[N], u[N], g[N], y[N], dgate[N], du[N] = {}, dd[N] = {};
         wave_sync();
         {
@@ -605,12 +616,9 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
           }
         }
         wave_sync();
-        for (int n = 0; n < p.states; ++n) {
+        const auto work = [&](int n, float start) {
           const float rate = rates[n * kWave + lane];
-          const float h0 = cut ? fmaf(exp2_fast(until * rate), begin, from) : from;
-          const int next = min(n + 1, p.states - 1);
-          if (starts != nullptr) from = lane_of(starts + next * stride, near);
-          if (cut) begin = lane_of(carry + int64_t(next) * p.channels, me.near);
+          const float h0 = cut ? fmaf(exp2_fast(until * rate), held[n * kWave + lane], start) : start;
           float bn[N], cn[N], e[N], h[N];
           read_head<K>(b, n, bn);
           read_head<K>(c, n, cn);
@@ -641,6 +649,15 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 16 ? 2 : 1) void scan_backwar
           }
           const float total = sixteen_sums(each);
           if (lane % 4 == 0) lane_of(sums + n * 2 * K, uint32_t(lane) / 4) = total;
+        };
+        for (int n0 = 0; n0 < p.states; n0 += kStarts) {
+          float ahead[kStarts];
+          load_starts(n0 + kStarts, ahead);
+#pragma unroll
+          for (int k = 0; k < kStarts; ++k)
+            if (n0 + k < p.states) work(n0 + k, from[k]);
+#pragma unroll
+          for (int k = 0; k < kStarts; ++k) from[k] = ahead[k];
         }
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -795,8 +812,10 @@ int64_t parts_of(const Scan &p, int64_t most) {
 // Segments of a row, chunks, the waves along rows and segments, and where the workspace's arrays lie; its bytes.
 size_t plan(Scan &p, bool backward, void *workspace) {
   // Waves of a column of channels beside those of the others: with fewer than one to each of 1,024 SIMDs rows are cut
-  // into segments, as many as the kernels' registers let them have at once.
-  constexpr int64_t kFew = 1024, kFill = 4096, kShortest = 2 * kTokens;
+  // into segments, as many as the kernels' registers let them have at once: four to a SIMD, and two in the gradients
+  // (4 rows of 4,096 tokens by 2,048 channels in bf16: 868 us in their two kernels, with four 919).
+  constexpr int64_t kFew = 1024, kShortest = 2 * kTokens;
+  const int64_t kFill = backward ? 2048 : 4096;
   const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
   int64_t segments = 1;
   if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
@@ -916,6 +935,7 @@ rdf2v_status launch_selective_scan_backward(const rdf2v_scan &a, const ScanInput
     }
     if (st != RDF2V_OK) return st;
     st = with_types(a.dtype, p.states, [&](auto t, auto most) {
+      constexpr int kGang = gang_of(most());
       const int64_t gangs = (p.parts + kGang - 1) / kGang * p.blocks * p.groups;
       return for_each_launch(gangs, kGang * kWave, 1, [&](int64_t first, int64_t count) {
         scan_backward_kernel<decltype(t), most()><<<dim3(unsigned(count)), dim3(kGang * kWave), 0, stream>>>(p, first);
