@@ -157,9 +157,11 @@ __device__ __forceinline__ void locate(const Norm &a, int64_t id, int64_t &row, 
 }
 
 constexpr int workgroup_of(int team) { return team < kThreads ? kThreads : team; }
+// Waves of each of a compute unit's four SIMDs, as the registers for a thread's vectors let them have.
+constexpr int waves_of(bool backward, int per) { return backward || per > 3 ? 4 : per > 2 ? 5 : 6; }
 
 template <class T, class R, int TEAM, int PER>
-__global__ __launch_bounds__(workgroup_of(TEAM)) void norm_kernel(Norm a) {
+__global__ __launch_bounds__(workgroup_of(TEAM), waves_of(false, PER)) void norm_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
   __shared__ float scratch[2][kBlock / kWave][1];
   const Own<TEAM, PER> own{int(threadIdx.x) % TEAM, a.channels};
@@ -258,7 +260,7 @@ __device__ __forceinline__ void store_part(float *part, const Own<TEAM, PER> &ow
 //   dhidden + (dn - n mean(dn n) - mean(dn)) / std        (the last mean where the norm is centred)
 // MORE: there is a scale, or gradients of the bias or the scale are wanted.
 template <class T, class R, bool MORE, int TEAM, int PER>
-__global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm a) {
+__global__ __launch_bounds__(workgroup_of(TEAM), waves_of(true, PER)) void norm_backward_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
   __shared__ float scratch[2][kBlock / kWave][2];
   __shared__ float parts[kTeams > 1 ? kBlock : 1][V];
@@ -332,8 +334,8 @@ __global__ __launch_bounds__(workgroup_of(TEAM)) void norm_backward_kernel(Norm 
 
 // Calls launch with constants for the size of a team and the vectors of a thread: the smallest team that needs two
 // at most, three in the forward call: the generator works for all lanes, with channels or without. In the gradients
-// a third costs more in waves than idle lanes do (69,632 tokens of 301 channels: teams of 32 with three vectors and
-// of 64 with two take 72 and 80 us forward, 115 and 94 us backward).
+// a third costs in waves what idle lanes do (69,632 tokens of 301 channels: teams of 32 with three vectors and of 64
+// with two take 69 and 80 us forward, 99 us both backward).
 template <bool BACKWARD, class Launch>
 rdf2v_status with_team(int channels, Launch launch) {
 #define RDF2V_TEAM(TEAM, PER) \
@@ -369,14 +371,14 @@ rdf2v_status with_flag(bool flag, Launch launch) {
   return flag ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
-// As many workgroups as the chip holds at once with 16 or 24 waves on each of its 256 compute units, at most one for
-// each workgroup's teams of tokens: they take tokens in turn, and a second round of some would leave units idle
-// (16,384 tokens of 4,096 channels, gradients: 349 us with 1,024 workgroups where 768 fit).
+// As many workgroups as the chip's 256 compute units hold at once, at most one for each workgroup's teams of tokens:
+// they take tokens in turn, and a second round of some would leave units idle (16,384 tokens of 4,096 channels,
+// gradients: 349 us with 1,024 workgroups where 768 fit).
 template <bool BACKWARD>
 int64_t workgroups_of(int64_t tokens, int channels) {
-  constexpr int64_t waves = BACKWARD ? 16 : 24;
   int64_t count = 1;
-  with_team<BACKWARD>(channels, [&](auto team, auto) {
+  with_team<BACKWARD>(channels, [&](auto team, auto per) {
+    const int64_t waves = 4 * waves_of(BACKWARD, per());
     const int64_t teams = workgroup_of(team()) / team();
     count = std::min((tokens + teams - 1) / teams, 256 * std::max<int64_t>(1, waves * kWave / workgroup_of(team())));
     return RDF2V_OK;
