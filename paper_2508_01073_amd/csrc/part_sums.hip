@@ -11,11 +11,11 @@ constexpr int kWaves = kValues * kRanks / kWave;
 // A value's threads take every 64th part each, eight loads in flight. Held in 64 bits: the parts are few, and their
 // sum is rounded once. 1,024 parts of 903 values: 20 us with 16 threads to each of 64 values of a workgroup, which
 // leaves 15 workgroups, 5 us so.
-__global__ __launch_bounds__(kValues *kRanks) void part_sums_kernel(PartSums a) {
+__global__ __launch_bounds__(kValues *kRanks) void part_sums_kernel(PartSums a, int64_t first) {
   constexpr int kAhead = 8;
   __shared__ double sums[kWaves][kValues];
   const int value = threadIdx.x % kValues, rank = threadIdx.x / kValues;
-  const int64_t n = a.count[0] + a.count[1] + a.count[2], at = int64_t(blockIdx.x) * kValues + value;
+  const int64_t n = a.count[0] + a.count[1] + a.count[2], at = (first + blockIdx.x) * kValues + value;
   double sum = 0.0;
   if (at < n)
     for (int64_t p = rank; p < a.parts; p += kAhead * kRanks) {
@@ -45,12 +45,11 @@ __global__ __launch_bounds__(kValues *kRanks) void part_sums_kernel(PartSums a) 
 
 rdf2v_status launch_part_sums(const PartSums &a, hipStream_t stream) {
   const int64_t n = a.count[0] + a.count[1] + a.count[2];
-  if (n == 0) return RDF2V_OK;
-  const int64_t blocks = (n + kValues - 1) / kValues;
-  if (blocks * kValues * kRanks > kMaxLaunchThreads) return RDF2V_ERR_TOO_LARGE;
-  hipLaunchKernelGGL(part_sums_kernel, dim3(uint32_t(blocks)), dim3(kValues * kRanks), 0, stream, a);
-  RDF2V_LAUNCH_CHECK();
-  return RDF2V_OK;
+  return for_each_launch((n + kValues - 1) / kValues, kValues * kRanks, 1, [&](int64_t first, int64_t count) {
+    part_sums_kernel<<<dim3(unsigned(count)), dim3(kValues * kRanks), 0, stream>>>(a, first);
+    RDF2V_LAUNCH_CHECK();
+    return RDF2V_OK;
+  });
 }
 
 }  // namespace rdf2v

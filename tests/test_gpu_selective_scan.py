@@ -220,3 +220,22 @@ def test_outputs_over_inputs_are_refused():
     one = {k: c[k][:, 0] for k in ("x", "dt", "b", "c", "gate")}
     with pytest.raises(rd.Rdf2vError):
         rd.rdf2v_selective_scan_step(**one, a=c["a"], state=held, parents=lengths([1, 0]), state_out=held)
+
+
+def test_parameters_of_more_values_than_a_launch_sums():
+    """2^20 + 64 channels of 64 states: gradients of 69 million parameters, equal to those of parts of the channels."""
+    say("[scan] many parameters")
+    d, states = (1 << 20) + 64, 64
+    gen = torch.Generator(device=device()).manual_seed(3)
+    x, dt, dout = (torch.randn(2, 1, d, generator=gen, device=device()) for _ in range(3))
+    b, c = (torch.randn(2, 1, 1, states, generator=gen, device=device()) for _ in range(2))
+    a = -torch.rand(d, states, generator=gen, device=device())
+    dt_bias, skip = (torch.randn(d, generator=gen, device=device()) for _ in range(2))
+    state = torch.randn(2, d, states, generator=gen, device=device())
+    got = rd.rdf2v_selective_scan_backward(x, dt, a, b, c, dout, dt_bias=dt_bias, skip=skip, state=state)
+    half = d // 128 * 64
+    for s in (slice(0, half), slice(half, d)):
+        want = rd.rdf2v_selective_scan_backward(x[..., s], dt[..., s], a[s], b, c, dout[..., s], dt_bias=dt_bias[s],
+                                                skip=skip[s], state=state[:, s].contiguous())
+        for name in ("da", "ddt_bias", "dskip"):
+            assert torch.equal(getattr(got, name)[s], getattr(want, name)), name
