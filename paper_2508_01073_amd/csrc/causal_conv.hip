@@ -238,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
   }
 }
 
-// One token more: a thread to a row's vector of channels. 512 rows of 2,048 channels in bf16, width 4: 9.8 us for 15 MB,
-// most of it the latency of a parent's id and then its state.
+// One token more: a thread to a row's vector of channels. 512 rows of 2,048 channels in bf16, width 4: 9.8 us for
+// 15 MB, most of it the latency of a parent's id and then its state.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_step_kernel(Conv a, int64_t first) {
   constexpr int V = 16 / sizeof(T);

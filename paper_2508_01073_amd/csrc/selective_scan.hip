@@ -3,12 +3,12 @@
 //   h_t[n] = exp(delta_t a[n]) h_{t-1}[n] + delta_t x_t b_t[n],   y_t = sum_n c_t[n] h_t[n] + skip x_t
 //
 // for every channel by itself: per token, channel and state one exponential and three multiply-adds, so with 16
-// states vector instructions bound it, the exponentials (a quarter of the rate) half of them; memory comes next.
+// states vector instructions bound it, memory comes next. An exponential takes the time of two other instructions.
 //
-// A wave takes 64 channels (a lane each) of a row, or of a segment of it, 16 tokens at a time, and nothing is
-// shared with other waves: no barrier, no value made twice. It takes the channels' states in turn, each through
-// the chunk's 16 tokens, whose values stay in registers meanwhile: the number of states is a loop's, not a
-// register file's. b and c of the chunk lie in LDS and are read by all lanes at once.
+// A wave takes 64 channels (a lane each) of a row, or of a segment of it, 16 tokens at a time, and nothing but the
+// gradients' rates is shared with other waves: no barrier, no value made twice. It takes the channels' states in
+// turn, each through the chunk's 16 tokens, whose values stay in registers meanwhile: the number of states is a
+// loop's, not a register file's. b and c of the chunk lie in LDS and are read by all lanes at once.
 //
 // Rows too few to fill the chip are cut into segments: every segment's state from zeros (scan_states_kernel), the
 // states' way through the segments (scan_join_kernel), then all segments at once. That costs the exponentials
