@@ -1610,8 +1610,8 @@ class _Norm:
             raise TypeError(f"residual must be {x.dtype} or float32, got {hidden_dtype}")
         if not 0.0 <= drop < 1.0 - 2.0 ** -32:
             raise ValueError(f"drop must be in [0, 1), got {drop}")
-        if row_begin < 0:
-            raise ValueError("row_begin must not be negative")
+        if not 0 <= row_begin < 1 << 63:
+            raise ValueError("row_begin must be in [0, 2^63)")
         self.hidden_dtype = hidden_dtype
         self.views = (_tokens_view(x, "x", x.dtype, dev, shape),
                       None if residual is None else _tokens_view(residual, "residual", hidden_dtype, dev, shape))

@@ -93,6 +93,51 @@ def test_replays_equal_the_eager_run(n, length):
         before = mask
 
 
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+def test_a_captured_training_step(type_):
+    """A layer forward and backward through autograd, workspaces and all its own, in a graph that is replayed."""
+    say(f"[layer capture] training step {type_}")
+    n, length, d, states = 30, 17, 70, 11
+    leaves = [rand(n, length, d, type_=type_, seed=1), rand(n, length, d, seed=2), rand(d, seed=3),
+              rand(d, 4, seed=4), -rand(d, states, seed=5).abs(), rand(n, length, 1, states, type_=type_, seed=6),
+              rand(d, seed=7)]
+    for t in leaves:
+        t.requires_grad_()
+    x, stream, weight, taps, a, b, skip = leaves
+    lens = lengths([(7 * r) % (length + 1) for r in range(n)])
+    offset = torch.zeros(1, dtype=torch.int64, device=device())
+    dout, dstream = rand(n, length, d, type_=type_, seed=8), rand(n, length, d, seed=9)
+
+    def step():
+        y, hidden, _ = rd.rdf2v_residual_norm(x, stream, weight, drop=0.2, seed=3, seed_offset=offset, lens=lens)
+        u, _ = rd.rdf2v_causal_conv(y, taps, lens=lens)
+        out, _ = rd.rdf2v_selective_scan(u, y, a, b, b, skip=skip, gate=u, lens=lens)
+        return (out, hidden, *torch.autograd.grad((out, hidden), leaves, (dout, dstream)))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = [t.detach() for t in step()]
+    for seed in (1, 2, 3):
+        gen = torch.Generator(device=device()).manual_seed(seed)
+        with torch.no_grad():
+            for t in (x, stream, b, dout, dstream):
+                t.copy_(torch.randn(t.shape, device=device(), generator=gen))
+            offset.fill_(seed)
+        eager = [t.detach().clone() for t in step()]
+        for t in captured:
+            t.fill_(-1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (got, want) in enumerate(zip(captured, eager)):
+            assert torch.equal(got, want), (seed, i)
+
+
 def test_another_stream():
     """Calls on a stream that is not the current one, with what they allocate."""
     say("[layer capture] another stream")
