@@ -28,9 +28,7 @@ namespace {
 
 constexpr int kTokens = 16;  // of a chunk
 constexpr int kBackTokens = 8;  // of a chunk in the gradients: what is held of each sets how many waves there are
-// Waves of a workgroup in the gradients, which have the rates in common: what 64 states need of shared memory (120 KB)
-// leaves room for two.
-constexpr int gang_of(int most) { return most <= 16 ? 4 : 2; }
+constexpr int kGang = 4;        // waves of a workgroup in the gradients, which have the rates in common
 constexpr int kThreads = 256;  // of a workgroup where waves need not be alone
 
 struct Scan {
@@ -538,11 +536,12 @@ __device__ __forceinline__ void backwards(Each each) {
 // 4 rows of 4,096 tokens by 2,048 channels of 16 states: 531 us, 72 % of the issue, the rest waits of the two waves
 // that a SIMD's registers hold. Three, with segments for them, took 570 us for 589, but the states 352 for 279.
 template <class T, int NMAX>
-__global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan_backward_kernel(Scan p,
-                                                                                                   int64_t first) {
-  constexpr int K = kBackTokens, kGang = gang_of(NMAX), kStarts = 4;
+__global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
+  constexpr int K = kBackTokens, kStarts = 4;
+  // what a segment begins with; of more states it would cost every other wave (64: 3,855 us for 2,529)
+  constexpr bool kHeld = NMAX <= 16;
   __shared__ float rates[NMAX * kWave], all_grads[kGang][NMAX * kWave], all_da[kGang][NMAX * kWave];
-  __shared__ float all_held[kGang][NMAX * kWave], all_b[kGang][NMAX * K], all_c[kGang][NMAX * K];
+  __shared__ float all_held[kGang][kHeld ? NMAX * kWave : 1], all_b[kGang][NMAX * K], all_c[kGang][NMAX * K];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   float *grads = all_grads[wave], *da = all_da[wave], *held = all_held[wave], *b = all_b[wave], *c = all_c[wave];
   const int64_t columns = p.blocks * p.groups, column = (first + blockIdx.x) % columns,
@@ -564,8 +563,9 @@ __global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan
       load_states(p, w, p.dstate_out, grads);
     } else {
       load_carry(p, w, p.back + item * p.states * p.channels, me.near, grads);
-      load_carry(p, w, p.carry + item * p.states * p.channels, me.near, held);
+      if (kHeld) load_carry(p, w, p.carry + item * p.states * p.channels, me.near, held);
     }
+    const float *carry = p.carry + item * p.states * p.channels + w.c0;
     const int64_t last = w.begin + (w.stop - w.begin - 1) / K * K;  // chunk
     for (int64_t t0 = last; t0 >= w.begin && w.begin < w.stop; t0 -= K) {
       const int count = int(min(int64_t(K), w.stop - t0));
@@ -582,13 +582,16 @@ __global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan
       with_tokens<K>(count, [&](auto tokens) {
         constexpr int N = tokens();
         // four states' at a time, read while the four before are worked on
-        const auto load_starts = [&](int n0, float (&from)[kStarts]) {
+        const auto load_starts = [&](int n0, float (&from)[kStarts], float (&begin)[kStarts]) {
 #pragma unroll
-          for (int k = 0; k < kStarts; ++k)
-            from[k] = starts != nullptr ? lane_of(starts + min(n0 + k, p.states - 1) * stride, near) : 0.0f;
+          for (int k = 0; k < kStarts; ++k) {
+            const int n = min(n0 + k, p.states - 1);
+            from[k] = starts != nullptr ? lane_of(starts + n * stride, near) : 0.0f;
+            begin[k] = !kHeld && cut ? lane_of(carry + int64_t(n) * p.channels, me.near) : 0.0f;
+          }
         };
-        float from[kStarts];
-        load_starts(0, from);
+        float from[kStarts], begin[kStarts];
+        load_starts(0, from, begin);
         float xs[N], delta[N], slope[N], u[N], g[N], y[N], dgate[N], du[N] = {}, dd[N] = {};
         wave_sync();
         {
@@ -623,9 +626,10 @@ __global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan
           }
         }
         wave_sync();
-        const auto work = [&](int n, float start) {
+        const auto work = [&](int n, float start, float first) {
           const float rate = rates[n * kWave + lane];
-          const float h0 = cut ? fmaf(exp2_fast(until * rate), held[n * kWave + lane], start) : start;
+          if (kHeld && cut) first = held[n * kWave + lane];
+          const float h0 = cut ? fmaf(exp2_fast(until * rate), first, start) : start;
           float bn[N], cn[N], e[N], h[N];
           read_head<K>(b, n, bn);
           read_head<K>(c, n, cn);
@@ -658,13 +662,13 @@ __global__ __launch_bounds__(gang_of(NMAX) *kWave, NMAX <= 16 ? 2 : 1) void scan
           if (lane % 4 == 0) lane_of(sums + n * 2 * K, uint32_t(lane) / 4) = total;
         };
         for (int n0 = 0; n0 < p.states; n0 += kStarts) {
-          float ahead[kStarts];
-          load_starts(n0 + kStarts, ahead);
+          float ahead[kStarts], begin_ahead[kStarts];
+          load_starts(n0 + kStarts, ahead, begin_ahead);
 #pragma unroll
           for (int k = 0; k < kStarts; ++k)
-            if (n0 + k < p.states) work(n0 + k, from[k]);
+            if (n0 + k < p.states) work(n0 + k, from[k], begin[k]);
 #pragma unroll
-          for (int k = 0; k < kStarts; ++k) from[k] = ahead[k];
+          for (int k = 0; k < kStarts; ++k) from[k] = ahead[k], begin[k] = begin_ahead[k];
         }
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -852,11 +856,15 @@ size_t plan(Scan &p, bool backward, void *workspace) {
   return bytes;
 }
 
-// Calls launch with a value of the element type and a constant for the most states.
+// Calls launch with a value of the element type and a constant for the most states. Shared memory sets how many waves
+// there are: 16 states leave four to a SIMD (two in the gradients, by their registers), 32 two, 64 one. 4 rows of 4,096
+// tokens by 1,024 channels of 24 states: 240 us by the kernels for 32, 402 by those for 64.
 template <class Launch>
 rdf2v_status with_types(int dtype, int states, Launch launch) {
   const auto sized = [&](auto t) {
-    return states <= 16 ? launch(t, std::integral_constant<int, 16>{}) : launch(t, std::integral_constant<int, 64>{});
+    if (states <= 16) return launch(t, std::integral_constant<int, 16>{});
+    if (states <= 32) return launch(t, std::integral_constant<int, 32>{});
+    return launch(t, std::integral_constant<int, 64>{});
   };
   return dtype == RDF2V_BF16 ? sized(bf16{}) : sized(float{});
 }
@@ -942,7 +950,6 @@ rdf2v_status launch_selective_scan_backward(const rdf2v_scan &a, const ScanInput
     }
     if (st != RDF2V_OK) return st;
     st = with_types(a.dtype, p.states, [&](auto t, auto most) {
-      constexpr int kGang = gang_of(most());
       const int64_t gangs = (p.parts + kGang - 1) / kGang * p.blocks * p.groups;
       return for_each_launch(gangs, kGang * kWave, 1, [&](int64_t first, int64_t count) {
         scan_backward_kernel<decltype(t), most()><<<dim3(unsigned(count)), dim3(kGang * kWave), 0, stream>>>(p, first);

@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 
 # rows, length, channels, groups, states
 SIZES = [(1, 1, 1, 1, 1), (2, 1, 6, 2, 4), (3, 17, 64, 1, 16), (4, 33, 70, 1, 11), (2, 16, 24, 4, 3), (3, 5, 130, 2, 16),
-         (1, 100, 20, 1, 64), (2, 47, 129, 3, 17), (1, 300, 80, 1, 16), (1, 531, 66, 2, 5)]
+         (1, 100, 20, 1, 64), (2, 47, 129, 3, 17), (1, 300, 80, 1, 16), (1, 531, 66, 2, 5), (2, 90, 65, 1, 32),
+         (1, 130, 30, 2, 23), (3, 33, 70, 1, 33)]
 
 
 def case(n, t, d, groups, states, type_, state=True, ragged=True, extras=True, seed=0):
