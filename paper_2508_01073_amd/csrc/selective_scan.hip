@@ -820,21 +820,52 @@ int64_t parts_of(const Scan &p, int64_t most) {
   return std::max<int64_t>(1, std::min(p.rows * p.segments, most / (p.blocks * p.groups)));
 }
 
+// Sets how many tokens a segment has, and how many segments, `segments` or fewer, that makes.
+void cut_rows(Scan &p, int64_t segments, int64_t chunk) {
+  p.segment = (p.length + segments - 1) / segments;
+  p.segment = std::max(chunk, (p.segment + chunk - 1) / chunk * chunk);
+  p.segments = std::max<int64_t>(1, (p.length + p.segment - 1) / p.segment);
+}
+
+constexpr int64_t kSimds = 1024;
+constexpr int64_t kShortest = 32;  // tokens of a segment at least
+
+// Forward rows are cut where a wave to a row's column of channels is less than one to a SIMD, as it takes a second look
+// at all tokens: into as many segments as there are waves that the registers let the chip have at once, four to a SIMD.
+void plan_forward(Scan &p) {
+  const int64_t whole = std::max<int64_t>(1, p.rows * p.blocks * p.groups);
+  const int64_t segments = whole < kSimds ? std::min(4 * kSimds / whole, p.length / kShortest) : 1;
+  cut_rows(p, std::max<int64_t>(1, segments), kTokens);
+  p.parts = parts_of(p, 8 * kSimds);
+}
+
+// The gradients look at all tokens twice anyway, and their waves, two to a SIMD, take segments in turn. Where whole
+// rows are fewer: of the numbers of segments that fill 1, 2, .. turns the one that gives the busiest wave the fewest
+// tokens, with 8 for what a segment costs by itself; a wave alone on its SIMD takes three quarters of the time, and rows
+// that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and 464
+// cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
+void plan_backward(Scan &p) {
+  const int64_t most = 2 * kSimds, columns = p.blocks * p.groups, rows = std::max<int64_t>(1, p.rows);
+  const auto cost = [&](int64_t segments) {
+    cut_rows(p, segments, kBackTokens);
+    p.parts = parts_of(p, most);
+    const int64_t turns = (rows * p.segments + p.parts - 1) / p.parts;
+    return turns * (p.segment + 8) * (p.parts * columns <= kSimds ? 3 : 4) * (p.segments > 1 ? 9 : 8);
+  };
+  int64_t best = 1, least = cost(1);
+  for (int64_t turns = 1; turns <= 8 && rows * columns < most; ++turns) {
+    const int64_t segments = std::min(turns * std::max<int64_t>(1, most / columns) / rows, p.length / kShortest);
+    if (segments < 2) continue;
+    const int64_t of = cost(segments);
+    if (of < least) best = segments, least = of;
+  }
+  cost(best);
+}
+
 // Segments of a row, chunks, the waves along rows and segments, and where the workspace's arrays lie; its bytes.
 size_t plan(Scan &p, bool backward, void *workspace) {
-  // Waves of a column of channels beside those of the others: with fewer than one to each of 1,024 SIMDs rows are cut
-  // into segments, as many as the kernels' registers let them have at once: four to a SIMD, and two in the gradients
-  // (4 rows of 4,096 tokens by 2,048 channels in bf16: 868 us in their two kernels, with four 919).
-  constexpr int64_t kFew = 1024, kShortest = 2 * kTokens;
-  const int64_t kFill = backward ? 2048 : 4096;
-  const int64_t columns = p.blocks * p.groups, whole = std::max<int64_t>(1, p.rows * columns);
-  int64_t segments = 1;
-  if (whole < kFew) segments = std::max<int64_t>(1, std::min(kFill / whole, p.length / kShortest));
-  p.segment = std::max<int64_t>(1, (p.length + segments - 1) / segments);
-  p.segment = (p.segment + kTokens - 1) / kTokens * kTokens;
-  p.segments = std::max<int64_t>(1, (p.length + p.segment - 1) / p.segment);
+  backward ? plan_backward(p) : plan_forward(p);
   p.chunks = (p.length + kBackTokens - 1) / kBackTokens;
-  p.parts = parts_of(p, backward ? 2048 : 8192);
   size_t bytes = 0;
   const auto take = [&](float *&at, int64_t count) {
     at = workspace != nullptr ? reinterpret_cast<float *>(static_cast<char *>(workspace) + bytes) : nullptr;
