@@ -723,12 +723,14 @@ __global__ __launch_bounds__(kThreads) void scan_bc_kernel(Scan p, int64_t first
   static_cast<T *>(p.dc)[item] = from_f32<T>(dc);
 }
 
-// One token more. `lanes` threads, a power of two, take a channel's states, V neighbouring ones at a time; a
-// workgroup takes a tile of channels of kStepRows rows, whose loads are all in flight at once, and the rates once
-// for them. HBM-bound: states are read and written. 512 rows of 2,048 channels by 16 states: 33 us, 143 MB.
+// One token more. `lanes` threads, a power of two, take a channel's states, four neighbouring ones at a time (WHOLE:
+// the last of them has four, too); a workgroup takes a tile of channels of kStepRows rows, whose loads are all in flight at
+// once, and the rates once for them. HBM-bound: states are read and written. 512 rows of 2,048 channels by 16 states:
+// 32 us, 143 MB; by 17 states 74 us, and 147 with a thread to each state.
 constexpr int kStepRows = 4;
-template <class T, int V>
+template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, int64_t tiles, int64_t first) {
+  constexpr int V = 4;
   const int64_t block = first + blockIdx.x, row0 = block / tiles * kStepRows;
   const int lane = threadIdx.x % lanes;
   const int64_t at = block % tiles * (kThreads / lanes) + threadIdx.x / lanes;
@@ -751,15 +753,18 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, 
   }
   for (int n = lane * V; n < p.states; n += lanes * V) {
     float rate[V], h[kStepRows][V], b[kStepRows][V], c[kStepRows][V];
-    load_values<float, V>(p.a + channel * p.states + n, V, rate);
+    const int count = WHOLE ? V : min(V, p.states - n);
+    load_values<float, V>(p.a + channel * p.states + n, count, rate);
 #pragma unroll
     for (int r = 0; r < kStepRows; ++r) {
       const int64_t row = row0 + min(r, rows - 1);
       const bool known = from[r] >= 0 && from[r] < p.num_states;
       load_values<float, V>(p.state + ((known ? from[r] : 0) * p.channels + channel) * p.states + n,
-                            p.num_states > 0 ? V : 0, h[r]);
-      load_values<T, V>(static_cast<const T *>(p.b.data) + row * p.b.row_stride + group * p.b.head_stride + n, V, b[r]);
-      load_values<T, V>(static_cast<const T *>(p.c.data) + row * p.c.row_stride + group * p.c.head_stride + n, V, c[r]);
+                            p.num_states > 0 ? count : 0, h[r]);
+      load_values<T, V>(static_cast<const T *>(p.b.data) + row * p.b.row_stride + group * p.b.head_stride + n, count,
+                        b[r]);
+      load_values<T, V>(static_cast<const T *>(p.c.data) + row * p.c.row_stride + group * p.c.head_stride + n, count,
+                        c[r]);
 #pragma unroll
       for (int i = 0; i < V; ++i) h[r][i] = known ? h[r][i] : 0.0f;
     }
@@ -773,11 +778,12 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, 
       const float u = d[r] * x[r];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
+        if (!WHOLE && i >= count) break;  // 0 times an infinite u would be no number
         h[r][i] = fmaf(exp2_fast(d[r] * rate[i]), h[r][i], u * b[r][i]);
         y[r] = fmaf(h[r][i], c[r][i], y[r]);
       }
       if (there && r < rows)
-        store_values<float, V>(p.state_out + ((row0 + r) * p.channels + channel) * p.states + n, V, h[r]);
+        store_values<float, V>(p.state_out + ((row0 + r) * p.channels + channel) * p.states + n, count, h[r]);
     }
   }
 #pragma unroll
@@ -841,8 +847,8 @@ void plan_forward(Scan &p) {
 
 // The gradients look at all tokens twice anyway, and their waves, two to a SIMD, take segments in turn. Where whole
 // rows are fewer: of the numbers of segments that fill 1, 2, .. turns the one that gives the busiest wave the fewest
-// tokens, with 8 for what a segment costs by itself; a wave alone on its SIMD takes three quarters of the time, and rows
-// that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and 464
+// tokens, with 8 for what a segment costs by itself; a wave alone on its SIMD takes three quarters of the time, and
+// rows that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and 464
 // cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
 void plan_backward(Scan &p) {
   const int64_t most = 2 * kSimds, columns = p.blocks * p.groups, rows = std::max<int64_t>(1, p.rows);
@@ -1016,21 +1022,20 @@ rdf2v_status launch_selective_scan_step(const rdf2v_scan &a, const ScanInputs &i
   p.parents = parents;
   p.out = out;
   p.state_out = state_out;
-  // whole vectors of four states where there are no others
-  const int each = p.states % 4 == 0 ? 4 : 1;
+  const bool whole = p.states % 4 == 0;
   int lanes = 1;
-  while (lanes < kWave && lanes * each < p.states) lanes *= 2;
+  while (lanes < kWave && lanes * 4 < p.states) lanes *= 2;
   const int64_t per = kThreads / lanes, tiles = (p.channels + per - 1) / per;
   return for_each_launch((p.rows + kStepRows - 1) / kStepRows * tiles, kThreads, 1, [&](int64_t first, int64_t count) {
     const dim3 grid(static_cast<unsigned>(count)), block(kThreads);
-    if (a.dtype == RDF2V_BF16 && each == 4)
-      scan_step_kernel<bf16, 4><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+    if (a.dtype == RDF2V_BF16 && whole)
+      scan_step_kernel<bf16, true><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
     else if (a.dtype == RDF2V_BF16)
-      scan_step_kernel<bf16, 1><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
-    else if (each == 4)
-      scan_step_kernel<float, 4><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+      scan_step_kernel<bf16, false><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+    else if (whole)
+      scan_step_kernel<float, true><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
     else
-      scan_step_kernel<float, 1><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
+      scan_step_kernel<float, false><<<grid, block, 0, stream>>>(p, lanes, tiles, first);
     RDF2V_LAUNCH_CHECK();
     return RDF2V_OK;
   });

@@ -240,3 +240,16 @@ def test_parameters_of_more_values_than_a_launch_sums():
                                                 skip=skip[s], state=state[:, s].contiguous())
         for name in ("da", "ddt_bias", "dskip"):
             assert torch.equal(getattr(got, name)[s], getattr(want, name)), name
+
+
+@pytest.mark.parametrize("states", [1, 3, 4, 6, 33])
+def test_an_infinite_input_stays_infinite_in_a_step(states):
+    """Places of a vector that hold no state add nothing, whatever the token is."""
+    say(f"[scan] infinite input, {states} states")
+    x = torch.full((2, 5), float("inf"), device=device())
+    x[1] = 1.0
+    one = torch.ones(2, 1, states, device=device())
+    out, state = rd.rdf2v_selective_scan_step(x, torch.zeros_like(x), -torch.ones(5, states, device=device()), one, one,
+                                              torch.zeros(2, 5, states, device=device()))
+    assert bool((out[0] == float("inf")).all()) and bool((state[0] == float("inf")).all())
+    assert bool(torch.isfinite(out[1]).all()) and bool(torch.isfinite(state[1]).all())
