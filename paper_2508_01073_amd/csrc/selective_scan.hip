@@ -293,11 +293,11 @@ __device__ __forceinline__ void store_zeros(void *out, int64_t from, int64_t to,
 struct Lane {
   int lane, channel;
   uint32_t near;  // what the channel is beyond the block's first
-  bool there, gated;
+  bool there, gated, skips;  // skips: 0 in the place of a skip that is not there would make no number of infinity
   float bias, skip;
   __device__ __forceinline__ Lane(const Scan &p, const Place &w)
       : lane(lane_id()), channel(w.c0 + (lane < w.count ? lane : 0)), near(lane < w.count ? lane : 0),
-        there(lane < w.count), gated(p.gate.data != nullptr),
+        there(lane < w.count), gated(p.gate.data != nullptr), skips(p.skip != nullptr),
         bias(p.dt_bias != nullptr ? p.dt_bias[channel] : 0.0f), skip(p.skip != nullptr ? p.skip[channel] : 0.0f) {}
 };
 
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Sca
         float delta[N], u[N], y[N];
         make_steps(x, dt, me.bias, count, delta, u);
 #pragma unroll
-        for (int t = 0; t < N; ++t) y[t] = me.skip * to_f32(x[t]);
+        for (int t = 0; t < N; ++t) y[t] = me.skips ? me.skip * to_f32(x[t]) : 0.0f;
         __syncthreads();
         for (int n = 0; n < p.states; ++n) {
           const float rate = rates[n * kWave + me.lane];
@@ -622,7 +622,7 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backwar
 #pragma unroll
           for (int t = 0; t < N; ++t) {
             dskip = counts<N>(t, count) ? fmaf(g[t], xs[t], dskip) : dskip;
-            y[t] = me.skip * xs[t];
+            y[t] = me.skips ? me.skip * xs[t] : 0.0f;
           }
         }
         wave_sync();
@@ -673,7 +673,7 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backwar
 #pragma unroll
         for (int t = 0; t < N; ++t) {
           dd[t] = fmaf(dd[t], kLn2, xs[t] * du[t]) * slope[t];
-          du[t] = fmaf(delta[t], du[t], me.skip * g[t]);
+          du[t] = fmaf(delta[t], du[t], me.skips ? me.skip * g[t] : 0.0f);
           y[t] *= dgate[t];
           if (counts<N>(t, count)) ddt_bias += dd[t];
         }
@@ -724,9 +724,9 @@ __global__ __launch_bounds__(kThreads) void scan_bc_kernel(Scan p, int64_t first
 }
 
 // One token more. `lanes` threads, a power of two, take a channel's states, four neighbouring ones at a time (WHOLE:
-// the last of them has four, too); a workgroup takes a tile of channels of kStepRows rows, whose loads are all in flight at
-// once, and the rates once for them. HBM-bound: states are read and written. 512 rows of 2,048 channels by 16 states:
-// 32 us, 143 MB; by 17 states 74 us, and 147 with a thread to each state.
+// the last of them has four, too); a workgroup takes a tile of channels of kStepRows rows, whose loads are all in
+// flight at once, and the rates once for them. HBM-bound: states are read and written. 512 rows of 2,048 channels by 16
+// states: 32 us, 143 MB; by 17 states 74 us, and 147 with a thread to each state.
 constexpr int kStepRows = 4;
 template <class T, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, int64_t tiles, int64_t first) {
@@ -792,7 +792,7 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(Scan p, int lanes, 
     if (r >= rows || lane != 0 || !there) continue;
     if (channel == 0 && p.status != nullptr && (from[r] < 0 || from[r] >= p.num_states))
       atomicOr(p.status, RDF2V_STATUS_ID_OUT_OF_RANGE);
-    y[r] = fmaf(skip, x[r], y[r]);
+    if (p.skip != nullptr) y[r] = fmaf(skip, x[r], y[r]);
     if (p.gate.data != nullptr) y[r] *= silu(z[r]);
     static_cast<T *>(p.out)[(row0 + r) * p.channels + channel] = from_f32<T>(y[r]);
   }
@@ -848,8 +848,8 @@ void plan_forward(Scan &p) {
 // The gradients look at all tokens twice anyway, and their waves, two to a SIMD, take segments in turn. Where whole
 // rows are fewer: of the numbers of segments that fill 1, 2, .. turns the one that gives the busiest wave the fewest
 // tokens, with 8 for what a segment costs by itself; a wave alone on its SIMD takes three quarters of the time, and
-// rows that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and 464
-// cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
+// rows that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and
+// 464 cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
 void plan_backward(Scan &p) {
   const int64_t most = 2 * kSimds, columns = p.blocks * p.groups, rows = std::max<int64_t>(1, p.rows);
   const auto cost = [&](int64_t segments) {

@@ -253,3 +253,21 @@ def test_an_infinite_input_stays_infinite_in_a_step(states):
                                               torch.zeros(2, 5, states, device=device()))
     assert bool((out[0] == float("inf")).all()) and bool((state[0] == float("inf")).all())
     assert bool(torch.isfinite(out[1]).all()) and bool(torch.isfinite(state[1]).all())
+
+
+def test_without_a_skip_nothing_is_added():
+    """An infinite token without a skip: infinite outputs and gradients where the formula has them, not 0 times
+    infinity."""
+    say("[scan] infinite input without a skip")
+    x = torch.ones(2, 5, 70, device=device())
+    x[0, 2] = float("inf")
+    one = torch.ones(2, 5, 1, 6, device=device())
+    given = (x, torch.zeros_like(x), -torch.ones(70, 6, device=device()), one, one)
+    out, _ = rd.rdf2v_selective_scan(*given)
+    assert bool((out[0, 2:] == float("inf")).all())
+    assert bool(torch.isfinite(out[0, :2]).all()) and bool(torch.isfinite(out[1]).all())
+    dout = torch.ones_like(x)
+    dout[1, 3] = float("inf")
+    g = rd.rdf2v_selective_scan_backward(*given, dout)
+    assert bool((g.dx[1, :4] == float("inf")).all())
+    assert bool(torch.isfinite(g.dx[1, 4]).all()) and bool(torch.isfinite(g.dx[0]).all())
