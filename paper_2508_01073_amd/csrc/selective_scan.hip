@@ -303,8 +303,8 @@ struct Lane {
 
 // The outputs of a segment. A wave's barriers cost nothing: it is alone in its workgroup. Bound by the issue of vector
 // instructions: 9 for a token's state, its share of the token's own (the step's logarithm, conversions, the gate)
-// among them. 20,011 tokens of 2,048 channels by 16 states: 215 us, 94 % of the issue with exponentials as two
-// instructions each; 4,000 ragged rows of 17 tokens by 256 channels: 72 us.
+// among them. 20,011 tokens of 2,048 channels by 16 states: 213 us, 94 % of the issue with exponentials as two
+// instructions each; 4,000 ragged rows of 17 tokens by 256 channels: 73 us.
 template <class T, int NMAX>
 __global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Scan p, int64_t first) {
   __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens], c[NMAX * kTokens];
@@ -365,8 +365,8 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Sca
 // The states that a segment ends with, from zeros; BACK, for the gradients: the states before its chunks (from the
 // row's own state where there is one segment), and the gradient that its outputs give the state before it,
 // sum_t (product of the decays up to t) c_t g_t, which needs no second way through the tokens. 20,011 tokens of 2,048
-// channels by 16 states: 159 us, 89 % of the issue; 4 rows of 4,096 tokens, BACK: 280 us, 67 %. Reading a chunk's
-// inputs while the one before is worked on takes the registers of a wave (159 us: 164; BACK: 261).
+// channels by 16 states: 157 us, 89 % of the issue; 4 rows of 4,096 tokens, BACK: 279 us, 67 %. Reading a chunk's
+// inputs while the one before is worked on takes the registers of a wave (157 us: 164; BACK: 261).
 template <class T, int NMAX, bool BACK, bool CUT>
 __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t first) {
   constexpr bool kBoth = BACK && CUT;
@@ -533,7 +533,7 @@ __device__ __forceinline__ void backwards(Each each) {
 
 // Gradients of a segment, chunk after chunk from its end; a wave takes several segments of its channels in turn
 // and holds the parameters' gradients meanwhile. 25 instructions for a token's state, 4 of them the sums over channels.
-// 4 rows of 4,096 tokens by 2,048 channels of 16 states: 531 us, 72 % of the issue, the rest waits of the two waves
+// 4 rows of 4,096 tokens by 2,048 channels of 16 states: 528 us, 72 % of the issue, the rest waits of the two waves
 // that a SIMD's registers hold. Three, with segments for them, took 570 us for 589, but the states 352 for 279.
 template <class T, int NMAX>
 __global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
