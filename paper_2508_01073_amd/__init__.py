@@ -820,11 +820,32 @@ def _no_gradient(call: str, names: str) -> None:
                   "torch.no_grad()", stacklevel=3)
 
 
+def _recorded(function, dev: torch.device, stream, *args):
+    """function.apply(*args) with the call's stream current: autograd makes the backward call on the stream that is
+    current here. What the forward call keeps for it belongs to that stream, is read in its order and given back in its
+    order."""
+    with _on_stream(dev, stream):
+        return function.apply(*args)
+
+
+def _saved(ctx):
+    """What a recorded call has saved. On a stream that the call was given, inputs may belong to another one: their
+    memory is not used anew before the backward call, which is the last that holds them, has read them."""
+    saved = ctx.saved_tensors
+    if ctx.moved:
+        current = torch.cuda.current_stream(saved[0].device)
+        for t in saved:
+            if t is not None:
+                t.record_stream(current)
+    return saved
+
+
 class _DecayAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, state, scale, lens, want_state, workspace, status, stream):
         out, state_out = rdf2v_decay_attention(q, k, v, log_decay, scale=scale, lens=lens, state=state,
                                                want_state=want_state, workspace=workspace, status=status, stream=stream)
+        ctx.moved = stream is not None
         ctx.save_for_backward(q, k, v, log_decay, state, lens)
         ctx.scale = scale
         ctx.set_materialize_grads(False)
@@ -833,7 +854,7 @@ class _DecayAttention(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dstate_out=None):
-        q, k, v, log_decay, state, lens = ctx.saved_tensors
+        q, k, v, log_decay, state, lens = _saved(ctx)
         if dout is None:                                   # the states alone were used
             dout = q.new_zeros((*q.shape[:-1], v.shape[-1]))
         elif dout.stride(-1) != 1:
@@ -882,7 +903,8 @@ def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         if out is not None or state_out is not None:
             raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
                              "gradients")
-        got = _DecayAttention.apply(q, k, v, log_decay, state, scale, lens, want_state, workspace, status, stream)
+        got = _recorded(_DecayAttention, dev, stream, q, k, v, log_decay, state, scale, lens, want_state, workspace,
+                        status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
         shape = (c.rows, c.heads, c.dk, c.dv)
@@ -1102,6 +1124,7 @@ class _DistillLoss(torch.autograd.Function):
     def forward(ctx, logits, ids, teacher, temperature, workspace, status, stream):
         loss, lse = rdf2v_distill_loss(logits, ids, teacher, temperature=temperature, workspace=workspace,
                                        status=status, stream=stream)
+        ctx.moved = stream is not None
         ctx.save_for_backward(logits, ids, teacher, lse)
         ctx.temperature = temperature
         ctx.mark_non_differentiable(lse)
@@ -1110,7 +1133,7 @@ class _DistillLoss(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dloss, _):
-        logits, ids, teacher, lse = ctx.saved_tensors
+        logits, ids, teacher, lse = _saved(ctx)
         grad = rdf2v_distill_loss_backward(logits, ids, teacher, lse, dloss.contiguous(), temperature=ctx.temperature)
         return grad, None, None, None, None, None, None
 
@@ -1135,7 +1158,7 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
     if dloss is None and dlogits is None and _records(logits):
         if loss is not None or lse is not None:
             raise ValueError("loss and lse cannot be given where autograd records the call: logits requires gradients")
-        return _DistillLoss.apply(logits, ids, teacher, temperature, workspace, status, stream)
+        return _recorded(_DistillLoss, dev, stream, logits, ids, teacher, temperature, workspace, status, stream)
     with _on_stream(dev, stream) as h:
         rows, vocab = logits.shape
         loss = torch.empty(rows, dtype=torch.float32, device=dev) if loss is None else \
@@ -1281,6 +1304,7 @@ class _CausalConv(torch.autograd.Function):
     def forward(ctx, x, weight, bias, state, silu, lens, want_state, status, stream):
         out, state_out = rdf2v_causal_conv(x, weight, bias, silu=silu, lens=lens, state=state, want_state=want_state,
                                            status=status, stream=stream)
+        ctx.moved = stream is not None
         ctx.save_for_backward(x, weight, bias, state, lens)
         ctx.silu = silu
         ctx.set_materialize_grads(False)
@@ -1289,7 +1313,7 @@ class _CausalConv(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dstate_out=None):
-        x, weight, bias, state, lens = ctx.saved_tensors
+        x, weight, bias, state, lens = _saved(ctx)
         if dstate_out is not None:
             dstate_out = dstate_out.contiguous()
         dx, dweight, dbias, dstate = rdf2v_causal_conv_backward(
@@ -1318,7 +1342,7 @@ def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
         if out is not None or state_out is not None:
             raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
                              "gradients")
-        got = _CausalConv.apply(x, weight, bias, state, silu, lens, want_state, status, stream)
+        got = _recorded(_CausalConv, dev, stream, x, weight, bias, state, silu, lens, want_state, status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
         out = _new_like(out, "out", x)
@@ -1447,6 +1471,7 @@ class _SelectiveScan(torch.autograd.Function):
         out, state_out = rdf2v_selective_scan(x, dt, a, b, c, dt_bias=dt_bias, skip=skip, gate=gate, lens=lens,
                                               state=state, want_state=want_state, workspace=workspace, status=status,
                                               stream=stream)
+        ctx.moved = stream is not None
         ctx.save_for_backward(x, dt, a, b, c, dt_bias, skip, gate, state, lens)
         ctx.set_materialize_grads(False)
         return (out, state_out) if want_state else out
@@ -1454,7 +1479,7 @@ class _SelectiveScan(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dstate_out=None):
-        x, dt, a, b, c, dt_bias, skip, gate, state, lens = ctx.saved_tensors
+        x, dt, a, b, c, dt_bias, skip, gate, state, lens = _saved(ctx)
         if dstate_out is not None:
             dstate_out = dstate_out.contiguous()
         g = rdf2v_selective_scan_backward(x, dt, a, b, c, _gradient(dout, (x.shape, x.dtype, x.device)),
@@ -1498,8 +1523,8 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
         if out is not None or state_out is not None:
             raise ValueError("out and state_out cannot be given where autograd records the call: an input requires "
                              "gradients")
-        got = _SelectiveScan.apply(x, dt, a, b, c, dt_bias, skip, gate, state, lens, want_state, workspace, status,
-                                   stream)
+        got = _recorded(_SelectiveScan, dev, stream, x, dt, a, b, c, dt_bias, skip, gate, state, lens, want_state,
+                        workspace, status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
         out = _new_like(out, "out", x)
@@ -1632,6 +1657,7 @@ class _ResidualNorm(torch.autograd.Function):
     def forward(ctx, x, residual, weight, bias, scale, seed_offset, lens, given, status, stream):
         out, hidden, stats = rdf2v_residual_norm(x, residual, weight, bias, scale=scale, seed_offset=seed_offset,
                                                  lens=lens, status=status, stream=stream, **given)
+        ctx.moved = stream is not None
         ctx.save_for_backward(x, residual, weight, bias, scale, seed_offset, lens, stats)
         ctx.given = given
         ctx.hidden_dtype = hidden.dtype
@@ -1642,7 +1668,7 @@ class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dhidden, _):
-        x, residual, weight, bias, scale, seed_offset, lens, stats = ctx.saved_tensors
+        x, residual, weight, bias, scale, seed_offset, lens, stats = _saved(ctx)
         if dhidden is not None:
             dhidden = _gradient(dhidden, None)
         g = rdf2v_residual_norm_backward(x, residual, weight, bias, stats, _gradient(dout, (x.shape, x.dtype, x.device)),
@@ -1679,7 +1705,8 @@ def rdf2v_residual_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: 
             raise ValueError("out, hidden and stats cannot be given where autograd records the call: an input requires "
                              "gradients")
         given = dict(drop=drop, seed=seed, row_begin=row_begin, center=center, eps=eps, hidden_dtype=hidden_dtype)
-        return _ResidualNorm.apply(x, residual, weight, bias, scale, seed_offset, lens, given, status, stream)
+        return _recorded(_ResidualNorm, dev, stream, x, residual, weight, bias, scale, seed_offset, lens, given, status,
+                         stream)
     with _on_stream(dev, stream) as h:
         out = _new_like(out, "out", x)
         hidden = _new_like(hidden, "hidden", x, n.hidden_dtype)
