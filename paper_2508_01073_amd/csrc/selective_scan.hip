@@ -649,7 +649,8 @@ __global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backwar
             r *= e[t];
             const float q = r * (t > 0 ? h[t > 0 ? t - 1 : 0] : h0);
             dd[t] = fmaf(q, rate, dd[t]);
-            rates_sum = fmaf(q, delta[t], rates_sum);
+            // of the tokens that count: what the row leaves behind, infinite or no number, is no part of the sum
+            rates_sum = counts<N>(t, count) ? fmaf(q, delta[t], rates_sum) : rates_sum;
           });
           grads[n * kWave + lane] = r;
           da[n * kWave + lane] += rates_sum;
