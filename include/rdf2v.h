@@ -791,7 +791,8 @@ typedef struct rdf2v_scan {
   int32_t states;        /* of a channel, 1 .. RDF2V_MAX_SCAN_STATES */
   int32_t dtype;         /* rdf2v_dtype of x, dt, b, c, gate, out and their gradients */
   /* [channels][states] float32 (device): rates, finite and <= 0. Others raise
-   * RDF2V_STATUS_BAD_VALUE and are taken as 0 (no decay). */
+   * RDF2V_STATUS_BAD_VALUE and are taken as 0 (no decay). Rates below -2^95
+   * are taken as -2^95, with which a step of 2^-88 forgets everything. */
   const float *a;
   const float *dt_bias;  /* [channels] float32 (device) or NULL: zeros */
   const float *skip;     /* [channels] float32 (device) or NULL: zeros */

@@ -1511,7 +1511,8 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
 
     x, dt and gate [rows, length, channels] and b and c [rows, length, groups, states] are float32 or bfloat16 in any
     layout whose last dimension is contiguous; channel d reads group d // (channels // groups). a [channels, states]
-    (finite, <= 0), dt_bias and skip [channels] are float32. lens: int32 [rows], the tokens of each row that count.
+    (finite, <= 0; below -2^95 it counts as that), dt_bias and skip [channels] are float32. lens: int32 [rows], the
+    tokens of each row that count.
     state: float32 [rows, channels, states] to begin from. Returns (out, state_out), state_out being None unless it is
     given or want_state is set.
 

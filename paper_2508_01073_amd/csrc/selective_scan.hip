@@ -102,8 +102,10 @@ __device__ __forceinline__ float softplus(float v, float &slope) {
   return v <= 0.0f ? log1 : v + log1;
 }
 
+// A rate as the kernels take it. Not below -2^95, which forgets all in a step of 2^-88: the lowest finite values would
+// be -inf over ln 2, and a step of 0, as the tokens have that fill a chunk, times that no number.
 __device__ __forceinline__ float checked_rate(float a, int32_t *status) {
-  if (a <= 0.0f && a > -kInf) return a;
+  if (a <= 0.0f && a > -kInf) return fmaxf(a, -0x1p95f);
   if (status != nullptr) atomicOr(status, RDF2V_STATUS_BAD_VALUE);
   return 0.0f;
 }

@@ -1,12 +1,12 @@
-"""Selective scan: infinities and NaN in a row's last token and in the states' gradients. The tokens that fill a row's
-last chunk are not there, whatever the row leaves behind."""
+"""Selective scan: infinities and NaN in a row's last token and in the states' gradients, and rates of any size. The
+tokens that fill a row's last chunk are not there, whatever the row leaves behind."""
 
 import pytest
 import torch
 
 import layer_refs as refs
 import paper_2508_01073_amd as rd
-from gpu_helpers import device, say
+from gpu_helpers import device, new_status, say
 from layer_helpers import BF16, F32, check, lengths, rand, scan_kinds
 
 pytestmark = pytest.mark.gpu
@@ -101,3 +101,49 @@ def test_infinite_gradients_of_states(t):
         u[0, 3, 1] = float("inf")
         ref = _held(c, lens, w, u, F32, "dstate_out")
         assert float(ref["da"][3, 1]) == float("inf") and int((~ref["da"].isfinite()).sum()) == 1
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("t", [1, 4, 5, 6, 7, 18, 297, 299])
+def test_rates_of_any_size(t, type_):
+    """The lowest rate there is forgets everything, tokens with a step of 0 (and those that fill a chunk) nothing."""
+    say(f"[scan numbers] rates, {t} tokens, {type_}")
+    for ragged in (False, True):
+        lens = _lens(t, ragged)
+        n = len(lens)
+        c = _case(n, t, type_)
+        a = c["a"].clone()
+        a[1, 0] = a[2, 3] = a[5, 4] = torch.finfo(F32).min
+        a[0, 1], a[3, 3], a[4, 0] = -3e38, -2.0 ** 100, -1e-40
+        w, u = rand(n, t, D, type_=type_, seed=20), rand(n, D, STATES, seed=21)
+        ref = _held(c | dict(a=a), lens, w, u, type_, "rates")
+        assert all(bool(v.isfinite().all()) for v in ref.values())
+        dt = c["dt"].clone()
+        dt[:, t // 2] = torch.finfo(type_).min if ragged else float("-inf")                 # steps of 0
+        given = c | dict(a=a, dt=dt)
+        status = new_status()
+        out, end = rd.rdf2v_selective_scan(**given, lens=lengths(lens), want_state=True, status=status)
+        g = rd.rdf2v_selective_scan_backward(dout=w, dstate_out=u, **given, lens=lengths(lens), status=status)
+        rd.check_device_status(status)
+        low = given | dict(dt=dt.float().clamp(min=-1000.0))                                # a step of 0 in 64 bits too
+        ref, size = (_rows(low, lens, w, u, absolute) for absolute in (False, True))
+        check(dict(out=out, state=end) | g._asdict(), ref, size, scan_kinds(t, STATES, D, n), type_, "no step", F32_OUTS)
+
+
+@pytest.mark.parametrize("states", [1, 4, 7, 16])
+def test_a_step_with_rates_of_any_size(states):
+    say(f"[scan numbers] step, {states} states")
+    n, d = 5, 9
+    a = -rand(d, states, seed=1).abs()
+    a[::2] = torch.finfo(F32).min
+    dt = rand(n, d, seed=2)
+    dt[1] = float("-inf")
+    b = rand(n, 1, states, seed=3)
+    state, x = rand(n, d, states, seed=4), rand(n, d, seed=5)
+    status = new_status()
+    out, new = rd.rdf2v_selective_scan_step(x, dt, a, b, b, state.clone(), status=status)
+    rd.check_device_status(status)
+    given = dict(x=x[:, None], dt=dt[:, None].clamp(min=-1000.0), a=a, b=b[:, None], c=b[:, None], state=state)
+    check(dict(out=out[:, None], state=new), refs.scan(**given), refs.scan(**given, absolute=True),
+          scan_kinds(1, states, d, n), F32, "step", ("state",))
+    assert torch.equal(new[1], state[1])
