@@ -53,6 +53,14 @@ struct Taps {
       for (int i = 0; i < V; ++i) bias[i] = 0.0f;
     }
   }
+  __device__ __forceinline__ bool finite() const {
+    bool all = true;
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) all = all && fabsf(w[j][i]) < __builtin_inff();
+    return all;
+  }
 };
 
 // The input `at` tokens after a row's first: of the row, of the state before it, or zeros.
@@ -174,55 +182,65 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
         const int64_t rest = length - begin;
         const int own = int(stop - begin), to = own + W - 1, real = int(min(rest, int64_t(to)));
         zeros -= own;
-        for (int t = 0; t < to; t += kAhead) {
-          Values<T, V> nx[kAhead], nd[kAhead];
+        const auto walk = [&](auto finite) {
+          constexpr bool FINITE = finite();
+          for (int t = 0; t < to; t += kAhead) {
+            Values<T, V> nx[kAhead], nd[kAhead];
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            nx[k].load(px, t + k < real ? n : 0);
-            nd[k].load(pd, t + k < real ? n : 0);
-            if (t + k + 1 < real) {
-              px += a.token_stride;
-              pd += a.dout_token_stride;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            const int s = t + k, p = s - (W - 1);
-            if (s >= to) break;
-            shift<W, V>(x);
-            shift<W, V>(du);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              x[W - 1][i] = nx[k][i];
-              float d = nd[k][i];
-              if (SILU && s < real) {
-                const float u = tap_sum<W, V>(taps, x, i);
-                d *= silu_slope(u, sigmoid(u));
-              }
-              du[W - 1][i] = d;
-              if (s < own) {
-                db[i] += d;
-#pragma unroll
-                for (int j = 0; j < W; ++j) dw[j][i] = fmaf(d, x[j][i], dw[j][i]);
+            for (int k = 0; k < kAhead; ++k) {
+              nx[k].load(px, t + k < real ? n : 0);
+              nd[k].load(pd, t + k < real ? n : 0);
+              if (t + k + 1 < real) {
+                px += a.token_stride;
+                pd += a.dout_token_stride;
               }
             }
-            if (p < 0 && !states) continue;
-            float g[V] = {};
-            const int64_t slot = p - (rest - (W - 1));  // of the state that the row leaves
-            if (slot >= 0 && a.dstate_out != nullptr)
-              load_values<T, V>(static_cast<const T *>(a.dstate_out) + (row * (W - 1) + slot) * a.channels + c, n, g);
 #pragma unroll
-            for (int i = 0; i < V; ++i)
+            for (int k = 0; k < kAhead; ++k) {
+              const int s = t + k, p = s - (W - 1);
+              if (s >= to) break;
+              shift<W, V>(x);
+              shift<W, V>(du);
 #pragma unroll
-              for (int j = 0; j < W; ++j) g[i] = fmaf(taps.w[j][i], du[W - 1 - j][i], g[i]);
-            if (p >= 0) {
-              store_values<T, V>(dx, n, g);
-              dx += a.channels;
-            } else {
-              store_values<T, V>(static_cast<T *>(a.dstate) + (row * (W - 1) + p + W - 1) * a.channels + c, n, g);
+              for (int i = 0; i < V; ++i) {
+                x[W - 1][i] = nx[k][i];
+                float d = nd[k][i];
+                if (SILU && s < real) {
+                  const float u = tap_sum<W, V>(taps, x, i);
+                  d *= silu_slope(u, sigmoid(u));
+                }
+                du[W - 1][i] = d;
+                if (s < own) {
+                  db[i] += d;
+#pragma unroll
+                  for (int j = 0; j < W; ++j) dw[j][i] = fmaf(d, x[j][i], dw[j][i]);
+                }
+              }
+              if (p < 0 && !states) continue;
+              float g[V] = {};
+              const int64_t slot = p - (rest - (W - 1));  // of the state that the row leaves
+              if (slot >= 0 && a.dstate_out != nullptr)
+                load_values<T, V>(static_cast<const T *>(a.dstate_out) + (row * (W - 1) + slot) * a.channels + c, n, g);
+#pragma unroll
+              for (int j = 0; j < W; ++j)
+                if (FINITE || (s >= j && s - j < real))  // what is not there is 0, and no number times infinity
+#pragma unroll
+                  for (int i = 0; i < V; ++i) g[i] = fmaf(taps.w[j][i], du[W - 1 - j][i], g[i]);
+              if (p >= 0) {
+                store_values<T, V>(dx, n, g);
+                dx += a.channels;
+              } else {
+                store_values<T, V>(static_cast<T *>(a.dstate) + (row * (W - 1) + p + W - 1) * a.channels + c, n, g);
+              }
             }
           }
-        }
+        };
+        // Taps that are all finite, as ever but by accident, need no look at where a tap's token lies: with one for each
+        // tap 4,096 rows of 17 tokens take 84 us for 73.
+        if (taps.finite())
+          walk(std::true_type{});
+        else
+          walk(std::false_type{});
       }
       const float zero[V] = {};
       for (; zeros > 0; --zeros, dx += a.channels) store_values<T, V>(dx, n, zero);
