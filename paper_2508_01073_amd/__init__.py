@@ -840,6 +840,14 @@ def _saved(ctx):
     return saved
 
 
+def _written(*tensors) -> None:
+    """Tells autograd that a call has written to these tensors of the caller (None: not given), as an operation of
+    torch in place does: gradients that would read what was there before raise an error."""
+    given = [t for t in tensors if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
+
+
 class _DecayAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, log_decay, state, scale, lens, want_state, workspace, status, stream):
@@ -907,6 +915,7 @@ def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
                         status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
+        given = out, state_out
         shape = (c.rows, c.heads, c.dk, c.dv)
         if out is None:
             out = torch.empty((c.rows, c.length, c.heads, c.dv), dtype=q.dtype, device=dev)
@@ -927,6 +936,7 @@ def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         st = _native().rdf2v_decay_attention(ref, vq, vk, vv, _ptr(state), _ptr(out), _ptr(state_out),
                                              _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_decay_attention")
+        _written(*given)
         return out, state_out
 
 
@@ -943,6 +953,7 @@ def rdf2v_decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Te
     a = _Attention(q, k, v, log_decay, scale, lens, 4)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
+        given = dq, dk, dv, dstate
         shape = (c.rows, c.heads, c.dk, c.dv)
         view = _heads_view(dout, "dout", q.dtype, dev, (c.rows, c.length, c.heads, c.dv))
         grads = []
@@ -967,6 +978,7 @@ def rdf2v_decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Te
                                                       _ptr(dk), _ptr(dv), _ptr(dstate), _ptr(workspace),
                                                       _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_decay_attention_backward")
+        _written(*given)
         return dq, dk, dv, dstate
 
 
@@ -985,6 +997,7 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
     a = _Attention(q, k, v, log_decay, scale, None, 3)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
+        given = out, state if state_out is None and parents is None else state_out
         shape = (c.rows, c.heads, c.dk, c.dv)
         num_states = c.rows
         if parents is not None:
@@ -1010,6 +1023,7 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
         st = _native().rdf2v_decay_attention_step(ctypes.byref(c), vq, vk, vv, _ptr(state), num_states,
                                                   _ptr(parents), _ptr(out), _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_decay_attention_step")
+        _written(*given)
         return out, state_out
 
 
@@ -1035,6 +1049,7 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
         raise ValueError("logits must have shape [groups, beams, vocab]")
     dev = logits.device
     with _on_stream(dev, stream) as h:
+        given = scores_out, tokens, parents
         groups, beams, vocab = logits.shape
         gs, bs, vs = logits.stride()
         if (vs != 1 and vocab > 1) or (gs != beams * bs and groups > 1 and beams > 1):
@@ -1061,6 +1076,7 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
                                    num_out, _ptr(scores_out), _ptr(tokens), _ptr(parents), _ptr(workspace),
                                    _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_beam_select")
+        _written(*given)
         return scores_out, tokens, parents
 
 
@@ -1075,6 +1091,7 @@ def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.T
     if src.dim() < 1 or not src.is_contiguous():
         raise ValueError("src must be contiguous rows")
     with _on_stream(dev, stream) as h:
+        given = (out,)
         rows, shape = parents.numel(), src.shape[1:]
         if out is None:
             out = torch.empty((rows,) + shape, dtype=src.dtype, device=dev)
@@ -1085,6 +1102,7 @@ def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.T
         st = _native().rdf2v_beam_reorder(_ptr(src), src.shape[0], row_bytes, _ptr(parents), rows, _ptr(out),
                                           _ptr(status), h)
         _check(st, "rdf2v_beam_reorder")
+        _written(*given)
         return out
 
 
@@ -1160,6 +1178,7 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
             raise ValueError("loss and lse cannot be given where autograd records the call: logits requires gradients")
         return _recorded(_DistillLoss, dev, stream, logits, ids, teacher, temperature, workspace, status, stream)
     with _on_stream(dev, stream) as h:
+        given = loss, lse, dlogits
         rows, vocab = logits.shape
         loss = torch.empty(rows, dtype=torch.float32, device=dev) if loss is None else \
             _exact(loss, "loss", torch.float32, (rows,), dev)
@@ -1183,6 +1202,7 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
                                     temperature, _ptr(loss), _ptr(lse), _ptr(dloss), _ptr(dlogits), dstride,
                                     _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_distill_loss")
+        _written(*given)
         return (loss, lse) if dloss is None else (loss, lse, dlogits)
 
 
@@ -1193,6 +1213,7 @@ def rdf2v_distill_loss_backward(logits: torch.Tensor, ids: torch.Tensor, teacher
     """The gradient of the logits alone, with the lse that rdf2v_distill_loss returned."""
     dtype, stride, dev = _teacher(logits, ids, teacher)
     with _on_stream(dev, stream) as h:
+        given = (dlogits,)
         rows, vocab = logits.shape
         _exact(lse, "lse", torch.float32, (rows,), dev)
         _exact(dloss, "dloss", torch.float32, (rows,), dev)
@@ -1210,6 +1231,7 @@ def rdf2v_distill_loss_backward(logits: torch.Tensor, ids: torch.Tensor, teacher
                                              ids.shape[1], temperature, _ptr(lse), _ptr(dloss), _ptr(dlogits),
                                              dstride, _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_distill_loss_backward")
+        _written(*given)
         return dlogits
 
 
@@ -1345,6 +1367,7 @@ def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
         got = _recorded(_CausalConv, dev, stream, x, weight, bias, state, silu, lens, want_state, status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
+        given = out, state_out
         out = _new_like(out, "out", x)
         if want_state or state_out is not None:
             state_out = _new(state_out, "state_out", a.dtype, a.states, dev)
@@ -1353,6 +1376,7 @@ def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
         _status(status, dev)
         st = _native().rdf2v_causal_conv(c, a.view, _ptr(state), _ptr(out), _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_causal_conv")
+        _written(*given)
         return out, state_out
 
 
@@ -1374,6 +1398,7 @@ def rdf2v_causal_conv_backward(x: torch.Tensor, weight: torch.Tensor, bias: torc
     a = _Conv(x, weight, bias, silu, lens, 3)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
+        given = dx, dweight, dbias, dstate
         view = _tokens_view(dout, "dout", a.dtype, dev, a.shape)
         dx = _new_like(dx, "dx", x)
         dweight = _new(dweight, "dweight", torch.float32, weight.shape, dev)
@@ -1392,6 +1417,7 @@ def rdf2v_causal_conv_backward(x: torch.Tensor, weight: torch.Tensor, bias: torc
                                             _ptr(dbias), _ptr(dstate), _ptr(workspace), _ws_bytes(workspace),
                                             _ptr(status), h)
         _check(st, "rdf2v_causal_conv_backward")
+        _written(*given)
         return dx, dweight, dbias, dstate
 
 
@@ -1404,6 +1430,7 @@ def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Te
     a = _Conv(x, weight, bias, silu, None, 2)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
+        given = out, state if state_out is None and parents is None else state_out
         num_states = _parents_and_states(parents, state, c.rows, a.states[1:], a.dtype, dev)
         out = _new_like(out, "out", x)
         if state_out is None and parents is None:
@@ -1415,6 +1442,7 @@ def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Te
         st = _native().rdf2v_causal_conv_step(c, a.view, _ptr(state), num_states, _ptr(parents), _ptr(out),
                                               _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_causal_conv_step")
+        _written(*given)
         return out, state_out
 
 
@@ -1528,6 +1556,7 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
                         workspace, status, stream)
         return got if want_state else (got, None)
     with _on_stream(dev, stream) as h:
+        given = out, state_out
         out = _new_like(out, "out", x)
         if want_state or state_out is not None:
             state_out = _new(state_out, "state_out", torch.float32, s.states, dev)
@@ -1539,6 +1568,7 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
         st = lib.rdf2v_selective_scan(s.c, *s.views, _ptr(state), _ptr(out), _ptr(state_out), _ptr(workspace),
                                       _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_selective_scan")
+        _written(*given)
         return out, state_out
 
 
@@ -1574,6 +1604,7 @@ def rdf2v_selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, a: torch.Te
         st = lib.rdf2v_selective_scan_backward(s.c, *s.views, view, _ptr(state), _ptr(dstate_out), to,
                                                _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_selective_scan_backward")
+        _written(*given)
         return g
 
 
@@ -1588,6 +1619,7 @@ def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor
     s = _Scan(x, dt, a, b, c, dt_bias, skip, gate, None, 2)
     dev = s.dev
     with _on_stream(dev, stream) as h:
+        given = out, state if state_out is None and parents is None else state_out
         num_states = _parents_and_states(parents, state, s.c.rows, s.states[1:], torch.float32, dev)
         out = _new_like(out, "out", x)
         if state_out is None and parents is None:
@@ -1599,6 +1631,7 @@ def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor
         st = _native().rdf2v_selective_scan_step(s.c, *s.views, _ptr(state), num_states, _ptr(parents), _ptr(out),
                                                  _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_selective_scan_step")
+        _written(*given)
         return out, state_out
 
 
@@ -1709,12 +1742,14 @@ def rdf2v_residual_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: 
         return _recorded(_ResidualNorm, dev, stream, x, residual, weight, bias, scale, seed_offset, lens, given, status,
                          stream)
     with _on_stream(dev, stream) as h:
+        given = out, hidden, stats
         out = _new_like(out, "out", x)
         hidden = _new_like(hidden, "hidden", x, n.hidden_dtype)
         stats = _new(stats, "stats", torch.float32, n.stats, dev)
         _status(status, dev)
         st = _native().rdf2v_residual_norm(n.c, *n.views, _ptr(out), _ptr(hidden), _ptr(stats), _ptr(status), h)
         _check(st, "rdf2v_residual_norm")
+        _written(*given)
         return out, hidden, stats
 
 
@@ -1755,6 +1790,7 @@ def rdf2v_residual_norm_backward(x: torch.Tensor, residual: torch.Tensor | None,
                                               _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dscale), _ptr(workspace),
                                               _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_residual_norm_backward")
+        _written(*given)
         return g
 
 
