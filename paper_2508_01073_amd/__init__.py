@@ -22,6 +22,7 @@ from dataclasses import dataclass
 from typing import NamedTuple
 
 import torch
+from torch.autograd import forward_ad
 
 __all__ = [
     "Csr", "Rdf2vError", "RDF2V_MAX_DEPTH", "RDF2V_STATUS_ID_OUT_OF_RANGE", "RDF2V_STATUS_BAD_CSR",
@@ -806,7 +807,12 @@ class _Attention:
 
 
 def _records(*tensors) -> bool:
-    """Whether autograd records what is done with any of these (None: not there)."""
+    """Whether autograd records what is done with any of these (None: not there). Tangents, which no call carries on,
+    are refused, as torch's own functions do that have no forward derivative."""
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError("the operators have no forward-mode derivatives: an input has a tangent")
     if torch.is_grad_enabled():
         for t in tensors:
             if t is not None and t.requires_grad:
@@ -1173,7 +1179,7 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
     dtype, stride, dev = _teacher(logits, ids, teacher)
     if _records(teacher):
         _no_gradient("rdf2v_distill_loss", "teacher")
-    if dloss is None and dlogits is None and _records(logits):
+    if _records(logits) and dloss is None and dlogits is None:
         if loss is not None or lse is not None:
             raise ValueError("loss and lse cannot be given where autograd records the call: logits requires gradients")
         return _recorded(_DistillLoss, dev, stream, logits, ids, teacher, temperature, workspace, status, stream)
