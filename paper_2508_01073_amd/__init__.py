@@ -846,12 +846,16 @@ def _saved(ctx):
     return saved
 
 
-def _written(*tensors) -> None:
-    """Tells autograd that a call has written to these tensors of the caller (None: not given), as an operation of
-    torch in place does: gradients that would read what was there before raise an error."""
-    given = [t for t in tensors if t is not None]
-    if given:
-        torch.autograd.graph.increment_version(given)
+# Tells autograd that a call has written to these tensors, as an operation of torch in place does: gradients that would
+# read what was there before raise an error. torch.autograd.graph.increment_version, at half of its time.
+_written = torch._C._increment_version
+
+
+def _written_of(*given) -> None:
+    """The same of outputs that the caller may have given (None: a new one, which nothing has seen)."""
+    for t in given:
+        if t is not None:
+            _written((t,))
 
 
 class _DecayAttention(torch.autograd.Function):
@@ -942,7 +946,7 @@ def rdf2v_decay_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
         st = _native().rdf2v_decay_attention(ref, vq, vk, vv, _ptr(state), _ptr(out), _ptr(state_out),
                                              _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_decay_attention")
-        _written(*given)
+        _written_of(*given)
         return out, state_out
 
 
@@ -984,7 +988,7 @@ def rdf2v_decay_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Te
                                                       _ptr(dk), _ptr(dv), _ptr(dstate), _ptr(workspace),
                                                       _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_decay_attention_backward")
-        _written(*given)
+        _written_of(*given)
         return dq, dk, dv, dstate
 
 
@@ -1003,7 +1007,7 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
     a = _Attention(q, k, v, log_decay, scale, None, 3)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
-        given = out, state if state_out is None and parents is None else state_out
+        given = out
         shape = (c.rows, c.heads, c.dk, c.dv)
         num_states = c.rows
         if parents is not None:
@@ -1029,7 +1033,7 @@ def rdf2v_decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor
         st = _native().rdf2v_decay_attention_step(ctypes.byref(c), vq, vk, vv, _ptr(state), num_states,
                                                   _ptr(parents), _ptr(out), _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_decay_attention_step")
-        _written(*given)
+        _written((state_out,) if given is None else (given, state_out))
         return out, state_out
 
 
@@ -1082,7 +1086,7 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
                                    num_out, _ptr(scores_out), _ptr(tokens), _ptr(parents), _ptr(workspace),
                                    _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_beam_select")
-        _written(*given)
+        _written_of(*given)
         return scores_out, tokens, parents
 
 
@@ -1108,7 +1112,7 @@ def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.T
         st = _native().rdf2v_beam_reorder(_ptr(src), src.shape[0], row_bytes, _ptr(parents), rows, _ptr(out),
                                           _ptr(status), h)
         _check(st, "rdf2v_beam_reorder")
-        _written(*given)
+        _written_of(*given)
         return out
 
 
@@ -1208,7 +1212,7 @@ def rdf2v_distill_loss(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.T
                                     temperature, _ptr(loss), _ptr(lse), _ptr(dloss), _ptr(dlogits), dstride,
                                     _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_distill_loss")
-        _written(*given)
+        _written_of(*given)
         return (loss, lse) if dloss is None else (loss, lse, dlogits)
 
 
@@ -1237,7 +1241,7 @@ def rdf2v_distill_loss_backward(logits: torch.Tensor, ids: torch.Tensor, teacher
                                              ids.shape[1], temperature, _ptr(lse), _ptr(dloss), _ptr(dlogits),
                                              dstride, _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_distill_loss_backward")
-        _written(*given)
+        _written_of(*given)
         return dlogits
 
 
@@ -1382,7 +1386,7 @@ def rdf2v_causal_conv(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor 
         _status(status, dev)
         st = _native().rdf2v_causal_conv(c, a.view, _ptr(state), _ptr(out), _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_causal_conv")
-        _written(*given)
+        _written_of(*given)
         return out, state_out
 
 
@@ -1423,7 +1427,7 @@ def rdf2v_causal_conv_backward(x: torch.Tensor, weight: torch.Tensor, bias: torc
                                             _ptr(dbias), _ptr(dstate), _ptr(workspace), _ws_bytes(workspace),
                                             _ptr(status), h)
         _check(st, "rdf2v_causal_conv_backward")
-        _written(*given)
+        _written_of(*given)
         return dx, dweight, dbias, dstate
 
 
@@ -1436,7 +1440,7 @@ def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Te
     a = _Conv(x, weight, bias, silu, None, 2)
     dev, c = a.dev, a.c
     with _on_stream(dev, stream) as h:
-        given = out, state if state_out is None and parents is None else state_out
+        given = out
         num_states = _parents_and_states(parents, state, c.rows, a.states[1:], a.dtype, dev)
         out = _new_like(out, "out", x)
         if state_out is None and parents is None:
@@ -1448,7 +1452,7 @@ def rdf2v_causal_conv_step(x: torch.Tensor, weight: torch.Tensor, bias: torch.Te
         st = _native().rdf2v_causal_conv_step(c, a.view, _ptr(state), num_states, _ptr(parents), _ptr(out),
                                               _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_causal_conv_step")
-        _written(*given)
+        _written((state_out,) if given is None else (given, state_out))
         return out, state_out
 
 
@@ -1574,7 +1578,7 @@ def rdf2v_selective_scan(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor, b: 
         st = lib.rdf2v_selective_scan(s.c, *s.views, _ptr(state), _ptr(out), _ptr(state_out), _ptr(workspace),
                                       _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_selective_scan")
-        _written(*given)
+        _written_of(*given)
         return out, state_out
 
 
@@ -1610,7 +1614,7 @@ def rdf2v_selective_scan_backward(x: torch.Tensor, dt: torch.Tensor, a: torch.Te
         st = lib.rdf2v_selective_scan_backward(s.c, *s.views, view, _ptr(state), _ptr(dstate_out), to,
                                                _ptr(workspace), _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_selective_scan_backward")
-        _written(*given)
+        _written_of(*given)
         return g
 
 
@@ -1625,7 +1629,7 @@ def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor
     s = _Scan(x, dt, a, b, c, dt_bias, skip, gate, None, 2)
     dev = s.dev
     with _on_stream(dev, stream) as h:
-        given = out, state if state_out is None and parents is None else state_out
+        given = out
         num_states = _parents_and_states(parents, state, s.c.rows, s.states[1:], torch.float32, dev)
         out = _new_like(out, "out", x)
         if state_out is None and parents is None:
@@ -1637,7 +1641,7 @@ def rdf2v_selective_scan_step(x: torch.Tensor, dt: torch.Tensor, a: torch.Tensor
         st = _native().rdf2v_selective_scan_step(s.c, *s.views, _ptr(state), num_states, _ptr(parents), _ptr(out),
                                                  _ptr(state_out), _ptr(status), h)
         _check(st, "rdf2v_selective_scan_step")
-        _written(*given)
+        _written((state_out,) if given is None else (given, state_out))
         return out, state_out
 
 
@@ -1755,7 +1759,7 @@ def rdf2v_residual_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: 
         _status(status, dev)
         st = _native().rdf2v_residual_norm(n.c, *n.views, _ptr(out), _ptr(hidden), _ptr(stats), _ptr(status), h)
         _check(st, "rdf2v_residual_norm")
-        _written(*given)
+        _written_of(*given)
         return out, hidden, stats
 
 
@@ -1796,7 +1800,7 @@ def rdf2v_residual_norm_backward(x: torch.Tensor, residual: torch.Tensor | None,
                                               _ptr(g.dweight), _ptr(g.dbias), _ptr(g.dscale), _ptr(workspace),
                                               _ws_bytes(workspace), _ptr(status), h)
         _check(st, "rdf2v_residual_norm_backward")
-        _written(*given)
+        _written_of(*given)
         return g
 
 

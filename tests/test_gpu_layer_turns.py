@@ -3,7 +3,7 @@ round: the second tile of a thread, the second segment of a wave, the second tok
 
 Bounds of the parameters' gradients count the values that one thread adds up one after the other, and no more: what a
 thread leaves is added up by a workgroup in a few steps, and in 64 bits from there. A sum over all tokens that lacks a
-turn is off by a hundred times as much and more."""
+turn is off by ten times as much and more."""
 
 import pytest
 import torch
