@@ -4,6 +4,9 @@
 // is x read once and the output written once; for the gradients x and dout read, dx written. A thread takes a
 // few channels side by side and a tile of tokens, holding the width - 1 inputs before it in registers: all that
 // is read twice are these, at the tiles' ends.
+//
+// Kernels' times here and below are means under the profiler, up to an eighth longer than among other calls; times of
+// calls are without it.
 
 #include "vectors.hpp"
 
@@ -93,7 +96,7 @@ __device__ __forceinline__ float tap_sum(const Taps<W, V> &taps, const float (&x
 }
 
 // Whole rows: a thread to a vector of channels and a tile of tokens, four of which are read at once. 20,011 tokens of
-// 2,048 channels in bf16: 38 us, 4.4 TB/s of what has to be read and written; vectors of eight channels need twice the
+// 2,048 channels in bf16: 37 us, 4.4 TB/s of what has to be read and written; vectors of eight channels need twice the
 // registers and leave half as many waves (48 us for 58 when both were timed).
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_kernel(Conv a, int64_t first) {
@@ -235,8 +238,8 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
             }
           }
         };
-        // Taps that are all finite, as ever but by accident, need no look at where a tap's token lies: with one for each
-        // tap 4,096 rows of 17 tokens take 84 us for 73.
+        // Taps that are all finite, as ever but by accident, need no look at where a tap's token lies: with one for
+        // each tap 4,096 rows of 17 tokens by 408 channels take 84 us for 74.
         if (taps.finite())
           walk(std::true_type{});
         else
@@ -265,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(Conv a, int64_t
   }
 }
 
-// One token more: a thread to a row's vector of channels. 512 rows of 2,048 channels in bf16, width 4: 7.8 us for
+// One token more: a thread to a row's vector of channels. 512 rows of 2,048 channels in bf16, width 4: 7.5 us for
 // 15 MB, most of it the latency of a parent's id and then its state.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void conv_step_kernel(Conv a, int64_t first) {

@@ -8,6 +8,9 @@
 //
 // Gradients are computed from x and residual again, not from hidden as it was rounded: the parameters'
 // gradients have 32 bits, and would have lost them.
+//
+// Kernels' times here and below are means under the profiler, up to an eighth longer than among other calls; times of
+// calls are without it.
 
 #include "vectors.hpp"
 
@@ -160,8 +163,8 @@ constexpr int workgroup_of(int team) { return team < kThreads ? kThreads : team;
 // Waves of each of a compute unit's four SIMDs, as the registers for a thread's vectors let them have.
 constexpr int waves_of(bool backward, int per) { return backward || per > 3 ? 4 : per > 2 ? 5 : 6; }
 
-// 16,384 tokens of 4,096 channels, bf16 beside a float32 residual: 146 us, 805 MB at 5.5 TB/s; 69,632 tokens of 301
-// channels, half of them padding, float32: 69 us, 250 MB.
+// 16,384 tokens of 4,096 channels, bf16 beside a float32 residual: 145 us, 805 MB at 5.6 TB/s; 69,632 tokens of 301
+// channels, half of them padding, float32: 70 us, 250 MB.
 template <class T, class R, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM), waves_of(false, PER)) void norm_kernel(Norm a) {
   constexpr int kBlock = workgroup_of(TEAM), kTeams = kBlock / TEAM;
@@ -260,8 +263,8 @@ __device__ __forceinline__ void store_part(float *part, const Own<TEAM, PER> &ow
 
 // With n = (hidden - mean) / std and dn = dout * weight, a token's gradient is
 //   dhidden + (dn - n mean(dn n) - mean(dn)) / std        (the last mean where the norm is centred)
-// MORE: there is a scale, or gradients of the bias or the scale are wanted. The same tokens as above: 280 us, 1.2 GB at
-// 4.3 TB/s, and 99 us, 341 MB: loads, sums and stores of a token follow one another, and 16 waves to a compute unit are
+// MORE: there is a scale, or gradients of the bias or the scale are wanted. The same tokens as above: 276 us, 1.2 GB at
+// 4.4 TB/s, and 100 us, 341 MB: loads, sums and stores of a token follow one another, and 16 waves to a compute unit are
 // what the parameters' sums leave registers for.
 template <class T, class R, bool MORE, int TEAM, int PER>
 __global__ __launch_bounds__(workgroup_of(TEAM), waves_of(true, PER)) void norm_backward_kernel(Norm a) {

@@ -17,6 +17,9 @@
 // Gradients go backwards through the chunks: a chunk's states are made again from the one before it, which
 // scan_states_kernel has left in memory, and stay in registers for the way back. The sums over states (for x and
 // dt) are a lane's own; the sums over channels (for b and c) are taken for sixteen values at once, see sixteen_sums.
+//
+// Kernels' times here and below are means under the profiler, up to an eighth longer than among other calls; times of
+// calls are without it.
 
 #include "vectors.hpp"
 
@@ -305,8 +308,8 @@ struct Lane {
 
 // The outputs of a segment. A wave's barriers cost nothing: it is alone in its workgroup. Bound by the issue of vector
 // instructions: 9 for a token's state, its share of the token's own (the step's logarithm, conversions, the gate)
-// among them. 20,011 tokens of 2,048 channels by 16 states: 213 us, 94 % of the issue with exponentials as two
-// instructions each; 4,000 ragged rows of 17 tokens by 256 channels: 73 us.
+// among them. 20,011 tokens of 2,048 channels by 16 states: 208 us, 94 % of the issue with exponentials as two
+// instructions each; 4,000 ragged rows of 17 tokens by 256 channels: 78 us, 81 %, 14 instructions for a token's state.
 template <class T, int NMAX>
 __global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Scan p, int64_t first) {
   __shared__ float rates[NMAX * kWave], held[NMAX * kWave], b[NMAX * kTokens], c[NMAX * kTokens];
@@ -367,8 +370,9 @@ __global__ __launch_bounds__(kWave, NMAX <= 16 ? 4 : 1) void scan_out_kernel(Sca
 // The states that a segment ends with, from zeros; BACK, for the gradients: the states before its chunks (from the
 // row's own state where there is one segment), and the gradient that its outputs give the state before it,
 // sum_t (product of the decays up to t) c_t g_t, which needs no second way through the tokens. 20,011 tokens of 2,048
-// channels by 16 states: 157 us, 89 % of the issue; 4 rows of 4,096 tokens, BACK: 279 us, 67 %. Reading a chunk's
-// inputs while the one before is worked on takes the registers of a wave (157 us: 164; BACK: 261).
+// channels by 16 states: 154 us, 88 % of the issue; 4 rows of 4,096 tokens, BACK: 284 us, 66 %. Reading a chunk's
+// inputs while the one before is worked on takes the registers of a wave (164 us for 157; BACK 261 for 280, a hundredth
+// of a training case).
 template <class T, int NMAX, bool BACK, bool CUT>
 __global__ __launch_bounds__(kWave) void scan_states_kernel(Scan p, int64_t first) {
   constexpr bool kBoth = BACK && CUT;
@@ -535,7 +539,7 @@ __device__ __forceinline__ void backwards(Each each) {
 
 // Gradients of a segment, chunk after chunk from its end; a wave takes several segments of its channels in turn
 // and holds the parameters' gradients meanwhile. 25 instructions for a token's state, 4 of them the sums over channels.
-// 4 rows of 4,096 tokens by 2,048 channels of 16 states: 528 us, 72 % of the issue, the rest waits of the two waves
+// 4 rows of 4,096 tokens by 2,048 channels of 16 states: 541 us, 73 % of the issue, the rest waits of the two waves
 // that a SIMD's registers hold. Three, with segments for them, took 570 us for 589, but the states 352 for 279.
 template <class T, int NMAX>
 __global__ __launch_bounds__(kGang *kWave, NMAX <= 32 ? 2 : 1) void scan_backward_kernel(Scan p, int64_t first) {
@@ -851,8 +855,8 @@ void plan_forward(Scan &p) {
 // The gradients look at all tokens twice anyway, and their waves, two to a SIMD, take segments in turn. Where whole
 // rows are fewer: of the numbers of segments that fill 1, 2, .. turns the one that gives the busiest wave the fewest
 // tokens, with 8 for what a segment costs by itself; a wave alone on its SIMD takes three quarters of the time, and
-// rows that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: 64 of them 521 us whole and
-// 464 cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
+// rows that are cut an eighth more. Rows of 256 tokens by 1,024 channels, 16 states, bf16: calls with 64 of them take 521 us
+// whole and 464 cut, 80 651 and 584, 110 695 and 720. With more rows cutting costs (130 rows of 126 tokens: 471 and 516).
 void plan_backward(Scan &p) {
   const int64_t most = 2 * kSimds, columns = p.blocks * p.groups, rows = std::max<int64_t>(1, p.rows);
   const auto cost = [&](int64_t segments) {
@@ -898,7 +902,7 @@ size_t plan(Scan &p, bool backward, void *workspace) {
 
 // Calls launch with a value of the element type and a constant for the most states. Shared memory sets how many waves
 // there are: 16 states leave four to a SIMD (two in the gradients, by their registers), 32 two, 64 one. 4 rows of 4,096
-// tokens by 1,024 channels of 24 states: 240 us by the kernels for 32, 402 by those for 64.
+// tokens by 1,024 channels of 24 states: a call takes 240 us by the kernels for 32, 402 by those for 64.
 template <class Launch>
 rdf2v_status with_types(int dtype, int states, Launch launch) {
   const auto sized = [&](auto t) {
