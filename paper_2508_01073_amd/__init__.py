@@ -1093,7 +1093,7 @@ def rdf2v_beam_select(logits: torch.Tensor, scores: torch.Tensor, num_out: int, 
 def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.Tensor | None = None,
                        status: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Rows of src (any type, contiguous) in the order of parents (int32, any shape): out[r] =
-    src[parents.flatten()[r]]."""
+    src[parents.flatten()[r]]. For answering: autograd does not record it."""
     _dev_i32(parents, "parents")
     dev = parents.device
     if not isinstance(src, torch.Tensor) or src.device != dev:
@@ -1108,6 +1108,8 @@ def rdf2v_beam_reorder(src: torch.Tensor, parents: torch.Tensor, *, out: torch.T
         else:
             _exact(out, "out", src.dtype, (rows,) + shape, dev)
         _status(status, dev)
+        if _records(src):
+            _no_gradient("rdf2v_beam_reorder", "src")
         row_bytes = src.element_size() * shape.numel()
         st = _native().rdf2v_beam_reorder(_ptr(src), src.shape[0], row_bytes, _ptr(parents), rows, _ptr(out),
                                           _ptr(status), h)

@@ -34,19 +34,27 @@ def _calls():
         "distill, gradients too": (lambda **k: rd.rdf2v_distill_loss(ids=ids, dloss=torch.ones(N, device=device()), **k),
                                    dict(logits=z, teacher=teacher)),
         "select": (lambda **k: rd.rdf2v_beam_select(num_out=2, **k), dict(logits=z.view(1, N, 20),
-                                                                          scores=rand(1, N, seed=13)))}
+                                                                          scores=rand(1, N, seed=13))),
+        "reorder": (lambda **k: rd.rdf2v_beam_reorder(parents=lengths([2, 0, 1]), **k), dict(src=z))}
 
 
 @pytest.mark.parametrize("name", ["conv", "conv step", "scan", "scan step", "norm", "attention", "attention step",
-                                  "distill", "distill, gradients too", "select"])
+                                  "distill", "distill, gradients too", "select", "reorder"])
 @pytest.mark.parametrize("recorded", [False, True])
 def test_a_tangent_is_refused(name, recorded):
     say(f"[forward mode] {name}, recorded {recorded}")
     call, arguments = _calls()[name]
     with torch.set_grad_enabled(recorded), forward_ad.dual_level():
         for key, t in arguments.items():
-            if recorded and "step" not in name and name != "select":
+            if recorded and "step" not in name and name not in ("select", "reorder"):
                 t = t.clone().requires_grad_()
             with pytest.raises(NotImplementedError):
                 call(**(arguments | {key: forward_ad.make_dual(t, torch.ones_like(t))}))
         call(**arguments)                                      # without one they are as ever
+
+
+def test_a_reordering_says_that_it_has_no_gradient():
+    say("[forward mode] reordering")
+    src = rand(3, 20, seed=11).requires_grad_()
+    with pytest.warns(UserWarning, match="no gradient"):
+        rd.rdf2v_beam_reorder(src, lengths([2, 0, 1]))
